@@ -18,7 +18,8 @@ CALIB_SOURCES = ["esp_calib.hip"]
 # the fused kernels' instances are split by R over esp_inst_*.hip
 SOURCES = ["esp_api.hip", "esp_kernels.hip", "esp_extras.hip",
            "esp_inst_dense12.hip", "esp_inst_dense34.hip", "esp_inst_dense56.hip", "esp_inst_dense78.hip",
-           "esp_inst_csr1234.hip", "esp_inst_csr5678.hip"]
+           "esp_inst_csr1234.hip", "esp_inst_csr5678.hip",
+           "kv_write.hip", "kv_pages.hip", "kv_attend.hip"]
 ARCH = "gfx950"
 
 COMPILE_FLAGS = [

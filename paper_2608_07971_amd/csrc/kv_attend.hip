@@ -5,6 +5,7 @@ namespace esp_kv {
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kTile = 64;                   // tokens a wavefront takes at a time
+constexpr int kDies = 8;                    // workgroups go round the dies
 constexpr int kCols = 16;                   // (token, query head) rows of a unit: the columns of the matrix products
 constexpr float kLift = 14.0f;              // softmax weights are taken times 2^14, so that fp16 holds them down to 2^-38 of the largest
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -21,7 +22,7 @@ struct AttendArgs {
     View q, out;
     float *lse;
     float scale;                            // softmax scale times log2 e
-    int32_t layer, q_heads, group, window, max_new, max_length, target, wide;
+    int32_t layer, q_heads, group, window, max_new, max_length, groups, wide, wide_out;
     uint32_t *counters;
     float *partial;
 };
@@ -37,12 +38,17 @@ __device__ __forceinline__ Span span_of(int p0, int p1, int window) {
     return {first / kTile, p1 / kTile + 1};
 }
 
-// One workgroup's work: tiles of a unit (16 rows of queries of one sequence
-// and key head), and how the units of its row are numbered.
-struct Plan {
-    Row row;
-    int unit, chunk, chunks, first, per;    // first: the chunk index of the unit's chunk 0; per: tiles a chunk
-    bool any;
+// The work of one head is a list of tiles: units (16 rows of queries of one
+// sequence and key head) one after another, every unit of a row with as many
+// tiles as the row's longest (one where there is none, so that empty rows are
+// written too).  The list is cut evenly over the workgroups, which all run at
+// once: ragged batches and single long sequences fill the GPU alike, and a
+// workgroup has at most two units that it shares with others.
+//
+// 64 rows of the list at a time, worked out by the first wavefront.
+struct Window {
+    Row row[64];
+    int units[64], tiles[64], end[64];      // end: tiles of the list up to and with this row
 };
 
 __device__ __forceinline__ Row usable_row(const AttendArgs &a, int b) {
@@ -56,65 +62,42 @@ __device__ __forceinline__ Row usable_row(const AttendArgs &a, int b) {
     }
     return r;
 }
+__device__ __forceinline__ int units_of(const AttendArgs &a, const Row &r) { return (r.n * a.group + kCols - 1) / kCols; }
+__device__ __forceinline__ int tiles_of(const AttendArgs &a, const Row &r) { return max(1, span_of(r.length - r.n, r.length - 1, a.window).size()); }
 
-// Work is cut into chunks of `per` tiles, `per` from the sum over all rows, so
-// that ragged batches fill the GPU like even ones.  Every wavefront works the
-// cut out for itself, a row a lane.
-__device__ Plan plan_of(const AttendArgs &a, int index) {
-    const int lane = threadIdx.x & 63;
-    const int rows = a.rows.rows;
-    int64_t total = 0, tokens = 0;
-    for (int b = lane; b < rows; b += 64) {
-        const Row r = usable_row(a, b);
-        tokens += r.n;
-        const int units = (r.n * a.group + kCols - 1) / kCols;
-        total += int64_t(units) * span_of(r.length - r.n, r.length - 1, a.window).size();
-    }
-#pragma unroll
-    for (int m = 32; m; m >>= 1) {
-        total += __shfl_xor(total, m);
-        tokens += __shfl_xor(tokens, m);
-    }
-    Plan p;
-    p.any = false;
-    if (tokens > a.rows.tokens) {           // rows that overlap: the launch has no room for them
-        record(a.c, ESP_ERR_SHAPE);
-        return p;
-    }
-    const int64_t share = (total + a.target - 1) / a.target;
-    p.per = int((max(share, int64_t(kWaves)) + kWaves - 1) / kWaves * kWaves);
-    int before = 0;
-    for (int b0 = 0; b0 < rows; b0 += 64) {
+// All threads: the rows from b0 on, `before` tiles before them.
+__device__ __forceinline__ void load_window(const AttendArgs &a, int b0, int before, Window &w) {
+    __syncthreads();
+    if (threadIdx.x < 64) {
+        const int lane = threadIdx.x;
         const Row r = usable_row(a, b0 + lane);
-        const int units = (r.n * a.group + kCols - 1) / kCols;
-        const int chunks = max(1, (span_of(r.length - r.n, r.length - 1, a.window).size() + p.per - 1) / p.per);
-        int sum = units * chunks;
+        const int units = units_of(a, r), tiles = tiles_of(a, r);
+        int end = units * tiles;
 #pragma unroll
         for (int m = 1; m < 64; m <<= 1) {
-            const int v = __shfl_up(sum, m);
-            sum += lane >= m ? v : 0;
+            const int v = __shfl_up(end, m);
+            end += lane >= m ? v : 0;
         }
-        const uint64_t past = __ballot(before + sum > index);
-        if (past) {
-            const int at = __builtin_ctzll(past);
-            const int in_row = index - before - __shfl(sum - units * chunks, at);
-            p.row = Row{__shfl(r.first, at), __shfl(r.n, at), __shfl(r.seq, at), __shfl(r.length, at)};
-            p.chunks = __shfl(chunks, at);
-            p.unit = in_row / p.chunks;
-            p.chunk = in_row - p.unit * p.chunks;
-            p.first = index - p.chunk;
-            p.any = true;
-            break;
-        }
-        before += __shfl(sum, 63);
+        w.row[lane] = r;
+        w.units[lane] = units;
+        w.tiles[lane] = tiles;
+        w.end[lane] = before + end;
     }
-    return p;
+    __syncthreads();
 }
 
 // Maximum and sum over the four lanes that hold one column's tokens.
 __device__ __forceinline__ float across_max(float x) {
-    x = fmaxf(x, __shfl_xor(x, 16));
-    return fmaxf(x, __shfl_xor(x, 32));
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ int across_max(int x) {
+    auto r = __builtin_amdgcn_permlane16_swap(uint32_t(x), uint32_t(x), false, false);
+    x = max(int(r[0]), int(r[1]));
+    r = __builtin_amdgcn_permlane32_swap(uint32_t(x), uint32_t(x), false, false);
+    return max(int(r[0]), int(r[1]));
 }
 __device__ __forceinline__ float across_sum(float x) {
     x += __shfl_xor(x, 16);
@@ -134,15 +117,25 @@ __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
     return (hit >> 7) * 0xffu;
 }
 
-// A unit's running softmax: column n = lane % 16 of the transposed products,
-// so that the statistics of a column lie in the lanes that hold it.
-template <int Dim> struct Running {
-    float4v o[Dim / 16];                    // row 16 dt + 4 (lane / 16) + i of out^T
-    float m, l;                             // largest score (log 2), sum of weights: of this lane's tokens
-    int e;                                  // out is held divided by 2^e
-};
+__device__ __forceinline__ void store_pair(float *p, float x, float y) {
+    __hip_atomic_store(reinterpret_cast<uint64_t *>(p), uint64_t(__float_as_uint(x)) | uint64_t(__float_as_uint(y)) << 32, __ATOMIC_RELAXED,
+                       __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 load_pair(const float *p) {
+    const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t *>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return make_float2(__uint_as_float(uint32_t(v)), __uint_as_float(uint32_t(v >> 32)));
+}
 
-template <typename T, int Dim> __global__ __launch_bounds__(kThreads) void k_attend(AttendArgs a) {
+// Workgroups of one compute unit, by what the registers hold.
+template <int Dim> constexpr int kPerUnit = Dim == 64 ? 3 : 2;
+
+// A wavefront takes 64 tokens of a unit at a time.  Scores and output are held
+// transposed (rows tokens or output values, columns queries), so a query's
+// statistics lie in the lanes that hold its column, and the weights are in
+// place for the value product as the score product leaves them: matrix row
+// 4 g + i of score tile j is token 16 g + 4 j + i.  No data passes through LDS
+// until the wavefronts join.
+template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, kPerUnit<Dim>) void k_attend(AttendArgs a) {
     typedef typename Pack<T>::v8 V8;
     typedef typename Pack<T>::v2 V2;
     constexpr int kSteps = Dim / 32;        // matrix steps of a score
@@ -152,124 +145,249 @@ template <typename T, int Dim> __global__ __launch_bounds__(kThreads) void k_att
     __shared__ float sm[kWaves][kCols], sl[kWaves][kCols];
     __shared__ int se[kWaves];
     __shared__ uint32_t ticket;
+    __shared__ Window win;
 
     const Cache &c = a.c;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
-    const int head = blockIdx.x % c.heads;
-    const Plan p = plan_of(a, blockIdx.x / c.heads);
-    if (!p.any) return;
-    const Row &row = p.row;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
+    const int turn = blockIdx.x / kDies, head = turn % c.heads, me = turn / c.heads * kDies + blockIdx.x % kDies;
+    const int k_group = col >> 2;
 
-    // this lane's query: row r of the unit is (token r / group, query head r % group)
-    const int n_rows = row.n * a.group, r0 = p.unit * kCols, r = r0 + col, p0 = row.length - row.n;
-    const int token = r / a.group, q_head = head * a.group + r - token * a.group;
-    const int pos = r < n_rows ? p0 + token : -1, low = a.window > 0 ? pos - a.window : -1;
-    const int pos_first = p0 + r0 / a.group, pos_last = p0 + (min(r0 + kCols, n_rows) - 1) / a.group;
-    Span span = span_of(pos_first, pos_last, a.window);
-    span.from += p.chunk * p.per;
-    span.to = min(span.to, span.from + p.per);
+    const uint32_t page_step = uint32_t(c.layers * c.heads) * (Page * Dim);
+    const int64_t block_at = int64_t(a.layer * c.heads + head) * (Page * Dim);
+    const uint8_t *keys = c.k + block_at, *vals = c.v + block_at;
+    const float *scales = c.scale + 2 * a.layer * c.heads + head;
 
-    V8 q[kSteps];
-    {
-        const T *src = static_cast<const T *>(a.q.data) + int64_t(row.first + token) * a.q.token + int64_t(q_head) * a.q.head + quad * (Dim / 4);
-#pragma unroll
-        for (int s = 0; s < kSteps; s++) {
-            V8 x{};
-            if (r < n_rows) {
-                if (a.wide) x = *reinterpret_cast<const V8 *>(src + 8 * s);
-                else
-#pragma unroll
-                    for (int j = 0; j < 8; j++) x[j] = src[8 * s + j];
-            }
-            q[s] = x;
-        }
+    // this workgroup's share [at, stop) of the list
+    int64_t total = 0, tokens = 0;
+    for (int b = lane; b < a.rows.rows; b += 64) {
+        const Row r = usable_row(a, b);
+        total += int64_t(units_of(a, r)) * tiles_of(a, r);
+        tokens += r.n;
     }
-
-    Running<Dim> u;
 #pragma unroll
-    for (int d = 0; d < kTiles; d++) u.o[d] = float4v{0, 0, 0, 0};
-    u.m = -INFINITY;
-    u.l = 0.0f;
-    u.e = kNoScale;
+    for (int m = 32; m; m >>= 1) {
+        total += __shfl_xor(total, m);
+        tokens += __shfl_xor(tokens, m);
+    }
+    if (tokens > a.rows.tokens || total > INT32_MAX) {          // rows that overlap, or a list that cannot be numbered
+        if (threadIdx.x == 0) record(c, ESP_ERR_SHAPE);
+        return;
+    }
+    const int all = __builtin_amdgcn_readfirstlane(int(total)), per = max(kWaves, (all + a.groups - 1) / a.groups);
+    if (int64_t(me) * per >= all) return;
+    int at = me * per;
+    const int stop = min(all, at + per);
+    int b0 = 0;
+    load_window(a, 0, 0, win);
+    while (at < stop) {
+        // the row that holds list place `at`
+        uint64_t past = __ballot(win.end[lane] > at);
+        while (!past) {
+            b0 += 64;
+            load_window(a, b0, win.end[63], win);
+            past = __ballot(win.end[lane] > at);
+        }
+        const int in = __builtin_ctzll(past);
+        auto same = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+        const Row row{same(win.row[in].first), same(win.row[in].n), same(win.row[in].seq), same(win.row[in].length)};
+        const int tiles = same(win.tiles[in]), row_at = same(win.end[in]) - same(win.units[in]) * tiles;
+        const int unit = (at - row_at) / tiles, unit_at = row_at + unit * tiles, skip = at - unit_at;
+        const int count = min(tiles - skip, stop - at);
+        const int first_part = unit_at / per, parts = (unit_at + tiles - 1) / per - first_part + 1;
+        at += count;
 
-    const int32_t *table = c.table + int64_t(row.seq) * c.width;
-    const int in_page = c.tokens - 1;
-    const int k_group = col >> 2;           // keys: matrix row 4 k_group + i of tile j is token 16 k_group + 4 j + i
-    for (int t = span.from + wave; t < span.to; t += kWaves) {
-        const int at_k = t * kTile + 16 * k_group, at_v = t * kTile + 16 * quad;
-        int page_k = at_k < row.length ? table[at_k >> c.shift] : -1, page_v = at_v < row.length ? table[at_v >> c.shift] : -1;
-        const bool ok = page_v >= 0 && page_v < c.pages;
-        if (!ok && at_v < row.length && col == 0) record(c, ESP_ERR_SHAPE);
-        if (page_k < 0 || page_k >= c.pages) page_k = 0;       // read something; it is masked below
-        if (!ok) page_v = 0;
-        const uint8_t *kp = c.k + c.block(page_k, a.layer, head) + ((at_k & in_page) + (col & 3)) * Dim + quad * (Dim / 4);
-        const uint8_t *vp = c.v + c.block(page_v, a.layer, head) + (col << c.shift) + (at_v & in_page);
+        // this lane's query: row r of the sequence is (token r / group, query head r % group)
+        const int n_rows = row.n * a.group, r0 = unit * kCols, r = r0 + col, p0 = row.length - row.n;
+        const int token = r / a.group, q_head = head * a.group + r - token * a.group;
+        const int pos = r < n_rows ? p0 + token : -1, low = a.window > 0 ? pos - a.window : -1;
+        const int pos_first = p0 + r0 / a.group, pos_last = p0 + (min(r0 + kCols, n_rows) - 1) / a.group;
+        Span span = span_of(pos_first, pos_last, a.window);
+        span.from += skip;
+        span.to = min(span.to, span.from + count);
+
+        // matrix step 2 s + k of a score takes elements 64 s + 16 quad + 8 k + (0..7)
+        V8 q[kSteps];
+        {
+            const T *src = static_cast<const T *>(a.q.data) + int64_t(row.first + token) * a.q.token + int64_t(q_head) * a.q.head + 16 * quad;
+#pragma unroll
+            for (int s = 0; s < kSteps; s++) {
+                V8 x{};
+                if (r < n_rows) {
+                    const T *from = src + 64 * (s >> 1) + 8 * (s & 1);
+                    if (a.wide) x = *reinterpret_cast<const V8 *>(from);
+                    else
+#pragma unroll
+                        for (int j = 0; j < 8; j++) x[j] = from[j];
+                }
+                q[s] = x;
+            }
+        }
+
+        float4v o[kTiles];                  // row 16 d + 4 quad + i of out^T, divided by 2^o_exp
+#pragma unroll
+        for (int d = 0; d < kTiles; d++) o[d] = float4v{0, 0, 0, 0};
+        float m_run = -INFINITY, l_run = 0.0f;   // largest score (log 2); sum of the weights of this lane's tokens
+        int o_exp = kNoScale;
+
+        // What a wavefront holds of a tile.  Keys: this lane reads 16 bytes of rows of
+        // page_k's tokens; values: 16 tokens of page_v at 16 dimensions.
+        const int32_t *table = c.table + int64_t(row.seq) * c.width;
+        int page_k = -1, page_v = -1;
         uint4v kw[4][Dim / 64], vw[kTiles];
+        float k_scale = 0.0f, v_scale = 0.0f;
+        bool ok = false;
+        auto pages_of = [&](int t) {
+            const int at_k = t * kTile + 16 * k_group, at_v = t * kTile + 16 * quad;
+            page_k = at_k < row.length ? table[at_k / Page] : -1;
+            page_v = at_v < row.length ? table[at_v / Page] : -1;
+        };
+        auto load_keys = [&](int t) {
+            const int at_k = t * kTile + 16 * k_group;
+            const bool k_ok = uint32_t(page_k) < uint32_t(c.pages);
+            ok = uint32_t(page_v) < uint32_t(c.pages);
+            const uint8_t *kp = keys + uint64_t(k_ok ? page_k : 0) * page_step + ((at_k % Page + (col & 3)) * Dim + quad * 16);
 #pragma unroll
-        for (int j = 0; j < 4; j++)
+            for (int j = 0; j < 4; j++)
 #pragma unroll
-            for (int s = 0; s < Dim / 64; s++) kw[j][s] = *reinterpret_cast<const uint4v *>(kp + 4 * j * Dim + 16 * s);
+                for (int s = 0; s < Dim / 64; s++) kw[j][s] = *reinterpret_cast<const uint4v *>(kp + (4 * j * Dim + 64 * s));
+            const float *sp = scales + uint64_t(ok ? page_v : 0) * uint32_t(2 * c.layers * c.heads);
+            k_scale = sp[0];
+            v_scale = sp[c.heads];
+            if (!__all(k_ok))               // past the end, or a page that is not there: zeros
 #pragma unroll
-        for (int d = 0; d < kTiles; d++) vw[d] = *reinterpret_cast<const uint4v *>(vp + (d << (4 + c.shift)));
-        const float k_scale = *c.block_scale(page_v, a.layer, 0, head) * a.scale, v_scale = *c.block_scale(page_v, a.layer, 1, head);
+                for (int j = 0; j < 4; j++)
+#pragma unroll
+                    for (int s = 0; s < Dim / 64; s++) kw[j][s] = k_ok ? kw[j][s] : uint4v{0, 0, 0, 0};
+        };
+        auto load_values = [&](int t) {
+            const int at_v = t * kTile + 16 * quad;
+            const bool v_ok = uint32_t(page_v) < uint32_t(c.pages);
+            const uint8_t *vp = vals + uint64_t(v_ok ? page_v : 0) * page_step + (col * Page + at_v % Page);
+#pragma unroll
+            for (int d = 0; d < kTiles; d++) vw[d] = *reinterpret_cast<const uint4v *>(vp + d * 16 * Page);
+            if (!__all(v_ok)) {
+                if (!v_ok && at_v < row.length && col == 0) record(c, ESP_ERR_SHAPE);
+#pragma unroll
+                for (int d = 0; d < kTiles; d++) vw[d] = v_ok ? vw[d] : uint4v{0, 0, 0, 0};
+            }
+        };
+        auto scores = [&](float4v (&s)[4]) {
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                s[j] = float4v{0, 0, 0, 0};
+#pragma unroll
+                for (int k = 0; k < kSteps; k++) {
+                    const uint4v w = kw[j][k >> 1];
+                    s[j] = product(codes8<V8, V2>(w[2 * (k & 1)], w[2 * (k & 1) + 1]), q[k], s[j]);
+                }
+            }
+        };
+        // The running maximum takes the tile's scores in; the output follows.
+        auto raise = [&](const float4v (&s)[4], float vs, bool held_page) {
+            float top = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < 4; j++)
+#pragma unroll
+                for (int i = 0; i < 4; i++) top = fmaxf(top, s[j][i]);
+            top = across_max(top);
+            if (__any(top > m_run)) {
+                const float m = fmaxf(m_run, top), by = m_run == m ? 1.0f : __builtin_amdgcn_exp2f(m_run - m);
+                m_run = m;
+                l_run *= by;
+#pragma unroll
+                for (int d = 0; d < kTiles; d++) o[d] *= by;
+            }
+            // value scales relative to the largest so far, so that fp16 holds weight * scale
+            int e = max(-126, min(126, int((__float_as_uint(vs) >> 23) & 255) - 127));
+            e = across_max(held_page ? e : kNoScale);
+            if (__any(e > o_exp)) {
+                const float by = ldexpf(1.0f, max(o_exp - e, -200));
+#pragma unroll
+                for (int d = 0; d < kTiles; d++) o[d] *= by;
+                o_exp = e;
+            }
+        };
+        auto values = [&](const half8 (&w)[2]) {
+#pragma unroll
+            for (int d = 0; d < kTiles; d++)
+#pragma unroll
+                for (int k = 0; k < 2; k++) o[d] = product(codes8<half8, half2>(vw[d][2 * k], vw[d][2 * k + 1]), w[k], o[d]);
+        };
 
-        float4v s[4];
+        // Tiles that every row sees whole.  Pages are read two steps ahead, keys and
+        // values one: the next keys are asked for as soon as the scores have used the
+        // present ones, the next values after the value product, so that a wavefront
+        // has a tile in flight nearly always.
+        const int in_window = a.window > 0 ? max(0, pos_last - a.window + kTile) / kTile : 0;
+        const int whole_from = max(span.from, in_window), whole_to = max(whole_from, min(span.to, (pos_first + 1) / kTile));
+        int t = whole_from + wave;
+        if (t < whole_to) {
+            pages_of(t);
+            load_keys(t);
+            load_values(t);
+            if (t + kWaves < whole_to) pages_of(t + kWaves);
+        }
+        for (; t < whole_to; t += kWaves) {
+            float4v s[4];
+            scores(s);
+            const float ks = ok ? k_scale * a.scale : 0.0f, vs = v_scale, none = ok ? 0.0f : -INFINITY;
+            const bool held_page = ok, more = t + kWaves < whole_to;
+            if (more) load_keys(t + kWaves);
 #pragma unroll
-        for (int j = 0; j < 4; j++) {
-            s[j] = float4v{0, 0, 0, 0};
+            for (int j = 0; j < 4; j++)
 #pragma unroll
-            for (int k = 0; k < kSteps; k++) {
-                const uint4v w = kw[j][k >> 1];
-                s[j] = product(codes8<V8, V2>(w[2 * (k & 1)], w[2 * (k & 1) + 1]), q[k], s[j]);
+                for (int i = 0; i < 4; i++) s[j][i] = __builtin_fmaf(s[j][i], ks, none);
+            raise(s, vs, held_page);
+            const float base = m_run == -INFINITY ? 0.0f : m_run - kLift, v_rel = held_page ? ldexpf(vs, -o_exp) : 0.0f;
+            half8 w[2];
+#pragma unroll
+            for (int j = 0; j < 4; j++)
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const float x = __builtin_amdgcn_exp2f(s[j][i] - base);
+                    l_run += x;
+                    w[j >> 1][4 * (j & 1) + i] = _Float16(x * v_rel);
+                }
+            values(w);
+            if (more) {
+                load_values(t + kWaves);
+                if (t + 2 * kWaves < whole_to) pages_of(t + 2 * kWaves);
             }
         }
-        const bool whole = t * kTile + kTile - 1 <= pos_first && (a.window <= 0 || t * kTile > pos_last - a.window) && __all(ok);
-        float top = -INFINITY;
+
+        // The others: at the window's start and at the end.
+        const int head_tiles = min(whole_from, span.to) - span.from, rest = head_tiles + max(0, span.to - whole_to);
+        for (int x = wave; x < rest; x += kWaves) {
+            const int t = x < head_tiles ? span.from + x : whole_to + x - head_tiles, at_v = t * kTile + 16 * quad;
+            pages_of(t);
+            load_keys(t);
+            load_values(t);
+            float4v s[4];
+            scores(s);
+            const float ks = k_scale * a.scale;
 #pragma unroll
-        for (int j = 0; j < 4; j++)
+            for (int j = 0; j < 4; j++)
 #pragma unroll
-            for (int i = 0; i < 4; i++) {
-                const int tt = at_v + 4 * j + i;
-                s[j][i] = whole || (tt <= pos && tt > low && ok) ? s[j][i] * k_scale : -INFINITY;
-                top = fmaxf(top, s[j][i]);
-            }
-        top = across_max(top);
-        if (__any(top > u.m)) {
-            const float m = fmaxf(u.m, top), by = u.m == m ? 1.0f : __builtin_amdgcn_exp2f(u.m - m);
-            u.m = m;
-            u.l *= by;
+                for (int i = 0; i < 4; i++) {
+                    const int tt = at_v + 4 * j + i;
+                    s[j][i] = tt <= pos && tt > low && ok ? s[j][i] * ks : -INFINITY;
+                }
+            raise(s, v_scale, ok);
+            const float base = m_run == -INFINITY ? 0.0f : m_run - kLift, v_rel = ldexpf(v_scale, -o_exp);
+            half8 w[2], seen[2];
 #pragma unroll
-            for (int d = 0; d < kTiles; d++) u.o[d] *= by;
-        }
-        const float base = u.m == -INFINITY ? 0.0f : u.m - kLift;
-        // value scales relative to the largest so far, so that fp16 holds weight * scale
-        int e = max(-126, min(126, int((__float_as_uint(v_scale) >> 23) & 255) - 127));
-        e = ok ? e : kNoScale;
-        e = max(e, __shfl_xor(e, 16));
-        e = max(e, __shfl_xor(e, 32));
-        if (e > u.e) {
-            const float by = ldexpf(1.0f, max(u.e - e, -200));
+            for (int j = 0; j < 4; j++)
 #pragma unroll
-            for (int d = 0; d < kTiles; d++) u.o[d] *= by;
-            u.e = e;
-        }
-        const float v_rel = ldexpf(v_scale, -u.e);
-        half8 w[2], seen[2];
-#pragma unroll
-        for (int j = 0; j < 4; j++)
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                const int tt = at_v + 4 * j + i;
-                const bool vis = whole || (tt <= pos && tt > low && ok);
-                const float x = __builtin_amdgcn_exp2f(s[j][i] - base);
-                u.l += x;
-                w[j >> 1][4 * (j & 1) + i] = vis ? _Float16(x * v_rel) : _Float16(0.0f);
-                seen[j >> 1][4 * (j & 1) + i] = vis ? _Float16(1.0f) : _Float16(0.0f);
-            }
-        if (!whole) {
+                for (int i = 0; i < 4; i++) {
+                    const bool hidden = s[j][i] == -INFINITY;
+                    const float x = __builtin_amdgcn_exp2f(s[j][i] - base);
+                    l_run += x;
+                    w[j >> 1][4 * (j & 1) + i] = hidden ? _Float16(0.0f) : _Float16(x * v_rel);    // 0 * an infinite scale
+                    seen[j >> 1][4 * (j & 1) + i] = hidden ? _Float16(0.0f) : _Float16(1.0f);
+                }
             // tokens past the end hold anything: their codes become 0.  A NaN that
             // only some rows see must not reach the others through 0 * NaN.
-            const int held = ok ? max(0, min(16, row.length - at_v)) : 0;
+            const int held = max(0, min(16, row.length - at_v));
             uint32_t nans = 0;
 #pragma unroll
             for (int i = 0; i < 4; i++) {
@@ -287,104 +405,137 @@ template <typename T, int Dim> __global__ __launch_bounds__(kThreads) void k_att
                     float4v hit{0, 0, 0, 0};
 #pragma unroll
                     for (int k = 0; k < 2; k++) {
-                        const uint32_t x = nan_bytes(vw[d][2 * k]), y = nan_bytes(vw[d][2 * k + 1]);
-                        hit = product(codes8<half8, half2>(x & 0x38383838u, y & 0x38383838u), seen[k], hit);
-                        vw[d][2 * k] &= ~x;
-                        vw[d][2 * k + 1] &= ~y;
+                        const uint32_t y = nan_bytes(vw[d][2 * k]), z = nan_bytes(vw[d][2 * k + 1]);
+                        hit = product(codes8<half8, half2>(y & 0x38383838u, z & 0x38383838u), seen[k], hit);
+                        vw[d][2 * k] &= ~y;
+                        vw[d][2 * k + 1] &= ~z;
                     }
 #pragma unroll
                     for (int i = 0; i < 4; i++)
-                        if (hit[i] > 0.0f) u.o[d][i] = NAN;
+                        if (hit[i] > 0.0f) o[d][i] = NAN;
                 }
             }
+            values(w);
         }
-#pragma unroll
-        for (int d = 0; d < kTiles; d++)
-#pragma unroll
-            for (int k = 0; k < 2; k++) u.o[d] = product(codes8<half8, half2>(vw[d][2 * k], vw[d][2 * k + 1]), w[k], u.o[d]);
-    }
 
-    // join the wavefronts
-    u.l = across_sum(u.l);
+        // join the wavefronts
+        l_run = across_sum(l_run);
+        __syncthreads();                    // the unit before has been read
 #pragma unroll
-    for (int d = 0; d < kTiles; d++) *reinterpret_cast<float4v *>(&so[wave][col][16 * d + 4 * quad]) = u.o[d];
-    if (quad == 0) {
-        sm[wave][col] = u.m;
-        sl[wave][col] = u.l;
-    }
-    if (lane == 0) se[wave] = u.e;
-    __syncthreads();
-    constexpr int kMine = Dim / 16;         // values of a row a thread finishes
-    const int n = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * kMine, rn = r0 + n;
-    float m = -INFINITY, l = 0.0f, o[kMine];
-    int e = kNoScale;
+        for (int d = 0; d < kTiles; d++) *reinterpret_cast<float4v *>(&so[wave][col][16 * d + 4 * quad]) = o[d];
+        if (quad == 0) {
+            sm[wave][col] = m_run;
+            sl[wave][col] = l_run;
+        }
+        if (lane == 0) se[wave] = o_exp;
+        __syncthreads();
+        constexpr int kMine = Dim / 16;     // values of a row a thread finishes
+        const int n = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * kMine, rn = r0 + n;
+        float m = -INFINITY, l = 0.0f, y[kMine];
+        int e = kNoScale;
 #pragma unroll
-    for (int w = 0; w < kWaves; w++) {
-        m = fmaxf(m, sm[w][n]);
-        e = max(e, se[w]);
-    }
+        for (int w = 0; w < kWaves; w++) {
+            m = fmaxf(m, sm[w][n]);
+            e = max(e, se[w]);
+        }
 #pragma unroll
-    for (int i = 0; i < kMine; i++) o[i] = 0.0f;
+        for (int i = 0; i < kMine; i++) y[i] = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kWaves; w++) {
-        const float f = sm[w][n] == m ? 1.0f : __builtin_amdgcn_exp2f(sm[w][n] - m), g = f * ldexpf(1.0f, max(se[w] - e, -200));
-        l = __builtin_fmaf(sl[w][n], f, l);
+        for (int w = 0; w < kWaves; w++) {
+            const float f = sm[w][n] == m ? 1.0f : __builtin_amdgcn_exp2f(sm[w][n] - m), g = f * ldexpf(1.0f, max(se[w] - e, -200));
+            l = __builtin_fmaf(sl[w][n], f, l);
 #pragma unroll
-        for (int i = 0; i < kMine; i++) o[i] = __builtin_fmaf(so[w][n][d0 + i], g, o[i]);
-    }
-    const bool none = m == -INFINITY && !(l != l);
-    float lse = none ? -INFINITY : m - kLift + __builtin_log2f(l);
+            for (int i = 0; i < kMine; i++) y[i] = __builtin_fmaf(so[w][n][d0 + i], g, y[i]);
+        }
+        const bool none = m == -INFINITY && !(l != l);
+        float lse = none ? -INFINITY : m - kLift + __builtin_log2f(l);
 #pragma unroll
-    for (int i = 0; i < kMine; i++) o[i] = none ? 0.0f : ldexpf(o[i] / l, e);
+        for (int i = 0; i < kMine; i++) y[i] = none ? 0.0f : ldexpf(y[i] / l, e);
 
-    if (p.chunks > 1) {
-        // every chunk leaves its part; the last to arrive joins them in order
-        float *mine = a.partial + (int64_t(p.first + p.chunk) * c.heads + head) * (kCols * (Dim + 1));
-        if (rn < n_rows) {
+        if (parts > 1) {
+            // Every part is left in the place of its workgroup (2 w + 1 for a unit that
+            // begins there, 2 w for one that goes on); the last to arrive joins them in
+            // order.  Parts and tickets go by agent-scope atomics, which pass the dies'
+            // own caches: each thread's stores have been performed (vmcnt 0) before the
+            // ticket is drawn.  Fences in their place write the whole cache back and
+            // took 110 of 300 us at 512 workgroups.
+            constexpr int kPart = kCols * (Dim + 2), kBatch = 8;
+            const int64_t step = int64_t(c.heads) * 2 * kPart;
+            float *base = a.partial + int64_t(head) * 2 * kPart, *mine = base + me * step + (me == first_part ? kPart : 0);
+            if (rn < n_rows) {
 #pragma unroll
-            for (int i = 0; i < kMine; i++) mine[n * Dim + d0 + i] = o[i];
-            if (d0 == 0) mine[kCols * Dim + n] = lse;
-        }
-        __threadfence();
-        __syncthreads();
-        uint32_t *counter = a.counters + int64_t(p.first) * c.heads + head;
-        if (threadIdx.x == 0) ticket = atomicAdd(counter, 1u);
-        __syncthreads();
-        if (ticket != uint32_t(p.chunks) - 1) return;
-        __threadfence();
-        if (threadIdx.x == 0) *counter = 0;
-        const float *parts = a.partial + (int64_t(p.first) * c.heads + head) * (kCols * (Dim + 1));
-        const int64_t step = int64_t(c.heads) * (kCols * (Dim + 1));
-        m = -INFINITY;
-        l = 0.0f;
-#pragma unroll
-        for (int i = 0; i < kMine; i++) o[i] = 0.0f;
-        if (rn < n_rows) {
-            bool nan = false;
-            for (int k = 0; k < p.chunks; k++) {
-                const float x = parts[k * step + kCols * Dim + n];
-                nan |= x != x;
-                m = fmaxf(m, x);
+                for (int i = 0; i < kMine; i += 2) store_pair(mine + n * Dim + d0 + i, y[i], y[i + 1]);
+                if (d0 == 0) store_pair(mine + kCols * Dim + 2 * n, lse, 0.0f);
             }
-            for (int k = 0; k < p.chunks; k++) {
-                const float x = parts[k * step + kCols * Dim + n], f = x == -INFINITY ? 0.0f : x == m ? 1.0f : __builtin_amdgcn_exp2f(x - m);
-                l += f;
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            uint32_t *counter = a.counters + int64_t(first_part) * c.heads + head;
+            if (threadIdx.x == 0) ticket = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __syncthreads();
+            if (ticket != uint32_t(parts) - 1) continue;
+            if (threadIdx.x == 0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            m = -INFINITY;
+            l = 0.0f;
 #pragma unroll
-                for (int i = 0; i < kMine; i++) o[i] = __builtin_fmaf(parts[k * step + n * Dim + d0 + i], f, o[i]);
+            for (int i = 0; i < kMine; i++) y[i] = 0.0f;
+            if (rn < n_rows) {
+                bool nan = false;
+                for (int k0 = 0; k0 < parts; k0 += kBatch) {    // so many loads in flight at a time
+                    float x[kBatch];
+                    float2 z[kBatch][kMine / 2];
+#pragma unroll
+                    for (int k = 0; k < kBatch; k++) {
+                        const int part = min(k0 + k, parts - 1);
+                        const float *from = base + (first_part + part) * step + (part ? 0 : kPart);
+                        x[k] = load_pair(from + kCols * Dim + 2 * n).x;
+#pragma unroll
+                        for (int i = 0; i < kMine / 2; i++) z[k][i] = load_pair(from + n * Dim + d0 + 2 * i);
+                    }
+                    float top = m;
+#pragma unroll
+                    for (int k = 0; k < kBatch; k++) {
+                        nan |= x[k] != x[k];
+                        top = fmaxf(top, x[k]);
+                    }
+                    const float by = top == m ? 1.0f : __builtin_amdgcn_exp2f(m - top);
+                    m = top;
+                    l *= by;
+#pragma unroll
+                    for (int i = 0; i < kMine; i++) y[i] *= by;
+#pragma unroll
+                    for (int k = 0; k < kBatch; k++) {
+                        const float f = k0 + k >= parts || x[k] == -INFINITY ? 0.0f : x[k] == m ? 1.0f : __builtin_amdgcn_exp2f(x[k] - m);
+                        l += f;
+#pragma unroll
+                        for (int i = 0; i < kMine / 2; i++) {
+                            y[2 * i] = __builtin_fmaf(z[k][i].x, f, y[2 * i]);
+                            y[2 * i + 1] = __builtin_fmaf(z[k][i].y, f, y[2 * i + 1]);
+                        }
+                    }
+                }
+                if (nan) l = NAN;
             }
-            if (nan) l = NAN;
-        }
-        const bool empty = m == -INFINITY && !(l != l);
-        lse = empty ? -INFINITY : m + __builtin_log2f(l);
+            const bool empty = m == -INFINITY && !(l != l);
+            lse = empty ? -INFINITY : m + __builtin_log2f(l);
 #pragma unroll
-        for (int i = 0; i < kMine; i++) o[i] = empty ? 0.0f : o[i] / l;
+            for (int i = 0; i < kMine; i++) y[i] = empty ? 0.0f : y[i] / l;
+        }
+        if (rn < n_rows) {
+        const int tok = row.first + rn / a.group, qh = head * a.group + rn % a.group;
+        T *dst = static_cast<T *>(a.out.data) + int64_t(tok) * a.out.token + int64_t(qh) * a.out.head + d0;
+        if (a.wide_out) {
+            typedef T Out __attribute__((ext_vector_type(kMine)));
+            Out z;
+#pragma unroll
+            for (int i = 0; i < kMine; i++) z[i] = T(y[i]);
+            *reinterpret_cast<Out *>(dst) = z;
+        } else {
+#pragma unroll
+            for (int i = 0; i < kMine; i++) dst[i] = T(y[i]);
+        }
+        if (d0 == 0 && a.lse) a.lse[int64_t(tok) * a.q_heads + qh] = lse * kLn2;
+        }
     }
-    if (rn >= n_rows) return;
-    const int tok = row.first + rn / a.group, qh = head * a.group + rn % a.group;
-    T *dst = static_cast<T *>(a.out.data) + int64_t(tok) * a.out.token + int64_t(qh) * a.out.head + d0;
-#pragma unroll
-    for (int i = 0; i < kMine; i++) dst[i] = T(o[i]);
-    if (d0 == 0 && a.lse) a.lse[int64_t(tok) * a.q_heads + qh] = lse * kLn2;
 }
 
 }  // namespace esp_kv
@@ -393,13 +544,10 @@ using namespace esp_kv;
 
 namespace {
 
-// Chunks that all heads together are cut into: three workgroups of four
-// wavefronts fit a compute unit, 256 units.
-constexpr int kChunksWanted = 768;
+constexpr int kComputeUnits = 256;
 
 struct Shape {
-    int32_t target;
-    int64_t chunks;                          // bound on the chunks of one head
+    int32_t groups;                          // workgroups of one head
     size_t counters, bytes;
 };
 esp_status shape_of(const esp_kv_cache *c, int32_t rows, int64_t tokens, int32_t q_heads, int32_t max_new, int32_t max_length, Shape &s) {
@@ -407,13 +555,29 @@ esp_status shape_of(const esp_kv_cache *c, int32_t rows, int64_t tokens, int32_t
     if (q_heads < 1 || q_heads > 65536 || q_heads % c->kv_heads) return ESP_ERR_SHAPE;
     const int64_t group = q_heads / c->kv_heads;
     if (int64_t(max_new) * group > INT32_MAX / 2) return ESP_ERR_SHAPE;
-    s.target = kChunksWanted / c->kv_heads > 1 ? kChunksWanted / c->kv_heads : 1;
-    const int64_t by_tokens = tokens * group / kCols + rows, by_rows = int64_t(rows) * ((int64_t(max_new) * group + kCols - 1) / kCols);
-    s.chunks = (by_tokens < by_rows ? by_tokens : by_rows) + s.target;
-    if (s.chunks * c->kv_heads > INT32_MAX) return ESP_ERR_SHAPE;
-    s.counters = (size_t(s.chunks) * c->kv_heads * 4 + 255) / 256 * 256;
-    s.bytes = s.counters + size_t(s.chunks) * c->kv_heads * kCols * (c->head_dim + 1) * 4;
+    const int slots = kComputeUnits * (c->head_dim == 64 ? kPerUnit<64> : kPerUnit<128>);
+    s.groups = slots / c->kv_heads > 1 ? slots / c->kv_heads : 1;
+    // no more than one for every four tiles of the longest rows
+    const int64_t units = int64_t(rows) * ((int64_t(max_new) * group + kCols - 1) / kCols), tiles = units * (max_length / kTile + 2);
+    if (tiles / kWaves + 1 < s.groups) s.groups = int32_t(tiles / kWaves + 1);
+    s.counters = (size_t(s.groups) * c->kv_heads * 4 + 255) / 256 * 256;
+    s.bytes = s.counters + size_t(s.groups) * c->kv_heads * 2 * kCols * (c->head_dim + 2) * 4;
     return ESP_OK;
+}
+
+}  // namespace
+
+namespace {
+
+template <typename T, int Dim> void launch_dim(const AttendArgs &a, unsigned blocks, hipStream_t s) {
+    switch (a.c.tokens) {
+    case 16: k_attend<T, Dim, 16><<<blocks, kThreads, 0, s>>>(a); break;
+    case 32: k_attend<T, Dim, 32><<<blocks, kThreads, 0, s>>>(a); break;
+    default: k_attend<T, Dim, 64><<<blocks, kThreads, 0, s>>>(a); break;
+    }
+}
+template <typename T> void launch(const AttendArgs &a, unsigned blocks, hipStream_t s) {
+    a.c.dim == 64 ? launch_dim<T, 64>(a, blocks, s) : launch_dim<T, 128>(a, blocks, s);
 }
 
 }  // namespace
@@ -442,13 +606,14 @@ extern "C" esp_status esp_kv_attend(const esp_kv_cache *cache, int32_t layer, in
     if (!offsets || !q.data || !out.data) return ESP_ERR_INVALID_ARG;
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < s.bytes) return ESP_ERR_WORKSPACE;
     const bool wide = (reinterpret_cast<uintptr_t>(q.data) & 15) == 0 && q.token_stride % 8 == 0 && q.head_stride % 8 == 0;
+    const bool wide_out = (reinterpret_cast<uintptr_t>(out.data) & 15) == 0 && out.token_stride % 8 == 0 && out.head_stride % 8 == 0;
     const AttendArgs a{cache_of(cache), Rows{offsets, seqs, rows, tokens}, View{q.data, q.token_stride, q.head_stride},
                        View{out.data, out.token_stride, out.head_stride}, lse, scale * kLog2e, layer, q_heads, q_heads / cache->kv_heads,
-                       window, max_new, max_length, s.target, wide, static_cast<uint32_t *>(workspace),
+                       window, max_new, max_length, s.groups, wide, wide_out, static_cast<uint32_t *>(workspace),
                        reinterpret_cast<float *>(static_cast<char *>(workspace) + s.counters)};
     const hipStream_t h = static_cast<hipStream_t>(stream);
-    const unsigned blocks = unsigned(s.chunks * cache->kv_heads);
-    if (type == ESP_KV_BF16) cache->head_dim == 64 ? k_attend<__bf16, 64><<<blocks, kThreads, 0, h>>>(a) : k_attend<__bf16, 128><<<blocks, kThreads, 0, h>>>(a);
-    else cache->head_dim == 64 ? k_attend<_Float16, 64><<<blocks, kThreads, 0, h>>>(a) : k_attend<_Float16, 128><<<blocks, kThreads, 0, h>>>(a);
+    const unsigned blocks = unsigned((s.groups + kDies - 1) / kDies * kDies) * unsigned(cache->kv_heads);
+    if (type == ESP_KV_BF16) launch<__bf16>(a, blocks, h);
+    else launch<_Float16>(a, blocks, h);
     return launched();
 }

@@ -282,7 +282,7 @@ esp_status check_cache(const esp_kv_cache *c) {
     const bool dim = c->head_dim == 64 || c->head_dim == 128;
     if (!page || !dim || c->pages < 1 || c->layers < 1 || c->kv_heads < 1 || c->sequences < 1 || c->table_width < 1) return ESP_ERR_SHAPE;
     if (c->kv_heads > 65536 || c->layers > 65536 || int64_t(c->table_width) * c->page_tokens > INT32_MAX ||
-        int64_t(c->sequences) * c->table_width > INT32_MAX)
+        int64_t(c->sequences) * c->table_width > INT32_MAX || int64_t(c->layers) * c->kv_heads * c->page_tokens * c->head_dim > INT32_MAX)
         return ESP_ERR_SHAPE;
     return ESP_OK;
 }

@@ -19,7 +19,7 @@ CALIB_SOURCES = ["esp_calib.hip"]
 SOURCES = ["esp_api.hip", "esp_kernels.hip", "esp_extras.hip",
            "esp_inst_dense12.hip", "esp_inst_dense34.hip", "esp_inst_dense56.hip", "esp_inst_dense78.hip",
            "esp_inst_csr1234.hip", "esp_inst_csr5678.hip",
-           "kv_write.hip", "kv_pages.hip", "kv_attend.hip"]
+           "kv_write.hip", "kv_pages.hip", "kv_attend.hip", "kv_prompt.hip"]
 ARCH = "gfx950"
 
 COMPILE_FLAGS = [

@@ -1,42 +1,7 @@
 // Attention over the paged 8-bit cache.
-#include "kv_internal.hpp"
+#include "kv_attend.hpp"
 
 namespace esp_kv {
-
-constexpr int kWaves = 4, kThreads = 64 * kWaves;
-constexpr int kTile = 64;                   // tokens a wavefront takes at a time
-constexpr int kDies = 8;                    // workgroups go round the dies
-constexpr int kCols = 16;                   // (token, query head) rows of a unit: the columns of the matrix products
-constexpr float kLift = 14.0f;              // softmax weights are taken times 2^14, so that fp16 holds them down to 2^-38 of the largest
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kNoScale = -200;              // exponent of a value scale below any
-
-struct View {
-    void *data;
-    int64_t token, head;
-};
-
-struct AttendArgs {
-    Cache c;
-    Rows rows;
-    View q, out;
-    float *lse;
-    float scale;                            // softmax scale times log2 e
-    int32_t layer, q_heads, group, window, max_new, max_length, groups, wide, wide_out;
-    uint32_t *counters;
-    float *partial;
-};
-
-// Tiles of tokens that queries at positions [p0, p1] see.
-struct Span {
-    int from, to;                           // tiles [from, to)
-    __device__ __forceinline__ int size() const { return to > from ? to - from : 0; }
-};
-__device__ __forceinline__ Span span_of(int p0, int p1, int window) {
-    if (p1 < 0) return {0, 0};
-    const int first = window > 0 ? max(0, max(p0, 0) - window + 1) : 0;
-    return {first / kTile, p1 / kTile + 1};
-}
 
 // The work of one head is a list of tiles: units (16 rows of queries of one
 // sequence and key head) one after another, every unit of a row with as many
@@ -51,17 +16,6 @@ struct Window {
     int units[64], tiles[64], end[64];      // end: tiles of the list up to and with this row
 };
 
-__device__ __forceinline__ Row usable_row(const AttendArgs &a, int b) {
-    Row r{};
-    if (b < a.rows.rows) {
-        r = row_of(a.c, a.rows, b);
-        if (r.n > a.max_new || r.length > a.max_length) {
-            record(a.c, ESP_ERR_SHAPE);
-            r.n = 0;
-        }
-    }
-    return r;
-}
 __device__ __forceinline__ int units_of(const AttendArgs &a, const Row &r) { return (r.n * a.group + kCols - 1) / kCols; }
 __device__ __forceinline__ int tiles_of(const AttendArgs &a, const Row &r) { return max(1, span_of(r.length - r.n, r.length - 1, a.window).size()); }
 
@@ -106,25 +60,6 @@ __device__ __forceinline__ float across_sum(float x) {
 
 __device__ __forceinline__ float4v product(half8 x, half8 y, float4v z) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(x, y, z, 0, 0, 0); }
 __device__ __forceinline__ float4v product(bhalf8 x, bhalf8 y, float4v z) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, z, 0, 0, 0); }
-
-template <typename T> struct Pack;
-template <> struct Pack<_Float16> { typedef half8 v8; typedef half2 v2; };
-template <> struct Pack<__bf16> { typedef bhalf8 v8; typedef bhalf2 v2; };
-
-// Bytes whose low seven bits are all set: e4m3's NaN.
-__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
-    const uint32_t hit = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
-    return (hit >> 7) * 0xffu;
-}
-
-__device__ __forceinline__ void store_pair(float *p, float x, float y) {
-    __hip_atomic_store(reinterpret_cast<uint64_t *>(p), uint64_t(__float_as_uint(x)) | uint64_t(__float_as_uint(y)) << 32, __ATOMIC_RELAXED,
-                       __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ float2 load_pair(const float *p) {
-    const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t *>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    return make_float2(__uint_as_float(uint32_t(v)), __uint_as_float(uint32_t(v >> 32)));
-}
 
 // Workgroups of one compute unit, by what the registers hold.
 template <int Dim> constexpr int kPerUnit = Dim == 64 ? 3 : 2;
@@ -290,7 +225,7 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 
 #pragma unroll
                 for (int i = 0; i < 4; i++) top = fmaxf(top, s[j][i]);
             top = across_max(top);
-            if (__any(top > m_run)) {
+            if (__any(top > m_run + kSlack)) {
                 const float m = fmaxf(m_run, top), by = m_run == m ? 1.0f : __builtin_amdgcn_exp2f(m_run - m);
                 m_run = m;
                 l_run *= by;
@@ -545,9 +480,12 @@ using namespace esp_kv;
 namespace {
 
 constexpr int kComputeUnits = 256;
+constexpr int kManyRows = 48;                // rows of a sequence and key head from which on k_prompt is taken
 
 struct Shape {
-    int32_t groups;                          // workgroups of one head
+    bool prompt;
+    int32_t groups;                          // k_attend: workgroups of one head
+    int32_t units, splits;                   // k_prompt: units of one head at most, parts of each
     size_t counters, bytes;
 };
 esp_status shape_of(const esp_kv_cache *c, int32_t rows, int64_t tokens, int32_t q_heads, int32_t max_new, int32_t max_length, Shape &s) {
@@ -555,6 +493,23 @@ esp_status shape_of(const esp_kv_cache *c, int32_t rows, int64_t tokens, int32_t
     if (q_heads < 1 || q_heads > 65536 || q_heads % c->kv_heads) return ESP_ERR_SHAPE;
     const int64_t group = q_heads / c->kv_heads;
     if (int64_t(max_new) * group > INT32_MAX / 2) return ESP_ERR_SHAPE;
+    s = Shape{};
+    s.prompt = rows && tokens * group >= int64_t(rows) * kManyRows;
+    if (s.prompt) {
+        const int64_t units = tokens * group / kPromptRows + rows, places = 2 * kComputeUnits;
+        if (units * c->kv_heads > INT32_MAX / 2) return ESP_ERR_SHAPE;
+        // too few units for the GPU: their tiles are shared out, eight at least to a part
+        int64_t splits = places / (units * c->kv_heads);
+        if (splits > max_length / (8 * kTile)) splits = max_length / (8 * kTile);
+        s.units = int32_t(units);
+        s.splits = int32_t(splits > 1 ? splits : 1);
+        if (s.splits > 1) {
+            s.counters = (size_t(units) * c->kv_heads * 4 + 255) / 256 * 256;
+            s.bytes = s.counters + size_t(units) * c->kv_heads * s.splits * kPromptRows * (c->head_dim + 2) * 4;
+        }
+        if (s.bytes < 256) s.bytes = 256;
+        return ESP_OK;
+    }
     const int slots = kComputeUnits * (c->head_dim == 64 ? kPerUnit<64> : kPerUnit<128>);
     s.groups = slots / c->kv_heads > 1 ? slots / c->kv_heads : 1;
     // no more than one for every four tiles of the longest rows
@@ -609,9 +564,13 @@ extern "C" esp_status esp_kv_attend(const esp_kv_cache *cache, int32_t layer, in
     const bool wide_out = (reinterpret_cast<uintptr_t>(out.data) & 15) == 0 && out.token_stride % 8 == 0 && out.head_stride % 8 == 0;
     const AttendArgs a{cache_of(cache), Rows{offsets, seqs, rows, tokens}, View{q.data, q.token_stride, q.head_stride},
                        View{out.data, out.token_stride, out.head_stride}, lse, scale * kLog2e, layer, q_heads, q_heads / cache->kv_heads,
-                       window, max_new, max_length, s.groups, wide, wide_out, static_cast<uint32_t *>(workspace),
+                       window, max_new, max_length, s.groups, wide, wide_out, s.units, s.splits, static_cast<uint32_t *>(workspace),
                        reinterpret_cast<float *>(static_cast<char *>(workspace) + s.counters)};
     const hipStream_t h = static_cast<hipStream_t>(stream);
+    if (s.prompt) {
+        launch_prompt(a, type, h);
+        return launched();
+    }
     const unsigned blocks = unsigned((s.groups + kDies - 1) / kDies * kDies) * unsigned(cache->kv_heads);
     if (type == ESP_KV_BF16) launch<__bf16>(a, blocks, h);
     else launch<_Float16>(a, blocks, h);

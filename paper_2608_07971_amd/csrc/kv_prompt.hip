@@ -1,0 +1,432 @@
+// Attention of many new tokens over the paged 8-bit cache.
+#include "kv_attend.hpp"
+
+namespace esp_kv {
+
+typedef float float16v __attribute__((ext_vector_type(16)));
+
+__device__ __forceinline__ float16v product32(half8 x, half8 y, float16v z) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(x, y, z, 0, 0, 0); }
+__device__ __forceinline__ float16v product32(bhalf8 x, bhalf8 y, float16v z) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, z, 0, 0, 0); }
+
+// Four codes times 2^k (the exponent of `by`).
+__device__ __forceinline__ half8 scaled8(uint32_t a, uint32_t b, float by) {
+    const half2 x = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, by, false), y = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, by, true);
+    const half2 z = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, by, false), w = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, by, true);
+    return half8{x[0], x[1], y[0], y[1], z[0], z[1], w[0], w[1]};
+}
+
+__device__ __forceinline__ float power(int e) { return __uint_as_float(uint32_t(max(1, min(254, e + 127))) << 23); }
+
+// A workgroup takes 128 rows (token, query head) of one sequence and key head
+// against tiles of 64 tokens, each of its four wavefronts 32 rows.  Codes
+// become 16-bit numbers once, on their way into LDS, for all four; while a tile
+// is worked on, the codes of the next are on their way into registers.  Scores
+// and output are held transposed, as in k_attend: the rows of the key matrix
+// are taken in the order that leaves the softmax weights in place for the
+// value product.  V's block scales enter as the codes are widened, K's with the
+// softmax scale.
+template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendArgs a) {
+    typedef typename Pack<T>::v8 V8;
+    typedef typename Pack<T>::v2 V2;
+    constexpr int kSteps = Dim / 16;        // matrix steps of a score
+    constexpr int kOut = Dim / 32;          // matrix tiles of an output
+    constexpr int kKeyUnits = kTile * Dim / 16 / kThreads, kSegs = Dim / 16;
+    constexpr int kKeyRow = Dim * 2;        // bytes of a token in LDS
+    __shared__ __align__(16) uint8_t sk[2][kTile * Dim * 2], sv[2][kTile * Dim * 2];
+    __shared__ uint32_t nans[2];
+    __shared__ uint32_t ticket;
+
+    const Cache &c = a.c;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5;
+    // the dies take stretches of the list [head][part][unit], so that a die's cache holds the keys of few heads
+    const int per_die = gridDim.x / kDies, item = blockIdx.x % kDies * per_die + blockIdx.x / kDies;
+    const int per_head = a.units * a.splits, head = item / per_head;
+    if (head >= c.heads) return;
+    const int part = (item - head * per_head) / a.units, index = a.units - 1 - (item - head * per_head - part * a.units);
+
+    // units: row b's begin at offsets[b] * group / 128 + b at the earliest
+    int lo = 0, hi = a.rows.rows - 1;
+    auto base_of = [&](int b) { return int64_t(a.rows.offsets[b]) * a.group / kPromptRows + b; };
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (base_of(mid) <= index) lo = mid;
+        else hi = mid - 1;
+    }
+    Row row = usable_row(a, lo);
+    row.first = __builtin_amdgcn_readfirstlane(row.first);
+    row.n = __builtin_amdgcn_readfirstlane(row.n);
+    row.seq = __builtin_amdgcn_readfirstlane(row.seq);
+    row.length = __builtin_amdgcn_readfirstlane(row.length);
+    const int64_t unit64 = index - base_of(lo);
+    const int n_rows = row.n * a.group;
+    if (unit64 < 0 || unit64 * kPromptRows >= n_rows) return;
+    const int r0 = __builtin_amdgcn_readfirstlane(int(unit64)) * kPromptRows, p0 = row.length - row.n;
+
+    // this lane's query; the wavefront's and the workgroup's positions
+    const int r = r0 + wave * 32 + col, token = r / a.group, q_head = head * a.group + r - token * a.group;
+    const int pos = r < n_rows ? p0 + token : -1, low = a.window > 0 ? pos - a.window : -1;
+    const int w0 = min(r0 + wave * 32, n_rows - 1), w1 = min(r0 + wave * 32 + 31, n_rows - 1);
+    const int pos_first = p0 + w0 / a.group, pos_last = p0 + w1 / a.group;
+    Span span = span_of(p0 + r0 / a.group, p0 + min(r0 + kPromptRows - 1, n_rows - 1) / a.group, a.window);
+    {
+        const int share = (span.size() + a.splits - 1) / a.splits;
+        span.from += part * share;
+        span.to = min(span.to, span.from + share);
+    }
+
+    // the softmax scale's sign goes into the queries, so that a larger product is a larger score
+    const float scale = fabsf(a.scale);
+    V8 q[kSteps];
+    {
+        const T *src = static_cast<const T *>(a.q.data) + int64_t(row.first + token) * a.q.token + int64_t(q_head) * a.q.head + 8 * half;
+#pragma unroll
+        for (int s = 0; s < kSteps; s++) {
+            V8 x{};
+            if (r < n_rows) {
+                if (a.wide) x = *reinterpret_cast<const V8 *>(src + 16 * s);
+                else
+#pragma unroll
+                    for (int j = 0; j < 8; j++) x[j] = src[16 * s + j];
+            }
+            if (a.scale < 0.0f)
+#pragma unroll
+                for (int j = 0; j < 8; j++) x[j] = -x[j];
+            q[s] = x;
+        }
+    }
+    float16v o[kOut];                       // row 8 b + 4 half + i of tile d: element 32 d + 16 half + 4 b + i
+#pragma unroll
+    for (int d = 0; d < kOut; d++)
+#pragma unroll
+        for (int i = 0; i < 16; i++) o[d][i] = 0.0f;
+    float m_run = -INFINITY, l_run = 0.0f;
+    int o_exp = kNoScale;
+
+    const uint32_t page_step = uint32_t(c.layers * c.heads) * (Page * Dim);
+    const int64_t block_at = int64_t(a.layer * c.heads + head) * (Page * Dim);
+    const uint8_t *keys = c.k + block_at, *vals = c.v + block_at;
+    const float *scales = c.scale + 2 * a.layer * c.heads + head;
+    const int32_t *table = c.table + int64_t(row.seq) * c.width;
+
+    // What is known of a tile's four groups of 16 tokens: lane g has group g's page and scales.
+    struct Group {
+        int page;
+        float k, v;
+    };
+    auto page_of = [&](int t) {
+        const int at = t * kTile + 16 * (lane & 3);
+        const int page = at < row.length ? table[at / Page] : -1;
+        return uint32_t(page) < uint32_t(c.pages) ? page : -1;
+    };
+    auto scales_of = [&](int page) {
+        const float *p = scales + uint64_t(max(page, 0)) * uint32_t(2 * c.layers * c.heads);
+        return Group{page, page >= 0 ? p[0] : 0.0f, page >= 0 ? p[c.heads] : 0.0f};
+    };
+    auto group_page = [&](int page, int g) { return __builtin_amdgcn_readlane(page, g); };
+    auto group_float = [&](float x, int g) { return __uint_as_float(uint32_t(__builtin_amdgcn_readlane(__float_as_uint(x), g))); };
+
+    // Unit u of the keys: 16 bytes of token u / kSegs.  Unit u of the values: 16
+    // tokens of one dimension, in the order in which pages hold them.
+    constexpr int kPageGroups = Page / 16;
+    auto key_token = [&](int i) { return (tid + i * kThreads) / kSegs; };
+    auto value_place = [&](int i, int &d, int &g) {
+        const int u = tid + i * kThreads;
+        d = u / kPageGroups % Dim;
+        g = u / (kPageGroups * Dim) * kPageGroups + u % kPageGroups;
+    };
+    uint4v kw[kKeyUnits], vw[kKeyUnits];
+    auto load = [&](int page) {
+#pragma unroll
+        for (int i = 0; i < kKeyUnits; i++) {
+            const int token = key_token(i), pk = __builtin_amdgcn_readfirstlane(group_page(page, __builtin_amdgcn_readfirstlane(token >> 4)));
+            int d, g;
+            value_place(i, d, g);
+            const int pv = __builtin_amdgcn_readfirstlane(group_page(page, __builtin_amdgcn_readfirstlane(g) / kPageGroups * kPageGroups));
+            kw[i] = pk < 0 ? uint4v{0, 0, 0, 0}
+                           : *reinterpret_cast<const uint4v *>(keys + uint64_t(uint32_t(pk)) * page_step + (token % Page * Dim + tid % kSegs * 16));
+            // a page that ends inside the tile has its first group; its others lie past the end
+            vw[i] = pv < 0 ? uint4v{0, 0, 0, 0}
+                           : *reinterpret_cast<const uint4v *>(vals + uint64_t(uint32_t(pv)) * page_step + (d * Page + g % kPageGroups * 16));
+        }
+    };
+    // Widens the loaded tile into LDS.  Values come out divided by 2^e_ref.  A
+    // 16-byte chunk's place in its row is turned by the row, so that the 16 rows
+    // that a matrix step reads at once lie in different banks.
+    auto key_chunk = [](int token, int chunk) {
+        return Dim == 128 ? token * kKeyRow + ((chunk ^ (token & 15)) << 4) : token * kKeyRow + ((chunk ^ ((token >> 1) & 7)) << 4);
+    };
+    auto value_chunk = [](int d, int chunk) { return d * (kTile * 2) + ((chunk ^ (((d >> 1) & 3) | ((d >> 2) & 4))) << 4); };
+    auto store = [&](int t, int buffer, const Group &grp, int e_ref, bool whole) {
+#pragma unroll
+        for (int i = 0; i < kKeyUnits; i++) {
+            const int token = key_token(i), seg = tid % kSegs;
+            *reinterpret_cast<V8 *>(&sk[buffer][key_chunk(token, 2 * seg)]) = codes8<V8, V2>(kw[i][0], kw[i][1]);
+            *reinterpret_cast<V8 *>(&sk[buffer][key_chunk(token, 2 * seg + 1)]) = codes8<V8, V2>(kw[i][2], kw[i][3]);
+            int d, g;
+            value_place(i, d, g);
+            if (!whole) {                   // tokens past the end hold anything: their codes become 0
+                const int held = row.length - t * kTile - 16 * g;
+                uint32_t bad = 0;
+#pragma unroll
+                for (int x = 0; x < 4; x++) {
+                    const int left = held - 4 * x;
+                    const uint32_t keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
+                    vw[i][x] = vw[i][x] & keep;
+                    bad |= nan_bytes(vw[i][x]);
+                }
+                if (bad) nans[buffer] = t + 1;
+            }
+            const float v = group_float(grp.v, __builtin_amdgcn_readfirstlane(g) / kPageGroups * kPageGroups);
+            const int e = max(-126, min(126, int((__float_as_uint(v) >> 23) & 255) - 127));
+            const float by = power(e - e_ref), rest = ldexpf(v, -e);
+            half8 x = scaled8(vw[i][0], vw[i][1], by), y = scaled8(vw[i][2], vw[i][3], by);
+            if (rest != 1.0f) {             // a scale that is no power of two: one more rounding, to fp16
+#pragma unroll
+                for (int j = 0; j < 8; j++) {
+                    x[j] = _Float16(float(x[j]) * rest);
+                    y[j] = _Float16(float(y[j]) * rest);
+                }
+            }
+            *reinterpret_cast<half8 *>(&sv[buffer][value_chunk(d, 2 * g)]) = x;
+            *reinterpret_cast<half8 *>(&sv[buffer][value_chunk(d, 2 * g + 1)]) = y;
+        }
+    };
+    auto largest = [&](const Group &grp) {  // exponent of the largest value scale of a tile
+        int e = kNoScale;
+#pragma unroll
+        for (int g = 0; g < 4; g++) {
+            const int x = int((uint32_t(__builtin_amdgcn_readlane(__float_as_uint(grp.v), g)) >> 23) & 255) - 127;
+            if (group_page(grp.page, g) >= 0) e = max(e, max(-126, min(126, x)));
+        }
+        return e;
+    };
+    // whether every row of the workgroup sees all of a tile
+    const int first_of_all = p0 + r0 / a.group, last_of_all = p0 + min(r0 + kPromptRows - 1, n_rows - 1) / a.group;
+    auto inside = [&](int t) { return t * kTile + kTile - 1 <= first_of_all && (a.window <= 0 || t * kTile > last_of_all - a.window); };
+
+    if (tid < 2) nans[tid] = 0;
+    Group now{-1, 0.0f, 0.0f}, next{-1, 0.0f, 0.0f};
+    int after = -1;                         // pages of the tile after next
+    int e_now = kNoScale;
+    if (span.from < span.to) {
+        now = scales_of(page_of(span.from));
+        load(now.page);
+        if (span.from + 1 < span.to) after = page_of(span.from + 1);
+        e_now = largest(now);
+        __syncthreads();
+        store(span.from, 0, now, e_now, inside(span.from));
+    }
+    __syncthreads();
+    // key row m of a matrix tile is the token whose bits 2 and 3 are those of m exchanged
+    const int key_row = (col & 19) | (col & 4) << 1 | (col & 8) >> 1;
+    const int value_row = (col & 4) << 2 | (col & 24) >> 1 | (col & 3);
+    for (int t = span.from; t < span.to; t++) {
+        const int buffer = (t - span.from) & 1;
+        const bool more = t + 1 < span.to;
+        if (more) {
+            next = scales_of(after);
+            load(next.page);
+            if (t + 2 < span.to) after = page_of(t + 2);
+        }
+        float16v s[2];
+#pragma unroll
+        for (int j = 0; j < 2; j++) {
+#pragma unroll
+            for (int i = 0; i < 16; i++) s[j][i] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < kSteps; k++)
+                s[j] = product32(*reinterpret_cast<const V8 *>(&sk[buffer][key_chunk(32 * j + key_row, 2 * k + half)]), q[k], s[j]);
+        }
+        // s[j][4 b + i]: token 32 j + 16 (b / 2) + 8 half + 4 (b % 2) + i, so that
+        // s[g / 2][8 (g % 2) + i] is token 8 half + i of group g
+        float ks[4];
+        bool there = true;
+#pragma unroll
+        for (int g = 0; g < 4; g++) {
+            ks[g] = group_float(now.k, g) * scale;
+            there &= group_page(now.page, g) >= 0;
+        }
+        const bool whole = there && t * kTile + kTile - 1 <= pos_first && (a.window <= 0 || t * kTile > pos_last - a.window);
+        if (!whole) {
+            bool lost = false;
+#pragma unroll
+            for (int g = 0; g < 4; g++) {
+                const bool ok = group_page(now.page, g) >= 0;
+                lost |= !ok && t * kTile + 16 * g < row.length;
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    const int tt = t * kTile + 16 * g + 8 * half + i;
+                    s[g >> 1][8 * (g & 1) + i] = tt <= pos && tt > low && ok ? s[g >> 1][8 * (g & 1) + i] * ks[g] : -INFINITY;
+                }
+                ks[g] = 1.0f;
+            }
+            if (lost && lane == 0) record(c, ESP_ERR_SHAPE);
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int g = 0; g < 4; g++) {
+            float x = s[g >> 1][8 * (g & 1)];
+#pragma unroll
+            for (int i = 1; i < 8; i++) x = fmaxf(x, s[g >> 1][8 * (g & 1) + i]);
+            top = fmaxf(top, x * ks[g]);    // ks >= 0
+        }
+        {
+            const auto z = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+            top = fmaxf(__uint_as_float(z[0]), __uint_as_float(z[1]));
+        }
+        if (__any(top > m_run + kSlack) || e_now > o_exp) {
+            const float m = fmaxf(m_run, top), by = m_run == m ? 1.0f : __builtin_amdgcn_exp2f(m_run - m);
+            const float down = by * (e_now > o_exp ? ldexpf(1.0f, max(o_exp - e_now, -200)) : 1.0f);
+            m_run = m;
+            o_exp = max(o_exp, e_now);
+            l_run *= by;
+#pragma unroll
+            for (int d = 0; d < kOut; d++) o[d] *= down;
+        }
+        const float base = m_run == -INFINITY ? 0.0f : m_run - kLift;
+        half8 w[4];
+#pragma unroll
+        for (int g = 0; g < 4; g++)
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[g >> 1][8 * (g & 1) + i], ks[g], -base));
+                l_run += x;
+                w[g][i] = _Float16(x);
+            }
+        if (nans[buffer] == uint32_t(t + 1)) {
+            // A NaN value that only some rows see must not reach the others through
+            // 0 * NaN: it is looked for token by token, then it becomes 0 in LDS.
+            for (int x = 0; x < kTile; x++) {
+                const int tt = t * kTile + x;
+                if (tt > pos || tt <= low) continue;
+#pragma unroll
+                for (int d = 0; d < kOut; d++)
+#pragma unroll
+                    for (int i = 0; i < 16; i++) {
+                        const _Float16 v = *reinterpret_cast<const _Float16 *>(&sv[buffer][value_chunk(32 * d + 16 * half + i, x >> 3) + 2 * (x & 7)]);
+                        if (v != v) o[d][i] = NAN;
+                    }
+            }
+            __syncthreads();                // the same for the whole workgroup
+            for (int x = tid; x < kTile * Dim; x += kThreads) {
+                _Float16 *v = reinterpret_cast<_Float16 *>(sv[buffer]) + x;
+                if (*v != *v) *v = _Float16(0.0f);
+            }
+            __syncthreads();
+        }
+#pragma unroll
+        for (int d = 0; d < kOut; d++)
+#pragma unroll
+            for (int g = 0; g < 4; g++)
+                o[d] = product32(*reinterpret_cast<const half8 *>(&sv[buffer][value_chunk(32 * d + value_row, 2 * g + half)]), w[g], o[d]);
+        if (more) {
+            e_now = max(o_exp, largest(next));
+            store(t + 1, buffer ^ 1, next, e_now, inside(t + 1));
+            now = next;
+        }
+        __syncthreads();
+    }
+
+    // finish: element 32 d + 16 half + x of this lane's row is o[d][x]
+    {
+        const auto z = __builtin_amdgcn_permlane32_swap(__float_as_uint(l_run), __float_as_uint(l_run), false, false);
+        l_run = __uint_as_float(z[0]) + __uint_as_float(z[1]);
+    }
+    const bool none = m_run == -INFINITY && !(l_run != l_run);
+    float lse = none ? -INFINITY : m_run - kLift + __builtin_log2f(l_run);
+    const float by = none ? 0.0f : ldexpf(1.0f, max(o_exp, -149)) / l_run;
+#pragma unroll
+    for (int d = 0; d < kOut; d++)
+#pragma unroll
+        for (int i = 0; i < 16; i++) o[d][i] = none ? 0.0f : o[d][i] * by;
+
+    if (a.splits > 1) {
+        // as in k_attend: parts by agent-scope atomics, the last to arrive joins them in order
+        constexpr int kPart = kPromptRows * (Dim + 2);
+        const int64_t unit_id = int64_t(head) * a.units + index;
+        float *parts = a.partial + unit_id * a.splits * kPart + (wave * 32 + col) * (Dim + 2);
+        if (r < n_rows) {
+            float *mine = parts + part * kPart;
+#pragma unroll
+            for (int d = 0; d < kOut; d++)
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) store_pair(mine + 32 * d + 16 * half + i, o[d][i], o[d][i + 1]);
+            if (half == 0) store_pair(mine + Dim, lse, 0.0f);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (tid == 0) ticket = __hip_atomic_fetch_add(a.counters + unit_id, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __syncthreads();
+        if (ticket != uint32_t(a.splits) - 1) return;
+        if (tid == 0) __hip_atomic_store(a.counters + unit_id, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (r >= n_rows) return;
+        float m = -INFINITY, l = 0.0f;
+#pragma unroll
+        for (int d = 0; d < kOut; d++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) o[d][i] = 0.0f;
+        bool nan = false;
+        for (int k = 0; k < a.splits; k++) {
+            const float *from = parts + k * kPart;
+            const float x = load_pair(from + Dim).x, m_new = fmaxf(m, x), was = m == m_new ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);
+            const float f = x == -INFINITY ? 0.0f : x == m_new ? 1.0f : __builtin_amdgcn_exp2f(x - m_new);
+            nan |= x != x;
+            m = m_new;
+            l = l * was + f;
+#pragma unroll
+            for (int d = 0; d < kOut; d++)
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) {
+                    const float2 z = load_pair(from + 32 * d + 16 * half + i);
+                    o[d][i] = __builtin_fmaf(z.x, f, o[d][i] * was);
+                    o[d][i + 1] = __builtin_fmaf(z.y, f, o[d][i + 1] * was);
+                }
+        }
+        if (nan) l = NAN;
+        const bool empty = m == -INFINITY && !nan;
+        lse = empty ? -INFINITY : m + __builtin_log2f(l);
+#pragma unroll
+        for (int d = 0; d < kOut; d++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) o[d][i] = empty ? 0.0f : o[d][i] / l;
+    }
+    if (r >= n_rows) return;
+    T *dst = static_cast<T *>(a.out.data) + int64_t(row.first + token) * a.out.token + int64_t(q_head) * a.out.head + 16 * half;
+#pragma unroll
+    for (int d = 0; d < kOut; d++) {
+        V8 x, y;
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            x[i] = T(o[d][i]);
+            y[i] = T(o[d][8 + i]);
+        }
+        if (a.wide_out) {
+            *reinterpret_cast<V8 *>(dst + 32 * d) = x;
+            *reinterpret_cast<V8 *>(dst + 32 * d + 8) = y;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                dst[32 * d + i] = x[i];
+                dst[32 * d + 8 + i] = y[i];
+            }
+        }
+    }
+    if (half == 0 && a.lse) a.lse[int64_t(row.first + token) * a.q_heads + q_head] = lse * kLn2;
+}
+
+template <typename T, int Dim> static void launch_dim(const AttendArgs &a, unsigned blocks, hipStream_t s) {
+    switch (a.c.tokens) {
+    case 16: k_prompt<T, Dim, 16><<<blocks, kThreads, 0, s>>>(a); break;
+    case 32: k_prompt<T, Dim, 32><<<blocks, kThreads, 0, s>>>(a); break;
+    default: k_prompt<T, Dim, 64><<<blocks, kThreads, 0, s>>>(a); break;
+    }
+}
+
+void launch_prompt(const AttendArgs &a, int32_t type, hipStream_t s) {
+    const int64_t items = int64_t(a.units) * a.splits * a.c.heads;
+    const unsigned blocks = unsigned((items + kDies - 1) / kDies * kDies);
+    if (type == ESP_KV_BF16) a.c.dim == 64 ? launch_dim<__bf16, 64>(a, blocks, s) : launch_dim<__bf16, 128>(a, blocks, s);
+    else a.c.dim == 64 ? launch_dim<_Float16, 64>(a, blocks, s) : launch_dim<_Float16, 128>(a, blocks, s);
+}
+
+}  // namespace esp_kv

@@ -15,8 +15,6 @@ __device__ __forceinline__ half8 scaled8(uint32_t a, uint32_t b, float by) {
     return half8{x[0], x[1], y[0], y[1], z[0], z[1], w[0], w[1]};
 }
 
-__device__ __forceinline__ float power(int e) { return __uint_as_float(uint32_t(max(1, min(254, e + 127))) << 23); }
-
 // A workgroup takes 128 rows (token, query head) of one sequence and key head
 // against tiles of 64 tokens, each of its four wavefronts 32 rows.  Codes
 // become 16-bit numbers once, on their way into LDS, for all four; while a tile
@@ -32,7 +30,8 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 
     constexpr int kOut = Dim / 32;          // matrix tiles of an output
     constexpr int kKeyUnits = kTile * Dim / 16 / kThreads, kSegs = Dim / 16;
     constexpr int kKeyRow = Dim * 2;        // bytes of a token in LDS
-    __shared__ __align__(16) uint8_t sk[2][kTile * Dim * 2], sv[2][kTile * Dim * 2];
+    constexpr int kHalf = kTile * Dim * 2;  // bytes of a tile's keys in LDS, and of its values
+    __shared__ __align__(16) uint8_t lds[2][2 * kHalf];          // two tiles: keys, then values
     __shared__ uint32_t nans[2];
     __shared__ uint32_t ticket;
 
@@ -108,7 +107,8 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 
     const float *scales = c.scale + 2 * a.layer * c.heads + head;
     const int32_t *table = c.table + int64_t(row.seq) * c.width;
 
-    // What is known of a tile's four groups of 16 tokens: lane g has group g's page and scales.
+    // What is known of a tile's four groups of 16 tokens: lane g (and 4 + g, ...) has
+    // group g's page (-1 none) and scales.
     struct Group {
         int page;
         float k, v;
@@ -120,52 +120,59 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 
     };
     auto scales_of = [&](int page) {
         const float *p = scales + uint64_t(max(page, 0)) * uint32_t(2 * c.layers * c.heads);
-        return Group{page, page >= 0 ? p[0] : 0.0f, page >= 0 ? p[c.heads] : 0.0f};
+        return Group{page, p[0], p[c.heads]};
     };
-    auto group_page = [&](int page, int g) { return __builtin_amdgcn_readlane(page, g); };
-    auto group_float = [&](float x, int g) { return __uint_as_float(uint32_t(__builtin_amdgcn_readlane(__float_as_uint(x), g))); };
+    auto lane_float = [&](float x, int g) { return __uint_as_float(uint32_t(__builtin_amdgcn_readlane(__float_as_uint(x), g))); };
+    auto exponent = [](float x) { return max(-126, min(126, int((__float_as_uint(x) >> 23) & 255) - 127)); };
 
     // Unit u of the keys: 16 bytes of token u / kSegs.  Unit u of the values: 16
-    // tokens of one dimension, in the order in which pages hold them.
+    // tokens of one dimension, in the order in which pages hold them.  A wavefront's
+    // units of one kind lie in one page.
     constexpr int kPageGroups = Page / 16;
-    auto key_token = [&](int i) { return (tid + i * kThreads) / kSegs; };
-    auto value_place = [&](int i, int &d, int &g) {
-        const int u = tid + i * kThreads;
-        d = u / kPageGroups % Dim;
-        g = u / (kPageGroups * Dim) * kPageGroups + u % kPageGroups;
-    };
+    uint32_t key_from[kKeyUnits], value_from[kKeyUnits];         // place in the page
+    uint32_t key_to[kKeyUnits], value_to[kKeyUnits];             // and in LDS
+    int key_group[kKeyUnits], value_group[kKeyUnits], value_first[kKeyUnits];
+    // A 16-byte chunk's place in its row of LDS is turned by the row, so that the 16
+    // rows that a matrix step reads at once lie in different banks.
+    auto key_turn = [](int token) { return Dim == 128 ? token & 15 : (token >> 1) & 7; };
+    auto value_turn = [](int d) { return ((d >> 1) & 3) | ((d >> 2) & 4); };
+#pragma unroll
+    for (int i = 0; i < kKeyUnits; i++) {
+        const int u = tid + i * kThreads, token = u / kSegs, seg = u % kSegs;
+        key_from[i] = token % Page * Dim + seg * 16;
+        key_to[i] = token * kKeyRow + ((2 * seg ^ key_turn(token)) << 4);
+        key_group[i] = __builtin_amdgcn_readfirstlane(token >> 4);
+        const int d = u / kPageGroups % Dim, first = u / (kPageGroups * Dim) * kPageGroups, g = first + u % kPageGroups;
+        value_from[i] = d * Page + g % kPageGroups * 16;
+        value_to[i] = kHalf + d * (kTile * 2) + ((2 * g ^ value_turn(d)) << 4);
+        value_group[i] = g;
+        value_first[i] = __builtin_amdgcn_readfirstlane(first);
+    }
     uint4v kw[kKeyUnits], vw[kKeyUnits];
+    // Pages that are not there are read as page 0: what came in is masked.
     auto load = [&](int page) {
 #pragma unroll
         for (int i = 0; i < kKeyUnits; i++) {
-            const int token = key_token(i), pk = __builtin_amdgcn_readfirstlane(group_page(page, __builtin_amdgcn_readfirstlane(token >> 4)));
-            int d, g;
-            value_place(i, d, g);
-            const int pv = __builtin_amdgcn_readfirstlane(group_page(page, __builtin_amdgcn_readfirstlane(g) / kPageGroups * kPageGroups));
-            kw[i] = pk < 0 ? uint4v{0, 0, 0, 0}
-                           : *reinterpret_cast<const uint4v *>(keys + uint64_t(uint32_t(pk)) * page_step + (token % Page * Dim + tid % kSegs * 16));
-            // a page that ends inside the tile has its first group; its others lie past the end
-            vw[i] = pv < 0 ? uint4v{0, 0, 0, 0}
-                           : *reinterpret_cast<const uint4v *>(vals + uint64_t(uint32_t(pv)) * page_step + (d * Page + g % kPageGroups * 16));
+            const uint32_t pk = max(__builtin_amdgcn_readlane(page, key_group[i]), 0), pv = max(__builtin_amdgcn_readlane(page, value_first[i]), 0);
+            kw[i] = *reinterpret_cast<const uint4v *>(keys + uint64_t(pk) * page_step + key_from[i]);
+            vw[i] = *reinterpret_cast<const uint4v *>(vals + uint64_t(pv) * page_step + value_from[i]);
         }
     };
-    // Widens the loaded tile into LDS.  Values come out divided by 2^e_ref.  A
-    // 16-byte chunk's place in its row is turned by the row, so that the 16 rows
-    // that a matrix step reads at once lie in different banks.
-    auto key_chunk = [](int token, int chunk) {
-        return Dim == 128 ? token * kKeyRow + ((chunk ^ (token & 15)) << 4) : token * kKeyRow + ((chunk ^ ((token >> 1) & 7)) << 4);
-    };
-    auto value_chunk = [](int d, int chunk) { return d * (kTile * 2) + ((chunk ^ (((d >> 1) & 3) | ((d >> 2) & 4))) << 4); };
+    // Widens the loaded tile into LDS, values divided by 2^e_ref.
     auto store = [&](int t, int buffer, const Group &grp, int e_ref, bool whole) {
+        const int e = exponent(grp.v);
+        const float by = __uint_as_float(uint32_t(max(1, min(254, e - e_ref + 127))) << 23), rest = ldexpf(grp.v, -e);
+        const bool powers = __all(rest == 1.0f || grp.page < 0);
 #pragma unroll
         for (int i = 0; i < kKeyUnits; i++) {
-            const int token = key_token(i), seg = tid % kSegs;
-            *reinterpret_cast<V8 *>(&sk[buffer][key_chunk(token, 2 * seg)]) = codes8<V8, V2>(kw[i][0], kw[i][1]);
-            *reinterpret_cast<V8 *>(&sk[buffer][key_chunk(token, 2 * seg + 1)]) = codes8<V8, V2>(kw[i][2], kw[i][3]);
-            int d, g;
-            value_place(i, d, g);
-            if (!whole) {                   // tokens past the end hold anything: their codes become 0
-                const int held = row.length - t * kTile - 16 * g;
+            V8 *to = reinterpret_cast<V8 *>(&lds[buffer][key_to[i]]), *to2 = reinterpret_cast<V8 *>(&lds[buffer][key_to[i] ^ 16]);
+            *to = codes8<V8, V2>(kw[i][0], kw[i][1]);
+            *to2 = codes8<V8, V2>(kw[i][2], kw[i][3]);
+        }
+#pragma unroll
+        for (int i = 0; i < kKeyUnits; i++) {
+            if (!whole) {                   // past the end, or without a page: codes of 0
+                const int held = __builtin_amdgcn_readlane(grp.page, value_first[i]) < 0 ? 0 : row.length - t * kTile - 16 * value_group[i];
                 uint32_t bad = 0;
 #pragma unroll
                 for (int x = 0; x < 4; x++) {
@@ -176,33 +183,29 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 
                 }
                 if (bad) nans[buffer] = t + 1;
             }
-            const float v = group_float(grp.v, __builtin_amdgcn_readfirstlane(g) / kPageGroups * kPageGroups);
-            const int e = max(-126, min(126, int((__float_as_uint(v) >> 23) & 255) - 127));
-            const float by = power(e - e_ref), rest = ldexpf(v, -e);
-            half8 x = scaled8(vw[i][0], vw[i][1], by), y = scaled8(vw[i][2], vw[i][3], by);
-            if (rest != 1.0f) {             // a scale that is no power of two: one more rounding, to fp16
+            const float f = lane_float(by, value_first[i]);
+            half8 x = scaled8(vw[i][0], vw[i][1], f), y = scaled8(vw[i][2], vw[i][3], f);
+            if (!powers) {                  // a scale that is no power of two: one more rounding, to fp16
+                const float z = __builtin_amdgcn_readlane(grp.page, value_first[i]) < 0 ? 0.0f : lane_float(rest, value_first[i]);
 #pragma unroll
                 for (int j = 0; j < 8; j++) {
-                    x[j] = _Float16(float(x[j]) * rest);
-                    y[j] = _Float16(float(y[j]) * rest);
+                    x[j] = _Float16(float(x[j]) * z);
+                    y[j] = _Float16(float(y[j]) * z);
                 }
             }
-            *reinterpret_cast<half8 *>(&sv[buffer][value_chunk(d, 2 * g)]) = x;
-            *reinterpret_cast<half8 *>(&sv[buffer][value_chunk(d, 2 * g + 1)]) = y;
+            *reinterpret_cast<half8 *>(&lds[buffer][value_to[i]]) = x;
+            *reinterpret_cast<half8 *>(&lds[buffer][value_to[i] ^ 16]) = y;
         }
     };
     auto largest = [&](const Group &grp) {  // exponent of the largest value scale of a tile
-        int e = kNoScale;
-#pragma unroll
-        for (int g = 0; g < 4; g++) {
-            const int x = int((uint32_t(__builtin_amdgcn_readlane(__float_as_uint(grp.v), g)) >> 23) & 255) - 127;
-            if (group_page(grp.page, g) >= 0) e = max(e, max(-126, min(126, x)));
-        }
-        return e;
+        const int e = grp.page >= 0 ? exponent(grp.v) : kNoScale;
+        return max(max(__builtin_amdgcn_readlane(e, 0), __builtin_amdgcn_readlane(e, 1)), max(__builtin_amdgcn_readlane(e, 2), __builtin_amdgcn_readlane(e, 3)));
     };
     // whether every row of the workgroup sees all of a tile
     const int first_of_all = p0 + r0 / a.group, last_of_all = p0 + min(r0 + kPromptRows - 1, n_rows - 1) / a.group;
-    auto inside = [&](int t) { return t * kTile + kTile - 1 <= first_of_all && (a.window <= 0 || t * kTile > last_of_all - a.window); };
+    auto inside = [&](int t, const Group &grp) {
+        return t * kTile + kTile - 1 <= first_of_all && (a.window <= 0 || t * kTile > last_of_all - a.window) && __all(grp.page >= 0);
+    };
 
     if (tid < 2) nans[tid] = 0;
     Group now{-1, 0.0f, 0.0f}, next{-1, 0.0f, 0.0f};
@@ -214,12 +217,14 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 
         if (span.from + 1 < span.to) after = page_of(span.from + 1);
         e_now = largest(now);
         __syncthreads();
-        store(span.from, 0, now, e_now, inside(span.from));
+        store(span.from, 0, now, e_now, inside(span.from, now));
     }
     __syncthreads();
     // key row m of a matrix tile is the token whose bits 2 and 3 are those of m exchanged
     const int key_row = (col & 19) | (col & 4) << 1 | (col & 8) >> 1;
     const int value_row = (col & 4) << 2 | (col & 24) >> 1 | (col & 3);
+    const uint32_t key_at = key_row * kKeyRow + ((half ^ key_turn(key_row)) << 4);
+    const uint32_t value_at = kHalf + value_row * (kTile * 2) + ((half ^ value_turn(value_row)) << 4);
     for (int t = span.from; t < span.to; t++) {
         const int buffer = (t - span.from) & 1;
         const bool more = t + 1 < span.to;
@@ -235,23 +240,21 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 
             for (int i = 0; i < 16; i++) s[j][i] = 0.0f;
 #pragma unroll
             for (int k = 0; k < kSteps; k++)
-                s[j] = product32(*reinterpret_cast<const V8 *>(&sk[buffer][key_chunk(32 * j + key_row, 2 * k + half)]), q[k], s[j]);
+                s[j] = product32(*reinterpret_cast<const V8 *>(&lds[buffer][(key_at ^ (k << 5)) + j * 32 * kKeyRow]), q[k], s[j]);
         }
         // s[j][4 b + i]: token 32 j + 16 (b / 2) + 8 half + 4 (b % 2) + i, so that
         // s[g / 2][8 (g % 2) + i] is token 8 half + i of group g
         float ks[4];
-        bool there = true;
+        const float scaled = now.k * scale;
+        const bool there = __all(now.page >= 0);
 #pragma unroll
-        for (int g = 0; g < 4; g++) {
-            ks[g] = group_float(now.k, g) * scale;
-            there &= group_page(now.page, g) >= 0;
-        }
+        for (int g = 0; g < 4; g++) ks[g] = lane_float(scaled, g);
         const bool whole = there && t * kTile + kTile - 1 <= pos_first && (a.window <= 0 || t * kTile > pos_last - a.window);
         if (!whole) {
             bool lost = false;
 #pragma unroll
             for (int g = 0; g < 4; g++) {
-                const bool ok = group_page(now.page, g) >= 0;
+                const bool ok = __builtin_amdgcn_readlane(now.page, g) >= 0;
                 lost |= !ok && t * kTile + 16 * g < row.length;
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
@@ -303,13 +306,13 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 
                 for (int d = 0; d < kOut; d++)
 #pragma unroll
                     for (int i = 0; i < 16; i++) {
-                        const _Float16 v = *reinterpret_cast<const _Float16 *>(&sv[buffer][value_chunk(32 * d + 16 * half + i, x >> 3) + 2 * (x & 7)]);
+                        const _Float16 v = *reinterpret_cast<const _Float16 *>(&lds[buffer][kHalf + (32 * d + 16 * half + i) * (kTile * 2) + ((x >> 3 ^ value_turn(16 * half + i)) << 4) + 2 * (x & 7)]);
                         if (v != v) o[d][i] = NAN;
                     }
             }
             __syncthreads();                // the same for the whole workgroup
             for (int x = tid; x < kTile * Dim; x += kThreads) {
-                _Float16 *v = reinterpret_cast<_Float16 *>(sv[buffer]) + x;
+                _Float16 *v = reinterpret_cast<_Float16 *>(lds[buffer] + kHalf) + x;
                 if (*v != *v) *v = _Float16(0.0f);
             }
             __syncthreads();
@@ -318,10 +321,10 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 
         for (int d = 0; d < kOut; d++)
 #pragma unroll
             for (int g = 0; g < 4; g++)
-                o[d] = product32(*reinterpret_cast<const half8 *>(&sv[buffer][value_chunk(32 * d + value_row, 2 * g + half)]), w[g], o[d]);
+                o[d] = product32(*reinterpret_cast<const half8 *>(&lds[buffer][(value_at ^ (g << 5)) + d * 32 * (kTile * 2)]), w[g], o[d]);
         if (more) {
             e_now = max(o_exp, largest(next));
-            store(t + 1, buffer ^ 1, next, e_now, inside(t + 1));
+            store(t + 1, buffer ^ 1, next, e_now, inside(t + 1, next));
             now = next;
         }
         __syncthreads();

@@ -480,7 +480,12 @@ using namespace esp_kv;
 namespace {
 
 constexpr int kComputeUnits = 256;
-constexpr int kManyRows = 48;                // rows of a sequence and key head from which on k_prompt is taken
+// k_prompt from kManyRows rows of a sequence and key head on, if there are kManyUnits units.
+// Measured on 8 key heads of 128 with 4 query heads each (k_prompt against k_attend):
+// 8 sequences of 8,192 tokens, 64 rows 89 / 90 us, 128 rows 105 / 156, 256 rows 183 / 300;
+// 64 of 2,048, 64 rows 177 / 160, 128 rows 204 / 304; a single one of 16,384, 256 rows
+// (24 units) 87 / 63; of 8,192, 1,200 rows (80 units) 78 / 162.
+constexpr int kManyRows = 96, kManyUnits = 64;
 
 struct Shape {
     bool prompt;
@@ -494,9 +499,10 @@ esp_status shape_of(const esp_kv_cache *c, int32_t rows, int64_t tokens, int32_t
     const int64_t group = q_heads / c->kv_heads;
     if (int64_t(max_new) * group > INT32_MAX / 2) return ESP_ERR_SHAPE;
     s = Shape{};
-    s.prompt = rows && tokens * group >= int64_t(rows) * kManyRows;
+    const int64_t units = rows ? tokens * group / kPromptRows + rows : 0;
+    s.prompt = tokens * group >= int64_t(rows) * kManyRows && units * c->kv_heads >= kManyUnits;
     if (s.prompt) {
-        const int64_t units = tokens * group / kPromptRows + rows, places = 2 * kComputeUnits;
+        const int64_t places = 2 * kComputeUnits;
         if (units * c->kv_heads > INT32_MAX / 2) return ESP_ERR_SHAPE;
         // too few units for the GPU: their tiles are shared out, eight at least to a part
         int64_t splits = places / (units * c->kv_heads);
@@ -513,7 +519,7 @@ esp_status shape_of(const esp_kv_cache *c, int32_t rows, int64_t tokens, int32_t
     const int slots = kComputeUnits * (c->head_dim == 64 ? kPerUnit<64> : kPerUnit<128>);
     s.groups = slots / c->kv_heads > 1 ? slots / c->kv_heads : 1;
     // no more than one for every four tiles of the longest rows
-    const int64_t units = int64_t(rows) * ((int64_t(max_new) * group + kCols - 1) / kCols), tiles = units * (max_length / kTile + 2);
+    const int64_t few = int64_t(rows) * ((int64_t(max_new) * group + kCols - 1) / kCols), tiles = few * (max_length / kTile + 2);
     if (tiles / kWaves + 1 < s.groups) s.groups = int32_t(tiles / kWaves + 1);
     s.counters = (size_t(s.groups) * c->kv_heads * 4 + 255) / 256 * 256;
     s.bytes = s.counters + size_t(s.groups) * c->kv_heads * 2 * kCols * (c->head_dim + 2) * 4;

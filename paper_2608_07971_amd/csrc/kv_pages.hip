@@ -1,234 +1,382 @@
 // Page operations of the paged 8-bit cache: resize, fork, compact.
 //
-// Each is one workgroup that settles the integers (references, free pages,
-// table) and a second launch that copies the pages on the list it left.  All
-// choices are by index (the lowest free page, in order of sequence and slot),
-// so results do not depend on the order of atomics.
+// All choices are by index (the lowest free page, in order of sequence and
+// slot), so results do not depend on the order of atomics.  An operation is
+// three short launches over many workgroups that settle the integers and one
+// that copies the pages on the list they left:
+//   1  references of dropped pages go down; what is wrong is noted
+//   2  free pages and entries that need one are marked in bit masks and counted
+//      by blocks
+//   3  every workgroup adds up the blocks before its own, so that it knows the
+//      rank of its entries and finds the page of a rank by a binary search over
+//      the blocks and the bits of one; or, where something is wrong or pages do
+//      not suffice, takes step 1 back
+// (One workgroup doing all of it took 170 us for 256 sequences of up to 256
+// pages in a pool of 65,536; the launches of a step 3-5 us each.)
 #include "kv_internal.hpp"
+
+#include <type_traits>
 
 namespace esp_kv {
 
-constexpr int kIndexThreads = 1024, kIndexWaves = kIndexThreads / 64;
+constexpr int kThreads = 256;
 constexpr int kCopyThreads = 256;
+constexpr int kMaxBlocks = 1024;            // blocks of pages, and of entries: added up by every workgroup
 
-struct Work {
-    int32_t *count;                  // copies to make
-    int2 *copies;                    // [pages] from, to
-    int32_t *list;                   // [pages] free pages, lowest first
-    int32_t *other;                  // [pages or sequences] replaced pages, marks or new places
+// Pages or table entries [0, n) in at most kMaxBlocks blocks of `words` mask words.
+struct Blocks {
+    int64_t n;
+    int32_t words, blocks;
+    static Blocks of(int64_t n, int least) {
+        const int64_t all = (n + 63) / 64, per = (all + kMaxBlocks - 1) / kMaxBlocks;
+        Blocks b{n, int32_t(per > least ? per : least), 0};
+        b.blocks = int32_t((all + b.words - 1) / b.words);
+        return b;
+    }
 };
 
-// References change by atomics and are read past the compute unit's cache.
-__device__ __forceinline__ int32_t refs_now(const Cache &c, int32_t p) {
-    return __hip_atomic_load(c.refs + p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
+struct Work {
+    Blocks pages, entries;
+    uint64_t *page_mask;                    // free (or, compact: live) pages
+    uint64_t *need_mask, *split_mask;       // entries that take a page; of these, entries that copy one
+    int32_t *page_sum, *need_sum, *split_sum, *bad;
+    int32_t *count;                         // copies to make
+    int2 *copies;                           // from, to
+    int32_t *goes;                          // [pages] new places
+};
 
 __device__ __forceinline__ int lanes_below(uint64_t mask) {
     return __builtin_amdgcn_mbcnt_hi(uint32_t(mask >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(mask), 0));
 }
 
-// Numbers the items i of [0, n) that `has` holds for, in order: each wavefront
-// counts a run of its own, the runs are added up, and use(i, rank) is called
-// for every item held.  Returns how many there are.  `go(total)` decides after
-// the count whether they are used.
-template <typename Has, typename Go, typename Use>
-__device__ int number(int64_t n, int *lds, Has has, Go go, Use use) {
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int64_t run = ((n + kIndexWaves - 1) / kIndexWaves + 63) / 64 * 64;
-    const int64_t from = min(n, run * wave), to = min(n, from + run);
+// Sum of x over the workgroup.
+__device__ __forceinline__ int block_sum(int x, int *lds) {
+#pragma unroll
+    for (int m = 32; m; m >>= 1) x += __shfl_xor(x, m);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
+    __syncthreads();
+    return lds[0] + lds[1] + lds[2] + lds[3];
+}
+
+// Exclusive prefix of n <= kMaxBlocks values into at[0 .. n], all threads.
+__device__ __forceinline__ void prefix(const int32_t *values, int n, int *at, int *lds) {
+    int x[4], sum = 0;
+#pragma unroll
+    for (int k = 0; k < 4; k++) {
+        const int i = threadIdx.x * 4 + k;
+        x[k] = i < n ? values[i] : 0;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; k++) sum += x[k];
+    int before = sum;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        const int v = __shfl_up(before, m);
+        before += int(threadIdx.x & 63) >= m ? v : 0;
+    }
+    __syncthreads();
+    if ((threadIdx.x & 63) == 63) lds[threadIdx.x >> 6] = before;
+    __syncthreads();
+    before -= sum;
+    for (int w = 0; w < int(threadIdx.x >> 6); w++) before += lds[w];
+#pragma unroll
+    for (int k = 0; k < 4; k++) {
+        const int i = threadIdx.x * 4 + k;
+        if (i <= n) at[i] = before;
+        before += x[k];
+    }
+    if (threadIdx.x == kThreads - 1 && n == kMaxBlocks) at[n] = before;
+    __syncthreads();
+}
+
+// The page of rank r among those whose bit is set (flip 0) or clear (flip ~0);
+// at(b): how many there are before block b.
+template <typename At> __device__ int select(const Work &w, At at, uint64_t flip, int r) {
+    int lo = 0, hi = w.pages.blocks - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (at(mid) <= r) lo = mid;
+        else hi = mid - 1;
+    }
+    r -= at(lo);
+    const int64_t words = (w.pages.n + 63) / 64, from = int64_t(lo) * w.pages.words;
+    for (int x = 0; x < w.pages.words; x += 4) {
+        uint64_t m[4];
+#pragma unroll
+        for (int k = 0; k < 4; k++) m[k] = x + k < w.pages.words && from + x + k < words ? w.page_mask[from + x + k] ^ flip : 0;
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            const int held = __popcll(m[k]);
+            if (r < held) {
+                for (; r > 0; r--) m[k] &= m[k] - 1;
+                return int((from + x + k) * 64 + __builtin_ctzll(m[k]));
+            }
+            r -= held;
+        }
+    }
+    return -1;
+}
+
+// Marks the items of block `block` that `has` holds for: four wavefronts, a word each at a time.
+template <typename Has> __device__ __forceinline__ void mark(const Blocks &b, int block, uint64_t *mask, int32_t *sum, int *lds, Has has) {
+    const int64_t words = (b.n + 63) / 64, from = int64_t(block) * b.words, to = min(words, from + b.words);
     int mine = 0;
-    for (int64_t i = from; i < to; i += 64) mine += __popcll(__ballot(i + lane < to && has(i + lane)));
-    __syncthreads();
-    if (lane == 0) lds[wave] = mine;
-    __syncthreads();
-    int before = 0, total = 0;
-    for (int w = 0; w < kIndexWaves; w++) {
-        before += w < wave ? lds[w] : 0;
-        total += lds[w];
-    }
-    if (go(total)) {
-        for (int64_t i = from; i < to; i += 64) {
-            const bool held = i + lane < to && has(i + lane);
-            const uint64_t mask = __ballot(held);
-            if (held) use(i + lane, before + lanes_below(mask));
-            before += __popcll(mask);
+    for (int64_t x = from + (threadIdx.x >> 6); x < to; x += 4) {
+        const int64_t i = x * 64 + (threadIdx.x & 63);
+        const uint64_t m = __ballot(i < b.n && has(i));
+        if ((threadIdx.x & 63) == 0) {
+            mask[x] = m;
+            mine += __popcll(m);
         }
     }
-    __syncthreads();
-    return total;
+    mine = block_sum(mine, lds);
+    if (threadIdx.x == 0) sum[block] = mine;
 }
 
-__global__ __launch_bounds__(kIndexThreads) void k_resize(Cache c, const int32_t *lengths, Work w) {
-    __shared__ int lds[kIndexWaves];
-    __shared__ int copies;
-    const int tid = threadIdx.x;
-    const int64_t entries = int64_t(c.sequences) * c.width;
-    if (tid == 0) {
-        copies = 0;
-        *w.count = 0;
-    }
-    int bad = 0;
-    for (int s = tid; s < c.sequences; s += kIndexThreads) bad |= lengths[s] < 0 || lengths[s] > int64_t(c.width) << c.shift;
-    for (int64_t i = tid; i < entries; i += kIndexThreads) bad |= c.table[i] < -1 || c.table[i] >= c.pages;
-    if (__syncthreads_or(bad)) {
-        if (tid == 0) record(c, ESP_ERR_SHAPE);
-        return;
-    }
-    auto wanted = [&](int64_t i, int &seq) {
-        seq = int(i / c.width);
-        return int(i - int64_t(seq) * c.width) < (lengths[seq] + c.tokens - 1) >> c.shift;
-    };
-    auto drop = [&](int by) {
-        for (int64_t i = tid; i < entries; i += kIndexThreads) {
-            int seq;
-            const int32_t p = c.table[i];
-            if (p >= 0 && !wanted(i, seq)) atomicAdd(c.refs + p, by);
+// Calls use(i, held, rank, held2, rank2) for every item of a block: whether its
+// bit is set in each of two masks, and how many set bits come before it, from
+// `before` and `before2` at the block's start.
+template <typename Use>
+__device__ __forceinline__ void ranked(const Blocks &b, int block, const uint64_t *mask, int before, const uint64_t *mask2, int before2, Use use) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t words = (b.n + 63) / 64, from = int64_t(block) * b.words, to = min(words, from + b.words);
+    for (int64_t x0 = from; x0 < to; x0 += 64) {                 // a word a lane
+        const uint64_t m = x0 + lane < to ? mask[x0 + lane] : 0, m2 = x0 + lane < to ? mask2[x0 + lane] : 0;
+        int at = __popcll(m), at2 = __popcll(m2);
+        const int own = at, own2 = at2;
+#pragma unroll
+        for (int s = 1; s < 64; s <<= 1) {
+            const int v = __shfl_up(at, s), v2 = __shfl_up(at2, s);
+            at += lane >= s ? v : 0;
+            at2 += lane >= s ? v2 : 0;
         }
-        __threadfence();
-        __syncthreads();
-    };
-    drop(-1);
-    // a kept page that ends inside its sequence and still has other owners
-    auto split = [&](int64_t i, int seq, int32_t p) {
-        const int last = min(c.lengths[seq], lengths[seq]);
-        return int(i - int64_t(seq) * c.width) == last >> c.shift && (last & (c.tokens - 1)) && refs_now(c, p) > 1;
-    };
-    auto needs = [&](int64_t i) {
-        int seq;
+        for (int x = wave; x < 64 && x0 + x < to; x += 4) {      // an item a lane
+            const uint64_t n = __shfl(m, x), n2 = __shfl(m2, x);
+            const int r = before + __shfl(at - own, x), r2 = before2 + __shfl(at2 - own2, x);
+            const int64_t i = (x0 + x) * 64 + lane;
+            if (i < b.n) use(i, bool(n >> lane & 1), r + lanes_below(n), bool(n2 >> lane & 1), r2 + lanes_below(n2));
+        }
+        before += __shfl(at, 63);
+        before2 += __shfl(at2, 63);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Resize: table entries by blocks
+// ---------------------------------------------------------------------------
+
+struct Entry {
+    int seq, slot;
+    bool wanted;
+};
+__device__ __forceinline__ Entry entry_of(const Cache &c, const int32_t *lengths, int64_t i) {
+    const int seq = int(uint32_t(i) / uint32_t(c.width)), slot = int(uint32_t(i) - uint32_t(seq) * uint32_t(c.width));
+    return {seq, slot, slot < (lengths[seq] + c.tokens - 1) >> c.shift};
+}
+// Calls f(i) for the entries of a block.
+template <typename F> __device__ __forceinline__ void each(const Blocks &b, int block, F f) {
+    const int64_t from = int64_t(block) * b.words * 64, to = min(b.n, from + int64_t(b.words) * 64);
+    for (int64_t i = from + threadIdx.x; i < to; i += kThreads) f(i);
+}
+
+__global__ __launch_bounds__(kThreads) void k_resize_drop(Cache c, const int32_t *lengths, Work w) {
+    __shared__ int lds[4];
+    int bad = 0;
+    each(w.entries, blockIdx.x, [&](int64_t i) {
+        const Entry e = entry_of(c, lengths, i);
         const int32_t p = c.table[i];
-        return wanted(i, seq) && (p < 0 || split(i, seq, p));
-    };
-    const int need = number(entries, lds, needs, [](int) { return false; }, [](int64_t, int) {});
-    const int have = number(c.pages, lds, [&](int64_t p) { return refs_now(c, int32_t(p)) == 0; }, [&](int total) { return total >= need; },
-                            [&](int64_t p, int rank) { if (rank < need) w.list[rank] = int32_t(p); });
-    if (have < need) {
-        drop(1);
-        if (tid == 0) record(c, ESP_ERR_RANGE);
-        return;
-    }
-    __threadfence();
-    __syncthreads();
-    // the entry alone changes here; splits are judged by references, which change after
-    number(entries, lds, needs, [](int) { return true; }, [&](int64_t i, int rank) {
-        const int32_t p = c.table[i], to = w.list[rank];
-        if (p >= 0) w.copies[atomicAdd(&copies, 1)] = make_int2(p, to);
-        w.other[rank] = p;
-        c.table[i] = to;
+        bad |= lengths[e.seq] < 0 || lengths[e.seq] > int64_t(c.width) << c.shift || p < -1 || p >= c.pages;
+        if (p >= 0 && p < c.pages && !e.wanted) atomicAdd(c.refs + p, -1);
     });
-    for (int r = tid; r < need; r += kIndexThreads) {
-        c.refs[w.list[r]] = 1;
-        if (w.other[r] >= 0) atomicAdd(c.refs + w.other[r], -1);
-    }
-    for (int64_t i = tid; i < entries; i += kIndexThreads) {
-        int seq;
-        if (!wanted(i, seq)) c.table[i] = -1;
-    }
-    __syncthreads();
-    for (int s = tid; s < c.sequences; s += kIndexThreads) c.lengths[s] = lengths[s];
-    if (tid == 0) *w.count = copies;
+    bad = block_sum(bad, lds);
+    if (threadIdx.x == 0) w.bad[blockIdx.x] = bad;
 }
 
-__global__ __launch_bounds__(kIndexThreads) void k_fork(Cache c, int n, const int32_t *parents, const int32_t *children, Work w) {
-    __shared__ int lds[kIndexWaves];
-    const int tid = threadIdx.x;
-    const int64_t entries = int64_t(n) * c.width;
-    if (tid == 0) *w.count = 0;
-    int32_t *marks = w.other;
-    for (int s = tid; s < c.sequences; s += kIndexThreads) marks[s] = 0;
-    __threadfence();
-    __syncthreads();
+// Workgroups [0, entries.blocks): entries; the rest: pages.
+__global__ __launch_bounds__(kThreads) void k_resize_mark(Cache c, const int32_t *lengths, Work w) {
+    __shared__ int lds[4];
+    const int b = blockIdx.x;
+    if (b >= w.entries.blocks) {
+        mark(w.pages, b - w.entries.blocks, w.page_mask, w.page_sum, lds, [&](int64_t p) { return c.refs[p] == 0; });
+        return;
+    }
+    // a kept page that ends inside its sequence and still has other owners
+    auto split = [&](int64_t i) {
+        const Entry e = entry_of(c, lengths, i);
+        const int32_t p = c.table[i];
+        const int last = min(c.lengths[e.seq], lengths[e.seq]);
+        return e.wanted && p >= 0 && p < c.pages && e.slot == last >> c.shift && (last & (c.tokens - 1)) && c.refs[p] > 1;
+    };
+    mark(w.entries, b, w.split_mask, w.split_sum, lds, split);
+    mark(w.entries, b, w.need_mask, w.need_sum, lds, [&](int64_t i) { return (c.table[i] == -1 && entry_of(c, lengths, i).wanted) || split(i); });
+}
+
+__global__ __launch_bounds__(kThreads) void k_resize_take(Cache c, const int32_t *lengths, Work w) {
+    __shared__ int lds[4], free_at[kMaxBlocks + 1], need_at[kMaxBlocks + 1], split_at[kMaxBlocks + 1];
     int bad = 0;
-    for (int i = tid; i < n; i += kIndexThreads) {
-        const int p = parents[i], k = children[i];
-        if (p < 0 || p >= c.sequences || k < 0 || k >= c.sequences) bad = 1;
-        else bad |= atomicExch(marks + k, 1);
-    }
-    __threadfence();
-    if (!(bad = __syncthreads_or(bad)))
-        for (int i = tid; i < n; i += kIndexThreads) bad |= __hip_atomic_load(marks + parents[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (__syncthreads_or(bad)) {
-        if (tid == 0) record(c, ESP_ERR_INVALID_ARG);
-        return;
-    }
-    auto parted = [&](int i) { return (c.lengths[parents[i]] & (c.tokens - 1)) != 0; };
-    auto entry = [&](const int32_t *of, int64_t i) { return c.table + int64_t(of[i / c.width]) * c.width + i % c.width; };
-    for (int i = tid; i < n; i += kIndexThreads) {
-        const int length = c.lengths[parents[i]];
-        bad |= length < 0 || length > int64_t(c.width) << c.shift;
-        if (!bad && parted(i)) bad |= c.table[int64_t(parents[i]) * c.width + (length >> c.shift)] < 0;
-    }
-    for (int64_t i = tid; i < entries; i += kIndexThreads) {
-        const int32_t p = *entry(parents, i), k = *entry(children, i);
-        bad |= p < -1 || p >= c.pages || k < -1 || k >= c.pages;
-    }
-    if (__syncthreads_or(bad)) {
-        if (tid == 0) record(c, ESP_ERR_SHAPE);
-        return;
-    }
-    auto drop = [&](int by) {
-        for (int64_t i = tid; i < entries; i += kIndexThreads) {
-            const int32_t p = *entry(children, i);
-            if (p >= 0) atomicAdd(c.refs + p, by);
+    for (int b = threadIdx.x; b < w.entries.blocks; b += kThreads) bad |= w.bad[b];
+    bad = block_sum(bad, lds);
+    prefix(w.page_sum, w.pages.blocks, free_at, lds);
+    prefix(w.need_sum, w.entries.blocks, need_at, lds);
+    prefix(w.split_sum, w.entries.blocks, split_at, lds);
+    const bool short_of = free_at[w.pages.blocks] < need_at[w.entries.blocks];
+    if (bad || short_of) {
+        each(w.entries, blockIdx.x, [&](int64_t i) {
+            const int32_t p = c.table[i];
+            if (p >= 0 && p < c.pages && !entry_of(c, lengths, i).wanted) atomicAdd(c.refs + p, 1);
+        });
+        if (blockIdx.x == 0 && threadIdx.x == 0) {
+            *w.count = 0;
+            record(c, bad ? ESP_ERR_SHAPE : ESP_ERR_RANGE);
         }
-        __threadfence();
-        __syncthreads();
-    };
-    drop(-1);
-    const int need = number(n, lds, [&](int64_t i) { return parted(int(i)); }, [](int) { return false; }, [](int64_t, int) {});
-    const int have = number(c.pages, lds, [&](int64_t p) { return refs_now(c, int32_t(p)) == 0; }, [&](int total) { return total >= need; },
-                            [&](int64_t p, int rank) { if (rank < need) w.list[rank] = int32_t(p); });
-    if (have < need) {
-        drop(1);
-        if (tid == 0) record(c, ESP_ERR_RANGE);
         return;
     }
-    for (int64_t i = tid; i < entries; i += kIndexThreads) {
-        const int k = int(i / c.width), slot = int(i - int64_t(k) * c.width);
-        const int32_t p = *entry(parents, i);
-        if (parted(k) && slot == c.lengths[parents[k]] >> c.shift) continue;
-        if (p >= 0) atomicAdd(c.refs + p, 1);
-        *entry(children, i) = p;
-    }
-    number(n, lds, [&](int64_t i) { return parted(int(i)); }, [](int) { return true; }, [&](int64_t i, int rank) {
-        const int slot = c.lengths[parents[i]] >> c.shift;
-        const int32_t to = w.list[rank];
-        w.copies[rank] = make_int2(c.table[int64_t(parents[i]) * c.width + slot], to);
-        c.table[int64_t(children[i]) * c.width + slot] = to;
-        c.refs[to] = 1;
+    if (blockIdx.x == 0 && threadIdx.x == 0) *w.count = split_at[w.entries.blocks];
+    ranked(w.entries, blockIdx.x, w.need_mask, need_at[blockIdx.x], w.split_mask, split_at[blockIdx.x], [&](int64_t i, bool need, int rank, bool split, int copy) {
+        const Entry e = entry_of(c, lengths, i);
+        const int32_t p = c.table[i];
+        const int to = need ? select(w, [&](int b) { return free_at[b]; }, 0, rank) : -1;
+        if (to >= 0) {
+            if (split) {
+                w.copies[copy] = make_int2(p, to);
+                atomicAdd(c.refs + p, -1);
+            }
+            c.refs[to] = 1;
+            c.table[i] = to;
+        } else if (!e.wanted && p >= 0) {
+            c.table[i] = -1;
+        }
+        if (e.slot == 0) c.lengths[e.seq] = lengths[e.seq];
     });
-    for (int i = tid; i < n; i += kIndexThreads) c.lengths[children[i]] = c.lengths[parents[i]];
-    if (tid == 0) *w.count = need;
 }
 
-__global__ __launch_bounds__(kIndexThreads) void k_compact(Cache c, int limit, int32_t *refs_out, int32_t *live_out, Work w) {
-    __shared__ int lds[kIndexWaves];
-    const int tid = threadIdx.x;
-    const int live = number(c.pages, lds, [&](int64_t p) { return c.refs[p] > 0; }, [](int) { return false; }, [](int64_t, int) {});
-    if (limit < 0) limit = live;
-    limit = min(limit, c.pages);
-    if (tid == 0 && live_out) *live_out = live;
-    int32_t *goes = w.other;
-    for (int p = tid; p < c.pages; p += kIndexThreads) {
-        goes[p] = p;
-        refs_out[p] = c.refs[p];
-    }
-    int moved = 0;
-    if (live <= limit) {
-        number(limit, lds, [&](int64_t p) { return c.refs[p] <= 0; }, [](int) { return true; }, [&](int64_t p, int rank) { w.list[rank] = int32_t(p); });
-        moved = number(c.pages - limit, lds, [&](int64_t p) { return c.refs[limit + p] > 0; }, [](int) { return true; }, [&](int64_t p, int rank) {
-            const int32_t from = limit + int32_t(p), to = w.list[rank];
-            w.copies[rank] = make_int2(from, to);
-            goes[from] = to;
-        });
-        for (int r = tid; r < moved; r += kIndexThreads) {
-            const int2 m = w.copies[r];
-            refs_out[m.y] = c.refs[m.x];
-            refs_out[m.x] = 0;
+// ---------------------------------------------------------------------------
+// Fork: a workgroup a child
+// ---------------------------------------------------------------------------
+
+__global__ __launch_bounds__(kThreads) void k_fork_drop(Cache c, int n, const int32_t *parents, const int32_t *children, Work w) {
+    __shared__ int lds[4];
+    const int i = blockIdx.x, parent = parents[i], child = children[i];
+    const bool there = parent >= 0 && parent < c.sequences && child >= 0 && child < c.sequences;
+    int bad = 0;
+    for (int j = threadIdx.x; j < n; j += kThreads) bad |= parents[j] == child || (j != i && children[j] == child);
+    bad = block_sum(bad, lds) || !there;
+    int wrong = 0;
+    if (there) {
+        const int length = c.lengths[parent];
+        wrong = length < 0 || length > int64_t(c.width) << c.shift;
+        if (!wrong && (length & (c.tokens - 1))) wrong |= c.table[int64_t(parent) * c.width + (length >> c.shift)] < 0;
+        for (int x = threadIdx.x; x < c.width; x += kThreads) {
+            const int32_t p = c.table[int64_t(parent) * c.width + x], k = c.table[int64_t(child) * c.width + x];
+            wrong |= p < -1 || p >= c.pages || k < -1 || k >= c.pages;
+            if (k >= 0 && k < c.pages) atomicAdd(c.refs + k, -1);
         }
-    } else if (tid == 0) {
-        record(c, ESP_ERR_RANGE);
     }
-    if (tid == 0) *w.count = moved;
+    wrong = block_sum(wrong, lds);
+    if (threadIdx.x == 0) w.bad[i] = (bad ? 1 : 0) | (wrong ? 2 : 0);
+}
+
+__global__ __launch_bounds__(kThreads) void k_mark_free(Cache c, Work w) {
+    __shared__ int lds[4];
+    mark(w.pages, blockIdx.x, w.page_mask, w.page_sum, lds, [&](int64_t p) { return c.refs[p] == 0; });
+}
+
+__global__ __launch_bounds__(kThreads) void k_fork_take(Cache c, int n, const int32_t *parents, const int32_t *children, Work w) {
+    __shared__ int lds[4], free_at[kMaxBlocks + 1];
+    const int i = blockIdx.x, parent = parents[i], child = children[i];
+    auto parted = [&](int j) { return parents[j] >= 0 && parents[j] < c.sequences && (c.lengths[parents[j]] & (c.tokens - 1)) != 0; };
+    int invalid = 0, wrong = 0, need = 0, rank = 0;
+    for (int j = threadIdx.x; j < n; j += kThreads) {
+        const int one = parted(j);
+        invalid |= w.bad[j] & 1;
+        wrong |= w.bad[j] >> 1;
+        need += one;
+        rank += j < i ? one : 0;
+    }
+    invalid = block_sum(invalid, lds);
+    wrong = block_sum(wrong, lds);
+    need = block_sum(need, lds);
+    rank = block_sum(rank, lds);
+    prefix(w.page_sum, w.pages.blocks, free_at, lds);
+    if (invalid || wrong || free_at[w.pages.blocks] < need) {
+        if (parent >= 0 && parent < c.sequences && child >= 0 && child < c.sequences)
+            for (int x = threadIdx.x; x < c.width; x += kThreads) {
+                const int32_t k = c.table[int64_t(child) * c.width + x];
+                if (k >= 0 && k < c.pages) atomicAdd(c.refs + k, 1);
+            }
+        if (i == 0 && threadIdx.x == 0) {
+            *w.count = 0;
+            record(c, invalid ? ESP_ERR_INVALID_ARG : wrong ? ESP_ERR_SHAPE : ESP_ERR_RANGE);
+        }
+        return;
+    }
+    const int length = c.lengths[parent], part = parted(i) ? length >> c.shift : -1;
+    for (int x = threadIdx.x; x < c.width; x += kThreads) {
+        int32_t p = c.table[int64_t(parent) * c.width + x];
+        if (x == part) {                    // filled only in part: copied
+            const int to = select(w, [&](int b) { return free_at[b]; }, 0, rank);
+            if (to >= 0) {
+                w.copies[rank] = make_int2(p, to);
+                c.refs[to] = 1;
+            }
+            p = to;
+        } else if (p >= 0) {
+            atomicAdd(c.refs + p, 1);
+        }
+        c.table[int64_t(child) * c.width + x] = p;
+    }
+    if (threadIdx.x == 0) c.lengths[child] = length;
+    if (i == 0 && threadIdx.x == 0) *w.count = need;
+}
+
+// ---------------------------------------------------------------------------
+// Compact
+// ---------------------------------------------------------------------------
+
+__global__ __launch_bounds__(kThreads) void k_compact_mark(Cache c, int32_t *refs_out, Work w) {
+    __shared__ int lds[4];
+    mark(w.pages, blockIdx.x, w.page_mask, w.page_sum, lds, [&](int64_t p) {
+        const int32_t r = c.refs[p];
+        w.goes[p] = int32_t(p);
+        refs_out[p] = r;
+        return r > 0;
+    });
+}
+
+__global__ __launch_bounds__(kThreads) void k_compact_place(Cache c, int limit, int32_t *refs_out, int32_t *live_out, Work w) {
+    __shared__ int lds[4], live_at[kMaxBlocks + 1];
+    prefix(w.page_sum, w.pages.blocks, live_at, lds);
+    const int live = live_at[w.pages.blocks], per = w.pages.words * 64;
+    limit = min(limit < 0 ? live : limit, c.pages);
+    // live pages below the limit
+    int below = 0;
+    if (limit < c.pages) {
+        const int b = limit / per;
+        for (int64_t x = int64_t(b) * w.pages.words + threadIdx.x; x * 64 < limit; x += kThreads) {
+            const uint64_t m = w.page_mask[x];
+            below += __popcll(limit - x * 64 >= 64 ? m : m & ((uint64_t(1) << (limit - x * 64)) - 1));
+        }
+        below = block_sum(below, lds) + live_at[b];
+    } else {
+        below = live;
+    }
+    const bool fits = live <= limit;
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        if (live_out) *live_out = live;
+        *w.count = fits ? live - below : 0;
+        if (!fits) record(c, ESP_ERR_RANGE);
+    }
+    if (!fits) return;
+    ranked(w.pages, blockIdx.x, w.page_mask, live_at[blockIdx.x], w.page_mask, 0, [&](int64_t p, bool is_live, int rank, bool, int) {
+        if (!is_live || p < limit) return;
+        const int hole = select(w, [&](int b) { return b * per - live_at[b]; }, ~uint64_t(0), rank - below);
+        if (hole < 0) return;
+        w.copies[rank - below] = make_int2(int(p), hole);
+        w.goes[p] = hole;
+        refs_out[hole] = c.refs[p];
+        refs_out[p] = 0;
+    });
 }
 
 // Copies the listed pages (keys, values and scales of all layers): 16 KB of a
@@ -293,18 +441,30 @@ using namespace esp_kv;
 
 namespace {
 
-size_t pages_bytes(const esp_kv_cache *c) {
-    const size_t pages = size_t(c->pages), most = pages > size_t(c->sequences) ? pages : size_t(c->sequences);
-    return (256 + pages * 12 + most * 4 + 255) / 256 * 256;
+// Lays the work out behind `p`; returns its bytes.
+size_t lay_out(const esp_kv_cache *c, char *p, Work &w) {
+    w.pages = Blocks::of(c->pages, 4);
+    w.entries = Blocks::of(int64_t(c->sequences) * c->table_width, 16);
+    char *at = p;
+    auto take = [&](auto *&to, size_t n) {
+        to = reinterpret_cast<std::remove_reference_t<decltype(to)>>(at);
+        at += (n * sizeof(*to) + 255) / 256 * 256;
+    };
+    take(w.count, 1);
+    take(w.page_mask, (size_t(w.pages.n) + 63) / 64);
+    take(w.need_mask, (size_t(w.entries.n) + 63) / 64);
+    take(w.split_mask, (size_t(w.entries.n) + 63) / 64);
+    take(w.page_sum, kMaxBlocks);
+    take(w.need_sum, kMaxBlocks);
+    take(w.split_sum, kMaxBlocks);
+    take(w.bad, size_t(c->sequences) > size_t(kMaxBlocks) ? size_t(c->sequences) : size_t(kMaxBlocks));
+    take(w.copies, size_t(c->pages));
+    take(w.goes, size_t(c->pages));
+    return size_t(at - p);
 }
 esp_status work_of(const esp_kv_cache *c, void *workspace, size_t bytes, Work &w) {
-    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || bytes < pages_bytes(c)) return ESP_ERR_WORKSPACE;
-    char *p = static_cast<char *>(workspace);
-    w.count = reinterpret_cast<int32_t *>(p);
-    w.copies = reinterpret_cast<int2 *>(p + 256);
-    w.list = reinterpret_cast<int32_t *>(p + 256 + size_t(c->pages) * 8);
-    w.other = w.list + c->pages;
-    return ESP_OK;
+    const size_t need = lay_out(c, static_cast<char *>(workspace), w);
+    return workspace && (reinterpret_cast<uintptr_t>(workspace) & 255) == 0 && bytes >= need ? ESP_OK : ESP_ERR_WORKSPACE;
 }
 // Workgroups of the copy for at most `most` pages: 2,048 fill the GPU.
 unsigned copy_blocks(const esp_kv_cache *c, int64_t most) {
@@ -319,7 +479,8 @@ extern "C" esp_status esp_kv_pages_workspace(const esp_kv_cache *cache, int32_t 
     if (esp_status e = check_cache(cache)) return e;
     if (!bytes) return ESP_ERR_INVALID_ARG;
     if (n < 0 || n > cache->sequences) return ESP_ERR_SHAPE;
-    *bytes = pages_bytes(cache);
+    Work w;
+    *bytes = lay_out(cache, nullptr, w);
     return ESP_OK;
 }
 
@@ -330,7 +491,9 @@ extern "C" esp_status esp_kv_resize(const esp_kv_cache *cache, const int32_t *le
     if (esp_status e = work_of(cache, workspace, workspace_bytes, w)) return e;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const Cache c = cache_of(cache);
-    k_resize<<<1, kIndexThreads, 0, s>>>(c, lengths, w);
+    k_resize_drop<<<w.entries.blocks, kThreads, 0, s>>>(c, lengths, w);
+    k_resize_mark<<<w.entries.blocks + w.pages.blocks, kThreads, 0, s>>>(c, lengths, w);
+    k_resize_take<<<w.entries.blocks, kThreads, 0, s>>>(c, lengths, w);
     k_copy<<<copy_blocks(cache, cache->sequences), kCopyThreads, 0, s>>>(c, w.count, w.copies, nullptr, nullptr);
     return launched();
 }
@@ -345,7 +508,9 @@ extern "C" esp_status esp_kv_fork(const esp_kv_cache *cache, int32_t n, const in
     if (esp_status e = work_of(cache, workspace, workspace_bytes, w)) return e;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const Cache c = cache_of(cache);
-    k_fork<<<1, kIndexThreads, 0, s>>>(c, n, parents, children, w);
+    k_fork_drop<<<n, kThreads, 0, s>>>(c, n, parents, children, w);
+    k_mark_free<<<w.pages.blocks, kThreads, 0, s>>>(c, w);
+    k_fork_take<<<n, kThreads, 0, s>>>(c, n, parents, children, w);
     k_copy<<<copy_blocks(cache, n), kCopyThreads, 0, s>>>(c, w.count, w.copies, nullptr, nullptr);
     return launched();
 }
@@ -358,8 +523,9 @@ extern "C" esp_status esp_kv_compact(const esp_kv_cache *cache, int32_t limit, i
     if (esp_status e = work_of(cache, workspace, workspace_bytes, w)) return e;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const Cache c = cache_of(cache);
-    k_compact<<<1, kIndexThreads, 0, s>>>(c, limit, refs_out, live, w);
-    k_copy<<<copy_blocks(cache, cache->pages), kCopyThreads, 0, s>>>(c, w.count, w.copies, w.other, table_out);
+    k_compact_mark<<<w.pages.blocks, kThreads, 0, s>>>(c, refs_out, w);
+    k_compact_place<<<w.pages.blocks, kThreads, 0, s>>>(c, limit, refs_out, live, w);
+    k_copy<<<copy_blocks(cache, cache->pages), kCopyThreads, 0, s>>>(c, w.count, w.copies, w.goes, table_out);
     return launched();
 }
 

@@ -23,7 +23,7 @@ __device__ __forceinline__ half8 scaled8(uint32_t a, uint32_t b, float by) {
 // are taken in the order that leaves the softmax weights in place for the
 // value product.  V's block scales enter as the codes are widened, K's with the
 // softmax scale.
-template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 2) void k_prompt(AttendArgs a) {
+template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, Dim == 64 ? 3 : 2) void k_prompt(AttendArgs a) {
     typedef typename Pack<T>::v8 V8;
     typedef typename Pack<T>::v2 V2;
     constexpr int kSteps = Dim / 16;        // matrix steps of a score
@@ -347,14 +347,15 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 
         // as in k_attend: parts by agent-scope atomics, the last to arrive joins them in order
         constexpr int kPart = kPromptRows * (Dim + 2);
         const int64_t unit_id = int64_t(head) * a.units + index;
-        float *parts = a.partial + unit_id * a.splits * kPart + (wave * 32 + col) * (Dim + 2);
-        if (r < n_rows) {
-            float *mine = parts + part * kPart;
+        // pair x of lane y of a wavefront lies at 64 x + y; the last pairs hold lse
+        float *parts = a.partial + unit_id * a.splits * kPart + wave * (32 * (Dim + 2)) + 2 * lane;
+        {
+            float *mine = parts + int64_t(part) * kPart;
 #pragma unroll
             for (int d = 0; d < kOut; d++)
 #pragma unroll
-                for (int i = 0; i < 16; i += 2) store_pair(mine + 32 * d + 16 * half + i, o[d][i], o[d][i + 1]);
-            if (half == 0) store_pair(mine + Dim, lse, 0.0f);
+                for (int i = 0; i < 16; i += 2) store_pair(mine + (8 * d + i / 2) * 128, o[d][i], o[d][i + 1]);
+            if (half == 0) store_pair(mine + Dim * 32, lse, 0.0f);
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
@@ -370,8 +371,8 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 
             for (int i = 0; i < 16; i++) o[d][i] = 0.0f;
         bool nan = false;
         for (int k = 0; k < a.splits; k++) {
-            const float *from = parts + k * kPart;
-            const float x = load_pair(from + Dim).x, m_new = fmaxf(m, x), was = m == m_new ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);
+            const float *from = parts + int64_t(k) * kPart;
+            const float x = load_pair(from + Dim * 32 - 64 * half).x, m_new = fmaxf(m, x), was = m == m_new ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);
             const float f = x == -INFINITY ? 0.0f : x == m_new ? 1.0f : __builtin_amdgcn_exp2f(x - m_new);
             nan |= x != x;
             m = m_new;
@@ -380,7 +381,7 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 
             for (int d = 0; d < kOut; d++)
 #pragma unroll
                 for (int i = 0; i < 16; i += 2) {
-                    const float2 z = load_pair(from + 32 * d + 16 * half + i);
+                    const float2 z = load_pair(from + (8 * d + i / 2) * 128);
                     o[d][i] = __builtin_fmaf(z.x, f, o[d][i] * was);
                     o[d][i + 1] = __builtin_fmaf(z.y, f, o[d][i + 1] * was);
                 }

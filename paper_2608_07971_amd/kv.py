@@ -12,13 +12,16 @@ There is no CPU fallback.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
+import functools
 from typing import Optional
 
 import torch
 
-from . import ESP_OK, EspError, _stream, lib as _base_lib
+from . import ESP_OK, EspError, lib as _base_lib
+
+_raw_stream = torch._C._cuda_getCurrentRawStream
+_current_device = torch._C._cuda_getDevice
 
 BF16, FP16, FP32 = 0, 1, 2
 _TYPES = {torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32}
@@ -78,16 +81,21 @@ def _check(code: int, where: str) -> None:
         raise EspError(code, where)
 
 
-@contextlib.contextmanager
-def _on(stream, device):
-    """What the call allocates belongs to the stream it runs on."""
-    if stream is None:
-        with torch.cuda.device(device):
-            yield _stream(None)
-        return
-    s = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device)
-    with torch.cuda.stream(s):
-        yield int(s.cuda_stream)
+def _on_stream(call):
+    """call(..., s): with the handle of the stream that the work goes to, on its device, so that what the call
+    allocates belongs to that stream.  The current stream of the current device costs no context."""
+    @functools.wraps(call)
+    def entry(first, *args, stream=None, **more):
+        index = first.index
+        if stream is None and _current_device() == index:
+            return call(first, *args, s=_raw_stream(index), **more)
+        if stream is None:
+            with torch.cuda.device(index):
+                return call(first, *args, s=_raw_stream(index), **more)
+        own = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=first.device)
+        with torch.cuda.stream(own):
+            return call(first, *args, s=int(own.cuda_stream), **more)
+    return entry
 
 
 def _ints(t, n: Optional[int], what: str, device) -> int:
@@ -98,11 +106,12 @@ def _ints(t, n: Optional[int], what: str, device) -> int:
 
 
 def _view(t, tokens: int, heads: int, dim: int, what: str, device) -> esp_kv_view:
-    if t.dim() != 3 or tuple(t.shape) != (tokens, heads, dim) or t.device != device:
+    if t.shape != (tokens, heads, dim) or t.device != device:
         raise ValueError(f"{what}: tensor [{tokens}, {heads}, {dim}] on {device} expected")
-    if t.numel() and dim > 1 and t.stride(2) != 1:
+    a, b, c = t.stride()
+    if c != 1 and dim > 1 and t.numel():
         raise ValueError(f"{what}: the last dimension must be contiguous")
-    return esp_kv_view(t.data_ptr(), t.stride(0), t.stride(1))
+    return esp_kv_view(t.data_ptr(), a, b)
 
 
 _NO_VIEW = esp_kv_view(None, 0, 0)
@@ -129,27 +138,28 @@ class Rope:
         if self.rotary_dim > self.head_dim:
             raise ValueError("rotary_dim exceeds head_dim")
         self.turns = torch.tensor(turns, dtype=torch.float64, device=device)
+        self.device, self.index = self.turns.device, self.turns.device.index
         self.c = esp_kv_rope(self.turns.data_ptr(), self.magnitude, self.rotary_dim, int(bool(interleaved)))
         self.ptr = C.addressof(self.c)
 
 
+@_on_stream
 def rotate(rope: Rope, x: torch.Tensor, positions: torch.Tensor, inverse: bool = False, out: Optional[torch.Tensor] = None,
-           stream=None) -> torch.Tensor:
+           *, s: int) -> torch.Tensor:
     """x [tokens, heads, head_dim] turned by positions (int32 [tokens]); inverse: turned back, which is the gradient.
-    out may be x."""
-    if x.dim() != 3 or x.dtype not in _TYPES or not x.is_cuda:
-        raise ValueError("x: bfloat16, float16 or float32 device tensor [tokens, heads, head_dim] expected")
+    out may be x.  stream: the current one, unless given."""
+    kind = _TYPES.get(x.dtype)
+    if kind is None or x.dim() != 3 or x.device != rope.device:
+        raise ValueError(f"x: bfloat16, float16 or float32 tensor [tokens, heads, head_dim] on {rope.device} expected")
     T, H, D = x.shape
     if D != rope.head_dim:
         raise ValueError(f"x: heads of {rope.head_dim} elements expected")
-    with _on(stream, x.device) as s:
-        if out is None:
-            out = torch.empty((T, H, D), dtype=x.dtype, device=x.device)
-        if out.dtype != x.dtype:
-            raise ValueError("out: the type of x expected")
-        _check(lib().esp_kv_rotate(rope.ptr, _TYPES[x.dtype], T, H, D, _view(x, T, H, D, "x", x.device),
-                                   _ints(positions, T, "positions", x.device), int(bool(inverse)),
-                                   _view(out, T, H, D, "out", x.device), s), "esp_kv_rotate")
+    if out is None:
+        out = torch.empty((T, H, D), dtype=x.dtype, device=x.device)
+    elif out.dtype != x.dtype:
+        raise ValueError("out: the type of x expected")
+    _check(lib().esp_kv_rotate(rope.ptr, kind, T, H, D, _view(x, T, H, D, "x", x.device), _ints(positions, T, "positions", x.device),
+                               1 if inverse else 0, _view(out, T, H, D, "out", x.device), s), "esp_kv_rotate")
     return out
 
 
@@ -184,11 +194,12 @@ class PagedCache:
             if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous() or t.device != k.device or not t.is_cuda:
                 raise ValueError(f"{name}: contiguous {dtype} device tensor of shape {shape} expected")
         self.k, self.v, self.scale, self.table, self.lengths, self.refs = k, v, scale, table, lengths, refs
-        self.device = k.device
+        self.device, self.index = k.device, k.device.index
         self.status = torch.zeros(1, dtype=torch.int32, device=k.device)
         self.pages, self.layers, self.kv_heads, self.page_tokens, self.head_dim = P, L, H, T, D
         self.sequences, self.table_width = table.shape
-        self._work = {}
+        self._work, self._sizes = {}, {}
+        self._scale, self._pages_bytes = D ** -0.5, None
         self._describe()
 
     def _describe(self) -> None:
@@ -211,103 +222,114 @@ class PagedCache:
         return w
 
     def _rows(self, offsets, seqs):
-        if offsets.numel() < 1:
-            raise ValueError("offsets: [rows + 1] expected")
         rows = offsets.numel() - 1
-        if seqs is None and rows > self.sequences:
-            raise ValueError("more rows than sequences")
+        if rows < 0 or (seqs is None and rows > self.sequences):
+            raise ValueError("offsets: [rows + 1] expected, with no more rows than sequences")
         return rows, _ints(offsets, None, "offsets", self.device), None if seqs is None else _ints(seqs, rows, "seqs", self.device)
 
-    def append(self, layer: int, k, v, offsets, rope: Optional[Rope] = None, q=None, seqs=None, stream=None):
+    @_on_stream
+    def append(self, layer: int, k, v, offsets, rope: Optional[Rope] = None, q=None, seqs=None, *, s: int):
         """Writes the new tokens k, v [tokens, kv_heads, head_dim], the last ones of their sequences, rows cut by
         offsets (int32 [rows + 1]); q [tokens, q_heads, head_dim] is turned too and returned."""
-        if k.dim() != 3 or k.dtype not in (torch.bfloat16, torch.float16) or v.dtype != k.dtype or (q is not None and q.dtype != k.dtype):
+        kind = _TYPES.get(k.dtype)
+        if kind is None or kind == FP32 or k.dim() != 3 or v.dtype != k.dtype or (q is not None and (q.dtype != k.dtype or q.dim() != 3)):
             raise ValueError("k, v and q: bfloat16 or float16 [tokens, heads, head_dim] expected, of one type")
         if rope is not None and rope.head_dim != self.head_dim:
             raise ValueError("rope: made for another head_dim")
         if q is not None and rope is None:
             raise ValueError("q is given to be turned: rope expected")
-        T, H, D = k.shape[0], self.kv_heads, self.head_dim
+        T, H, D, dev = k.shape[0], self.kv_heads, self.head_dim, self.device
         rows, off, sq = self._rows(offsets, seqs)
-        with _on(stream, self.device) as s:
-            out, heads, vq, vo = None, 0, _NO_VIEW, _NO_VIEW
-            if q is not None:
-                heads = q.shape[1]
-                if q.numel() and (q.data_ptr() % 16 or q.stride(0) % 8 or q.stride(1) % 8):
-                    q = q.contiguous()
-                out = torch.empty((T, heads, D), dtype=q.dtype, device=self.device)
-                vq, vo = _view(q, T, heads, D, "q", self.device), _view(out, T, heads, D, "q", self.device)
-            _check(lib().esp_kv_append(self.ptr, int(layer), _TYPES[k.dtype], rows, T, off, sq, _view(k, T, H, D, "k", self.device),
-                                       _view(v, T, H, D, "v", self.device), None if rope is None else rope.ptr, heads, vq, vo, s),
-                   "esp_kv_append")
+        out, heads, vq, vo = None, 0, _NO_VIEW, _NO_VIEW
+        if q is not None:
+            heads = q.shape[1]
+            if q.numel() and (q.data_ptr() % 16 or q.stride(0) % 8 or q.stride(1) % 8):
+                q = q.contiguous()
+            out = torch.empty((T, heads, D), dtype=q.dtype, device=dev)
+            vq, vo = _view(q, T, heads, D, "q", dev), _view(out, T, heads, D, "q", dev)
+        _check(lib().esp_kv_append(self.ptr, layer, kind, rows, T, off, sq, _view(k, T, H, D, "k", dev), _view(v, T, H, D, "v", dev),
+                                   None if rope is None else rope.ptr, heads, vq, vo, s), "esp_kv_append")
         return out
 
-    def gather(self, layer: int, starts, offsets, tokens: int, dtype=torch.bfloat16, seqs=None, stream=None):
+    @_on_stream
+    def gather(self, layer: int, starts, offsets, tokens: int, dtype=torch.bfloat16, seqs=None, *, s: int):
         """Keys and values [tokens, kv_heads, head_dim] of row b's tokens from starts[b] on, as numbers; `tokens` is
         the last of offsets."""
-        if dtype not in (torch.bfloat16, torch.float16):
+        kind = _TYPES.get(dtype)
+        if kind is None or kind == FP32:
             raise ValueError("dtype: bfloat16 or float16 expected")
         rows, off, sq = self._rows(offsets, seqs)
-        with _on(stream, self.device) as s:
-            k, v = (torch.empty((tokens, self.kv_heads, self.head_dim), dtype=dtype, device=self.device) for _ in range(2))
-            _check(lib().esp_kv_gather(self.ptr, int(layer), _TYPES[dtype], rows, int(tokens), off, sq,
-                                       _ints(starts, rows, "starts", self.device), k.data_ptr(), v.data_ptr(), s), "esp_kv_gather")
+        k, v = torch.empty((2, tokens, self.kv_heads, self.head_dim), dtype=dtype, device=self.device)
+        _check(lib().esp_kv_gather(self.ptr, layer, kind, rows, tokens, off, sq, _ints(starts, rows, "starts", self.device),
+                                   k.data_ptr(), v.data_ptr(), s), "esp_kv_gather")
         return k, v
 
+    @_on_stream
     def attend(self, layer: int, q, offsets, scale: Optional[float] = None, window: int = 0, max_new: Optional[int] = None,
-               max_length: Optional[int] = None, out=None, lse: bool = True, seqs=None, stream=None):
+               max_length: Optional[int] = None, out=None, lse: bool = True, seqs=None, *, s: int):
         """(out, lse) of q [tokens, q_heads, head_dim] over the cache; scale defaults to head_dim ** -0.5.  max_new and
         max_length bound the rows' tokens and the sequences' lengths (default: what the shapes allow)."""
-        if q.dim() != 3 or q.dtype not in (torch.bfloat16, torch.float16):
+        kind = _TYPES.get(q.dtype)
+        if kind is None or kind == FP32 or q.dim() != 3:
             raise ValueError("q: bfloat16 or float16 [tokens, q_heads, head_dim] expected")
-        T, H, D = q.shape[0], q.shape[1], self.head_dim
+        T, H, D = q.shape
         rows, off, sq = self._rows(offsets, seqs)
-        scale = D ** -0.5 if scale is None else float(scale)
-        max_new = T if max_new is None else int(max_new)
-        max_length = self.table_width * self.page_tokens if max_length is None else int(max_length)
-        n = C.c_size_t(0)
-        _check(lib().esp_kv_attend_workspace(self.ptr, rows, T, H, max_new, max_length, C.byref(n)), "esp_kv_attend_workspace")
-        with _on(stream, self.device) as s:
-            if out is None:
-                out = torch.empty((T, H, D), dtype=q.dtype, device=self.device)
-            if out.dtype != q.dtype:
-                raise ValueError("out: the type of q expected")
-            stats = torch.empty((T, H), dtype=torch.float32, device=self.device) if lse else None
-            w = self._workspace("attend", n.value, s)
-            _check(lib().esp_kv_attend(self.ptr, int(layer), _TYPES[q.dtype], rows, T, off, sq, H, _view(q, T, H, D, "q", self.device),
-                                       scale, int(window), max_new, max_length, _view(out, T, H, D, "out", self.device),
-                                       None if stats is None else stats.data_ptr(), w.data_ptr(), w.numel(), s), "esp_kv_attend")
+        if scale is None:
+            scale = self._scale
+        if max_new is None:
+            max_new = T
+        if max_length is None:
+            max_length = self.table_width * self.page_tokens
+        shape = (rows, T, H, max_new, max_length)
+        size = self._sizes.get(shape)
+        if size is None:
+            n = C.c_size_t(0)
+            _check(lib().esp_kv_attend_workspace(self.ptr, *shape, C.byref(n)), "esp_kv_attend_workspace")
+            if len(self._sizes) >= 4096:
+                self._sizes.clear()
+            size = self._sizes[shape] = n.value
+        if out is None:
+            out = torch.empty((T, H, self.head_dim), dtype=q.dtype, device=self.device)
+        elif out.dtype != q.dtype:
+            raise ValueError("out: the type of q expected")
+        stats = torch.empty((T, H), dtype=torch.float32, device=self.device) if lse else None
+        w = self._workspace("attend", size, s)
+        _check(lib().esp_kv_attend(self.ptr, layer, kind, rows, T, off, sq, H, _view(q, T, H, self.head_dim, "q", self.device), scale,
+                                   window, max_new, max_length, _view(out, T, H, self.head_dim, "out", self.device),
+                                   None if stats is None else stats.data_ptr(), w.data_ptr(), w.numel(), s), "esp_kv_attend")
         return out, stats
 
-    def _pages_work(self, n: int, stream: int) -> torch.Tensor:
-        z = C.c_size_t(0)
-        _check(lib().esp_kv_pages_workspace(self.ptr, n, C.byref(z)), "esp_kv_pages_workspace")
-        return self._workspace("pages", z.value, stream)
+    def _pages_work(self, stream: int) -> torch.Tensor:
+        if self._pages_bytes is None:
+            z = C.c_size_t(0)
+            _check(lib().esp_kv_pages_workspace(self.ptr, self.sequences, C.byref(z)), "esp_kv_pages_workspace")
+            self._pages_bytes = z.value
+        return self._workspace("pages", self._pages_bytes, stream)
 
-    def resize(self, lengths, stream=None) -> None:
+    @_on_stream
+    def resize(self, lengths, *, s: int) -> None:
         """Sets every sequence's length (int32 [sequences]): pages are freed and the lowest free ones taken."""
-        with _on(stream, self.device) as s:
-            w = self._pages_work(0, s)
-            _check(lib().esp_kv_resize(self.ptr, _ints(lengths, self.sequences, "lengths", self.device), w.data_ptr(), w.numel(), s),
-                   "esp_kv_resize")
+        w = self._pages_work(s)
+        _check(lib().esp_kv_resize(self.ptr, _ints(lengths, self.sequences, "lengths", self.device), w.data_ptr(), w.numel(), s),
+               "esp_kv_resize")
 
-    def fork(self, parents, children, stream=None) -> None:
+    @_on_stream
+    def fork(self, parents, children, *, s: int) -> None:
         """children[i] drops its pages and continues parents[i] (int32 [n] each)."""
         n = parents.numel()
-        with _on(stream, self.device) as s:
-            w = self._pages_work(n, s)
-            _check(lib().esp_kv_fork(self.ptr, n, _ints(parents, n, "parents", self.device), _ints(children, n, "children", self.device),
-                                     w.data_ptr(), w.numel(), s), "esp_kv_fork")
+        w = self._pages_work(s)
+        _check(lib().esp_kv_fork(self.ptr, n, _ints(parents, n, "parents", self.device), _ints(children, n, "children", self.device),
+                                 w.data_ptr(), w.numel(), s), "esp_kv_fork")
 
-    def compact(self, limit: Optional[int] = None, stream=None):
+    @_on_stream
+    def compact(self, limit: Optional[int] = None, *, s: int):
         """(table, refs, live) with no live page from `limit` on (None: from the number of live pages on).  The cache
         goes on with its old table, whose pages stay intact, until `install` is given the new one."""
-        with _on(stream, self.device) as s:
-            table, refs = torch.empty_like(self.table), torch.empty_like(self.refs)
-            live = torch.empty((), dtype=torch.int32, device=self.device)
-            w = self._pages_work(0, s)
-            _check(lib().esp_kv_compact(self.ptr, -1 if limit is None else int(limit), table.data_ptr(), refs.data_ptr(), live.data_ptr(),
-                                        w.data_ptr(), w.numel(), s), "esp_kv_compact")
+        table, refs = torch.empty_like(self.table), torch.empty_like(self.refs)
+        live = torch.empty((), dtype=torch.int32, device=self.device)
+        w = self._pages_work(s)
+        _check(lib().esp_kv_compact(self.ptr, -1 if limit is None else limit, table.data_ptr(), refs.data_ptr(), live.data_ptr(),
+                                    w.data_ptr(), w.numel(), s), "esp_kv_compact")
         return table, refs, live
 
     def install(self, table, refs) -> None:
@@ -319,7 +341,7 @@ class PagedCache:
         self.table, self.refs = table, refs
         self._describe()
 
-    def device_status(self, stream=None) -> int:
+    @_on_stream
+    def device_status(self, *, s: int) -> int:
         """The first error that the GPU recorded since the last call (waits for the stream)."""
-        with _on(stream, self.device) as s:
-            return int(lib().esp_kv_device_status(self.ptr, s))
+        return int(lib().esp_kv_device_status(self.ptr, s))

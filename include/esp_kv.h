@@ -12,7 +12,7 @@
  * The pool is page-major, so a pool whose last pages are empty can be cut:
  *   k      [pages][layers][kv_heads][page_tokens][head_dim]   e4m3 (OCP), 1 byte
  *   v      [pages][layers][kv_heads][head_dim][page_tokens]   e4m3, token innermost
- *   scale  [pages][layers][2: k, v][kv_heads]                 float32, value = code * scale
+ *   scale  [pages][layers][2: k, v][kv_heads]                 float32 >= 0, value = code * scale
  *   table  [sequences][table_width]  page of tokens [i*page_tokens, (i+1)*page_tokens), -1 none
  *   lengths[sequences]               tokens held
  *   refs   [pages]                   table entries that name the page; 0 = free
@@ -107,8 +107,8 @@ esp_status esp_kv_append(const esp_kv_cache *cache, int32_t layer, int32_t type,
 /*
  * Reads tokens back: row b's tokens [starts[b], starts[b] + offsets[b+1] -
  * offsets[b]) of sequence seqs[b] as numbers, into k_out and v_out
- * [tokens][kv_heads][head_dim], contiguous, type bf16 or fp16.  Tokens beyond
- * a sequence's length read as 0.
+ * [tokens][kv_heads][head_dim], contiguous, type bf16 or fp16.  Tokens past a
+ * sequence's end read as 0; a row with a negative start is left out.
  */
 esp_status esp_kv_gather(const esp_kv_cache *cache, int32_t layer, int32_t type, int32_t rows, int64_t tokens,
                          const int32_t *offsets, const int32_t *seqs, const int32_t *starts, void *k_out, void *v_out,

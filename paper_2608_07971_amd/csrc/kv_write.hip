@@ -10,15 +10,21 @@ struct View {
     int64_t token, head;
 };
 
-// The row whose tokens hold token t: the last b with offsets[b] <= t.
-__device__ __forceinline__ int row_at(const int32_t *offsets, int rows, int64_t t) {
-    int lo = 0, hi = rows - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (offsets[mid] <= t) lo = mid;
-        else hi = mid - 1;
+// How many b in [0, rows) have f(b) <= x, f ascending: 64 at a time by the lanes of a wavefront.
+template <typename F> __device__ __forceinline__ int count_up_to(int rows, int64_t x, F f) {
+    const int lane = threadIdx.x & 63;
+    int n = 0;
+    for (int b0 = 0; b0 < rows; b0 += 256) {          // four loads in flight
+        int held = 0;
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            const int b = b0 + 64 * k + lane;
+            held += __popcll(__ballot(b < rows && f(b) <= x));
+        }
+        n += held;
+        if (held < 256) break;
     }
-    return lo;
+    return n;
 }
 
 // ---------------------------------------------------------------------------
@@ -140,17 +146,8 @@ struct AppendArgs {
     Rows rows;
     Rope rope;           // rotary = 0: none
     View k, v, q, q_out;
-    int32_t layer, q_heads, units;
+    int32_t layer, q_heads, units, writers, shares, per, wide;
 };
-
-__device__ __forceinline__ float block_max(float x, float *lds) {
-#pragma unroll
-    for (int m = 32; m; m >>= 1) x = fmaxf(x, __shfl_xor(x, m));
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
-    __syncthreads();
-    return fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]));
-}
 
 // The least exponent e with most <= 448 * 2^e (448 = 1.75 * 2^8), within +-100.
 __device__ __forceinline__ float least_scale(float most) {
@@ -166,147 +163,310 @@ __device__ __forceinline__ uint32_t code2(float a, float b) {
     return __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
 }
 
-// A workgroup writes one page's new tokens for one head, keys or values: the
-// values stay in registers between the largest and the codes.
-template <typename T, int Dim, int Page> __device__ void append_block(const AppendArgs &a, int unit, int head, int which) {
-    constexpr int kPairs = Dim / 2, kStep = kThreads / kPairs, kRounds = (Page + kStep - 1) / kStep;
-    __shared__ float lds[4];
-    const Cache &c = a.c;
-    // units: a row of n tokens touches at most n / Page + 2 pages
-    int lo = 0, hi = a.rows.rows - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (a.rows.offsets[mid] / Page + 2 * mid <= unit) lo = mid;
-        else hi = mid - 1;
+// A unit is one page that a row's tokens touch: row b's units are numbered from
+// offsets[b] / Page + 2 b (n tokens touch at most n / Page + 2 pages).
+struct Unit {
+    Row row;
+    int b, slot, page;                      // page -1: there is none
+    int from, to;                           // positions of the row's tokens in this page; from = to: nothing to do
+};
+template <int Page> __device__ __forceinline__ Unit unit_of(const Cache &c, const Rows &r, int unit, const int32_t *starts) {
+    auto base = [&](int b) { return r.offsets[b] / Page + 2 * b; };
+    Unit u{};
+    const int b = count_up_to(r.rows, unit, base) - 1;
+    if (b < 0) return u;
+    u.b = b;
+    u.row = row_of(c, r, b);
+    // new tokens: the last n of the sequence, none before its start; read back: any from `starts` on
+    const int64_t first = starts ? int64_t(starts[b]) : int64_t(u.row.length) - u.row.n, last = first + u.row.n;
+    if (starts && (first < 0 || last > INT32_MAX)) {
+        record(c, ESP_ERR_SHAPE);
+        return u;
     }
-    const Row row = row_of(c, a.rows, lo);
-    const int p0 = row.length - row.n, from = max(p0, 0);
-    const int slot = from / Page + unit - (a.rows.offsets[lo] / Page + 2 * lo);
-    if (row.n == 0 || unit < a.rows.offsets[lo] / Page + 2 * lo || int64_t(slot) * Page >= row.length) return;
-    const int32_t page = c.table[int64_t(row.seq) * c.width + slot];
-    if (page < 0 || page >= c.pages) {
-        if (threadIdx.x == 0) record(c, ESP_ERR_SHAPE);
-        return;
-    }
-    const int i = threadIdx.x % kPairs, t0 = threadIdx.x / kPairs;
-    int ea = 2 * i, eb = 2 * i + 1;
-    const bool turn = which == 0 && i < a.rope.rotary / 2;
-    if (which == 0 && a.rope.rotary) pair_of(a.rope, i, ea, eb);
-    const double turns = turn ? a.rope.turns[i] : 0.0;
-    const View &x = which ? a.v : a.k;
-    float va[kRounds], vb[kRounds], most = 0.0f;
-#pragma unroll
-    for (int k = 0; k < kRounds; k++) {
-        const int p = slot * Page + t0 + k * kStep;
-        va[k] = vb[k] = 0.0f;
-        if (p >= from && p < row.length && t0 + k * kStep < Page) {
-            const T *src = static_cast<const T *>(x.data) + int64_t(row.first + (p - p0)) * x.token + head * x.head;
-            va[k] = float(src[ea]);
-            vb[k] = float(src[eb]);
-            if (turn) {
-                float cs, sn;
-                cos_sin(double(p) * turns, cs, sn);
-                cs *= a.rope.magnitude;
-                sn *= a.rope.magnitude;
-                const float fa = va[k], fb = vb[k];
-                va[k] = __builtin_fmaf(fa, cs, -(fb * sn));
-                vb[k] = __builtin_fmaf(fa, sn, fb * cs);
-            }
-            const float ma = fabsf(va[k]), mb = fabsf(vb[k]);
-            most = fmaxf(most, fmaxf(ma < INFINITY ? ma : 0.0f, mb < INFINITY ? mb : 0.0f));
+    const int64_t from = max(first, int64_t(0)), slot = from / Page + unit - base(b);
+    if (u.row.n == 0 || unit < base(b) || slot * Page >= last) return u;
+    u.slot = int(slot);
+    u.from = int(max(from, slot * Page));
+    u.to = int(min(last, slot * Page + Page));
+    u.page = -1;
+    if (slot * Page < u.row.length) {
+        u.page = c.table[int64_t(u.row.seq) * c.width + u.slot];
+        if (u.page < 0 || u.page >= c.pages) {
+            record(c, ESP_ERR_SHAPE);
+            u.page = -1;
         }
     }
-    most = block_max(most, lds);
-    float *place = c.block_scale(page, a.layer, which, head);
-    const bool older = slot * Page < from;
-    const float least = least_scale(most), was = *place, scale = older ? fmaxf(was, least) : least;
-    uint8_t *block = (which ? c.v : c.k) + c.block(page, a.layer, head);
-    const int ta = which ? ea * Page : ea, tb = which ? eb * Page : eb, step = which ? 1 : Dim;
-    if (older && scale > was) {
-        const float by = was / scale;
-        for (int t = t0; slot * Page + t < from; t += kStep) {
-            uint8_t *pa = block + ta + t * step, *pb = block + tb + t * step;
-            const uint32_t w = uint32_t(*pa) | uint32_t(*pb) << 8;
-            const half2 n = codes<false>(w, static_cast<half2 *>(nullptr));
-            const uint32_t z = code2(float(n[0]) * by, float(n[1]) * by);
-            *pa = uint8_t(z);
-            *pb = uint8_t(z >> 8);
-        }
-    }
-    __syncthreads();                                  // every thread has read the old scale
-#pragma unroll
-    for (int k = 0; k < kRounds; k++) {
-        const int t = t0 + k * kStep, p = slot * Page + t;
-        if (p >= from && p < row.length && t < Page) {
-            const uint32_t z = code2(va[k] / scale, vb[k] / scale);
-            block[ta + t * step] = uint8_t(z);
-            block[tb + t * step] = uint8_t(z >> 8);
-        }
-    }
-    if (threadIdx.x == 0) *place = scale;
+    return u;
 }
 
-// Workgroups [0, units * heads * 2) write; the others turn the queries.
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+    for (int m = 32; m; m >>= 1) x = fmaxf(x, __shfl_xor(x, m));
+    return x;
+}
+__device__ __forceinline__ float finite_abs(float x) {
+    x = fabsf(x);
+    return x < INFINITY ? x : 0.0f;
+}
+
+template <typename T> struct Vec4 { T x[4]; };
+template <typename T> __device__ __forceinline__ Vec4<T> load4(const T *p, bool wide) {
+    Vec4<T> v;
+    if (wide) *reinterpret_cast<uint2v *>(v.x) = *reinterpret_cast<const uint2v *>(p);
+    else
+#pragma unroll
+        for (int i = 0; i < 4; i++) v.x[i] = p[i];
+    return v;
+}
+
+// Codes of a page that a growing scale makes smaller: 4 at a time.
+__device__ __forceinline__ uint32_t rescaled(uint32_t w, float by) {
+    const half2 a = codes<false>(w, static_cast<half2 *>(nullptr)), b = codes<true>(w, static_cast<half2 *>(nullptr));
+    return code2(float(a[0]) * by, float(a[1]) * by) | code2(float(b[0]) * by, float(b[1]) * by) << 16;
+}
+
+// The scale of a block, and its old codes brought to it.  `most`: of the new values.
+struct Scale {
+    float *place, was, now;
+    bool older;
+};
+__device__ __forceinline__ Scale scale_of(const AppendArgs &a, const Unit &u, int which, int head, int page_tokens, float most) {
+    Scale s;
+    s.place = a.c.block_scale(u.page, a.layer, which, head);
+    s.older = u.slot * page_tokens < u.from;
+    s.was = *s.place;
+    const float least = least_scale(most);
+    s.now = s.older ? fmaxf(s.was, least) : least;
+    return s;
+}
+
+// A wavefront writes a page's new keys of one head.  A lane takes four pairs of
+// one token, four (heads of 128) or eight (of 64) tokens at a time; the values
+// stay in registers between the largest and the codes.
+template <typename T, int Dim, int Page> __device__ __forceinline__ void append_keys(const AppendArgs &a, const Unit &u, int head) {
+    constexpr int kLanes = Dim / 8, kTokens = 64 / kLanes, kRounds = Page / kTokens;
+    const int lane = threadIdx.x & 63, part = lane % kLanes, t0 = u.slot * Page + lane / kLanes;
+    const int half = a.rope.rotary >> 1, i0 = 4 * part;
+    const bool turn = i0 < half, apart = turn && !a.rope.interleaved;
+    const int ea = apart ? i0 : 8 * part, eb = apart ? i0 + half : 8 * part + 4;      // elements ea.. and eb..
+    double turns[4];
+#pragma unroll
+    for (int j = 0; j < 4; j++) turns[j] = turn ? a.rope.turns[i0 + j] : 0.0;
+    const T *src = static_cast<const T *>(a.k.data) + head * a.k.head + (int64_t(u.row.first) + t0 - (u.row.length - u.row.n)) * a.k.token;
+    float x[kRounds][8], most = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kRounds; k++) {
+        const int p = t0 + k * kTokens;
+#pragma unroll
+        for (int j = 0; j < 8; j++) x[k][j] = 0.0f;
+        if (p >= u.from && p < u.to) {
+            const T *from = src + int64_t(k * kTokens) * a.k.token;
+            const Vec4<T> va = load4(from + ea, a.wide), vb = load4(from + eb, a.wide);
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                x[k][j] = float(va.x[j]);
+                x[k][4 + j] = float(vb.x[j]);
+            }
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kRounds; k++) {
+        const int p = t0 + k * kTokens;
+        if (kRounds > 1 && !__any(p >= u.from && p < u.to)) continue;
+        if (turn) {
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                float cs, sn;
+                cos_sin(double(p) * turns[j], cs, sn);
+                cs *= a.rope.magnitude;
+                sn *= a.rope.magnitude;
+                float &fa = apart ? x[k][j] : x[k][2 * j], &fb = apart ? x[k][4 + j] : x[k][2 * j + 1];
+                const float va = fa, vb = fb;
+                fa = __builtin_fmaf(va, cs, -(vb * sn));
+                fb = __builtin_fmaf(va, sn, vb * cs);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; j++) most = fmaxf(most, finite_abs(x[k][j]));
+    }
+    const Scale s = scale_of(a, u, 0, head, Page, wave_max(most));
+    uint8_t *block = a.c.k + a.c.block(u.page, a.layer, head);
+    if (s.older && s.now > s.was) {
+        const float by = s.was / s.now;
+        uint32_t *w = reinterpret_cast<uint32_t *>(block);
+        for (int i = lane; i < (u.from - u.slot * Page) * Dim / 4; i += 64) w[i] = rescaled(w[i], by);
+    }
+#pragma unroll
+    for (int k = 0; k < kRounds; k++) {
+        const int p = t0 + k * kTokens;
+        if (p >= u.from && p < u.to) {
+            uint32_t *to = reinterpret_cast<uint32_t *>(block + (p - u.slot * Page) * Dim);
+            to[ea / 4] = code2(x[k][0] / s.now, x[k][1] / s.now) | code2(x[k][2] / s.now, x[k][3] / s.now) << 16;
+            to[eb / 4] = code2(x[k][4] / s.now, x[k][5] / s.now) | code2(x[k][6] / s.now, x[k][7] / s.now) << 16;
+        }
+    }
+    if (lane == 0) *s.place = s.now;
+}
+
+// ... and its new values.  A lane takes all tokens of one (heads of 64) or two
+// dimensions, so that sixteen tokens go out at once, as pages hold them.
+template <typename T, int Dim, int Page> __device__ __forceinline__ void append_values(const AppendArgs &a, const Unit &u, int head) {
+    constexpr int kDims = Dim / 64;
+    const int lane = threadIdx.x & 63, d0 = lane * kDims, first = u.slot * Page;
+    const T *src = static_cast<const T *>(a.v.data) + head * a.v.head + (int64_t(u.row.first) + first - (u.row.length - u.row.n)) * a.v.token + d0;
+    float x[Page][kDims], most = 0.0f;
+#pragma unroll
+    for (int t = 0; t < Page; t++) {
+#pragma unroll
+        for (int d = 0; d < kDims; d++) x[t][d] = 0.0f;
+        if (first + t >= u.from && first + t < u.to) {
+            const T *from = src + int64_t(t) * a.v.token;
+            T v[kDims];
+            if (kDims == 2 && a.wide) *reinterpret_cast<uint32_t *>(v) = *reinterpret_cast<const uint32_t *>(from);
+            else
+#pragma unroll
+                for (int d = 0; d < kDims; d++) v[d] = from[d];
+#pragma unroll
+            for (int d = 0; d < kDims; d++) x[t][d] = float(v[d]);
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < Page; t++)
+#pragma unroll
+        for (int d = 0; d < kDims; d++) most = fmaxf(most, finite_abs(x[t][d]));
+    const Scale s = scale_of(a, u, 1, head, Page, wave_max(most));
+    uint8_t *block = a.c.v + a.c.block(u.page, a.layer, head) + d0 * Page;
+    if (s.older && s.now > s.was) {
+        const float by = s.was / s.now;
+        for (int d = 0; d < kDims; d++)
+            for (int t = 0; t < u.from - first; t += 4) {       // a word may reach into the new tokens: these are written after
+                uint32_t *w = reinterpret_cast<uint32_t *>(block + d * Page + t);
+                *w = rescaled(*w, by);
+            }
+    }
+#pragma unroll
+    for (int d = 0; d < kDims; d++)
+#pragma unroll
+        for (int g = 0; g < Page; g += 16) {
+            if (first + g + 16 <= u.from || first + g >= u.to) continue;
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                w[i] = code2(x[g + 4 * i][d] / s.now, x[g + 4 * i + 1][d] / s.now) | code2(x[g + 4 * i + 2][d] / s.now, x[g + 4 * i + 3][d] / s.now) << 16;
+            uint8_t *to = block + d * Page + g;
+            if (first + g >= u.from && first + g + 16 <= u.to) {
+                *reinterpret_cast<uint4v *>(to) = uint4v{w[0], w[1], w[2], w[3]};
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; i++)
+                    if (first + g + i >= u.from && first + g + i < u.to) to[i] = uint8_t(w[i >> 2] >> (8 * (i & 3)));
+            }
+        }
+    if (lane == 0) *s.place = s.now;
+}
+
+// Workgroups [0, writers): a wavefront writes some of the 2 * heads blocks of a
+// unit; the others turn the queries.
 template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads) void k_append(AppendArgs a) {
-    const int writers = a.units * a.c.heads * 2;
-    int w = blockIdx.x;
-    if (w < writers) {
-        const int which = w & 1;
-        w >>= 1;
-        append_block<T, Dim, Page>(a, w / a.c.heads, w % a.c.heads, which);
+    if (int(blockIdx.x) < a.writers) {
+        const int w = __builtin_amdgcn_readfirstlane(blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6));
+        const int unit = w / a.shares, share = w - unit * a.shares;
+        if (unit >= a.units) return;
+        const Unit u = unit_of<Page>(a.c, a.rows, unit, nullptr);
+        if (u.from >= u.to || u.page < 0) return;
+        for (int i = share; i < 2 * a.c.heads; i += a.shares) {
+            if (i < a.c.heads) append_keys<T, Dim, Page>(a, u, i);
+            else append_values<T, Dim, Page>(a, u, i - a.c.heads);
+        }
         return;
     }
     constexpr int kChunks = Dim / 16;
-    const int64_t u = int64_t(w - writers) * kThreads + threadIdx.x, th = u / kChunks;
-    const int64_t t = th / a.q_heads;
-    if (t >= a.rows.tokens) return;
-    const int b = row_at(a.rows.offsets, a.rows.rows, t);
+    const int groups = (a.q_heads + a.per - 1) / a.per;
+    const int64_t u = int64_t(int(blockIdx.x) - a.writers) * kThreads + threadIdx.x, tg = u / kChunks;
+    const int64_t t = min(tg / groups, a.rows.tokens - 1);
+    // the row of the wavefront's first token, then step by step
+    const int64_t t_first = __shfl(int(t), 0);
+    int b = max(0, count_up_to(a.rows.rows, t_first, [&](int x) { return a.rows.offsets[x]; }) - 1);
+    if (tg / groups >= a.rows.tokens) return;
+    while (b + 1 < a.rows.rows && a.rows.offsets[b + 1] <= t) b++;
     const Row row = row_of(a.c, a.rows, b);
-    rotate_chunk<T>(a.rope, a.q, a.q_out, t, row.length - row.n + int(t - row.first), int(th - t * a.q_heads), 1,
-                    int(u % kChunks), 1.0f);
+    const int head = int(tg - t * groups) * a.per;
+    rotate_chunk<T>(a.rope, a.q, a.q_out, t, row.length - row.n + int(t - row.first), head, min(a.per, a.q_heads - head), int(u % kChunks), 1.0f);
 }
 
 // ---------------------------------------------------------------------------
-// Gather: eight values of one token and head a thread.
+// Gather: the same units, read back.
 // ---------------------------------------------------------------------------
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void k_gather(Cache c, Rows rows, const int32_t *starts, int layer, T *k, T *v) {
-    const int chunks = c.dim / 8;
-    const int64_t u = int64_t(blockIdx.x) * kThreads + threadIdx.x;
-    const int d = int(u % chunks) * 8;
-    const int64_t th = u / chunks;
-    const int h = int(th % c.heads);
-    const int64_t t = th / c.heads;
-    if (t >= rows.tokens) return;
-    const int b = row_at(rows.offsets, rows.rows, t);
-    const Row row = row_of(c, rows, b);
-    const int64_t p = int64_t(starts[b]) + (t - row.first);
-    Vec8<T> ko{}, vo{};
-    if (row.n > 0 && t >= row.first && t < row.first + row.n && p >= 0 && p < row.length) {
-        const int32_t page = c.table[int64_t(row.seq) * c.width + (p >> c.shift)];
-        if (page < 0 || page >= c.pages) {
-            record(c, ESP_ERR_SHAPE);
-        } else {
-            const int at = int(p & (c.tokens - 1));
-            const int64_t block = c.block(page, layer, h);
-            const float sk = *c.block_scale(page, layer, 0, h), sv = *c.block_scale(page, layer, 1, h);
-            const uint2v kw = *reinterpret_cast<const uint2v *>(c.k + block + int64_t(at) * c.dim + d);
-            const half8 kn = codes8<half8, half2>(kw[0], kw[1]);
-            const uint8_t *vp = c.v + block + int64_t(d) * c.tokens + at;
-            uint32_t w[2] = {0, 0};
+struct GatherArgs {
+    Cache c;
+    Rows rows;
+    const int32_t *starts;
+    int32_t layer, shares, units;
+    void *k, *v;
+};
+
+template <typename T, int Dim, int Page> __device__ __forceinline__ void gather_block(const GatherArgs &a, const Unit &u, int head, bool values) {
+    const int lane = threadIdx.x & 63, first = u.slot * Page;
+    const int64_t row_size = int64_t(a.c.heads) * Dim;
+    // the output row of the page's first token
+    T *out = static_cast<T *>(values ? a.v : a.k) + (int64_t(u.row.first) + first - a.starts[u.b]) * row_size + int64_t(head) * Dim;
+    // past the end of the sequence, or without a page: 0
+    const int held = u.page < 0 ? u.from : min(u.to, u.row.length);
+    for (int t = max(u.from, held) + lane / (Dim / 8); t < u.to; t += 512 / Dim) store8(out + (t - first) * row_size + lane % (Dim / 8) * 8, Vec8<T>{});
+    if (held <= u.from) return;
+    const float s = *a.c.block_scale(u.page, a.layer, values, head);
+    if (!values) {
+        constexpr int kLanes = Dim / 8, kTokens = 64 / kLanes;
+        const uint8_t *block = a.c.k + a.c.block(u.page, a.layer, head);
 #pragma unroll
-            for (int j = 0; j < 8; j++) w[j >> 2] |= uint32_t(vp[int64_t(j) * c.tokens]) << (8 * (j & 3));
-            const half8 vn = codes8<half8, half2>(w[0], w[1]);
+        for (int k = 0; k < Page / kTokens; k++) {
+            const int t = k * kTokens + lane / kLanes, d = lane % kLanes * 8;
+            if (first + t < u.from || first + t >= held) continue;
+            const uint2v w = *reinterpret_cast<const uint2v *>(block + t * Dim + d);
+            const half8 n = codes8<half8, half2>(w[0], w[1]);
+            Vec8<T> o;
+#pragma unroll
+            for (int j = 0; j < 8; j++) o.x[j] = T(float(n[j]) * s);
+            store8(out + t * row_size + d, o);
+        }
+        return;
+    }
+    constexpr int kDims = Dim / 64;
+    const int d0 = lane * kDims;
+    const uint8_t *block = a.c.v + a.c.block(u.page, a.layer, head) + d0 * Page;
+#pragma unroll
+    for (int g = 0; g < Page; g += 16) {
+        if (first + g + 16 <= u.from || first + g >= held) continue;
+        uint4v w[kDims];
+#pragma unroll
+        for (int d = 0; d < kDims; d++) w[d] = *reinterpret_cast<const uint4v *>(block + d * Page + g);
+#pragma unroll
+        for (int i = 0; i < 16; i += 8) {
+            half8 n[kDims];
+#pragma unroll
+            for (int d = 0; d < kDims; d++) n[d] = codes8<half8, half2>(w[d][i / 4], w[d][i / 4 + 1]);
 #pragma unroll
             for (int j = 0; j < 8; j++) {
-                ko.x[j] = T(float(kn[j]) * sk);
-                vo.x[j] = T(float(vn[j]) * sv);
+                const int t = g + i + j;
+                if (first + t < u.from || first + t >= held) continue;
+                typedef T Out __attribute__((ext_vector_type(kDims)));
+                Out o;
+#pragma unroll
+                for (int d = 0; d < kDims; d++) o[d] = T(float(n[d][j]) * s);
+                *reinterpret_cast<Out *>(out + t * row_size + d0) = o;
             }
         }
     }
-    store8(k + th * c.dim + d, ko);
-    store8(v + th * c.dim + d, vo);
+}
+
+template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads) void k_gather(GatherArgs a) {
+    const int w = __builtin_amdgcn_readfirstlane(blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6));
+    const int unit = w / a.shares, share = w - unit * a.shares;
+    if (unit >= a.units) return;
+    const Unit u = unit_of<Page>(a.c, a.rows, unit, a.starts);
+    if (u.from < u.to)
+        for (int i = share; i < 2 * a.c.heads; i += a.shares) gather_block<T, Dim, Page>(a, u, i % a.c.heads, i >= a.c.heads);
 }
 
 }  // namespace esp_kv
@@ -356,6 +516,22 @@ template <typename T, int Dim> void append(const AppendArgs &a, unsigned blocks,
     case 32: k_append<T, Dim, 32><<<blocks, kThreads, 0, s>>>(a); break;
     default: k_append<T, Dim, 64><<<blocks, kThreads, 0, s>>>(a); break;
     }
+}
+template <typename T, int Dim> void gather(const GatherArgs &a, unsigned blocks, hipStream_t s) {
+    switch (a.c.tokens) {
+    case 16: k_gather<T, Dim, 16><<<blocks, kThreads, 0, s>>>(a); break;
+    case 32: k_gather<T, Dim, 32><<<blocks, kThreads, 0, s>>>(a); break;
+    default: k_gather<T, Dim, 64><<<blocks, kThreads, 0, s>>>(a); break;
+    }
+}
+
+// Wavefronts that share the 2 * heads blocks of a unit: one for each, while that
+// is not far more than the GPU holds (8,192); steps of many sequences take fewer,
+// so that the search for the row is made for several blocks.
+int32_t shares_of(int64_t units, int32_t heads) {
+    int64_t shares = 2 * int64_t(heads);
+    while (shares > 1 && units * shares > 16384) shares = (shares + 1) / 2;
+    return int32_t(shares);
 }
 
 }  // namespace
@@ -417,13 +593,18 @@ extern "C" esp_status esp_kv_append(const esp_kv_cache *cache, int32_t layer, in
     if (!k.data || !v.data || (q_heads && (!rope || !q.data || !q_out.data))) return ESP_ERR_INVALID_ARG;
     if (q_heads && !(wide(q, 2) && wide(q_out, 2))) return ESP_ERR_INVALID_ARG;
     const int64_t units = tokens / cache->page_tokens + 2 * int64_t(rows);
-    const int64_t blocks = units * cache->kv_heads * 2 + (tokens * q_heads * (cache->head_dim / 16) + kThreads - 1) / kThreads;
-    if (blocks > INT32_MAX) return ESP_ERR_SHAPE;
+    const int32_t shares = shares_of(units, cache->kv_heads), per = 4;
+    const int64_t writers = (units * shares + kThreads / 64 - 1) / (kThreads / 64);
+    const int64_t turners = (tokens * ((q_heads + per - 1) / per) * (cache->head_dim / 16) + kThreads - 1) / kThreads;
+    if (units * shares > INT32_MAX || writers + turners > INT32_MAX) return ESP_ERR_SHAPE;
+    const unsigned blocks = unsigned(writers + turners);
+    // loads of four keys or two values at a time
+    auto fours = [](const esp_kv_view &x) { return (reinterpret_cast<uintptr_t>(x.data) & 7) == 0 && x.token_stride % 4 == 0 && x.head_stride % 4 == 0; };
     const AppendArgs a{cache_of(cache), Rows{offsets, seqs, rows, tokens}, rope_of(rope), view_of(k), view_of(v), view_of(q), view_of(q_out),
-                       layer, q_heads, int32_t(units)};
+                       layer, q_heads, int32_t(units), int32_t(writers), shares, per, fours(k) && fours(v)};
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    if (type == ESP_KV_BF16) cache->head_dim == 64 ? append<__bf16, 64>(a, unsigned(blocks), s) : append<__bf16, 128>(a, unsigned(blocks), s);
-    else cache->head_dim == 64 ? append<_Float16, 64>(a, unsigned(blocks), s) : append<_Float16, 128>(a, unsigned(blocks), s);
+    if (type == ESP_KV_BF16) cache->head_dim == 64 ? append<__bf16, 64>(a, blocks, s) : append<__bf16, 128>(a, blocks, s);
+    else cache->head_dim == 64 ? append<_Float16, 64>(a, blocks, s) : append<_Float16, 128>(a, blocks, s);
     return launched();
 }
 
@@ -436,11 +617,13 @@ extern "C" esp_status esp_kv_gather(const esp_kv_cache *cache, int32_t layer, in
     if (esp_status e = check_rows(rows, tokens, offsets)) return e;
     if (rows == 0 || tokens == 0) return ESP_OK;
     if (!starts || !k_out || !v_out || !aligned16(k_out) || !aligned16(v_out)) return ESP_ERR_INVALID_ARG;
-    const int64_t blocks = (tokens * cache->kv_heads * (cache->head_dim / 8) + kThreads - 1) / kThreads;
-    if (blocks > INT32_MAX) return ESP_ERR_SHAPE;
+    const int64_t units = tokens / cache->page_tokens + 2 * int64_t(rows);
+    const int32_t shares = shares_of(units, cache->kv_heads);
+    if (units * shares > INT32_MAX) return ESP_ERR_SHAPE;
+    const unsigned blocks = unsigned((units * shares + kThreads / 64 - 1) / (kThreads / 64));
+    const GatherArgs a{cache_of(cache), Rows{offsets, seqs, rows, tokens}, starts, layer, shares, int32_t(units), k_out, v_out};
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    const Rows r{offsets, seqs, rows, tokens};
-    if (type == ESP_KV_BF16) k_gather<__bf16><<<unsigned(blocks), kThreads, 0, s>>>(cache_of(cache), r, starts, layer, static_cast<__bf16 *>(k_out), static_cast<__bf16 *>(v_out));
-    else k_gather<_Float16><<<unsigned(blocks), kThreads, 0, s>>>(cache_of(cache), r, starts, layer, static_cast<_Float16 *>(k_out), static_cast<_Float16 *>(v_out));
+    if (type == ESP_KV_BF16) cache->head_dim == 64 ? gather<__bf16, 64>(a, blocks, s) : gather<__bf16, 128>(a, blocks, s);
+    else cache->head_dim == 64 ? gather<_Float16, 64>(a, blocks, s) : gather<_Float16, 128>(a, blocks, s);
     return launched();
 }

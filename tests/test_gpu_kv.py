@@ -244,6 +244,25 @@ def test_append_strided_inputs_subset_of_sequences_and_layers():
     assert cache.device_status() == 0
 
 
+@pytest.mark.parametrize("page,dim", [(16, 64), (64, 128)])
+def test_gather_past_the_end_and_wrong_starts(page, dim):
+    cache = ref.make(kv, [70, 0, 33], heads=3, dim=dim, page=page)
+    dev = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    kp, vp = ref.host(cache)
+    table = cache.table.cpu().numpy()
+    k, v = cache.gather(0, dev([60, 5, 0]), ref.offsets([200, 3, 40]), 243, dtype=torch.float16)
+    assert cache.device_status() == 0
+    for pool, got in ((kp, k), (vp, v)):
+        want = np.zeros((243, 3, dim))
+        want[:10], want[203:236] = ref.tokens_of(pool, table[0], 70)[60:], ref.tokens_of(pool, table[2], 33)
+        assert (np.abs(_np(got) - want) <= 2.0 ** -11 * np.abs(want) + 2.0 ** -25).all()
+    good = cache.gather(0, dev([60, 0, 0]), ref.offsets([3, 0, 2]), 5)[0]
+    bad = cache.gather(0, dev([60, 0, -1]), ref.offsets([3, 0, 2]), 5)[0]
+    assert torch.equal(bad[:3], good[:3]) and cache.device_status() == esp.ESP_ERR_SHAPE
+    cache.table[0, 0] = -1
+    assert not cache.gather(0, dev([0]), ref.offsets([16]), 16)[0].any() and cache.device_status() == esp.ESP_ERR_SHAPE
+
+
 # ---------------------------------------------------------------------------
 # Attention
 # ---------------------------------------------------------------------------

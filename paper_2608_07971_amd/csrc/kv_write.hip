@@ -69,14 +69,6 @@ __global__ __launch_bounds__(kThreads) void k_rotate_any(Rope r, View x, View ou
 }
 
 template <typename T> struct Vec8 { T x[8]; };
-template <typename T> __device__ __forceinline__ Vec8<T> load8(const T *p) {
-    Vec8<T> v;
-    const uint4v *q = reinterpret_cast<const uint4v *>(p);
-    uint4v *w = reinterpret_cast<uint4v *>(v.x);
-#pragma unroll
-    for (int i = 0; i < int(sizeof(T)) / 2; i++) w[i] = q[i];
-    return v;
-}
 template <typename T> __device__ __forceinline__ void store8(T *p, const Vec8<T> &v) {
     uint4v *q = reinterpret_cast<uint4v *>(p);
     const uint4v *w = reinterpret_cast<const uint4v *>(v.x);
@@ -84,57 +76,78 @@ template <typename T> __device__ __forceinline__ void store8(T *p, const Vec8<T>
     for (int i = 0; i < int(sizeof(T)) / 2; i++) q[i] = w[i];
 }
 
-// Eight pairs a thread (16 elements), for `per` heads in turn, so that the
-// angles are worked out once for them.  Chunk c of a head: the pairs
-// [8c, 8c + 8); chunks past the rotary part pass through.
+// Two 16-byte vectors of a head a thread, for up to kPer heads, so that the
+// angles are worked out once for them and their loads are in flight together.
+// Neighbouring threads take neighbouring vectors: with halves thread c has
+// vectors c and c + n of the turned part's 2 n (a pair's two sides), with
+// neighbours as pairs the same vectors, each with pairs of its own; then the
+// same of the part that passes through.
+constexpr int kPer = 4;
 template <typename T>
 __device__ __forceinline__ void rotate_chunk(const Rope &r, const View &x, const View &out, int64_t t, int position,
-                                             int head, int heads, int c, float sign) {
-    const int half = r.rotary >> 1, i0 = 8 * c;
-    const bool turn = i0 < half;
-    float cs[8], sn[8];
-    if (turn) {
+                                             int head, int heads, int dim, int c, float sign) {
+    constexpr int kVec = 16 / sizeof(T);
+    union Vec {
+        uint4v w;
+        T x[kVec];
+    };
+    const int turned = r.rotary / (2 * kVec), rest = dim / (2 * kVec) - turned;
+    const bool turn = c < turned;
+    const int a = (turn ? c : c + turned) * kVec, b = a + (turn ? turned : rest) * kVec;
+    const T *p = static_cast<const T *>(x.data) + t * x.token + int64_t(head) * x.head;
+    T *o = static_cast<T *>(out.data) + t * out.token + int64_t(head) * out.head;
+    Vec u[kPer], v[kPer];
 #pragma unroll
-        for (int j = 0; j < 8; j++) {
-            cos_sin(double(position) * r.turns[i0 + j], cs[j], sn[j]);
+    for (int h = 0; h < kPer; h++) {
+        const T *from = p + min(h, heads - 1) * x.head;
+        u[h].w = *reinterpret_cast<const uint4v *>(from + a);
+        v[h].w = *reinterpret_cast<const uint4v *>(from + b);
+    }
+    if (turn) {
+        float cs[kVec], sn[kVec];
+#pragma unroll
+        for (int j = 0; j < kVec; j++) {
+            const int i = !r.interleaved ? a + j : j < kVec / 2 ? a / 2 + j : b / 2 + j - kVec / 2;
+            cos_sin(double(position) * r.turns[i], cs[j], sn[j]);
             cs[j] *= r.magnitude;
             sn[j] *= sign * r.magnitude;
         }
-    }
-    const int a = turn && !r.interleaved ? i0 : 16 * c, b = turn && !r.interleaved ? i0 + half : 16 * c + 8;
-    const T *p = static_cast<const T *>(x.data) + t * x.token + int64_t(head) * x.head;
-    T *o = static_cast<T *>(out.data) + t * out.token + int64_t(head) * out.head;
-    for (int h = 0; h < heads; h++, p += x.head, o += out.head) {
-        Vec8<T> u = load8(p + a), v = load8(p + b);
-        if (turn && r.interleaved) {
+        auto pair = [](T &ya, T &yb, float cs, float sn) {
+            const float fa = float(ya), fb = float(yb);
+            ya = T(__builtin_fmaf(fa, cs, -(fb * sn)));
+            yb = T(__builtin_fmaf(fa, sn, fb * cs));
+        };
+        if (r.interleaved) {
 #pragma unroll
-            for (int j = 0; j < 8; j++) {
-                T &va = j < 4 ? u.x[2 * j] : v.x[2 * j - 8], &vb = j < 4 ? u.x[2 * j + 1] : v.x[2 * j - 7];
-                const float fa = float(va), fb = float(vb);
-                va = T(__builtin_fmaf(fa, cs[j], -(fb * sn[j])));
-                vb = T(__builtin_fmaf(fa, sn[j], fb * cs[j]));
-            }
-        } else if (turn) {
+            for (int h = 0; h < kPer; h++)
 #pragma unroll
-            for (int j = 0; j < 8; j++) {
-                const float fa = float(u.x[j]), fb = float(v.x[j]);
-                u.x[j] = T(__builtin_fmaf(fa, cs[j], -(fb * sn[j])));
-                v.x[j] = T(__builtin_fmaf(fa, sn[j], fb * cs[j]));
-            }
+                for (int j = 0; j < kVec / 2; j++) {
+                    pair(u[h].x[2 * j], u[h].x[2 * j + 1], cs[j], sn[j]);
+                    pair(v[h].x[2 * j], v[h].x[2 * j + 1], cs[j + kVec / 2], sn[j + kVec / 2]);
+                }
+        } else {
+#pragma unroll
+            for (int h = 0; h < kPer; h++)
+#pragma unroll
+                for (int j = 0; j < kVec; j++) pair(u[h].x[j], v[h].x[j], cs[j], sn[j]);
         }
-        store8(o + a, u);
-        store8(o + b, v);
     }
+#pragma unroll
+    for (int h = 0; h < kPer; h++)
+        if (h < heads) {
+            *reinterpret_cast<uint4v *>(o + h * out.head + a) = u[h].w;
+            *reinterpret_cast<uint4v *>(o + h * out.head + b) = v[h].w;
+        }
 }
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_rotate(Rope r, View x, View out, const int32_t *positions, int64_t tokens,
-                                                     int heads, int per, int chunks, float sign) {
+                                                     int heads, int dim, int chunks, float sign) {
     const int64_t u = int64_t(blockIdx.x) * kThreads + threadIdx.x;
-    const int64_t t = u / chunks;
-    const int head = blockIdx.y * per;
+    const int64_t t = uint32_t(u) / uint32_t(chunks);           // tokens * chunks < 2^32
+    const int head = blockIdx.y * kPer;
     if (t >= tokens) return;
-    rotate_chunk<T>(r, x, out, t, positions[t], head, min(per, heads - head), int(u - t * chunks), sign);
+    rotate_chunk<T>(r, x, out, t, positions[t], head, min(kPer, heads - head), dim, int(u - t * chunks), sign);
 }
 
 // ---------------------------------------------------------------------------
@@ -146,7 +159,7 @@ struct AppendArgs {
     Rows rows;
     Rope rope;           // rotary = 0: none
     View k, v, q, q_out;
-    int32_t layer, q_heads, units, writers, shares, per, wide;
+    int32_t layer, q_heads, units, writers, shares, wide;
 };
 
 // The least exponent e with most <= 448 * 2^e (448 = 1.75 * 2^8), within +-100.
@@ -157,9 +170,10 @@ __device__ __forceinline__ float least_scale(float most) {
     return __uint_as_float(uint32_t(e + 127) << 23);
 }
 
+// Two codes; infinities take the largest, NaN stays.
 __device__ __forceinline__ uint32_t code2(float a, float b) {
-    a = a == a ? fminf(fmaxf(a, -448.0f), 448.0f) : a;
-    b = b == b ? fminf(fmaxf(b, -448.0f), 448.0f) : b;
+    a = a == a ? __builtin_amdgcn_fmed3f(a, -448.0f, 448.0f) : a;
+    b = b == b ? __builtin_amdgcn_fmed3f(b, -448.0f, 448.0f) : b;
     return __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
 }
 
@@ -227,7 +241,7 @@ __device__ __forceinline__ uint32_t rescaled(uint32_t w, float by) {
 
 // The scale of a block, and its old codes brought to it.  `most`: of the new values.
 struct Scale {
-    float *place, was, now;
+    float *place, was, now, by;             // by: 1 / now, exact for the powers of two that append makes
     bool older;
 };
 __device__ __forceinline__ Scale scale_of(const AppendArgs &a, const Unit &u, int which, int head, int page_tokens, float most) {
@@ -237,6 +251,7 @@ __device__ __forceinline__ Scale scale_of(const AppendArgs &a, const Unit &u, in
     s.was = *s.place;
     const float least = least_scale(most);
     s.now = s.older ? fmaxf(s.was, least) : least;
+    s.by = 1.0f / s.now;
     return s;
 }
 
@@ -280,10 +295,15 @@ template <typename T, int Dim, int Page> __device__ __forceinline__ void append_
                 cos_sin(double(p) * turns[j], cs, sn);
                 cs *= a.rope.magnitude;
                 sn *= a.rope.magnitude;
-                float &fa = apart ? x[k][j] : x[k][2 * j], &fb = apart ? x[k][4 + j] : x[k][2 * j + 1];
-                const float va = fa, vb = fb;
-                fa = __builtin_fmaf(va, cs, -(vb * sn));
-                fb = __builtin_fmaf(va, sn, vb * cs);
+                const float va = apart ? x[k][j] : x[k][2 * j], vb = apart ? x[k][4 + j] : x[k][2 * j + 1];
+                const float fa = __builtin_fmaf(va, cs, -(vb * sn)), fb = __builtin_fmaf(va, sn, vb * cs);
+                if (apart) {
+                    x[k][j] = fa;
+                    x[k][4 + j] = fb;
+                } else {
+                    x[k][2 * j] = fa;
+                    x[k][2 * j + 1] = fb;
+                }
             }
         }
 #pragma unroll
@@ -301,8 +321,8 @@ template <typename T, int Dim, int Page> __device__ __forceinline__ void append_
         const int p = t0 + k * kTokens;
         if (p >= u.from && p < u.to) {
             uint32_t *to = reinterpret_cast<uint32_t *>(block + (p - u.slot * Page) * Dim);
-            to[ea / 4] = code2(x[k][0] / s.now, x[k][1] / s.now) | code2(x[k][2] / s.now, x[k][3] / s.now) << 16;
-            to[eb / 4] = code2(x[k][4] / s.now, x[k][5] / s.now) | code2(x[k][6] / s.now, x[k][7] / s.now) << 16;
+            to[ea / 4] = code2(x[k][0] * s.by, x[k][1] * s.by) | code2(x[k][2] * s.by, x[k][3] * s.by) << 16;
+            to[eb / 4] = code2(x[k][4] * s.by, x[k][5] * s.by) | code2(x[k][6] * s.by, x[k][7] * s.by) << 16;
         }
     }
     if (lane == 0) *s.place = s.now;
@@ -352,7 +372,7 @@ template <typename T, int Dim, int Page> __device__ __forceinline__ void append_
             uint32_t w[4];
 #pragma unroll
             for (int i = 0; i < 4; i++)
-                w[i] = code2(x[g + 4 * i][d] / s.now, x[g + 4 * i + 1][d] / s.now) | code2(x[g + 4 * i + 2][d] / s.now, x[g + 4 * i + 3][d] / s.now) << 16;
+                w[i] = code2(x[g + 4 * i][d] * s.by, x[g + 4 * i + 1][d] * s.by) | code2(x[g + 4 * i + 2][d] * s.by, x[g + 4 * i + 3][d] * s.by) << 16;
             uint8_t *to = block + d * Page + g;
             if (first + g >= u.from && first + g + 16 <= u.to) {
                 *reinterpret_cast<uint4v *>(to) = uint4v{w[0], w[1], w[2], w[3]};
@@ -381,7 +401,7 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads) 
         return;
     }
     constexpr int kChunks = Dim / 16;
-    const int groups = (a.q_heads + a.per - 1) / a.per;
+    const int groups = (a.q_heads + kPer - 1) / kPer;
     const int64_t u = int64_t(int(blockIdx.x) - a.writers) * kThreads + threadIdx.x, tg = u / kChunks;
     const int64_t t = min(tg / groups, a.rows.tokens - 1);
     // the row of the wavefront's first token, then step by step
@@ -390,8 +410,8 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads) 
     if (tg / groups >= a.rows.tokens) return;
     while (b + 1 < a.rows.rows && a.rows.offsets[b + 1] <= t) b++;
     const Row row = row_of(a.c, a.rows, b);
-    const int head = int(tg - t * groups) * a.per;
-    rotate_chunk<T>(a.rope, a.q, a.q_out, t, row.length - row.n + int(t - row.first), head, min(a.per, a.q_heads - head), int(u % kChunks), 1.0f);
+    const int head = int(tg - t * groups) * kPer;
+    rotate_chunk<T>(a.rope, a.q, a.q_out, t, row.length - row.n + int(t - row.first), head, min(kPer, a.q_heads - head), Dim, int(u % kChunks), 1.0f);
 }
 
 // ---------------------------------------------------------------------------
@@ -482,7 +502,7 @@ namespace {
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 // Whether 16-byte accesses at multiples of 8 elements are aligned.
 bool wide(const esp_kv_view &v, int size) {
-    return aligned16(v.data) && (v.token_stride * size) % 16 == 0 && (v.head_stride * size) % 16 == 0;
+    return aligned16(v.data) && v.token_stride * size % 16 == 0 && v.head_stride * size % 16 == 0;
 }
 View view_of(const esp_kv_view &v) { return {v.data, v.token_stride, v.head_stride}; }
 Rope rope_of(const esp_kv_rope *r) { return r ? Rope{r->turns, r->magnitude, r->rotary_dim, r->interleaved} : Rope{nullptr, 1.0f, 0, 0}; }
@@ -501,9 +521,9 @@ template <typename T>
 void rotate(const Rope &r, View x, View out, const int32_t *positions, int64_t tokens, int heads, int dim, float sign,
             bool vector, hipStream_t s) {
     if (vector) {
-        const int chunks = dim / 16, per = 4;
+        const int chunks = dim / (32 / int(sizeof(T)));
         const int64_t blocks = (tokens * chunks + kThreads - 1) / kThreads;
-        k_rotate<T><<<dim3(unsigned(blocks), (heads + per - 1) / per), kThreads, 0, s>>>(r, x, out, positions, tokens, heads, per, chunks, sign);
+        k_rotate<T><<<dim3(unsigned(blocks), (heads + kPer - 1) / kPer), kThreads, 0, s>>>(r, x, out, positions, tokens, heads, dim, chunks, sign);
     } else {
         const int64_t blocks = (tokens * heads * (dim / 2) + kThreads - 1) / kThreads;
         k_rotate_any<T><<<unsigned(blocks < 65536 ? blocks : 65536), kThreads, 0, s>>>(r, x, out, positions, tokens, heads, dim, sign);
@@ -567,7 +587,9 @@ extern "C" esp_status esp_kv_rotate(const esp_kv_rope *rope, int32_t type, int64
     if (tokens == 0 || heads == 0) return ESP_OK;
     if (!x.data || !out.data || !positions) return ESP_ERR_INVALID_ARG;
     const int size = type == ESP_KV_FP32 ? 4 : 2;
-    const bool vector = wide(x, size) && wide(out, size) && rope->rotary_dim % 16 == 0 && head_dim % 16 == 0;
+    const int step = 32 / size;             // elements of two vectors
+    const bool vector = wide(x, size) && wide(out, size) && rope->rotary_dim % step == 0 && head_dim % step == 0 &&
+                        tokens * (head_dim / step) < (int64_t(1) << 32);
     const float sign = inverse ? -1.0f : 1.0f;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const Rope r = rope_of(rope);
@@ -593,15 +615,15 @@ extern "C" esp_status esp_kv_append(const esp_kv_cache *cache, int32_t layer, in
     if (!k.data || !v.data || (q_heads && (!rope || !q.data || !q_out.data))) return ESP_ERR_INVALID_ARG;
     if (q_heads && !(wide(q, 2) && wide(q_out, 2))) return ESP_ERR_INVALID_ARG;
     const int64_t units = tokens / cache->page_tokens + 2 * int64_t(rows);
-    const int32_t shares = shares_of(units, cache->kv_heads), per = 4;
+    const int32_t shares = shares_of(units, cache->kv_heads);
     const int64_t writers = (units * shares + kThreads / 64 - 1) / (kThreads / 64);
-    const int64_t turners = (tokens * ((q_heads + per - 1) / per) * (cache->head_dim / 16) + kThreads - 1) / kThreads;
+    const int64_t turners = (tokens * ((q_heads + kPer - 1) / kPer) * (cache->head_dim / 16) + kThreads - 1) / kThreads;
     if (units * shares > INT32_MAX || writers + turners > INT32_MAX) return ESP_ERR_SHAPE;
     const unsigned blocks = unsigned(writers + turners);
     // loads of four keys or two values at a time
     auto fours = [](const esp_kv_view &x) { return (reinterpret_cast<uintptr_t>(x.data) & 7) == 0 && x.token_stride % 4 == 0 && x.head_stride % 4 == 0; };
     const AppendArgs a{cache_of(cache), Rows{offsets, seqs, rows, tokens}, rope_of(rope), view_of(k), view_of(v), view_of(q), view_of(q_out),
-                       layer, q_heads, int32_t(units), int32_t(writers), shares, per, fours(k) && fours(v)};
+                       layer, q_heads, int32_t(units), int32_t(writers), shares, fours(k) && fours(v)};
     const hipStream_t s = static_cast<hipStream_t>(stream);
     if (type == ESP_KV_BF16) cache->head_dim == 64 ? append<__bf16, 64>(a, blocks, s) : append<__bf16, 128>(a, blocks, s);
     else cache->head_dim == 64 ? append<_Float16, 64>(a, blocks, s) : append<_Float16, 128>(a, blocks, s);

@@ -239,164 +239,192 @@ __device__ __forceinline__ uint32_t rescaled(uint32_t w, float by) {
     return code2(float(a[0]) * by, float(a[1]) * by) | code2(float(b[0]) * by, float(b[1]) * by) << 16;
 }
 
-// The scale of a block, and its old codes brought to it.  `most`: of the new values.
+// A block's scale.  `older`: the page has tokens from before.
 struct Scale {
-    float *place, was, now, by;             // by: 1 / now, exact for the powers of two that append makes
+    float was, now, by;                     // by: 1 / now, exact for the powers of two that append makes
     bool older;
 };
-__device__ __forceinline__ Scale scale_of(const AppendArgs &a, const Unit &u, int which, int head, int page_tokens, float most) {
-    Scale s;
-    s.place = a.c.block_scale(u.page, a.layer, which, head);
-    s.older = u.slot * page_tokens < u.from;
-    s.was = *s.place;
-    const float least = least_scale(most);
-    s.now = s.older ? fmaxf(s.was, least) : least;
-    s.by = 1.0f / s.now;
-    return s;
+__device__ __forceinline__ Scale scale_of(float was, bool older, float most) {
+    const float least = least_scale(most), now = older ? fmaxf(was, least) : least;
+    return {was, now, 1.0f / now, older};
+}
+// The largest over the kTeam wavefronts that share a block; lds[4], a buffer of its own each second time.
+template <int kTeam> __device__ __forceinline__ float team_max(float x, float *lds) {
+    x = wave_max(x);
+    if (kTeam > 1) {
+        const int wave = threadIdx.x >> 6;
+        if ((threadIdx.x & 63) == 0) lds[wave] = x;
+        __syncthreads();
+        for (int i = 0; i < kTeam; i++) x = fmaxf(x, lds[wave / kTeam * kTeam + i]);
+    }
+    return x;
 }
 
-// A wavefront writes a page's new keys of one head.  A lane takes four pairs of
-// one token, four (heads of 128) or eight (of 64) tokens at a time; the values
-// stay in registers between the largest and the codes.
-template <typename T, int Dim, int Page> __device__ __forceinline__ void append_keys(const AppendArgs &a, const Unit &u, int head) {
-    constexpr int kLanes = Dim / 8, kTokens = 64 / kLanes, kRounds = Page / kTokens;
-    const int lane = threadIdx.x & 63, part = lane % kLanes, t0 = u.slot * Page + lane / kLanes;
+// Sixteen tokens [c0, c0 + 16) of a page (One: the token c0 alone): what of them
+// is new is written.  A lane takes four pairs of one token's key, four (heads of
+// 128) or eight (of 64) tokens at a time; the values stay in registers between
+// the largest and the codes.  Tokens that are not new are read as their nearest
+// new one and left out, so that no load waits for another.
+template <typename T, int Dim, int Page, bool One, int kTeam>
+__device__ __forceinline__ void append_keys(const AppendArgs &a, const Unit &u, int head, int c0, bool active, float *lds) {
+    constexpr int kLanes = Dim / 8, kTokens = 64 / kLanes, kRounds = One ? 1 : 16 / kTokens;
+    const int lane = threadIdx.x & 63, part = lane % kLanes, first = u.slot * Page;
+    const int p0 = One ? lane < kLanes ? c0 : u.to : c0 + lane / kLanes;
     const int half = a.rope.rotary >> 1, i0 = 4 * part;
     const bool turn = i0 < half, apart = turn && !a.rope.interleaved;
     const int ea = apart ? i0 : 8 * part, eb = apart ? i0 + half : 8 * part + 4;      // elements ea.. and eb..
+    const T *src = static_cast<const T *>(a.k.data) + head * a.k.head + (int64_t(u.row.first) - (u.row.length - u.row.n)) * a.k.token;
+    Vec4<T> va[kRounds], vb[kRounds];
+#pragma unroll
+    for (int k = 0; k < kRounds; k++) {
+        const T *from = src + int64_t(max(u.from, min(u.to - 1, p0 + k * kTokens))) * a.k.token;
+        va[k] = load4(from + ea, a.wide);
+        vb[k] = load4(from + eb, a.wide);
+    }
+    float *place = a.c.block_scale(u.page, a.layer, 0, head);
+    const float was = *place;
     double turns[4];
 #pragma unroll
     for (int j = 0; j < 4; j++) turns[j] = turn ? a.rope.turns[i0 + j] : 0.0;
-    const T *src = static_cast<const T *>(a.k.data) + head * a.k.head + (int64_t(u.row.first) + t0 - (u.row.length - u.row.n)) * a.k.token;
     float x[kRounds][8], most = 0.0f;
 #pragma unroll
     for (int k = 0; k < kRounds; k++) {
-        const int p = t0 + k * kTokens;
+        const int p = p0 + k * kTokens;
 #pragma unroll
-        for (int j = 0; j < 8; j++) x[k][j] = 0.0f;
-        if (p >= u.from && p < u.to) {
-            const T *from = src + int64_t(k * kTokens) * a.k.token;
-            const Vec4<T> va = load4(from + ea, a.wide), vb = load4(from + eb, a.wide);
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-                x[k][j] = float(va.x[j]);
-                x[k][4 + j] = float(vb.x[j]);
-            }
+        for (int j = 0; j < 4; j++) {
+            x[k][j] = float(va[k].x[j]);
+            x[k][4 + j] = float(vb[k].x[j]);
         }
-    }
-#pragma unroll
-    for (int k = 0; k < kRounds; k++) {
-        const int p = t0 + k * kTokens;
-        if (kRounds > 1 && !__any(p >= u.from && p < u.to)) continue;
-        if (turn) {
+        if (a.rope.rotary) {
 #pragma unroll
             for (int j = 0; j < 4; j++) {
                 float cs, sn;
                 cos_sin(double(p) * turns[j], cs, sn);
                 cs *= a.rope.magnitude;
                 sn *= a.rope.magnitude;
-                const float va = apart ? x[k][j] : x[k][2 * j], vb = apart ? x[k][4 + j] : x[k][2 * j + 1];
-                const float fa = __builtin_fmaf(va, cs, -(vb * sn)), fb = __builtin_fmaf(va, sn, vb * cs);
+                const float fa = apart ? x[k][j] : x[k][2 * j], fb = apart ? x[k][4 + j] : x[k][2 * j + 1];
+                const float ya = __builtin_fmaf(fa, cs, -(fb * sn)), yb = __builtin_fmaf(fa, sn, fb * cs);
                 if (apart) {
-                    x[k][j] = fa;
-                    x[k][4 + j] = fb;
-                } else {
-                    x[k][2 * j] = fa;
-                    x[k][2 * j + 1] = fb;
+                    x[k][j] = ya;
+                    x[k][4 + j] = yb;
+                } else if (turn) {
+                    x[k][2 * j] = ya;
+                    x[k][2 * j + 1] = yb;
                 }
             }
         }
+        float top = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 8; j++) most = fmaxf(most, finite_abs(x[k][j]));
+        for (int j = 0; j < 8; j++) top = fmaxf(top, finite_abs(x[k][j]));
+        most = fmaxf(most, p >= u.from && p < u.to ? top : 0.0f);
     }
-    const Scale s = scale_of(a, u, 0, head, Page, wave_max(most));
+    const Scale s = scale_of(was, first < u.from, team_max<kTeam>(most, lds));
+    if (!active) return;
     uint8_t *block = a.c.k + a.c.block(u.page, a.layer, head);
-    if (s.older && s.now > s.was) {
+    if (s.older && s.now > s.was) {         // One: the page's first 16 tokens and on
         const float by = s.was / s.now;
         uint32_t *w = reinterpret_cast<uint32_t *>(block);
-        for (int i = lane; i < (u.from - u.slot * Page) * Dim / 4; i += 64) w[i] = rescaled(w[i], by);
+        const int from = One ? 0 : c0 - first, to = One ? u.from - first : min(u.from, c0 + 16) - first;
+        for (int i = from * (Dim / 4) + lane; i < to * (Dim / 4); i += 64) w[i] = rescaled(w[i], by);
     }
 #pragma unroll
     for (int k = 0; k < kRounds; k++) {
-        const int p = t0 + k * kTokens;
+        const int p = p0 + k * kTokens;
         if (p >= u.from && p < u.to) {
-            uint32_t *to = reinterpret_cast<uint32_t *>(block + (p - u.slot * Page) * Dim);
+            uint32_t *to = reinterpret_cast<uint32_t *>(block + (p - first) * Dim);
             to[ea / 4] = code2(x[k][0] * s.by, x[k][1] * s.by) | code2(x[k][2] * s.by, x[k][3] * s.by) << 16;
             to[eb / 4] = code2(x[k][4] * s.by, x[k][5] * s.by) | code2(x[k][6] * s.by, x[k][7] * s.by) << 16;
         }
     }
-    if (lane == 0) *s.place = s.now;
+    if (lane == 0 && (One || c0 == first)) *place = s.now;
 }
 
-// ... and its new values.  A lane takes all tokens of one (heads of 64) or two
+// ... and their values.  A lane takes all the tokens of one (heads of 64) or two
 // dimensions, so that sixteen tokens go out at once, as pages hold them.
-template <typename T, int Dim, int Page> __device__ __forceinline__ void append_values(const AppendArgs &a, const Unit &u, int head) {
-    constexpr int kDims = Dim / 64;
+template <typename T, int Dim, int Page, bool One, int kTeam>
+__device__ __forceinline__ void append_values(const AppendArgs &a, const Unit &u, int head, int c0, bool active, float *lds) {
+    constexpr int kDims = Dim / 64, kTokens = One ? 1 : 16;
     const int lane = threadIdx.x & 63, d0 = lane * kDims, first = u.slot * Page;
-    const T *src = static_cast<const T *>(a.v.data) + head * a.v.head + (int64_t(u.row.first) + first - (u.row.length - u.row.n)) * a.v.token + d0;
-    float x[Page][kDims], most = 0.0f;
+    const T *src = static_cast<const T *>(a.v.data) + head * a.v.head + (int64_t(u.row.first) - (u.row.length - u.row.n)) * a.v.token + d0;
+    union Dims {
+        uint32_t w;
+        T x[2];
+    } v[kTokens];
+    if (kDims == 2 && a.wide) {
 #pragma unroll
-    for (int t = 0; t < Page; t++) {
+        for (int t = 0; t < kTokens; t++) v[t].w = *reinterpret_cast<const uint32_t *>(src + int64_t(max(u.from, min(u.to - 1, c0 + t))) * a.v.token);
+    } else {
 #pragma unroll
-        for (int d = 0; d < kDims; d++) x[t][d] = 0.0f;
-        if (first + t >= u.from && first + t < u.to) {
-            const T *from = src + int64_t(t) * a.v.token;
-            T v[kDims];
-            if (kDims == 2 && a.wide) *reinterpret_cast<uint32_t *>(v) = *reinterpret_cast<const uint32_t *>(from);
-            else
+        for (int t = 0; t < kTokens; t++)
 #pragma unroll
-                for (int d = 0; d < kDims; d++) v[d] = from[d];
-#pragma unroll
-            for (int d = 0; d < kDims; d++) x[t][d] = float(v[d]);
-        }
+            for (int d = 0; d < kDims; d++) v[t].x[d] = src[int64_t(max(u.from, min(u.to - 1, c0 + t))) * a.v.token + d];
     }
+    float *place = a.c.block_scale(u.page, a.layer, 1, head);
+    const float was = *place;
+    float most = 0.0f;
 #pragma unroll
-    for (int t = 0; t < Page; t++)
+    for (int t = 0; t < kTokens; t++)
 #pragma unroll
-        for (int d = 0; d < kDims; d++) most = fmaxf(most, finite_abs(x[t][d]));
-    const Scale s = scale_of(a, u, 1, head, Page, wave_max(most));
+        for (int d = 0; d < kDims; d++) most = fmaxf(most, finite_abs(float(v[t].x[d])));     // a token read twice changes nothing
+    const Scale s = scale_of(was, first < u.from, team_max<kTeam>(most, lds));
+    if (!active) return;
     uint8_t *block = a.c.v + a.c.block(u.page, a.layer, head) + d0 * Page;
     if (s.older && s.now > s.was) {
         const float by = s.was / s.now;
+        const int from = One ? 0 : c0 - first, to = One ? u.from - first : min(u.from, c0 + 16) - first;
         for (int d = 0; d < kDims; d++)
-            for (int t = 0; t < u.from - first; t += 4) {       // a word may reach into the new tokens: these are written after
+            for (int t = from; t < to; t += 4) {       // a word may reach into the new tokens: these are written after
                 uint32_t *w = reinterpret_cast<uint32_t *>(block + d * Page + t);
                 *w = rescaled(*w, by);
             }
     }
+    if constexpr (One) {
 #pragma unroll
-    for (int d = 0; d < kDims; d++)
+        for (int d = 0; d < kDims; d++) block[d * Page + c0 - first] = uint8_t(code2(float(v[0].x[d]) * s.by, 0.0f));
+    } else if (c0 + 16 > u.from && c0 < u.to) {
 #pragma unroll
-        for (int g = 0; g < Page; g += 16) {
-            if (first + g + 16 <= u.from || first + g >= u.to) continue;
+        for (int d = 0; d < kDims; d++) {
             uint32_t w[4];
 #pragma unroll
             for (int i = 0; i < 4; i++)
-                w[i] = code2(x[g + 4 * i][d] * s.by, x[g + 4 * i + 1][d] * s.by) | code2(x[g + 4 * i + 2][d] * s.by, x[g + 4 * i + 3][d] * s.by) << 16;
-            uint8_t *to = block + d * Page + g;
-            if (first + g >= u.from && first + g + 16 <= u.to) {
+                w[i] = code2(float(v[4 * i].x[d]) * s.by, float(v[4 * i + 1].x[d]) * s.by) | code2(float(v[4 * i + 2].x[d]) * s.by, float(v[4 * i + 3].x[d]) * s.by) << 16;
+            uint8_t *to = block + d * Page + (c0 - first);
+            if (c0 >= u.from && c0 + 16 <= u.to) {
                 *reinterpret_cast<uint4v *>(to) = uint4v{w[0], w[1], w[2], w[3]};
             } else {
 #pragma unroll
                 for (int i = 0; i < 16; i++)
-                    if (first + g + i >= u.from && first + g + i < u.to) to[i] = uint8_t(w[i >> 2] >> (8 * (i & 3)));
+                    if (c0 + i >= u.from && c0 + i < u.to) to[i] = uint8_t(w[i >> 2] >> (8 * (i & 3)));
             }
         }
-    if (lane == 0) *s.place = s.now;
+    }
+    if (lane == 0 && (One || c0 == first)) *place = s.now;
 }
 
-// Workgroups [0, writers): a wavefront writes some of the 2 * heads blocks of a
-// unit; the others turn the queries.
+// Workgroups [0, writers): some of the 2 * heads blocks of one unit, a block by
+// as many wavefronts as the page has sixteens of tokens (a single token by one);
+// the others turn the queries.
 template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads) void k_append(AppendArgs a) {
+    constexpr int kTeam = Page / 16, kTeams = 4 / kTeam;
+    __shared__ float lds[2][4];
     if (int(blockIdx.x) < a.writers) {
-        const int w = __builtin_amdgcn_readfirstlane(blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6));
-        const int unit = w / a.shares, share = w - unit * a.shares;
-        if (unit >= a.units) return;
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int unit = blockIdx.x / a.shares, share = blockIdx.x - unit * a.shares;
         const Unit u = unit_of<Page>(a.c, a.rows, unit, nullptr);
         if (u.from >= u.to || u.page < 0) return;
-        for (int i = share; i < 2 * a.c.heads; i += a.shares) {
-            if (i < a.c.heads) append_keys<T, Dim, Page>(a, u, i);
-            else append_values<T, Dim, Page>(a, u, i - a.c.heads);
+        const int blocks = 2 * a.c.heads;
+        if (u.to - u.from == 1) {
+            for (int i = share * 4 + wave; i < blocks; i += a.shares * 4) {
+                if (i < a.c.heads) append_keys<T, Dim, Page, true, 1>(a, u, i, u.from, true, nullptr);
+                else append_values<T, Dim, Page, true, 1>(a, u, i - a.c.heads, u.from, true, nullptr);
+            }
+            return;
+        }
+        // even parts keys, odd parts values; every wavefront goes round as often, for the barriers
+        const int c0 = u.slot * Page + wave % kTeam * 16, step = a.shares / 2 * kTeams;
+        for (int i = 0, head = share / 2 * kTeams + wave / kTeam; i < (a.c.heads + step - 1) / step; i++, head += step) {
+            if (share & 1) append_values<T, Dim, Page, false, kTeam>(a, u, min(head, a.c.heads - 1), c0, head < a.c.heads, lds[i & 1]);
+            else append_keys<T, Dim, Page, false, kTeam>(a, u, min(head, a.c.heads - 1), c0, head < a.c.heads, lds[i & 1]);
         }
         return;
     }
@@ -439,12 +467,19 @@ template <typename T, int Dim, int Page> __device__ __forceinline__ void gather_
     if (!values) {
         constexpr int kLanes = Dim / 8, kTokens = 64 / kLanes;
         const uint8_t *block = a.c.k + a.c.block(u.page, a.layer, head);
+        constexpr int kRounds = Page / kTokens;
+        const int d = lane % kLanes * 8;
+        uint2v w[kRounds];
 #pragma unroll
-        for (int k = 0; k < Page / kTokens; k++) {
-            const int t = k * kTokens + lane / kLanes, d = lane % kLanes * 8;
+        for (int k = 0; k < kRounds; k++) {            // other tokens of the page are read as the nearest that is asked for
+            const int t = max(u.from, min(held - 1, first + k * kTokens + lane / kLanes)) - first;
+            w[k] = *reinterpret_cast<const uint2v *>(block + t * Dim + d);
+        }
+#pragma unroll
+        for (int k = 0; k < kRounds; k++) {
+            const int t = k * kTokens + lane / kLanes;
             if (first + t < u.from || first + t >= held) continue;
-            const uint2v w = *reinterpret_cast<const uint2v *>(block + t * Dim + d);
-            const half8 n = codes8<half8, half2>(w[0], w[1]);
+            const half8 n = codes8<half8, half2>(w[k][0], w[k][1]);
             Vec8<T> o;
 #pragma unroll
             for (int j = 0; j < 8; j++) o.x[j] = T(float(n[j]) * s);
@@ -455,12 +490,15 @@ template <typename T, int Dim, int Page> __device__ __forceinline__ void gather_
     constexpr int kDims = Dim / 64;
     const int d0 = lane * kDims;
     const uint8_t *block = a.c.v + a.c.block(u.page, a.layer, head) + d0 * Page;
+    uint4v all[Page / 16][kDims];
+#pragma unroll
+    for (int g = 0; g < Page; g += 16)
+#pragma unroll
+        for (int d = 0; d < kDims; d++) all[g / 16][d] = *reinterpret_cast<const uint4v *>(block + d * Page + g);
 #pragma unroll
     for (int g = 0; g < Page; g += 16) {
         if (first + g + 16 <= u.from || first + g >= held) continue;
-        uint4v w[kDims];
-#pragma unroll
-        for (int d = 0; d < kDims; d++) w[d] = *reinterpret_cast<const uint4v *>(block + d * Page + g);
+        const uint4v(&w)[kDims] = all[g / 16];
 #pragma unroll
         for (int i = 0; i < 16; i += 8) {
             half8 n[kDims];
@@ -545,13 +583,11 @@ template <typename T, int Dim> void gather(const GatherArgs &a, unsigned blocks,
     }
 }
 
-// Wavefronts that share the 2 * heads blocks of a unit: one for each, while that
-// is not far more than the GPU holds (8,192); steps of many sequences take fewer,
-// so that the search for the row is made for several blocks.
-int32_t shares_of(int64_t units, int32_t heads) {
-    int64_t shares = 2 * int64_t(heads);
-    while (shares > 1 && units * shares > 16384) shares = (shares + 1) / 2;
-    return int32_t(shares);
+// Parts of a unit's work, `most` at most, each of `waves` wavefronts: about 16,384
+// wavefronts in all, twice what the GPU holds; as few as finish in as many rounds.
+int32_t shares_of(int64_t units, int64_t most, int64_t waves) {
+    const int64_t fill = 16384 / (units * waves), shares = fill < 1 ? 1 : fill < most ? fill : most, rounds = (most + shares - 1) / shares;
+    return int32_t((most + rounds - 1) / rounds);
 }
 
 }  // namespace
@@ -615,8 +651,9 @@ extern "C" esp_status esp_kv_append(const esp_kv_cache *cache, int32_t layer, in
     if (!k.data || !v.data || (q_heads && (!rope || !q.data || !q_out.data))) return ESP_ERR_INVALID_ARG;
     if (q_heads && !(wide(q, 2) && wide(q_out, 2))) return ESP_ERR_INVALID_ARG;
     const int64_t units = tokens / cache->page_tokens + 2 * int64_t(rows);
-    const int32_t shares = shares_of(units, cache->kv_heads);
-    const int64_t writers = (units * shares + kThreads / 64 - 1) / (kThreads / 64);
+    const int32_t teams = 64 / cache->page_tokens,
+                  shares = 2 * shares_of(units, (cache->kv_heads + teams - 1) / teams, 8);
+    const int64_t writers = units * shares;
     const int64_t turners = (tokens * ((q_heads + kPer - 1) / kPer) * (cache->head_dim / 16) + kThreads - 1) / kThreads;
     if (units * shares > INT32_MAX || writers + turners > INT32_MAX) return ESP_ERR_SHAPE;
     const unsigned blocks = unsigned(writers + turners);
@@ -640,7 +677,7 @@ extern "C" esp_status esp_kv_gather(const esp_kv_cache *cache, int32_t layer, in
     if (rows == 0 || tokens == 0) return ESP_OK;
     if (!starts || !k_out || !v_out || !aligned16(k_out) || !aligned16(v_out)) return ESP_ERR_INVALID_ARG;
     const int64_t units = tokens / cache->page_tokens + 2 * int64_t(rows);
-    const int32_t shares = shares_of(units, cache->kv_heads);
+    const int32_t shares = shares_of(units, 2 * cache->kv_heads, 1);
     if (units * shares > INT32_MAX) return ESP_ERR_SHAPE;
     const unsigned blocks = unsigned((units * shares + kThreads / 64 - 1) / (kThreads / 64));
     const GatherArgs a{cache_of(cache), Rows{offsets, seqs, rows, tokens}, starts, layer, shares, int32_t(units), k_out, v_out};

@@ -400,10 +400,10 @@ __global__ __launch_bounds__(kCopyThreads) void k_copy(Cache c, const int32_t *c
         uint4v x[4];
 #pragma unroll
         for (int j = 0; j < 4; j++)
-            if (at + j * kCopyThreads < vectors) x[j] = from[at + j * kCopyThreads];
+            if (at + j * kCopyThreads < vectors) x[j] = __builtin_nontemporal_load(from + at + j * kCopyThreads);
 #pragma unroll
         for (int j = 0; j < 4; j++)
-            if (at + j * kCopyThreads < vectors) to[at + j * kCopyThreads] = x[j];
+            if (at + j * kCopyThreads < vectors) __builtin_nontemporal_store(x[j], to + at + j * kCopyThreads);
         if (rest == 0)
             for (int i = threadIdx.x; i < scales; i += kCopyThreads) c.scale[int64_t(m.y) * scales + i] = c.scale[int64_t(m.x) * scales + i];
     }

@@ -1,6 +1,8 @@
 // Attention of many new tokens over the paged 8-bit cache.
 #include "kv_attend.hpp"
 
+#include <type_traits>
+
 namespace esp_kv {
 
 typedef float float16v __attribute__((ext_vector_type(16)));
@@ -159,7 +161,7 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 
         }
     };
     // Widens the loaded tile into LDS, values divided by 2^e_ref.
-    auto store = [&](int t, int buffer, const Group &grp, int e_ref, bool whole) {
+    auto store = [&](auto fast, int t, int buffer, const Group &grp, int e_ref, bool whole) {
         const int e = exponent(grp.v);
         const float by = __uint_as_float(uint32_t(max(1, min(254, e - e_ref + 127))) << 23), rest = ldexpf(grp.v, -e);
         const bool powers = __all(rest == 1.0f || grp.page < 0);
@@ -171,7 +173,7 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 
         }
 #pragma unroll
         for (int i = 0; i < kKeyUnits; i++) {
-            if (!whole) {                   // past the end, or without a page: codes of 0
+            if (!decltype(fast)::value && !whole) {     // past the end, or without a page: codes of 0
                 const int held = __builtin_amdgcn_readlane(grp.page, value_first[i]) < 0 ? 0 : row.length - t * kTile - 16 * value_group[i];
                 uint32_t bad = 0;
 #pragma unroll
@@ -217,7 +219,7 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 
         if (span.from + 1 < span.to) after = page_of(span.from + 1);
         e_now = largest(now);
         __syncthreads();
-        store(span.from, 0, now, e_now, inside(span.from, now));
+        store(std::false_type{}, span.from, 0, now, e_now, inside(span.from, now));
     }
     __syncthreads();
     // key row m of a matrix tile is the token whose bits 2 and 3 are those of m exchanged
@@ -225,9 +227,11 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 
     const int value_row = (col & 4) << 2 | (col & 24) >> 1 | (col & 3);
     const uint32_t key_at = key_row * kKeyRow + ((half ^ key_turn(key_row)) << 4);
     const uint32_t value_at = kHalf + value_row * (kTile * 2) + ((half ^ value_turn(value_row)) << 4);
-    for (int t = span.from; t < span.to; t++) {
+    // A tile, and the next into LDS.  fast: every row of the workgroup sees all of both.
+    auto step = [&](auto fast, int t) {
+        constexpr bool Fast = decltype(fast)::value;
         const int buffer = (t - span.from) & 1;
-        const bool more = t + 1 < span.to;
+        const bool more = Fast || t + 1 < span.to;
         if (more) {
             next = scales_of(after);
             load(next.page);
@@ -235,21 +239,30 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 
         }
         float16v s[2];
 #pragma unroll
-        for (int j = 0; j < 2; j++) {
+        for (int j = 0; j < 2; j++)
 #pragma unroll
             for (int i = 0; i < 16; i++) s[j][i] = 0.0f;
 #pragma unroll
-            for (int k = 0; k < kSteps; k++)
+        for (int k = 0; k < kSteps; k++) {
+#pragma unroll
+            for (int j = 0; j < 2; j++)
                 s[j] = product32(*reinterpret_cast<const V8 *>(&lds[buffer][(key_at ^ (k << 5)) + j * 32 * kKeyRow]), q[k], s[j]);
         }
+        // the reads stay 2 steps ahead of the products
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+        for (int k = 0; k < kSteps - 2; k++) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
         // s[j][4 b + i]: token 32 j + 16 (b / 2) + 8 half + 4 (b % 2) + i, so that
         // s[g / 2][8 (g % 2) + i] is token 8 half + i of group g
         float ks[4];
         const float scaled = now.k * scale;
-        const bool there = __all(now.page >= 0);
 #pragma unroll
         for (int g = 0; g < 4; g++) ks[g] = lane_float(scaled, g);
-        const bool whole = there && t * kTile + kTile - 1 <= pos_first && (a.window <= 0 || t * kTile > pos_last - a.window);
+        const bool whole = Fast || (__all(now.page >= 0) && t * kTile + kTile - 1 <= pos_first && (a.window <= 0 || t * kTile > pos_last - a.window));
         if (!whole) {
             bool lost = false;
 #pragma unroll
@@ -296,7 +309,7 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 
                 l_run += x;
                 w[g][i] = _Float16(x);
             }
-        if (nans[buffer] == uint32_t(t + 1)) {
+        if (!Fast && nans[buffer] == uint32_t(t + 1)) {
             // A NaN value that only some rows see must not reach the others through
             // 0 * NaN: it is looked for token by token, then it becomes 0 in LDS.
             for (int x = 0; x < kTile; x++) {
@@ -318,16 +331,22 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 
             __syncthreads();
         }
 #pragma unroll
-        for (int d = 0; d < kOut; d++)
+        for (int g = 0; g < 4; g++)
 #pragma unroll
-            for (int g = 0; g < 4; g++)
+            for (int d = 0; d < kOut; d++)
                 o[d] = product32(*reinterpret_cast<const half8 *>(&lds[buffer][(value_at ^ (g << 5)) + d * 32 * (kTile * 2)]), w[g], o[d]);
         if (more) {
             e_now = max(o_exp, largest(next));
-            store(t + 1, buffer ^ 1, next, e_now, inside(t + 1, next));
+            store(fast, t + 1, buffer ^ 1, next, e_now, Fast || inside(t + 1, next));
             now = next;
         }
         __syncthreads();
+    };
+    // tiles that every row sees by its position
+    const int seen_from = a.window > 0 ? max(0, last_of_all - a.window + kTile) / kTile : 0, seen_to = (first_of_all + 1) / kTile;
+    for (int t = span.from; t < span.to; t++) {
+        for (; t >= seen_from && t + 1 < min(seen_to, span.to) && __all(now.page >= 0 && after >= 0); t++) step(std::true_type{}, t);
+        step(std::false_type{}, t);
     }
 
     // finish: element 32 d + 16 half + x of this lane's row is o[d][x]

@@ -90,6 +90,20 @@ __device__ __forceinline__ void prefix(const int32_t *values, int n, int *at, in
     __syncthreads();
 }
 
+// Place of the set bit that r others precede.
+__device__ __forceinline__ int nth_bit(uint64_t m, int r) {
+    int at = 0;
+#pragma unroll
+    for (int w = 32; w; w >>= 1) {
+        const int below = __popcll(m & ((uint64_t(1) << w) - 1));
+        const bool past = r >= below;
+        r -= past ? below : 0;
+        at += past ? w : 0;
+        m >>= past ? w : 0;
+    }
+    return at;
+}
+
 // The page of rank r among those whose bit is set (flip 0) or clear (flip ~0);
 // at(b): how many there are before block b.
 template <typename At> __device__ int select(const Work &w, At at, uint64_t flip, int r) {
@@ -108,10 +122,7 @@ template <typename At> __device__ int select(const Work &w, At at, uint64_t flip
 #pragma unroll
         for (int k = 0; k < 4; k++) {
             const int held = __popcll(m[k]);
-            if (r < held) {
-                for (; r > 0; r--) m[k] &= m[k] - 1;
-                return int((from + x + k) * 64 + __builtin_ctzll(m[k]));
-            }
+            if (r < held) return int((from + x + k) * 64 + nth_bit(m[k], r));
             r -= held;
         }
     }
@@ -201,15 +212,39 @@ __global__ __launch_bounds__(kThreads) void k_resize_mark(Cache c, const int32_t
         mark(w.pages, b - w.entries.blocks, w.page_mask, w.page_sum, lds, [&](int64_t p) { return c.refs[p] == 0; });
         return;
     }
-    // a kept page that ends inside its sequence and still has other owners
-    auto split = [&](int64_t i) {
-        const Entry e = entry_of(c, lengths, i);
-        const int32_t p = c.table[i];
-        const int last = min(c.lengths[e.seq], lengths[e.seq]);
-        return e.wanted && p >= 0 && p < c.pages && e.slot == last >> c.shift && (last & (c.tokens - 1)) && c.refs[p] > 1;
-    };
-    mark(w.entries, b, w.split_mask, w.split_sum, lds, split);
-    mark(w.entries, b, w.need_mask, w.need_sum, lds, [&](int64_t i) { return (c.table[i] == -1 && entry_of(c, lengths, i).wanted) || split(i); });
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t words = (w.entries.n + 63) / 64, from = int64_t(b) * w.entries.words, to = min(words, from + w.entries.words);
+    int needs = 0, splits = 0;
+    for (int64_t x0 = from + wave; x0 < to; x0 += 16) {          // four words in flight
+        int32_t page[4];
+#pragma unroll
+        for (int k = 0; k < 4; k++) page[k] = x0 + 4 * k < to ? c.table[min((x0 + 4 * k) * 64 + lane, w.entries.n - 1)] : -1;
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            const int64_t x = x0 + 4 * k, i = x * 64 + lane;
+            bool need = false, split = false;
+            if (x < to && i < w.entries.n) {
+                const Entry e = entry_of(c, lengths, i);
+                const int last = min(c.lengths[e.seq], lengths[e.seq]);
+                // a kept page that ends inside its sequence and still has other owners
+                split = e.wanted && page[k] >= 0 && page[k] < c.pages && e.slot == last >> c.shift && (last & (c.tokens - 1)) && c.refs[page[k]] > 1;
+                need = split || (e.wanted && page[k] == -1);
+            }
+            const uint64_t n = __ballot(need), s = __ballot(split);
+            if (x < to && lane == 0) {
+                w.need_mask[x] = n;
+                w.split_mask[x] = s;
+            }
+            needs += lane == 0 ? __popcll(n) : 0;
+            splits += lane == 0 ? __popcll(s) : 0;
+        }
+    }
+    needs = block_sum(needs, lds);
+    splits = block_sum(splits, lds);
+    if (threadIdx.x == 0) {
+        w.need_sum[b] = needs;
+        w.split_sum[b] = splits;
+    }
 }
 
 __global__ __launch_bounds__(kThreads) void k_resize_take(Cache c, const int32_t *lengths, Work w) {

@@ -99,21 +99,26 @@ template <typename T, int Dim, int Page, bool Stream> __global__ __launch_bounds
 
     // this workgroup's share [at, stop) of the list
     int64_t total = 0, tokens = 0;
+    int units = 0;
     for (int b = lane; b < a.rows.rows; b += 64) {
         const Row r = usable_row(a, b);
         total += int64_t(units_of(a, r)) * tiles_of(a, r);
         tokens += r.n;
+        units += units_of(a, r);
     }
 #pragma unroll
     for (int m = 32; m; m >>= 1) {
         total += __shfl_xor(total, m);
         tokens += __shfl_xor(tokens, m);
+        units += __shfl_xor(units, m);
     }
     if (tokens > a.rows.tokens || total > INT32_MAX) {          // rows that overlap, or a list that cannot be numbered
         if (threadIdx.x == 0) record(c, ESP_ERR_SHAPE);
         return;
     }
-    const int all = __builtin_amdgcn_readfirstlane(int(total)), per = max(kWaves, (all + a.groups - 1) / a.groups);
+    // a tile for every wavefront, unless the units are shorter: a unit each is quicker than several in turn
+    const int all = __builtin_amdgcn_readfirstlane(int(total)), each = max(1, __builtin_amdgcn_readfirstlane(units));
+    const int per = max(min(kWaves, (all + each - 1) / each), (all + a.groups - 1) / a.groups);
     if (int64_t(me) * per >= all) return;
     int at = me * per;
     const int stop = min(all, at + per);
@@ -527,9 +532,10 @@ esp_status shape_of(const esp_kv_cache *c, int32_t rows, int64_t tokens, int32_t
     // Read once (one unit a row), and more than the memory-side cache holds twice over: loads
     // that leave no trace, 195 -> 177 us for 1.04 GB; 46 -> 51 us for 268 MB read again and again.
     s.stream = int64_t(max_new) * group <= kCols && 2 * int64_t(rows) * max_length * c->kv_heads * c->head_dim > (int64_t(512) << 20);
-    // no more than one for every four tiles of the longest rows
+    // no more than one for every four tiles of the longest rows, or for every unit
     const int64_t few = int64_t(rows) * ((int64_t(max_new) * group + kCols - 1) / kCols), tiles = few * (max_length / kTile + 2);
-    if (tiles / kWaves + 1 < s.groups) s.groups = int32_t(tiles / kWaves + 1);
+    const int64_t most = tiles / kWaves + 1 > few ? tiles / kWaves + 1 : few;
+    if (most < s.groups) s.groups = int32_t(most);
     s.counters = (size_t(s.groups) * c->kv_heads * 4 + 255) / 256 * 256;
     s.bytes = s.counters + size_t(s.groups) * c->kv_heads * 2 * kCols * (c->head_dim + 2) * 4;
     return ESP_OK;

@@ -155,7 +155,7 @@ def rotate(rope: Rope, x: torch.Tensor, positions: torch.Tensor, inverse: bool =
     if D != rope.head_dim:
         raise ValueError(f"x: heads of {rope.head_dim} elements expected")
     if out is None:
-        out = torch.empty((T, H, D), dtype=x.dtype, device=x.device)
+        out = torch.empty_like(x) if x.is_contiguous() else torch.empty(x.shape, dtype=x.dtype, device=x.device)
     elif out.dtype != x.dtype:
         raise ValueError("out: the type of x expected")
     _check(lib().esp_kv_rotate(rope.ptr, kind, T, H, D, _view(x, T, H, D, "x", x.device), _ints(positions, T, "positions", x.device),
@@ -245,7 +245,7 @@ class PagedCache:
             heads = q.shape[1]
             if q.numel() and (q.data_ptr() % 16 or q.stride(0) % 8 or q.stride(1) % 8):
                 q = q.contiguous()
-            out = torch.empty((T, heads, D), dtype=q.dtype, device=dev)
+            out = torch.empty_like(q) if q.is_contiguous() else torch.empty(q.shape, dtype=q.dtype, device=dev)
             vq, vo = _view(q, T, heads, D, "q", dev), _view(out, T, heads, D, "q", dev)
         _check(lib().esp_kv_append(self.ptr, layer, kind, rows, T, off, sq, _view(k, T, H, D, "k", dev), _view(v, T, H, D, "v", dev),
                                    None if rope is None else rope.ptr, heads, vq, vo, s), "esp_kv_append")
@@ -289,7 +289,7 @@ class PagedCache:
                 self._sizes.clear()
             size = self._sizes[shape] = n.value
         if out is None:
-            out = torch.empty((T, H, self.head_dim), dtype=q.dtype, device=self.device)
+            out = torch.empty_like(q) if q.is_contiguous() else torch.empty(q.shape, dtype=q.dtype, device=self.device)
         elif out.dtype != q.dtype:
             raise ValueError("out: the type of q expected")
         stats = torch.empty((T, H), dtype=torch.float32, device=self.device) if lse else None

@@ -82,8 +82,9 @@ template <typename T> __device__ __forceinline__ void store8(T *p, const Vec8<T>
 // vectors c and c + n of the turned part's 2 n (a pair's two sides), with
 // neighbours as pairs the same vectors, each with pairs of its own; then the
 // same of the part that passes through.
-constexpr int kPer = 4;
-template <typename T>
+// Stream: what is read is not read again soon, and is read past the caches.
+constexpr int kRotateHeads = 4, kAppendHeads = 2;
+template <typename T, int kPer, bool Stream>
 __device__ __forceinline__ void rotate_chunk(const Rope &r, const View &x, const View &out, int64_t t, int position,
                                              int head, int heads, int dim, int c, float sign) {
     constexpr int kVec = 16 / sizeof(T);
@@ -100,8 +101,9 @@ __device__ __forceinline__ void rotate_chunk(const Rope &r, const View &x, const
 #pragma unroll
     for (int h = 0; h < kPer; h++) {
         const T *from = p + min(h, heads - 1) * x.head;
-        u[h].w = *reinterpret_cast<const uint4v *>(from + a);
-        v[h].w = *reinterpret_cast<const uint4v *>(from + b);
+        const uint4v *pa = reinterpret_cast<const uint4v *>(from + a), *pb = reinterpret_cast<const uint4v *>(from + b);
+        u[h].w = Stream ? __builtin_nontemporal_load(pa) : *pa;
+        v[h].w = Stream ? __builtin_nontemporal_load(pb) : *pb;
     }
     if (turn) {
         float cs[kVec], sn[kVec];
@@ -145,9 +147,9 @@ __global__ __launch_bounds__(kThreads) void k_rotate(Rope r, View x, View out, c
                                                      int heads, int dim, int chunks, float sign) {
     const int64_t u = int64_t(blockIdx.x) * kThreads + threadIdx.x;
     const int64_t t = uint32_t(u) / uint32_t(chunks);           // tokens * chunks < 2^32
-    const int head = blockIdx.y * kPer;
+    const int head = blockIdx.y * kRotateHeads;
     if (t >= tokens) return;
-    rotate_chunk<T>(r, x, out, t, positions[t], head, min(kPer, heads - head), dim, int(u - t * chunks), sign);
+    rotate_chunk<T, kRotateHeads, true>(r, x, out, t, positions[t], head, min(kRotateHeads, heads - head), dim, int(u - t * chunks), sign);
 }
 
 // ---------------------------------------------------------------------------
@@ -429,7 +431,7 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads) 
         return;
     }
     constexpr int kChunks = Dim / 16;
-    const int groups = (a.q_heads + kPer - 1) / kPer;
+    const int groups = (a.q_heads + kAppendHeads - 1) / kAppendHeads;
     const int64_t u = int64_t(int(blockIdx.x) - a.writers) * kThreads + threadIdx.x, tg = u / kChunks;
     const int64_t t = min(tg / groups, a.rows.tokens - 1);
     // the row of the wavefront's first token, then step by step
@@ -438,8 +440,8 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads) 
     if (tg / groups >= a.rows.tokens) return;
     while (b + 1 < a.rows.rows && a.rows.offsets[b + 1] <= t) b++;
     const Row row = row_of(a.c, a.rows, b);
-    const int head = int(tg - t * groups) * kPer;
-    rotate_chunk<T>(a.rope, a.q, a.q_out, t, row.length - row.n + int(t - row.first), head, min(kPer, a.q_heads - head), Dim, int(u % kChunks), 1.0f);
+    const int head = int(tg - t * groups) * kAppendHeads;
+    rotate_chunk<T, kAppendHeads, false>(a.rope, a.q, a.q_out, t, row.length - row.n + int(t - row.first), head, min(kAppendHeads, a.q_heads - head), Dim, int(u % kChunks), 1.0f);
 }
 
 // ---------------------------------------------------------------------------
@@ -561,7 +563,7 @@ void rotate(const Rope &r, View x, View out, const int32_t *positions, int64_t t
     if (vector) {
         const int chunks = dim / (32 / int(sizeof(T)));
         const int64_t blocks = (tokens * chunks + kThreads - 1) / kThreads;
-        k_rotate<T><<<dim3(unsigned(blocks), (heads + kPer - 1) / kPer), kThreads, 0, s>>>(r, x, out, positions, tokens, heads, dim, chunks, sign);
+        k_rotate<T><<<dim3(unsigned(blocks), (heads + kRotateHeads - 1) / kRotateHeads), kThreads, 0, s>>>(r, x, out, positions, tokens, heads, dim, chunks, sign);
     } else {
         const int64_t blocks = (tokens * heads * (dim / 2) + kThreads - 1) / kThreads;
         k_rotate_any<T><<<unsigned(blocks < 65536 ? blocks : 65536), kThreads, 0, s>>>(r, x, out, positions, tokens, heads, dim, sign);
@@ -654,7 +656,7 @@ extern "C" esp_status esp_kv_append(const esp_kv_cache *cache, int32_t layer, in
     const int32_t teams = 64 / cache->page_tokens,
                   shares = 2 * shares_of(units, (cache->kv_heads + teams - 1) / teams, 8);
     const int64_t writers = units * shares;
-    const int64_t turners = (tokens * ((q_heads + kPer - 1) / kPer) * (cache->head_dim / 16) + kThreads - 1) / kThreads;
+    const int64_t turners = (tokens * ((q_heads + kAppendHeads - 1) / kAppendHeads) * (cache->head_dim / 16) + kThreads - 1) / kThreads;
     if (units * shares > INT32_MAX || writers + turners > INT32_MAX) return ESP_ERR_SHAPE;
     const unsigned blocks = unsigned(writers + turners);
     // loads of four keys or two values at a time

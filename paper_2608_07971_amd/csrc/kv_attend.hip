@@ -510,6 +510,11 @@ esp_status shape_of(const esp_kv_cache *c, int32_t rows, int64_t tokens, int32_t
     const int64_t group = q_heads / c->kv_heads;
     if (int64_t(max_new) * group > INT32_MAX / 2) return ESP_ERR_SHAPE;
     s = Shape{};
+    // Counters lie in front, as many for every call on caches of this many heads, so that
+    // calls of other shapes leave them alone: k_attend takes groups * heads, k_prompt
+    // units * heads of at most half its 512 places.
+    s.counters = ((size_t(kComputeUnits) * 3 + c->kv_heads) * 4 + 255) / 256 * 256;
+    s.bytes = s.counters;
     const int64_t units = rows ? tokens * group / kPromptRows + rows : 0;
     s.prompt = tokens * group >= int64_t(rows) * kManyRows && units * c->kv_heads >= kManyUnits;
     if (s.prompt) {
@@ -520,11 +525,7 @@ esp_status shape_of(const esp_kv_cache *c, int32_t rows, int64_t tokens, int32_t
         if (splits > max_length / (8 * kTile)) splits = max_length / (8 * kTile);
         s.units = int32_t(units);
         s.splits = int32_t(splits > 1 ? splits : 1);
-        if (s.splits > 1) {
-            s.counters = (size_t(units) * c->kv_heads * 4 + 255) / 256 * 256;
-            s.bytes = s.counters + size_t(units) * c->kv_heads * s.splits * kPromptRows * (c->head_dim + 2) * 4;
-        }
-        if (s.bytes < 256) s.bytes = 256;
+        if (s.splits > 1) s.bytes += size_t(units) * c->kv_heads * s.splits * kPromptRows * (c->head_dim + 2) * 4;
         return ESP_OK;
     }
     const int slots = kComputeUnits * (c->head_dim == 64 ? kPerUnit<64> : kPerUnit<128>);
@@ -536,8 +537,7 @@ esp_status shape_of(const esp_kv_cache *c, int32_t rows, int64_t tokens, int32_t
     const int64_t few = int64_t(rows) * ((int64_t(max_new) * group + kCols - 1) / kCols), tiles = few * (max_length / kTile + 2);
     const int64_t most = tiles / kWaves + 1 > few ? tiles / kWaves + 1 : few;
     if (most < s.groups) s.groups = int32_t(most);
-    s.counters = (size_t(s.groups) * c->kv_heads * 4 + 255) / 256 * 256;
-    s.bytes = s.counters + size_t(s.groups) * c->kv_heads * 2 * kCols * (c->head_dim + 2) * 4;
+    s.bytes += size_t(s.groups) * c->kv_heads * 2 * kCols * (c->head_dim + 2) * 4;
     return ESP_OK;
 }
 

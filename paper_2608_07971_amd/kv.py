@@ -234,8 +234,8 @@ class PagedCache:
         kind = _TYPES.get(k.dtype)
         if kind is None or kind == FP32 or k.dim() != 3 or v.dtype != k.dtype or (q is not None and (q.dtype != k.dtype or q.dim() != 3)):
             raise ValueError("k, v and q: bfloat16 or float16 [tokens, heads, head_dim] expected, of one type")
-        if rope is not None and rope.head_dim != self.head_dim:
-            raise ValueError("rope: made for another head_dim")
+        if rope is not None and (rope.head_dim != self.head_dim or rope.index != self.index):
+            raise ValueError("rope: made for another head_dim or device")
         if q is not None and rope is None:
             raise ValueError("q is given to be turned: rope expected")
         T, H, D, dev = k.shape[0], self.kv_heads, self.head_dim, self.device

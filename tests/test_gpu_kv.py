@@ -369,6 +369,23 @@ def test_nan_reaches_only_the_queries_that_see_it(n, group, window):
             assert torch.isnan(out[sees][..., 3]).all() and not torch.isnan(out[sees][..., 4:]).any() and torch.equal(lse, want_lse)
 
 
+def test_one_workspace_serves_calls_of_any_shape():
+    """Calls of few and of many workgroups in turn, single tokens and prompts: what one leaves in the workspace is
+    nothing to the next."""
+    g = np.random.default_rng(3)
+    lengths = [5000, 9, 3000, 777] + [int(x) for x in g.integers(1, 400, 60)]
+    cache = ref.make(kv, lengths, heads=2, dim=64, seed=9)
+    dev = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    shapes = [([0], [1]), (list(range(64)), [1] * 64), ([2], [300]), ([0, 2], [1, 1]), ([0, 1, 2, 3], [40, 9, 200, 64]), (list(range(40)), [2] * 40), ([1], [1])]
+    for seqs, new in shapes * 2:
+        _say(f"workspace: rows {len(seqs)}, new {max(new)}")
+        q = _randn(len(seqs), sum(new), 8, 64, dtype=torch.float16)
+        got = cache.attend(0, q, ref.offsets(new), seqs=dev(seqs))
+        alone = kv.PagedCache.adopt(cache.k, cache.v, cache.scale, cache.table, cache.lengths, cache.refs)
+        want = alone.attend(0, q, ref.offsets(new), seqs=dev(seqs))
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 def test_attend_strides():
     cache = ref.make(kv, [90, 40], heads=2, dim=128)
     wide = _randn(1, 6, 9, 131, dtype=torch.bfloat16)
@@ -498,6 +515,18 @@ def test_a_compaction_leaves_the_old_places_readable():
     assert torch.equal(cache.attend(0, q, ref.offsets([1] * 4))[0], want)
 
 
+def test_a_compaction_in_place():
+    cache = ref.make(kv, [100, 30, 77, 5], heads=2, dim=64, pages=60)
+    q = _randn(1, 4, 4, 64, dtype=torch.bfloat16)
+    want = cache.attend(0, q, ref.offsets([1] * 4))[0]
+    table, refs, live = cache.compact()
+    work = torch.zeros(1 << 20, dtype=torch.uint8, device="cuda")
+    assert kv.lib().esp_kv_compact(cache.ptr, -1, cache.table.data_ptr(), cache.refs.data_ptr(), None, work.data_ptr(), work.numel(),
+                                   torch.cuda.current_stream().cuda_stream) == esp.ESP_OK
+    assert torch.equal(cache.table, table) and torch.equal(cache.refs, refs)
+    assert torch.equal(cache.attend(0, q, ref.offsets([1] * 4))[0], want)
+
+
 def test_forks_share_full_pages_and_write_apart():
     cache = ref.make(kv, [40, 0, 0], heads=1, dim=64, pages=12, width=4)
     dev = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
@@ -609,7 +638,7 @@ def test_the_binding_refuses_what_does_not_fit():
                  lambda: cache.append(0, k.float(), k.float(), offs), lambda: cache.attend(0, q.float(), offs), lambda: cache.attend(0, q, offs.cpu()),
                  lambda: cache.attend(0, q.transpose(1, 2).contiguous().transpose(1, 2), offs), lambda: cache.attend(0, q, offs, out=q.half()),
                  lambda: cache.resize(offs), lambda: cache.fork(offs[:1], offs[:2]), lambda: cache.install(cache.refs, cache.table),
-                 lambda: kv.rotate(rope, k, offs[:1]), lambda: kv.rotate(kv.Rope(128), k, offs[:2]), lambda: kv.rotate(rope, k.double(), offs[:2]),
+                 lambda: kv.rotate(rope, k.cpu(), offs[:2]), lambda: kv.rotate(rope, k, offs[:1]), lambda: kv.rotate(kv.Rope(128), k, offs[:2]), lambda: kv.rotate(rope, k.double(), offs[:2]),
                  lambda: kv.Rope(64, 128), lambda: kv.Rope(64, scaling="other"), lambda: kv.PagedCache.adopt(cache.v, cache.v, cache.scale, cache.table, cache.lengths, cache.refs)):
         with pytest.raises(ValueError):
             call()

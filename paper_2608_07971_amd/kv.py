@@ -198,7 +198,7 @@ class PagedCache:
         self.status = torch.zeros(1, dtype=torch.int32, device=k.device)
         self.pages, self.layers, self.kv_heads, self.page_tokens, self.head_dim = P, L, H, T, D
         self.sequences, self.table_width = table.shape
-        self._work, self._sizes = {}, {}
+        self._work, self._outgrown, self._sizes = {}, [], {}
         self._scale, self._pages_bytes = D ** -0.5, None
         self._describe()
 
@@ -214,9 +214,16 @@ class PagedCache:
         return 2 * self.layers * self.kv_heads * (self.page_tokens * self.head_dim + 4)
 
     def _workspace(self, kind: str, size, stream: int) -> torch.Tensor:
-        """Scratch of this kind of call on this stream, kept and grown."""
+        """Scratch of this kind of call on this stream, kept and grown; what it outgrew is kept too, since a captured
+        graph may name it.  A call captured before this stream has any takes scratch of the graph, which clears it in
+        every replay."""
         w = self._work.get((kind, stream))
         if w is None or w.numel() < size:
+            if torch.cuda.is_current_stream_capturing():
+                return torch.zeros(size, dtype=torch.uint8, device=self.device)
+            if w is not None:
+                self._outgrown.append(w)
+                size = max(size, 2 * w.numel())
             w = torch.zeros(max(size, 256), dtype=torch.uint8, device=self.device)
             self._work[(kind, stream)] = w
         return w

@@ -629,6 +629,56 @@ def test_a_step_in_a_graph():
     assert caches[0].device_status() == 0
 
 
+def test_graphs_without_a_warm_up():
+    """Graphs captured before their stream has scratch, replayed in another order than captured, with larger eager calls
+    on the stream between."""
+    offs = {n: ref.offsets([1] * n) for n in (1, 3)}
+    cache = ref.make(kv, [4000, 47, 900], heads=2, dim=64, seed=6)
+    q = {n: torch.zeros(n, 8, 64, dtype=torch.float16, device="cuda") for n in (1, 3)}
+    side, plain = torch.cuda.Stream(), kv.PagedCache.adopt(cache.k, cache.v, cache.scale, cache.table, cache.lengths, cache.refs)
+    torch.cuda.synchronize()
+    graphs, out = {}, {}
+    for n in (3, 1):
+        graphs[n] = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graphs[n], stream=side):
+            out[n] = [cache.attend(0, q[n], offs[n]) for _ in range(2)]
+    for i, n in enumerate((1, 3, 1, 1, 3)):
+        _say(f"graph of {n} rows, replay {i}")
+        q[n].copy_(_randn(i, n, 8, 64, dtype=torch.float16))
+        graphs[n].replay()
+        torch.cuda.synchronize()
+        want = plain.attend(0, q[n], offs[n])
+        for got in out[n]:
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        many = _randn(90 + i, 300 * (i + 1), 8, 64, dtype=torch.float16)
+        torch.cuda.synchronize()
+        got, want = (c.attend(0, many, ref.offsets([300 * (i + 1)]), stream=s) for c, s in ((cache, side), (plain, None)))
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_a_graph_keeps_its_scratch_when_the_cache_takes_more():
+    cache = ref.make(kv, [4000, 47], heads=2, dim=64, seed=7)
+    plain = kv.PagedCache.adopt(cache.k, cache.v, cache.scale, cache.table, cache.lengths, cache.refs)
+    offs, side = ref.offsets([1, 1]), torch.cuda.Stream()
+    q = _randn(1, 2, 8, 64, dtype=torch.float16)
+    want = plain.attend(0, q, offs)
+    torch.cuda.synchronize()
+    cache.attend(0, q, offs, stream=side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        got = cache.attend(0, q, offs)
+    for i in range(3):
+        many = torch.zeros(700 * (i + 1), 8, 64, dtype=torch.float16, device="cuda")
+        torch.cuda.synchronize()
+        cache.attend(0, many, ref.offsets([700 * (i + 1), 0]), stream=side)
+        with torch.cuda.stream(side):                            # what scratch given back would hold
+            junk = [torch.full((1 << n,), 255, dtype=torch.uint8, device="cuda") for n in range(12, 24)]
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and all(bool((x == 255).all()) for x in junk)
+
+
 def test_the_binding_refuses_what_does_not_fit():
     cache = ref.make(kv, [20, 20], heads=2, dim=64)
     rope, offs = kv.Rope(64), ref.offsets([1, 1])

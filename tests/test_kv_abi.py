@@ -130,3 +130,10 @@ def test_bad_page_operations_are_refused():
         assert L.esp_kv_compact(p, 1, A, A, A, w, s, None) == esp.ESP_ERR_WORKSPACE
     assert L.esp_kv_fork(p, 0, None, None, None, 0, None) == esp.ESP_OK
     assert L.esp_kv_device_status(None, None) == esp.ESP_ERR_INVALID_ARG
+
+
+def test_launches_beyond_32_bits_of_threads_are_refused():
+    L, c, r, v = kv.lib(), _cache(), _rope(), _view()
+    p, most = C.addressof(c), 2 ** 31 - 1
+    assert L.esp_kv_append(p, 0, 0, 1, most, A, None, v, v, C.addressof(r), 64, v, v, None) == esp.ESP_ERR_SHAPE
+    assert L.esp_kv_gather(p, 0, 0, 1, most, A, None, A, A, A, None) == esp.ESP_ERR_SHAPE

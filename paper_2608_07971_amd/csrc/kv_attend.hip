@@ -132,6 +132,7 @@ template <typename T, int Dim, int Page, bool Stream> __global__ __launch_bounds
         uint64_t past = __ballot(win.end[lane] > at);
         while (!past) {
             b0 += 64;
+            if (b0 >= a.rows.rows) return;  // lengths that change during the call
             load_window(a, b0, win.end[63], win);
             past = __ballot(win.end[lane] > at);
         }
@@ -469,19 +470,19 @@ template <typename T, int Dim, int Page, bool Stream> __global__ __launch_bounds
             for (int i = 0; i < kMine; i++) y[i] = empty ? 0.0f : y[i] / l;
         }
         if (rn < n_rows) {
-        const int tok = row.first + rn / a.group, qh = head * a.group + rn % a.group;
-        T *dst = static_cast<T *>(a.out.data) + int64_t(tok) * a.out.token + int64_t(qh) * a.out.head + d0;
-        if (a.wide_out) {
-            typedef T Out __attribute__((ext_vector_type(kMine)));
-            Out z;
+            const int tok = row.first + rn / a.group, qh = head * a.group + rn % a.group;
+            T *dst = static_cast<T *>(a.out.data) + int64_t(tok) * a.out.token + int64_t(qh) * a.out.head + d0;
+            if (a.wide_out) {
+                typedef T Out __attribute__((ext_vector_type(kMine)));
+                Out z;
 #pragma unroll
-            for (int i = 0; i < kMine; i++) z[i] = T(y[i]);
-            *reinterpret_cast<Out *>(dst) = z;
-        } else {
+                for (int i = 0; i < kMine; i++) z[i] = T(y[i]);
+                *reinterpret_cast<Out *>(dst) = z;
+            } else {
 #pragma unroll
-            for (int i = 0; i < kMine; i++) dst[i] = T(y[i]);
-        }
-        if (d0 == 0 && a.lse) a.lse[int64_t(tok) * a.q_heads + qh] = lse * kLn2;
+                for (int i = 0; i < kMine; i++) dst[i] = T(y[i]);
+            }
+            if (d0 == 0 && a.lse) a.lse[int64_t(tok) * a.q_heads + qh] = lse * kLn2;
         }
     }
 }

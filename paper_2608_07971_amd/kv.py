@@ -200,9 +200,7 @@ class PagedCache:
         self.sequences, self.table_width = table.shape
         self._work, self._outgrown, self._sizes = {}, [], {}
         self._scale, self._pages_bytes = D ** -0.5, None
-        self._describe()
-
-    def _describe(self) -> None:
+        # kernels and captured graphs take the addresses by value: the tensors stay for the cache's life
         self.c = esp_kv_cache(self.pages, self.layers, self.kv_heads, self.page_tokens, self.head_dim, self.sequences,
                               self.table_width, self.k.data_ptr(), self.v.data_ptr(), self.scale.data_ptr(), self.table.data_ptr(),
                               self.lengths.data_ptr(), self.refs.data_ptr(), self.status.data_ptr())
@@ -331,7 +329,8 @@ class PagedCache:
     @_on_stream
     def compact(self, limit: Optional[int] = None, *, s: int):
         """(table, refs, live) with no live page from `limit` on (None: from the number of live pages on).  The cache
-        goes on with its old table, whose pages stay intact, until `install` is given the new one."""
+        goes on with its old table, whose pages stay intact, until `install` is given the new one.  The pool keeps its
+        size; `adopt` over clones of its first pages is a smaller one."""
         table, refs = torch.empty_like(self.table), torch.empty_like(self.refs)
         live = torch.empty((), dtype=torch.int32, device=self.device)
         w = self._pages_work(s)
@@ -339,14 +338,17 @@ class PagedCache:
                                     w.data_ptr(), w.numel(), s), "esp_kv_compact")
         return table, refs, live
 
-    def install(self, table, refs) -> None:
-        """Takes the table and references of a compaction."""
+    @_on_stream
+    def install(self, table, refs, *, s: int) -> None:
+        """Takes the table and references of a compaction: copied into the cache's own tensors in stream order, so that
+        captured graphs and calls already enqueued go on naming live memory.  Readers on other streams see the old or
+        the new places, which hold the same until a later call writes pages: order them before that one."""
         _ints(table, self.table.numel(), "table", self.device)
         _ints(refs, self.pages, "refs", self.device)
         if table.shape != self.table.shape:
             raise ValueError("table: the cache's shape expected")
-        self.table, self.refs = table, refs
-        self._describe()
+        self.table.copy_(table)
+        self.refs.copy_(refs)
 
     @_on_stream
     def device_status(self, *, s: int) -> int:

@@ -43,8 +43,12 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 
 
     const Cache &c = a.c;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5;
+    if (blockIdx.x == 0) {                  // beside the list: what is wrong with any row, also one that no unit is found for
+        for (int b = tid; b < a.rows.rows; b += kThreads) usable_row(a, b);
+        return;
+    }
     // the dies take stretches of the list [head][part][unit], so that a die's cache holds the keys of few heads
-    const int per_die = gridDim.x / kDies, item = blockIdx.x % kDies * per_die + blockIdx.x / kDies;
+    const int place = blockIdx.x - 1, per_die = (gridDim.x - 1) / kDies, item = place % kDies * per_die + place / kDies;
     const int per_head = a.units * a.splits, head = item / per_head;
     if (head >= c.heads) return;
     const int part = (item - head * per_head) / a.units, index = a.units - 1 - (item - head * per_head - part * a.units);
@@ -451,7 +455,7 @@ template <typename T, int Dim> static void launch_dim(const AttendArgs &a, unsig
 
 void launch_prompt(const AttendArgs &a, int32_t type, hipStream_t s) {
     const int64_t items = int64_t(a.units) * a.splits * a.c.heads;
-    const unsigned blocks = unsigned((items + kDies - 1) / kDies * kDies);
+    const unsigned blocks = unsigned((items + kDies - 1) / kDies * kDies) + 1;
     if (type == ESP_KV_BF16) a.c.dim == 64 ? launch_dim<__bf16, 64>(a, blocks, s) : launch_dim<__bf16, 128>(a, blocks, s);
     else a.c.dim == 64 ? launch_dim<_Float16, 64>(a, blocks, s) : launch_dim<_Float16, 128>(a, blocks, s);
 }

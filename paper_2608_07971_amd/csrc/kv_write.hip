@@ -181,6 +181,12 @@ __device__ __forceinline__ uint32_t code2(float a, float b) {
     return __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
 }
 
+// Work of a launch's first workgroup, beside the others': records what is wrong with any
+// row, also with those that no unit is found for where offsets do not ascend.
+__device__ __forceinline__ void check_rows(const Cache &c, const Rows &r) {
+    for (int b = threadIdx.x; b < r.rows; b += kThreads) row_of(c, r, b);
+}
+
 // A unit is one page that a row's tokens touch: row b's units are numbered from
 // offsets[b] / Page + 2 b (n tokens touch at most n / Page + 2 pages).
 struct Unit {
@@ -407,16 +413,18 @@ __device__ __forceinline__ void append_values(const AppendArgs &a, const Unit &u
 
 // Workgroups [0, writers): some of the 2 * heads blocks of one unit, a block by
 // as many wavefronts as the page has sixteens of tokens (a single token by one);
-// the others turn the queries.
+// the others turn the queries.  One more, in front, checks the rows.
 // Bound by the chain load - largest - scale - store of each block: 256 single tokens
 // of 8 key and 32 query heads of 128, 19 MB with the reading back of their pages, 23 us
 // in two launches; 9 prompts of up to 4,096 tokens, 175 MB likewise, 55 us (3.2 TB/s).
 template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads) void k_append(AppendArgs a) {
     constexpr int kTeam = Page / 16, kTeams = 4 / kTeam;
     __shared__ float lds[2][4];
-    if (int(blockIdx.x) < a.writers) {
+    const int place = int(blockIdx.x) - 1;
+    if (place < 0) return check_rows(a.c, a.rows);
+    if (place < a.writers) {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        const int unit = blockIdx.x / a.shares, share = blockIdx.x - unit * a.shares;
+        const int unit = place / a.shares, share = place - unit * a.shares;
         const Unit u = unit_of<Page>(a.c, a.rows, unit, nullptr);
         if (u.from >= u.to || u.page < 0) return;
         const int blocks = 2 * a.c.heads;
@@ -437,7 +445,7 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads) 
     }
     constexpr int kChunks = Dim / 16;
     const int groups = (a.q_heads + kAppendHeads - 1) / kAppendHeads;
-    const int64_t u = int64_t(int(blockIdx.x) - a.writers) * kThreads + threadIdx.x, tg = u / kChunks;
+    const int64_t u = int64_t(place - a.writers) * kThreads + threadIdx.x, tg = u / kChunks;
     const int64_t t = min(tg / groups, a.rows.tokens - 1);
     // the row of the wavefront's first token, then step by step
     const int64_t t_first = __shfl(int(t), 0);
@@ -526,7 +534,9 @@ template <typename T, int Dim, int Page> __device__ __forceinline__ void gather_
 }
 
 template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads) void k_gather(GatherArgs a) {
-    const int w = __builtin_amdgcn_readfirstlane(blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6));
+    const int place = int(blockIdx.x) - 1;
+    if (place < 0) return check_rows(a.c, a.rows);
+    const int w = __builtin_amdgcn_readfirstlane(place * (kThreads / 64) + (threadIdx.x >> 6));
     const int unit = w / a.shares, share = w - unit * a.shares;
     if (unit >= a.units) return;
     const Unit u = unit_of<Page>(a.c, a.rows, unit, a.starts);
@@ -665,8 +675,8 @@ extern "C" esp_status esp_kv_append(const esp_kv_cache *cache, int32_t layer, in
                   shares = 2 * shares_of(units, (cache->kv_heads + teams - 1) / teams, 8);
     const int64_t writers = units * shares;
     const int64_t turners = (tokens * ((q_heads + kAppendHeads - 1) / kAppendHeads) * (cache->head_dim / 16) + kThreads - 1) / kThreads;
-    if (writers + turners > kMostThreads / kThreads) return ESP_ERR_SHAPE;
-    const unsigned blocks = unsigned(writers + turners);
+    if (writers + turners + 1 > kMostThreads / kThreads) return ESP_ERR_SHAPE;
+    const unsigned blocks = unsigned(writers + turners + 1);
     // loads of four keys or two values at a time
     auto fours = [](const esp_kv_view &x) { return (reinterpret_cast<uintptr_t>(x.data) & 7) == 0 && x.token_stride % 4 == 0 && x.head_stride % 4 == 0; };
     const AppendArgs a{cache_of(cache), Rows{offsets, seqs, rows, tokens}, rope_of(rope), view_of(k), view_of(v), view_of(q), view_of(q_out),
@@ -688,8 +698,9 @@ extern "C" esp_status esp_kv_gather(const esp_kv_cache *cache, int32_t layer, in
     if (!starts || !k_out || !v_out || !aligned16(k_out) || !aligned16(v_out)) return ESP_ERR_INVALID_ARG;
     const int64_t units = tokens / cache->page_tokens + 2 * int64_t(rows);
     const int32_t shares = shares_of(units, 2 * cache->kv_heads, 1);
-    if (units * shares > kMostThreads / 64) return ESP_ERR_SHAPE;
-    const unsigned blocks = unsigned((units * shares + kThreads / 64 - 1) / (kThreads / 64));
+    const int64_t workers = (units * shares + kThreads / 64 - 1) / (kThreads / 64);
+    if (workers + 1 > kMostThreads / kThreads) return ESP_ERR_SHAPE;
+    const unsigned blocks = unsigned(workers + 1);
     const GatherArgs a{cache_of(cache), Rows{offsets, seqs, rows, tokens}, starts, layer, shares, int32_t(units), k_out, v_out};
     const hipStream_t s = static_cast<hipStream_t>(stream);
     if (type == ESP_KV_BF16) cache->head_dim == 64 ? gather<__bf16, 64>(a, blocks, s) : gather<__bf16, 128>(a, blocks, s);

@@ -127,9 +127,11 @@ esp_status esp_kv_gather(const esp_kv_cache *cache, int32_t layer, int32_t type,
  * max_new >= every row's n and max_length >= every length are bounds the
  * caller knows (they choose the launch; larger ones cost little).  A row over
  * either bound is not computed and recorded as ESP_ERR_SHAPE.
- * workspace: at least esp_kv_attend_workspace bytes, 256-byte aligned, zeroed
- * once before its first use and left ready for the next call, of any shape, on
- * a cache of as many kv_heads; calls that may run at the same time need one each.
+ * workspace: at least esp_kv_attend_workspace bytes, 256-byte aligned, the first
+ * 4 * (768 + kv_heads) of them zeroed once before its first use and left ready
+ * for the next call, of any shape, on a cache of as many kv_heads; calls that
+ * may run at the same time need one each, so a graph that may be replayed beside
+ * other work needs its own.
  */
 esp_status esp_kv_attend_workspace(const esp_kv_cache *cache, int32_t rows, int64_t tokens, int32_t q_heads,
                                    int32_t max_new, int32_t max_length, size_t *bytes);

@@ -514,7 +514,7 @@ esp_status shape_of(const esp_kv_cache *c, int32_t rows, int64_t tokens, int32_t
     const int64_t group = q_heads / c->kv_heads;
     if (int64_t(max_new) * group > INT32_MAX / 2) return ESP_ERR_SHAPE;
     s = Shape{};
-    // Counters lie in front, as many for every call on caches of this many heads, so that
+    // Counters, all that has to be zero at first, lie in front, as many for every call on caches of this many heads, so that
     // calls of other shapes leave them alone: k_attend takes groups * heads, k_prompt
     // units * heads of at most half its 512 places.
     s.counters = ((size_t(kComputeUnits) * 3 + c->kv_heads) * 4 + 255) / 256 * 256;

@@ -72,8 +72,17 @@ def lib():
         for name, args in _SIGS.items():
             fn = getattr(L, name)
             fn.argtypes, fn.restype = args, C.c_int
+        L.hipStreamGetCaptureInfo.argtypes = [_P, C.POINTER(C.c_int), C.POINTER(C.c_ulonglong)]
         _lib = L
     return _lib
+
+
+def _capture(stream: int):
+    """What tells the capture that the current stream (of this handle) is in from others; None outside of one."""
+    if not torch.cuda.is_current_stream_capturing():
+        return None
+    status, number = C.c_int(0), C.c_ulonglong(0)
+    return number.value if lib().hipStreamGetCaptureInfo(stream, C.byref(status), C.byref(number)) == 0 else object()
 
 
 def _check(code: int, where: str) -> None:
@@ -198,7 +207,7 @@ class PagedCache:
         self.status = torch.zeros(1, dtype=torch.int32, device=k.device)
         self.pages, self.layers, self.kv_heads, self.page_tokens, self.head_dim = P, L, H, T, D
         self.sequences, self.table_width = table.shape
-        self._work, self._outgrown, self._sizes = {}, [], {}
+        self._work, self._graph_work, self._sizes = {}, (None, {}), {}
         self._scale, self._pages_bytes = D ** -0.5, None
         # kernels and captured graphs take the addresses by value: the tensors stay for the cache's life
         self.c = esp_kv_cache(self.pages, self.layers, self.kv_heads, self.page_tokens, self.head_dim, self.sequences,
@@ -212,18 +221,23 @@ class PagedCache:
         return 2 * self.layers * self.kv_heads * (self.page_tokens * self.head_dim + 4)
 
     def _workspace(self, kind: str, size, stream: int) -> torch.Tensor:
-        """Scratch of this kind of call on this stream, kept and grown; what it outgrew is kept too, since a captured
-        graph may name it.  A call captured before this stream has any takes scratch of the graph, which clears it in
-        every replay."""
-        w = self._work.get((kind, stream))
+        """Scratch of this kind of call on this stream, kept and grown.  Calls that are captured share scratch of their
+        graph instead, which may be replayed beside other work of any stream: its first use clears it in every replay."""
+        capture = _capture(stream)
+        if capture is None:
+            kept = self._work
+        else:
+            if capture != self._graph_work[0]:
+                self._graph_work = capture, {}
+            kept = self._graph_work[1]
+        w = kept.get((kind, stream))
         if w is None or w.numel() < size:
-            if torch.cuda.is_current_stream_capturing():
-                return torch.zeros(size, dtype=torch.uint8, device=self.device)
-            if w is not None:
-                self._outgrown.append(w)
+            if w is not None and capture is None:
                 size = max(size, 2 * w.numel())
-            w = torch.zeros(max(size, 256), dtype=torch.uint8, device=self.device)
-            self._work[(kind, stream)] = w
+            w = torch.empty(max(size, 256), dtype=torch.uint8, device=self.device)
+            if kind == "attend":
+                w[:4 * (768 + self.kv_heads)].zero_()
+            kept[(kind, stream)] = w
         return w
 
     def _rows(self, offsets, seqs):

@@ -78,3 +78,34 @@ def test_a_reader_on_another_stream_goes_on_during_an_installation():
     assert all(torch.equal(x, y) for x, y in zip(got, want))
     assert all(torch.equal(x, y) for x, y in zip(cache.attend(0, q, offs), want))
     assert all(bool((x == 0x7f7f7f7f).all()) for x in junk) and cache.device_status() == 0
+
+
+@pytest.mark.parametrize("new", [[1, 1], [700, 900]])
+def test_graphs_of_one_stream_replay_beside_each_other_and_eager_calls(new):
+    """Captured on a stream that has scratch, replayed on two others while that one runs calls of its own; units of
+    several parts throughout."""
+    cache = ref.make(kv, [9000, 7000], heads=4, dim=64, seed=5)
+    offs, streams = ref.offsets(new), [torch.cuda.Stream() for _ in range(3)]
+    qs = [torch.zeros(sum(new), 16, 64, dtype=torch.float16, device="cuda") for _ in range(3)]
+    torch.cuda.synchronize()
+    cache.attend(0, qs[2], offs, stream=streams[2])               # the capturing stream has scratch of its own
+    graphs, out = [], []
+    for q in qs[:2]:
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=streams[2]):
+            out.append([cache.attend(0, q, offs) for _ in range(3)])
+    for i in range(6):
+        _say(f"new {new}, replays {i}")
+        for j, q in enumerate(qs):
+            q.copy_(_randn(10 * i + j, *q.shape))
+        want = [cache.attend(0, q, offs) for q in qs]
+        torch.cuda.synchronize()
+        for graph, stream in zip(graphs, streams):
+            with torch.cuda.stream(stream):
+                graph.replay()
+        eager = [cache.attend(0, qs[2], offs, stream=streams[2]) for _ in range(3)]
+        torch.cuda.synchronize()
+        for w, got in zip(want, out + [eager]):
+            assert all(torch.equal(a, b) for g in got for a, b in zip(g, w))
+    assert cache.device_status() == 0

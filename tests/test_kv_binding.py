@@ -32,3 +32,26 @@ def test_install_keeps_the_addresses_that_calls_were_given(on_the_host):
         with pytest.raises(ValueError):
             cache.install(*bad)
     assert torch.equal(table, new[0]) and torch.equal(refs, new[1])
+
+
+def test_captured_calls_take_scratch_of_their_graph(on_the_host, monkeypatch):
+    cache, now = on_the_host, [None]
+    cache._work, cache._graph_work, cache._outgrown, cache.kv_heads = {}, (None, {}), [], 2
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: now[0] is not None)
+    monkeypatch.setattr(kv, "_capture", lambda stream: now[0], raising=False)
+    for kind in ("attend", "pages"):
+        now[0] = None
+        eager = cache._workspace(kind, 5000, 7)
+        seen = [eager]
+        for now[0] in (1, 2):                                     # two captures on a stream that has scratch
+            w = cache._workspace(kind, 5000, 7)
+            assert w.numel() >= 5000 and all(w.data_ptr() != x.data_ptr() for x in seen)
+            assert cache._workspace(kind, 4000, 7) is w           # the graph's calls share it
+            assert cache._workspace(kind, 5000, 8) is not w       # but not those on another stream of the capture
+            more = cache._workspace(kind, 9000, 7)
+            assert more.numel() >= 9000 and more is not w
+            seen += [w, more]
+        now[0] = None
+        assert cache._workspace(kind, 5000, 7) is eager
+        if kind == "attend":                                      # the counters are clear
+            assert not any(bool(x[:4 * (768 + 2)].any()) for x in seen)

@@ -155,8 +155,50 @@ class Rope:
 @_on_stream
 def rotate(rope: Rope, x: torch.Tensor, positions: torch.Tensor, inverse: bool = False, out: Optional[torch.Tensor] = None,
            *, s: int) -> torch.Tensor:
-    """x [tokens, heads, head_dim] turned by positions (int32 [tokens]); inverse: turned back, which is the gradient.
-    out may be x.  stream: the current one, unless given."""
+    """x [tokens, heads, head_dim] turned by positions (int32 [tokens]); inverse: turned back, which is the gradient, and
+    what backward() does.  out may be x.  stream: the current one, unless given."""
+    if torch.is_grad_enabled() and (x.requires_grad or (out is not None and out.requires_grad)):
+        return _Turned.apply(x, None if out is x else out, out is x, rope, positions, inverse, s)
+    return _turn(rope, x, positions, inverse, out, s)
+
+
+class _Turned(torch.autograd.Function):
+    """rotate with its gradient: the rotation times magnitude, transposed."""
+
+    @staticmethod
+    def forward(ctx, x, out, in_place, rope, positions, inverse, s):
+        if in_place:
+            out = x
+        if out is not None:
+            ctx.mark_dirty(out)
+        ctx.rope, ctx.inverse = rope, inverse
+        ctx.save_for_backward(positions)
+        return _turn(rope, x, positions, inverse, out, s)
+
+    @staticmethod
+    def backward(ctx, grad):
+        positions, = ctx.saved_tensors
+        if grad.stride(-1) != 1:
+            grad = grad.contiguous()
+        return rotate(ctx.rope, grad, positions, inverse=not ctx.inverse), None, None, None, None, None, None
+
+
+class _NoGradient(torch.autograd.Function):
+    """A result that depends on tensors that require gradients, through what has none: backward() says so."""
+
+    @staticmethod
+    def forward(ctx, what, source, result):
+        ctx.what = what
+        ctx.mark_dirty(result)
+        return result
+
+    @staticmethod
+    def backward(ctx, grad):
+        raise RuntimeError(f"{ctx.what} has no gradient: the cache holds its tokens rounded to 8 bits. Detach its inputs, or "
+                           "call it under torch.no_grad()")
+
+
+def _turn(rope, x, positions, inverse, out, s: int) -> torch.Tensor:
     kind = _TYPES.get(x.dtype)
     if kind is None or x.dim() != 3 or x.device != rope.device:
         raise ValueError(f"x: bfloat16, float16 or float32 tensor [tokens, heads, head_dim] on {rope.device} expected")
@@ -209,6 +251,7 @@ class PagedCache:
         self.sequences, self.table_width = table.shape
         self._work, self._graph_work, self._sizes = {}, (None, {}), {}
         self._scale, self._pages_bytes = D ** -0.5, None
+        self._source = None                     # requires gradients once tokens were appended that do
         # kernels and captured graphs take the addresses by value: the tensors stay for the cache's life
         self.c = esp_kv_cache(self.pages, self.layers, self.kv_heads, self.page_tokens, self.head_dim, self.sequences,
                               self.table_width, self.k.data_ptr(), self.v.data_ptr(), self.scale.data_ptr(), self.table.data_ptr(),
@@ -240,6 +283,13 @@ class PagedCache:
             kept[(kind, stream)] = w
         return w
 
+    def _results(self, what: str, q, *results):
+        """The results of a call on q, and on what the cache holds, whose gradients would be lost."""
+        if not torch.is_grad_enabled():
+            return results
+        source = q if q is not None and q.requires_grad else self._source
+        return results if source is None else tuple(_NoGradient.apply("PagedCache." + what, source, r) for r in results)
+
     def _rows(self, offsets, seqs):
         rows = offsets.numel() - 1
         if rows < 0 or (seqs is None and rows > self.sequences):
@@ -249,7 +299,8 @@ class PagedCache:
     @_on_stream
     def append(self, layer: int, k, v, offsets, rope: Optional[Rope] = None, q=None, seqs=None, *, s: int):
         """Writes the new tokens k, v [tokens, kv_heads, head_dim], the last ones of their sequences, rows cut by
-        offsets (int32 [rows + 1]); q [tokens, q_heads, head_dim] is turned too and returned."""
+        offsets (int32 [rows + 1]); q [tokens, q_heads, head_dim] is turned too and returned.  No gradient goes through
+        the cache or this turning (rotate has one): backward() raises where one would be lost."""
         kind = _TYPES.get(k.dtype)
         if kind is None or kind == FP32 or k.dim() != 3 or v.dtype != k.dtype or (q is not None and (q.dtype != k.dtype or q.dim() != 3)):
             raise ValueError("k, v and q: bfloat16 or float16 [tokens, heads, head_dim] expected, of one type")
@@ -268,7 +319,9 @@ class PagedCache:
             vq, vo = _view(q, T, heads, D, "q", dev), _view(out, T, heads, D, "q", dev)
         _check(lib().esp_kv_append(self.ptr, layer, kind, rows, T, off, sq, _view(k, T, H, D, "k", dev), _view(v, T, H, D, "v", dev),
                                    None if rope is None else rope.ptr, heads, vq, vo, s), "esp_kv_append")
-        return out
+        if torch.is_grad_enabled() and (k.requires_grad or v.requires_grad) and self._source is None:
+            self._source = torch.zeros((), requires_grad=True)
+        return out if out is None or not q.requires_grad else self._results("append", q, out)[0]
 
     @_on_stream
     def gather(self, layer: int, starts, offsets, tokens: int, dtype=torch.bfloat16, seqs=None, *, s: int):
@@ -278,10 +331,11 @@ class PagedCache:
         if kind is None or kind == FP32:
             raise ValueError("dtype: bfloat16 or float16 expected")
         rows, off, sq = self._rows(offsets, seqs)
-        k, v = torch.empty((2, tokens, self.kv_heads, self.head_dim), dtype=dtype, device=self.device)
+        both = torch.empty((2, tokens, self.kv_heads, self.head_dim), dtype=dtype, device=self.device)
+        k, v = both[0], both[1]
         _check(lib().esp_kv_gather(self.ptr, layer, kind, rows, tokens, off, sq, _ints(starts, rows, "starts", self.device),
                                    k.data_ptr(), v.data_ptr(), s), "esp_kv_gather")
-        return k, v
+        return self._results("gather", None, k, v)
 
     @_on_stream
     def attend(self, layer: int, q, offsets, scale: Optional[float] = None, window: int = 0, max_new: Optional[int] = None,
@@ -316,7 +370,9 @@ class PagedCache:
         _check(lib().esp_kv_attend(self.ptr, layer, kind, rows, T, off, sq, H, _view(q, T, H, self.head_dim, "q", self.device), scale,
                                    window, max_new, max_length, _view(out, T, H, self.head_dim, "out", self.device),
                                    None if stats is None else stats.data_ptr(), w.data_ptr(), w.numel(), s), "esp_kv_attend")
-        return out, stats
+        if stats is None:
+            return self._results("attend", q, out)[0], None
+        return self._results("attend", q, out, stats)
 
     def _pages_work(self, stream: int) -> torch.Tensor:
         if self._pages_bytes is None:

@@ -314,7 +314,7 @@ class PagedCache:
         if q is not None:
             heads = q.shape[1]
             if q.numel() and (q.data_ptr() % 16 or q.stride(0) % 8 or q.stride(1) % 8):
-                q = q.contiguous()
+                q = q.clone(memory_format=torch.contiguous_format)    # also of one that is contiguous at an odd place
             out = torch.empty_like(q) if q.is_contiguous() else torch.empty(q.shape, dtype=q.dtype, device=dev)
             vq, vo = _view(q, T, heads, D, "q", dev), _view(out, T, heads, D, "q", dev)
         _check(lib().esp_kv_append(self.ptr, layer, kind, rows, T, off, sq, _view(k, T, H, D, "k", dev), _view(v, T, H, D, "v", dev),

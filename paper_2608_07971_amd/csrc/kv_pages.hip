@@ -43,7 +43,7 @@ struct Work {
     int32_t *count;                         // copies to make
     int2 *copies;                           // from, to
     int32_t *goes;                          // [pages] new places
-    bool at_once;                           // small pages are copied by the workgroup that finds them
+    bool at_once;                           // pages are copied by the workgroup that finds them
 };
 
 __device__ __forceinline__ int lanes_below(uint64_t mask) {
@@ -508,10 +508,17 @@ using namespace esp_kv;
 
 namespace {
 
-// Bytes of a page up to which fork and resize copy it within their last step, a
-// workgroup a page: a fork of one child of 32 / 128 / 256 KB pages takes 10.4 / 12.3 /
-// 15.0 us so, 12.5 / 13.7 / 13.9 us with a launch of its own for the copies.
+// Bytes of a page up to which fork copies it within its last step, a workgroup a page:
+// a fork of one child of 32 / 128 / 256 KB pages takes 10.4 / 12.3 / 15.0 us so, 12.5 /
+// 13.7 / 13.9 us with a launch of its own for the copies.
 constexpr int64_t kAtOnce = 128 << 10;
+// A workgroup of resize's last step has the entries of many sequences, each of which may
+// need a copy.  It makes them, one after another, only if there can be no more than these
+// and no more bytes.  So / with a launch of its own, 2 KB pages: no or one copy 15.8 /
+// 17.1 us, 4 copies 21.5 / 21.1, 16 copies 28.5 / 21.0, 64 copies 57.5 / 23.1; 32 KB pages:
+// 4 copies 24.0 / 22.0, 16 copies 36.0 / 21.4; 1,024 copies of 128 KB by four workgroups
+// 845 / 70.
+constexpr int64_t kResizeCopies = 16, kResizeBytes = 64 << 10;
 
 // Lays the work out behind `p`; returns its bytes.
 size_t lay_out(const esp_kv_cache *c, char *p, Work &w) {
@@ -532,17 +539,22 @@ size_t lay_out(const esp_kv_cache *c, char *p, Work &w) {
     take(w.bad, size_t(c->sequences) > size_t(kMaxBlocks) ? size_t(c->sequences) : size_t(kMaxBlocks));
     take(w.copies, size_t(c->pages));
     take(w.goes, size_t(c->pages));
-    w.at_once = 2 * int64_t(c->layers) * c->kv_heads * c->page_tokens * c->head_dim <= kAtOnce;
+    w.at_once = false;
     return size_t(at - p);
 }
 esp_status work_of(const esp_kv_cache *c, void *workspace, size_t bytes, Work &w) {
     const size_t need = lay_out(c, static_cast<char *>(workspace), w);
     return workspace && (reinterpret_cast<uintptr_t>(workspace) & 255) == 0 && bytes >= need ? ESP_OK : ESP_ERR_WORKSPACE;
 }
+int64_t page_bytes(const esp_kv_cache *c) { return 2 * int64_t(c->layers) * c->kv_heads * c->page_tokens * c->head_dim; }
+// Copies that one workgroup of resize may have to make: one a sequence of its entries.
+int64_t copies_of(const esp_kv_cache *c, const Work &w) {
+    const int64_t sequences = (int64_t(w.entries.words) * 64 + c->table_width - 2) / c->table_width + 1;
+    return sequences < c->sequences ? sequences : c->sequences;
+}
 // Workgroups of the copy for at most `most` pages: 2,048 fill the GPU.
 unsigned copy_blocks(const esp_kv_cache *c, int64_t most) {
-    const int64_t bytes = int64_t(c->layers) * c->kv_heads * c->page_tokens * c->head_dim;
-    const int64_t blocks = most * 2 * ((bytes + kCopyThreads * 64 - 1) / (kCopyThreads * 64));
+    const int64_t blocks = most * 2 * ((page_bytes(c) / 2 + kCopyThreads * 64 - 1) / (kCopyThreads * 64));
     return unsigned(blocks < 1 ? 1 : blocks < 2048 ? blocks : 2048);
 }
 
@@ -564,6 +576,8 @@ extern "C" esp_status esp_kv_resize(const esp_kv_cache *cache, const int32_t *le
     if (esp_status e = work_of(cache, workspace, workspace_bytes, w)) return e;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const Cache c = cache_of(cache);
+    const int64_t copies = copies_of(cache, w);
+    w.at_once = copies <= kResizeCopies && copies * page_bytes(cache) <= kResizeBytes;
     k_resize_drop<<<w.entries.blocks, kThreads, 0, s>>>(c, lengths, w);
     k_resize_mark<<<w.entries.blocks + w.pages.blocks, kThreads, 0, s>>>(c, lengths, w);
     k_resize_take<<<w.entries.blocks, kThreads, 0, s>>>(c, lengths, w);
@@ -581,6 +595,7 @@ extern "C" esp_status esp_kv_fork(const esp_kv_cache *cache, int32_t n, const in
     if (esp_status e = work_of(cache, workspace, workspace_bytes, w)) return e;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const Cache c = cache_of(cache);
+    w.at_once = page_bytes(cache) <= kAtOnce;
     k_fork_drop<<<n, kThreads, 0, s>>>(c, n, parents, children, w);
     k_mark_free<<<w.pages.blocks, kThreads, 0, s>>>(c, w);
     k_fork_take<<<n, kThreads, 0, s>>>(c, n, parents, children, w);

@@ -131,7 +131,9 @@ esp_status esp_kv_gather(const esp_kv_cache *cache, int32_t layer, int32_t type,
  * 4 * (768 + kv_heads) of them zeroed once before its first use and left ready
  * for the next call, of any shape, on a cache of as many kv_heads; calls that
  * may run at the same time need one each, so a graph that may be replayed beside
- * other work needs its own.
+ * other work needs its own.  Lengths, offsets and sequence numbers must not
+ * change while a call that was given them runs: the outputs are then undefined,
+ * and the workspace is to be zeroed again before it serves another call.
  */
 esp_status esp_kv_attend_workspace(const esp_kv_cache *cache, int32_t rows, int64_t tokens, int32_t q_heads,
                                    int32_t max_new, int32_t max_length, size_t *bytes);

@@ -132,10 +132,11 @@ template <typename T, int Dim, int Page, bool Stream> __global__ __launch_bounds
         uint64_t past = __ballot(win.end[lane] > at);
         while (!past) {
             b0 += 64;
-            if (b0 >= a.rows.rows) return;  // lengths that change during the call
+            if (b0 >= a.rows.rows) break;
             load_window(a, b0, win.end[63], win);
             past = __ballot(win.end[lane] > at);
         }
+        if (!past) break;                   // lengths that change during the call
         const int in = __builtin_ctzll(past);
         auto same = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
         const Row row{same(win.row[in].first), same(win.row[in].n), same(win.row[in].seq), same(win.row[in].length)};
@@ -485,6 +486,7 @@ template <typename T, int Dim, int Page, bool Stream> __global__ __launch_bounds
             if (d0 == 0 && a.lse) a.lse[int64_t(tok) * a.q_heads + qh] = lse * kLn2;
         }
     }
+    if (at < stop && threadIdx.x == 0) record(c, ESP_ERR_SHAPE);
 }
 
 }  // namespace esp_kv

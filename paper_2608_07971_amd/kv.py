@@ -422,5 +422,9 @@ class PagedCache:
 
     @_on_stream
     def device_status(self, *, s: int) -> int:
-        """The first error that the GPU recorded since the last call (waits for the stream)."""
-        return int(lib().esp_kv_device_status(self.ptr, s))
+        """The first error that the GPU recorded since the last call (waits for the stream).  After one, calls take new
+        scratch: lengths that changed under a call may have left the old with parts that it waits for."""
+        code = int(lib().esp_kv_device_status(self.ptr, s))
+        if code != ESP_OK:
+            self._work.clear()
+        return code

@@ -109,3 +109,17 @@ def test_graphs_of_one_stream_replay_beside_each_other_and_eager_calls(new):
         for w, got in zip(want, out + [eager]):
             assert all(torch.equal(a, b) for g in got for a, b in zip(g, w))
     assert cache.device_status() == 0
+
+
+def test_an_error_taken_leaves_good_scratch():
+    """A call whose lengths changed under it may leave tickets behind: they are put there by hand."""
+    cache = ref.make(kv, [9000, 7000], heads=4, dim=64, seed=6)
+    q, offs = _randn(1, 2, 16, 64), ref.offsets([1, 1])
+    want = cache.attend(0, q, offs)
+    for (kind, _), w in cache._work.items():
+        if kind == "attend":
+            w[:4 * 768].view(torch.int32).fill_(1)
+    cache.status.fill_(2)                                         # what the call records
+    assert cache.device_status() == 2 and cache.device_status() == 0
+    got = cache.attend(0, q, offs)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and cache.device_status() == 0

@@ -1,5 +1,7 @@
 """The paged cache's binding without a GPU: what it does around the C calls."""
 
+import types
+
 import pytest
 import torch
 
@@ -55,3 +57,17 @@ def test_captured_calls_take_scratch_of_their_graph(on_the_host, monkeypatch):
         assert cache._workspace(kind, 5000, 7) is eager
         if kind == "attend":                                      # the counters are clear
             assert not any(bool(x[:4 * (768 + 2)].any()) for x in seen)
+
+
+def test_scratch_is_not_kept_past_an_error(on_the_host, monkeypatch):
+    cache, code = on_the_host, [0]
+    cache._work, cache._graph_work, cache._outgrown, cache.kv_heads, cache.ptr = {}, (None, {}), [], 2, 0
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    monkeypatch.setattr(kv, "lib", lambda: types.SimpleNamespace(esp_kv_device_status=lambda ptr, stream: code[0]))
+    w = cache._workspace("attend", 5000, 7)
+    w[40] = 3                                                     # a ticket that was drawn and not given back
+    assert cache.device_status() == 0 and cache._workspace("attend", 5000, 7) is w
+    code[0] = 2
+    assert cache.device_status() == 2
+    again = cache._workspace("attend", 5000, 7)
+    assert again is not w and not bool(again[:4 * (768 + 2)].any())

@@ -177,7 +177,7 @@ template <typename T, int Dim, int Page, bool Stream> __global__ __launch_bounds
 #pragma unroll
         for (int d = 0; d < kTiles; d++) o[d] = float4v{0, 0, 0, 0};
         float m_run = -INFINITY, l_run = 0.0f;   // largest score (log 2); sum of the weights of this lane's tokens
-        int o_exp = kNoScale;
+        int o_exp = kNoScale, o_top = kNoScale;      // o_top: the largest so far
 
         // What a wavefront holds of a tile.  Keys: this lane reads 16 bytes of rows of
         // page_k's tokens; values: 16 tokens of page_v at 16 dimensions.
@@ -233,7 +233,7 @@ template <typename T, int Dim, int Page, bool Stream> __global__ __launch_bounds
             }
         };
         // The running maximum takes the tile's scores in; the output follows.
-        auto raise = [&](const float4v (&s)[4], float vs, bool held_page) {
+        auto raise = [&](const float4v (&s)[4]) {
             float top = -INFINITY;
 #pragma unroll
             for (int j = 0; j < 4; j++)
@@ -247,21 +247,29 @@ template <typename T, int Dim, int Page, bool Stream> __global__ __launch_bounds
 #pragma unroll
                 for (int d = 0; d < kTiles; d++) o[d] *= by;
             }
-            // value scales relative to the largest so far, so that fp16 holds weight * scale
-            int e = max(-126, min(126, int((__float_as_uint(vs) >> 23) & 255) - 127));
-            e = across_max(held_page ? e : kNoScale);
-            if (__any(e > o_exp)) {
-                const float by = ldexpf(1.0f, max(o_exp - e, -200));
-#pragma unroll
-                for (int d = 0; d < kTiles; d++) o[d] *= by;
-                o_exp = e;
-            }
         };
-        auto values = [&](const half8 (&w)[2]) {
+        // Weights times values, of which this lane's 16 tokens have a scale of exponent e:
+        // in one go, unless the tile's blocks are too far apart.  A scale of 0 is near any.
+        auto values = [&](const half8 (&w)[2], int e) {
+            auto largest = [&] { return __builtin_amdgcn_readfirstlane(across_max(e)); };
+            for (int most = largest(); most > kNoScale; most = largest()) {
+                o_top = max(o_top, most);
+                if (most > o_exp || most < o_exp - kNear) {
+                    const int to = max(most, o_top - kDown);
+                    const float by = ldexpf(1.0f, max(o_exp - to, -200));
 #pragma unroll
-            for (int d = 0; d < kTiles; d++)
+                    for (int d = 0; d < kTiles; d++) o[d] *= by;
+                    o_exp = to;
+                }
+                const bool near = e >= min(o_exp - kNear, most);
+                const half8 u[2] = {near ? w[0] : half8{}, near ? w[1] : half8{}};
+                const float by = power(e - o_exp);
 #pragma unroll
-                for (int k = 0; k < 2; k++) o[d] = product(codes8<half8, half2>(vw[d][2 * k], vw[d][2 * k + 1]), w[k], o[d]);
+                for (int d = 0; d < kTiles; d++)
+#pragma unroll
+                    for (int k = 0; k < 2; k++) o[d] = product(scaled8(vw[d][2 * k], vw[d][2 * k + 1], by), u[k], o[d]);
+                e = near ? kNoScale : e;
+            }
         };
 
         // Tiles that every row sees whole.  Pages are read two steps ahead, keys and
@@ -287,8 +295,9 @@ template <typename T, int Dim, int Page, bool Stream> __global__ __launch_bounds
             for (int j = 0; j < 4; j++)
 #pragma unroll
                 for (int i = 0; i < 4; i++) s[j][i] = __builtin_fmaf(s[j][i], ks, none);
-            raise(s, vs, held_page);
-            const float base = m_run == -INFINITY ? 0.0f : m_run - kLift, v_rel = held_page ? ldexpf(vs, -o_exp) : 0.0f;
+            raise(s);
+            const int e = exponent(vs);
+            const float base = m_run == -INFINITY ? 0.0f : m_run - kLift, v_rest = held_page ? ldexpf(vs, -e) : 0.0f;
             half8 w[2];
 #pragma unroll
             for (int j = 0; j < 4; j++)
@@ -296,9 +305,9 @@ template <typename T, int Dim, int Page, bool Stream> __global__ __launch_bounds
                 for (int i = 0; i < 4; i++) {
                     const float x = __builtin_amdgcn_exp2f(s[j][i] - base);
                     l_run += x;
-                    w[j >> 1][4 * (j & 1) + i] = _Float16(x * v_rel);
+                    w[j >> 1][4 * (j & 1) + i] = _Float16(x * v_rest);
                 }
-            values(w);
+            values(w, !held_page ? kNoScale : vs != 0.0f ? e : max(o_exp, -126));
             if (more) {
                 load_values(t + kWaves);
                 if (t + 2 * kWaves < whole_to) pages_of(t + 2 * kWaves);
@@ -322,8 +331,9 @@ template <typename T, int Dim, int Page, bool Stream> __global__ __launch_bounds
                     const int tt = at_v + 4 * j + i;
                     s[j][i] = tt <= pos && tt > low && ok ? s[j][i] * ks : -INFINITY;
                 }
-            raise(s, v_scale, ok);
-            const float base = m_run == -INFINITY ? 0.0f : m_run - kLift, v_rel = ldexpf(v_scale, -o_exp);
+            raise(s);
+            const int e = exponent(v_scale);
+            const float base = m_run == -INFINITY ? 0.0f : m_run - kLift, v_rest = ldexpf(v_scale, -e);
             half8 w[2], seen[2];
 #pragma unroll
             for (int j = 0; j < 4; j++)
@@ -332,7 +342,7 @@ template <typename T, int Dim, int Page, bool Stream> __global__ __launch_bounds
                     const bool hidden = s[j][i] == -INFINITY;
                     const float x = __builtin_amdgcn_exp2f(s[j][i] - base);
                     l_run += x;
-                    w[j >> 1][4 * (j & 1) + i] = hidden ? _Float16(0.0f) : _Float16(x * v_rel);    // 0 * an infinite scale
+                    w[j >> 1][4 * (j & 1) + i] = hidden ? _Float16(0.0f) : _Float16(x * v_rest);    // 0 * an infinite scale
                     seen[j >> 1][4 * (j & 1) + i] = hidden ? _Float16(0.0f) : _Float16(1.0f);
                 }
             // tokens past the end hold anything: their codes become 0.  A NaN that
@@ -365,7 +375,7 @@ template <typename T, int Dim, int Page, bool Stream> __global__ __launch_bounds
                         if (hit[i] > 0.0f) o[d][i] = NAN;
                 }
             }
-            values(w);
+            values(w, !ok ? kNoScale : v_scale != 0.0f ? e : max(o_exp, -126));
         }
 
         // join the wavefronts

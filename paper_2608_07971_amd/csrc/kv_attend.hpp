@@ -15,6 +15,12 @@ constexpr int kCols = 16;                   // (token, query head) rows of a uni
 constexpr float kLift = 10.0f, kSlack = 4.0f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kPromptRows = 128;            // rows of a unit of many new tokens
+// Values enter their product in fp16 as code * scale / 2^r, with r the output's exponent.
+// That is exact for scales from 2^(r - kNear) to 2^r: e4m3's least step is 2^-9, fp16's
+// 2^-24.  Blocks outside of these move r, and the output with it, so that what one block
+// gives does not depend on how large others are; r stays within 2^kDown of the largest so
+// far, which keeps the output in float32's range.
+constexpr int kNear = 15, kDown = 80;
 constexpr int kNoScale = -200;              // exponent of a value scale below any
 
 struct View {
@@ -72,6 +78,17 @@ __device__ __forceinline__ void store_pair(float *p, float x, float y) {
 __device__ __forceinline__ float2 load_pair(const float *p) {
     const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t *>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     return make_float2(__uint_as_float(uint32_t(v)), __uint_as_float(uint32_t(v >> 32)));
+}
+
+// Exponent of a scale, and what is left of it: 1 for those that append makes.
+__device__ __forceinline__ int exponent(float x) { return max(-126, min(126, int((__float_as_uint(x) >> 23) & 255) - 127)); }
+// 2^e, from 2^-126 on.
+__device__ __forceinline__ float power(int e) { return __uint_as_float(uint32_t(max(1, min(254, e + 127))) << 23); }
+// Four codes times 2^k (the exponent of `by`).
+__device__ __forceinline__ half8 scaled8(uint32_t a, uint32_t b, float by) {
+    const half2 x = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, by, false), y = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, by, true);
+    const half2 z = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, by, false), w = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, by, true);
+    return half8{x[0], x[1], y[0], y[1], z[0], z[1], w[0], w[1]};
 }
 
 // Many new tokens: kv_prompt.hip.

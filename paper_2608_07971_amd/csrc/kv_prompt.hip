@@ -10,13 +10,6 @@ typedef float float16v __attribute__((ext_vector_type(16)));
 __device__ __forceinline__ float16v product32(half8 x, half8 y, float16v z) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(x, y, z, 0, 0, 0); }
 __device__ __forceinline__ float16v product32(bhalf8 x, bhalf8 y, float16v z) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, z, 0, 0, 0); }
 
-// Four codes times 2^k (the exponent of `by`).
-__device__ __forceinline__ half8 scaled8(uint32_t a, uint32_t b, float by) {
-    const half2 x = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, by, false), y = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, by, true);
-    const half2 z = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, by, false), w = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, by, true);
-    return half8{x[0], x[1], y[0], y[1], z[0], z[1], w[0], w[1]};
-}
-
 // A workgroup takes 128 rows (token, query head) of one sequence and key head
 // against tiles of 64 tokens, each of its four wavefronts 32 rows.  Codes
 // become 16-bit numbers once, on their way into LDS, for all four; while a tile
@@ -133,7 +126,6 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 
         return Group{page, p[0], p[c.heads]};
     };
     auto lane_float = [&](float x, int g) { return __uint_as_float(uint32_t(__builtin_amdgcn_readlane(__float_as_uint(x), g))); };
-    auto exponent = [](float x) { return max(-126, min(126, int((__float_as_uint(x) >> 23) & 255) - 127)); };
 
     // Unit u of the keys: 16 bytes of token u / kSegs.  Unit u of the values: 16
     // tokens of one dimension, in the order in which pages hold them.  A wavefront's

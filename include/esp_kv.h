@@ -123,7 +123,11 @@ esp_status esp_kv_gather(const esp_kv_cache *cache, int32_t layer, int32_t type,
  *   out = sum_t softmax_t(scale * q . k_t) v_t,   lse = ln sum_t exp(scale * q . k_t)
  * A token that sees nothing gets out = 0, lse = -inf.  lse: float32
  * [tokens][q_heads] contiguous, or NULL.  Every sum and statistic is float32;
- * the softmax weights enter the value product rounded to fp16.
+ * the softmax weights enter the value product rounded to fp16: 2^-11 of each,
+ * and those below 2^-34 of the largest vanish.  Values enter it exactly if their
+ * block's scale is a power of two, as append's are, whatever other blocks'
+ * scales (down to 2^-80 of the largest, then less exactly); with another scale
+ * they may be rounded to fp16 first.
  * max_new >= every row's n and max_length >= every length are bounds the
  * caller knows (they choose the launch; larger ones cost little).  A row over
  * either bound is not computed and recorded as ESP_ERR_SHAPE.

@@ -22,6 +22,7 @@ constexpr int kPromptRows = 128;            // rows of a unit of many new tokens
 // far, which keeps the output in float32's range.
 constexpr int kNear = 15, kDown = 80;
 constexpr int kNoScale = -200;              // exponent of a value scale below any
+constexpr int kApart = 1000;                // k_prompt: blocks of a tile that have no exponent in common
 
 struct View {
     void *data;

@@ -16,12 +16,12 @@ __device__ __forceinline__ float16v product32(bhalf8 x, bhalf8 y, float16v z) { 
 // is worked on, the codes of the next are on their way into registers.  Scores
 // and output are held transposed, as in k_attend: the rows of the key matrix
 // are taken in the order that leaves the softmax weights in place for the
-// value product.  V's block scales enter as the codes are widened, K's with the
-// softmax scale.
+// value product.  V's block scales enter as the codes are widened, exactly (kNear),
+// K's with the softmax scale.
 // Bound by the wavefronts' issue, products and the softmax between them: 3
 // sequences of up to 16,000 tokens, up to 2,048 of them new, 32 query heads of 128,
-// 847 GFLOP in 939 us (902 TFLOP/s); 16 heads of 64 in a window of 1,000 tokens, 21
-// GFLOP in 61 us (348 TFLOP/s, a third of it in tiles that only some rows see).
+// 847 GFLOP in 930 us (911 TFLOP/s); 16 heads of 64 in a window of 1,000 tokens, 21
+// GFLOP in 63.5 us (335 TFLOP/s, a third of it in tiles that only some rows see).
 template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, Dim == 64 ? 3 : 2) void k_prompt(AttendArgs a) {
     typedef typename Pack<T>::v8 V8;
     typedef typename Pack<T>::v2 V2;
@@ -102,7 +102,7 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 
 #pragma unroll
         for (int i = 0; i < 16; i++) o[d][i] = 0.0f;
     float m_run = -INFINITY, l_run = 0.0f;
-    int o_exp = kNoScale;
+    int o_exp = kNoScale, o_top = kNoScale; // exponent of the output, and the largest so far
 
     const uint32_t page_step = uint32_t(c.layers * c.heads) * (Page * Dim);
     const int64_t block_at = int64_t(a.layer * c.heads + head) * (Page * Dim);
@@ -160,10 +160,39 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 
             vw[i] = *reinterpret_cast<const uint4v *>(vals + uint64_t(pv) * page_step + value_from[i]);
         }
     };
-    // Widens the loaded tile into LDS, values divided by 2^e_ref.
-    auto store = [&](auto fast, int t, int buffer, const Group &grp, int e_ref, bool whole) {
+    // The exponent that a tile's values are taken relative to: that of the output, or the
+    // tile's largest where a block is too far from it; kApart where the blocks are too far
+    // from each other, and each has its own, in order.
+    auto scale_exponent = [&](const Group &grp) { return grp.page < 0 ? kNoScale : grp.v != 0.0f ? exponent(grp.v) : max(o_exp, -126); };
+    auto ref_of = [&](const Group &grp) {
+        const int e = scale_exponent(grp);
+        auto near = [&](int r) { return __all(e == kNoScale || (e <= r && e >= r - kNear)); };
+        if (near(o_exp)) return o_exp;
+        int most = kNoScale;
+#pragma unroll
+        for (int g = 0; g < 4; g++) most = max(most, __builtin_amdgcn_readlane(e, g));
+        const int to = max(most, max(o_top, most) - kDown);
+        return near(to) ? to : kApart;
+    };
+    // Where a tile's blocks are apart: after a group of exponent x.
+    auto ref_after = [&](int r, int &top, int x) {
+        top = max(top, x);
+        return x > r || (x > kNoScale && x < r - kNear) ? max(x, top - kDown) : r;
+    };
+    // Widens the loaded tile into LDS, values divided by 2^r.
+    auto store = [&](auto fast, int t, int buffer, const Group &grp, int ref, bool whole) {
         const int e = exponent(grp.v);
-        const float by = __uint_as_float(uint32_t(max(1, min(254, e - e_ref + 127))) << 23), rest = ldexpf(grp.v, -e);
+        int r = ref;
+        if (ref == kApart) {
+            const int own = scale_exponent(grp);
+            int at = o_exp, top = o_top;
+#pragma unroll
+            for (int g = 0; g < 4; g++) {
+                at = ref_after(at, top, __builtin_amdgcn_readlane(own, g));
+                r = (lane & 3) == g ? at : r;
+            }
+        }
+        const float by = power(e - r), rest = ldexpf(grp.v, -e);
         const bool powers = __all(rest == 1.0f || grp.page < 0);
 #pragma unroll
         for (int i = 0; i < kKeyUnits; i++) {
@@ -199,10 +228,6 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 
             *reinterpret_cast<half8 *>(&lds[buffer][value_to[i] ^ 16]) = y;
         }
     };
-    auto largest = [&](const Group &grp) {  // exponent of the largest value scale of a tile
-        const int e = grp.page >= 0 ? exponent(grp.v) : kNoScale;
-        return max(max(__builtin_amdgcn_readlane(e, 0), __builtin_amdgcn_readlane(e, 1)), max(__builtin_amdgcn_readlane(e, 2), __builtin_amdgcn_readlane(e, 3)));
-    };
     // whether every row of the workgroup sees all of a tile
     const int first_of_all = p0 + r0 / a.group, last_of_all = p0 + min(r0 + kPromptRows - 1, n_rows - 1) / a.group;
     auto inside = [&](int t, const Group &grp) {
@@ -212,14 +237,14 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 
     if (tid < 2) nans[tid] = 0;
     Group now{-1, 0.0f, 0.0f}, next{-1, 0.0f, 0.0f};
     int after = -1;                         // pages of the tile after next
-    int e_now = kNoScale;
+    int ref = kNoScale;                     // of the present tile
     if (span.from < span.to) {
         now = scales_of(page_of(span.from));
         load(now.page);
         if (span.from + 1 < span.to) after = page_of(span.from + 1);
-        e_now = largest(now);
+        ref = ref_of(now);
         __syncthreads();
-        store(std::false_type{}, span.from, 0, now, e_now, inside(span.from, now));
+        store(std::false_type{}, span.from, 0, now, ref, inside(span.from, now));
     }
     __syncthreads();
     // key row m of a matrix tile is the token whose bits 2 and 3 are those of m exchanged
@@ -227,7 +252,8 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 
     const int value_row = (col & 4) << 2 | (col & 24) >> 1 | (col & 3);
     const uint32_t key_at = key_row * kKeyRow + ((half ^ key_turn(key_row)) << 4);
     const uint32_t value_at = kHalf + value_row * (kTile * 2) + ((half ^ value_turn(value_row)) << 4);
-    // A tile, and the next into LDS.  fast: every row of the workgroup sees all of both.
+    // A tile, and the next into LDS.  fast: every row of the workgroup sees all of both, and
+    // this one's blocks are not apart.
     auto step = [&](auto fast, int t) {
         constexpr bool Fast = decltype(fast)::value;
         const int buffer = (t - span.from) & 1;
@@ -290,11 +316,13 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 
             const auto z = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
             top = fmaxf(__uint_as_float(z[0]), __uint_as_float(z[1]));
         }
-        if (__any(top > m_run + kSlack) || e_now > o_exp) {
+        const int to = !Fast && ref == kApart ? o_exp : ref;
+        if (__any(top > m_run + kSlack) || to != o_exp) {
             const float m = fmaxf(m_run, top), by = m_run == m ? 1.0f : __builtin_amdgcn_exp2f(m_run - m);
-            const float down = by * (e_now > o_exp ? ldexpf(1.0f, max(o_exp - e_now, -200)) : 1.0f);
+            const float down = by * (to != o_exp ? ldexpf(1.0f, max(o_exp - to, -200)) : 1.0f);
             m_run = m;
-            o_exp = max(o_exp, e_now);
+            o_exp = to;
+            o_top = max(o_top, to);
             l_run *= by;
 #pragma unroll
             for (int d = 0; d < kOut; d++) o[d] *= down;
@@ -330,14 +358,23 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 
             }
             __syncthreads();
         }
+        const int e_own = scale_exponent(now);
 #pragma unroll
-        for (int g = 0; g < 4; g++)
+        for (int g = 0; g < 4; g++) {
+            if (!Fast && ref == kApart) {
+                const int r = ref_after(o_exp, o_top, __builtin_amdgcn_readlane(e_own, g));
+                const float by = ldexpf(1.0f, max(o_exp - r, -200));
+                o_exp = r;
+#pragma unroll
+                for (int d = 0; d < kOut; d++) o[d] *= by;
+            }
 #pragma unroll
             for (int d = 0; d < kOut; d++)
                 o[d] = product32(*reinterpret_cast<const half8 *>(&lds[buffer][(value_at ^ (g << 5)) + d * 32 * (kTile * 2)]), w[g], o[d]);
+        }
         if (more) {
-            e_now = max(o_exp, largest(next));
-            store(fast, t + 1, buffer ^ 1, next, e_now, Fast || inside(t + 1, next));
+            ref = ref_of(next);
+            store(fast, t + 1, buffer ^ 1, next, ref, Fast || inside(t + 1, next));
             now = next;
         }
         __syncthreads();
@@ -345,7 +382,7 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 
     // tiles that every row sees by its position
     const int seen_from = a.window > 0 ? max(0, last_of_all - a.window + kTile) / kTile : 0, seen_to = (first_of_all + 1) / kTile;
     for (int t = span.from; t < span.to; t++) {
-        for (; t >= seen_from && t + 1 < min(seen_to, span.to) && __all(now.page >= 0 && after >= 0); t++) step(std::true_type{}, t);
+        for (; t >= seen_from && t + 1 < min(seen_to, span.to) && ref != kApart && __all(now.page >= 0 && after >= 0); t++) step(std::true_type{}, t);
         step(std::false_type{}, t);
     }
 

@@ -15,6 +15,8 @@ EPS = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}     # p significant
 SHAPES = [
     (1, 700, 2, 4, 64, 16, 0, torch.bfloat16, "few"), (40, 700, 1, 2, 128, 16, 0, torch.bfloat16, "few"),
     (33, 300, 2, 1, 64, 64, 100, torch.bfloat16, "few"), (90, 500, 1, 1, 128, 32, 0, torch.bfloat16, "few"),
+    (400, 700, 16, 1, 64, 16, 0, torch.bfloat16, "many"), (400, 900, 16, 1, 128, 32, 150, torch.bfloat16, "many"),
+    (400, 1700, 16, 2, 128, 16, 0, torch.bfloat16, "many"), (400, 1500, 16, 1, 64, 64, 0, torch.bfloat16, "many"),
 ]
 
 
@@ -68,7 +70,7 @@ def test_blocks_far_apart(n, L, heads, group, dim, page, window, dtype, launch, 
     _check(cache, q, n, L, window)
 
 
-@pytest.mark.parametrize("n,heads", [(30, 1)])
+@pytest.mark.parametrize("n,heads", [(30, 1), (400, 16)])
 def test_a_later_token_changes_no_earlier_row(n, heads):
     """The last page's values 2^25 times larger: rows before it keep every bit."""
     cache, q = _make(n, 640, heads, 1, 64, 16, torch.float16, "few" if n == 30 else "many", "falling")

@@ -92,8 +92,8 @@ esp_status esp_kv_rotate(const esp_kv_rope *rope, int32_t type, int64_t tokens, 
  * (esp_kv_resize).  Rows name distinct sequences.  Keys are turned by rope
  * (NULL: not; rotary_dim a multiple of 16) at their positions in the sequence.
  * Per page, head and of keys
- * and values apart: e is the least exponent with max|x| <= 448 * 2^e over the
- * finite new values, the block's scale 2^e, or the old scale where that is
+ * and values apart: e is the least exponent from -100 to 100 with
+ * max|x| <= 448 * 2^e over the finite new values, the block's scale 2^e, or the old scale where that is
  * larger and the page has older tokens (their codes are divided by the growth,
  * a power of two, so they change only where they leave e4m3's normal range).
  * Values are rounded to the nearest code once, from float32; infinities take
@@ -129,8 +129,10 @@ esp_status esp_kv_gather(const esp_kv_cache *cache, int32_t layer, int32_t type,
  * scales (down to 2^-80 of the largest, then less exactly); with another scale
  * they may be rounded to fp16 first.
  * max_new >= every row's n and max_length >= every length are bounds the
- * caller knows (they choose the launch; larger ones cost little).  A row over
- * either bound is not computed and recorded as ESP_ERR_SHAPE.
+ * caller knows.  They choose the launch and how it reads; loose ones have cost
+ * up to a tenth of a call.  A row over either bound is not computed and recorded
+ * as ESP_ERR_SHAPE; tokens of no row, or of one that is left out, keep what out
+ * and lse held.
  * workspace: at least esp_kv_attend_workspace bytes, 256-byte aligned, the first
  * 4 * (768 + kv_heads) of them zeroed once before its first use and left ready
  * for the next call, of any shape, on a cache of as many kv_heads; calls that
@@ -146,7 +148,7 @@ esp_status esp_kv_attend(const esp_kv_cache *cache, int32_t layer, int32_t type,
                          int32_t window, int32_t max_new, int32_t max_length, esp_kv_view out, float *lse,
                          void *workspace, size_t workspace_bytes, void *stream);
 
-/* Bytes that resize, fork (n = number of children) and compact need; 256-byte aligned, contents free. */
+/* Bytes that resize, fork (of n children; as many for any n up to sequences) and compact need; 256-byte aligned, contents free. */
 esp_status esp_kv_pages_workspace(const esp_kv_cache *cache, int32_t n, size_t *bytes);
 
 /*

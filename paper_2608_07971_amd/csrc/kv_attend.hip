@@ -76,7 +76,7 @@ template <bool Stream> __device__ __forceinline__ uint4v fetch(const uint8_t *p)
 // 4 g + i of score tile j is token 16 g + 4 j + i.  No data passes through LDS
 // until the wavefronts join.
 // Bound by reading the pages: 256 sequences of up to 8,192 tokens, 8 key heads of
-// 128, 1.35 GB in 254 us (5.3 TB/s); 4 of up to 131,001, 1.04 GB in 177 us (5.9 TB/s);
+// 128, 1.35 GB in 255 us (5.3 TB/s); 4 of up to 131,001, 1.04 GB in 176 us (5.9 TB/s);
 // one of 777 tokens 11 us, which is launches and latency.
 template <typename T, int Dim, int Page, bool Stream> __global__ __launch_bounds__(kThreads, kPerUnit<Dim>) void k_attend(AttendArgs a) {
     typedef typename Pack<T>::v8 V8;
@@ -507,10 +507,15 @@ namespace {
 
 constexpr int kComputeUnits = 256;
 // k_prompt from kManyRows rows of a sequence and key head on, if there are kManyUnits units.
-// Measured on 8 key heads of 128 with 4 query heads each (k_prompt against k_attend):
-// 8 sequences of 8,192 tokens, 64 rows 89 / 90 us, 128 rows 105 / 156, 256 rows 183 / 300;
-// 64 of 2,048, 64 rows 177 / 160, 128 rows 204 / 304; a single one of 16,384, 256 rows
-// (24 units) 87 / 63; of 8,192, 1,200 rows (80 units) 78 / 162.
+// Measured on 8 key heads with 4 query heads each (k_prompt / k_attend), us:
+//                                        heads of 128      heads of 64
+//   8 sequences of 8,192 tokens, 64 rows    83 /  97          60 /  50
+//                                96 rows    99 / 138          71 /  52
+//                               128 rows   102 / 166          71 /  91
+//   64 of 2,048,                 48 rows   164 / 130          82 /  66
+//                                96 rows   171 / 251          84 / 123
+//   1 of 16,384,     256 rows (24 units)    86 /  61          45 /  40
+//                  1,200 rows (80 units)   132 / 352          90 / 174
 constexpr int kManyRows = 96, kManyUnits = 64;
 
 struct Shape {
@@ -548,6 +553,9 @@ esp_status shape_of(const esp_kv_cache *c, int32_t rows, int64_t tokens, int32_t
     s.groups = slots / c->kv_heads > 1 ? slots / c->kv_heads : 1;
     // Read once (one unit a row), and more than the memory-side cache holds twice over: loads
     // that leave no trace, 195 -> 177 us for 1.04 GB; 46 -> 51 us for 268 MB read again and again.
+    // By the caller's bounds, for want of others: where these are loose it goes wrong by 3 to 8%
+    // (256 sequences of 300 tokens under a bound of 32,768: 48 -> 52 us; 256 of 4,096 with no
+    // bound on new tokens: 352 -> 368 us).
     s.stream = int64_t(max_new) * group <= kCols && 2 * int64_t(rows) * max_length * c->kv_heads * c->head_dim > (int64_t(512) << 20);
     // no more than one for every four tiles of the longest rows, or for every unit
     const int64_t few = int64_t(rows) * ((int64_t(max_new) * group + kCols - 1) / kCols), tiles = few * (max_length / kTile + 2);

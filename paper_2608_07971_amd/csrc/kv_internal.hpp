@@ -89,8 +89,6 @@ __device__ __forceinline__ void cos_sin(double t, float &c, float &s) {
     s = (q & 2) ? -b : b;
 }
 
-template <typename T> __device__ __forceinline__ float widen(T x) { return float(x); }
-
 template <int Type> struct TypeOf;
 template <> struct TypeOf<ESP_KV_BF16> { typedef __bf16 type; };
 template <> struct TypeOf<ESP_KV_FP16> { typedef _Float16 type; };

@@ -163,7 +163,7 @@ struct AppendArgs {
     Rows rows;
     Rope rope;           // rotary = 0: none
     View k, v, q, q_out;
-    int32_t layer, q_heads, units, writers, shares, wide;
+    int32_t layer, q_heads, writers, shares, wide;
 };
 
 // The least exponent e with most <= 448 * 2^e (448 = 1.75 * 2^8), within +-100.
@@ -680,7 +680,7 @@ extern "C" esp_status esp_kv_append(const esp_kv_cache *cache, int32_t layer, in
     // loads of four keys or two values at a time
     auto fours = [](const esp_kv_view &x) { return (reinterpret_cast<uintptr_t>(x.data) & 7) == 0 && x.token_stride % 4 == 0 && x.head_stride % 4 == 0; };
     const AppendArgs a{cache_of(cache), Rows{offsets, seqs, rows, tokens}, rope_of(rope), view_of(k), view_of(v), view_of(q), view_of(q_out),
-                       layer, q_heads, int32_t(units), int32_t(writers), shares, fours(k) && fours(v)};
+                       layer, q_heads, int32_t(writers), shares, fours(k) && fours(v)};
     const hipStream_t s = static_cast<hipStream_t>(stream);
     if (type == ESP_KV_BF16) cache->head_dim == 64 ? append<__bf16, 64>(a, blocks, s) : append<__bf16, 128>(a, blocks, s);
     else cache->head_dim == 64 ? append<_Float16, 64>(a, blocks, s) : append<_Float16, 128>(a, blocks, s);

@@ -5,7 +5,7 @@ and `PagedCache` own the tensors.  A step of an offline-inference job:
 
     cache.resize(lengths)                            # room for the new tokens
     q = cache.append(layer, k, v, offsets, rope=rope, q=q)
-    out, lse = cache.attend(layer, q, offsets)
+    out, lse = cache.attend(layer, q, offsets, max_new=1)
 
 `fork`, `resize` and `compact` make a changed batch or memory budget real.
 There is no CPU fallback.
@@ -341,7 +341,9 @@ class PagedCache:
     def attend(self, layer: int, q, offsets, scale: Optional[float] = None, window: int = 0, max_new: Optional[int] = None,
                max_length: Optional[int] = None, out=None, lse: bool = True, seqs=None, *, s: int):
         """(out, lse) of q [tokens, q_heads, head_dim] over the cache; scale defaults to head_dim ** -0.5.  max_new and
-        max_length bound the rows' tokens and the sequences' lengths (default: what the shapes allow)."""
+        max_length bound the rows' tokens and the sequences' lengths (default: what the shapes allow, with which a call
+        may take up to a tenth longer).  Rows that are left out leave out and lse as they were.  No gradient:
+        backward() raises where one would be lost."""
         kind = _TYPES.get(q.dtype)
         if kind is None or kind == FP32 or q.dim() != 3:
             raise ValueError("q: bfloat16 or float16 [tokens, q_heads, head_dim] expected")

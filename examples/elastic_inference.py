@@ -4,7 +4,8 @@ Eight jobs share a cluster; a job's configurations are batch sizes, each with
 the compute and the cache memory it takes.  The price loop picks one for every
 job.  Job 0 then runs in the paged 8-bit cache: prompts enter, each is forked
 to fill the batch, tokens are decoded, and when the cluster has less memory the
-job ends sequences, compacts its pages into the smaller budget and goes on.
+job ends sequences, compacts its pages into the smaller budget, gives the rest of
+the pool back and goes on.
 The layers are projections with random weights around the cache's operators.
 
     python examples/elastic_inference.py [--steps N]
@@ -117,13 +118,18 @@ class Job:
         return last
 
     def shrink(self, batch: int) -> int:
-        """Ends the sequences beyond the batch and moves the others' pages into the smaller budget; pages given back."""
+        """Ends the sequences beyond the batch, moves the others' pages into the smaller budget and goes on in a pool of
+        that size; pages given back."""
         for s in self.live()[batch:]:
             self.lengths[s] = 0
         self.cache.resize(self._ints(self.lengths))
         before, self.budget = self.budget, min(self.budget, batch * PAGES_A_SEQUENCE)
         table, refs, _ = self.cache.compact(self.budget)
         self.cache.install(table, refs)
+        if self.cache.device_status():
+            raise RuntimeError("the sequences left do not fit the budget")
+        c, n = self.cache, self.budget
+        self.cache = kv.PagedCache.adopt(*(t[:n].clone() for t in (c.k, c.v, c.scale)), c.table, c.lengths, c.refs[:n].clone())
         return before - self.budget
 
     def error(self, step) -> float:
@@ -150,7 +156,8 @@ def main(steps: int = 24) -> dict:
     freed = job.shrink(min(narrow, wide))
     highest = int(job.cache.table.max())
     second = job.error(job.decode(steps))
-    return dict(batches=(wide, narrow), pages=(wide * PAGES_A_SEQUENCE, job.budget), freed=freed, highest=highest,
+    return dict(batches=(wide, narrow), pages=(wide * PAGES_A_SEQUENCE, job.budget), freed=freed, bytes=freed * job.cache.page_bytes,
+                highest=highest,
                 lengths=[n for n in job.lengths if n], errors=(first, second), status=job.cache.device_status())
 
 
@@ -158,6 +165,6 @@ if __name__ == "__main__":
     p = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     p.add_argument("--steps", type=int, default=24, help="tokens decoded before and after the change of budget")
     r = main(p.parse_args().steps)
-    print(f"batch {r['batches'][0]} -> {r['batches'][1]}, pages {r['pages'][0]} -> {r['pages'][1]} ({r['freed']} given back, "
+    print(f"batch {r['batches'][0]} -> {r['batches'][1]}, pages {r['pages'][0]} -> {r['pages'][1]} ({r['freed']} of {r['bytes']:,} bytes given back, "
           f"highest page in use {r['highest']})")
     print(f"sequences of {r['lengths']} tokens; attention within {max(r['errors']):.1e} of 64 bits; status {r['status']}")

@@ -91,13 +91,13 @@ esp_status esp_kv_rotate(const esp_kv_rope *rope, int32_t type, int64_t tokens, 
  * last ones of sequence seqs[b] (NULL: b): its length has already grown
  * (esp_kv_resize).  Rows name distinct sequences.  Keys are turned by rope
  * (NULL: not; rotary_dim a multiple of 16) at their positions in the sequence.
- * Per page, head and of keys
- * and values apart: e is the least exponent from -100 to 100 with
- * max|x| <= 448 * 2^e over the finite new values, the block's scale 2^e, or the old scale where that is
- * larger and the page has older tokens (their codes are divided by the growth,
- * a power of two, so they change only where they leave e4m3's normal range).
- * Values are rounded to the nearest code once, from float32; infinities take
- * the largest code, NaN stays NaN.  q (q_heads > 0): turned the same way into
+ * Per page, head and of keys and values apart: e is the least exponent from -100
+ * to 100 with max|x| <= 448 * 2^e over the finite new values, the block's scale
+ * 2^e, or the old scale where that is larger and the page has older tokens (their
+ * codes are divided by the growth, a power of two, so they change only where they
+ * leave e4m3's normal range).  Values are rounded to the nearest code once, from
+ * float32; infinities, and what lies beyond 448 * 2^100, take the largest code,
+ * NaN stays NaN.  q (q_heads > 0): turned the same way into
  * q_out in the same launch; both 16-byte aligned, with strides that keep it so.
  */
 esp_status esp_kv_append(const esp_kv_cache *cache, int32_t layer, int32_t type, int32_t rows, int64_t tokens,

@@ -92,7 +92,8 @@ def _check(code: int, where: str) -> None:
 
 def _on_stream(call):
     """call(..., s): with the handle of the stream that the work goes to, on its device, so that what the call
-    allocates belongs to that stream.  The current stream of the current device costs no context."""
+    allocates belongs to that stream.  The current stream of the current device costs no context.  A stream that is
+    given is noted at the tensors that it is to read, so that the allocator keeps those that the caller drops."""
     @functools.wraps(call)
     def entry(first, *args, stream=None, **more):
         index = first.index
@@ -103,7 +104,11 @@ def _on_stream(call):
                 return call(first, *args, s=_raw_stream(index), **more)
         own = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=first.device)
         with torch.cuda.stream(own):
-            return call(first, *args, s=int(own.cuda_stream), **more)
+            result = call(first, *args, s=int(own.cuda_stream), **more)
+        for x in (first, *args, *more.values()):
+            for t in (x,) if isinstance(x, torch.Tensor) else getattr(x, "tensors", ()):
+                t.record_stream(own)
+        return result
     return entry
 
 
@@ -147,7 +152,7 @@ class Rope:
         if self.rotary_dim > self.head_dim:
             raise ValueError("rotary_dim exceeds head_dim")
         self.turns = torch.tensor(turns, dtype=torch.float64, device=device)
-        self.device, self.index = self.turns.device, self.turns.device.index
+        self.device, self.index, self.tensors = self.turns.device, self.turns.device.index, (self.turns,)
         self.c = esp_kv_rope(self.turns.data_ptr(), self.magnitude, self.rotary_dim, int(bool(interleaved)))
         self.ptr = C.addressof(self.c)
 
@@ -247,6 +252,7 @@ class PagedCache:
         self.k, self.v, self.scale, self.table, self.lengths, self.refs = k, v, scale, table, lengths, refs
         self.device, self.index = k.device, k.device.index
         self.status = torch.zeros(1, dtype=torch.int32, device=k.device)
+        self.tensors = (k, v, scale, table, lengths, refs, self.status)
         self.pages, self.layers, self.kv_heads, self.page_tokens, self.head_dim = P, L, H, T, D
         self.sequences, self.table_width = table.shape
         self._work, self._graph_work, self._sizes = {}, (None, {}), {}

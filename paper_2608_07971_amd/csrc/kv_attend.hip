@@ -540,7 +540,8 @@ esp_status shape_of(const esp_kv_cache *c, int32_t rows, int64_t tokens, int32_t
     s.prompt = tokens * group >= int64_t(rows) * kManyRows && units * c->kv_heads >= kManyUnits;
     if (s.prompt) {
         const int64_t places = 2 * kComputeUnits;
-        if (units * c->kv_heads > INT32_MAX / 2) return ESP_ERR_SHAPE;
+        // a workgroup each (one part: they are many), one more and some to fill up; a launch's threads are numbered in 32 bits
+        if (units * c->kv_heads > (int64_t(1) << 32) / kThreads - 2 * kDies) return ESP_ERR_SHAPE;
         // too few units for the GPU: their tiles are shared out, eight at least to a part
         int64_t splits = places / (units * c->kv_heads);
         if (splits > max_length / (8 * kTile)) splits = max_length / (8 * kTile);

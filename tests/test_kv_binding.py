@@ -1,10 +1,12 @@
 """The paged cache's binding without a GPU: what it does around the C calls."""
 
+import ctypes as C
 import types
 
 import pytest
 import torch
 
+import paper_2608_07971_amd as esp
 from paper_2608_07971_amd import kv
 
 
@@ -71,3 +73,14 @@ def test_scratch_is_not_kept_past_an_error(on_the_host, monkeypatch):
     assert cache.device_status() == 2
     again = cache._workspace("attend", 5000, 7)
     assert again is not w and not bool(again[:4 * (768 + 2)].any())
+
+
+def test_attention_beyond_32_bits_of_threads_is_refused():
+    at = 0x10000                                                  # stands for a device address: never read
+    c = kv.esp_kv_cache(8, 1, 2, 16, 64, 4, 4, at, at, at, at, at, at, at)
+    p, n, view = C.addressof(c), C.c_size_t(0), kv.esp_kv_view(at, 0, 0)
+    ask = lambda tokens: kv.lib().esp_kv_attend_workspace(p, 1, tokens, 8, 1000, 64, C.byref(n))  # noqa: E731
+    most = (2 ** 24 - 16) // 2 * 128 // 4                         # tokens of 2 heads' units of 128 rows, 4 a token
+    assert ask(most - 128) == esp.ESP_OK and n.value < 1 << 20
+    assert ask(most + 128) == ask(2 ** 31 - 1) == esp.ESP_ERR_SHAPE
+    assert kv.lib().esp_kv_attend(p, 0, 0, 1, 2 ** 31 - 1, at, None, 8, view, 0.1, 0, 1000, 64, view, None, at, 1 << 20, None) == esp.ESP_ERR_SHAPE

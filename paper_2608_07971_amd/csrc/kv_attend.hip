@@ -77,7 +77,7 @@ template <bool Stream> __device__ __forceinline__ uint4v fetch(const uint8_t *p)
 // until the wavefronts join.
 // Bound by reading the pages: 256 sequences of up to 8,192 tokens, 8 key heads of
 // 128, 1.35 GB in 255 us (5.3 TB/s); 4 of up to 131,001, 1.04 GB in 176 us (5.9 TB/s);
-// one of 777 tokens 11 us, which is launches and latency.
+// one of 777 tokens 11 us, a chain of reads: rows twice, table, page, parts.
 template <typename T, int Dim, int Page, bool Stream> __global__ __launch_bounds__(kThreads, kPerUnit<Dim>) void k_attend(AttendArgs a) {
     typedef typename Pack<T>::v8 V8;
     typedef typename Pack<T>::v2 V2;

@@ -86,6 +86,56 @@ esp_status esp_kv_rotate(const esp_kv_rope *rope, int32_t type, int64_t tokens, 
                          esp_kv_view x, const int32_t *positions, int32_t inverse, esp_kv_view out, void *stream);
 
 /*
+ * Norms of queries and keys for each head with the rotation in the same pass:
+ *   n = x (sum x^2 / head_dim + eps)^-1/2,   y = n w turned by the token's position (esp_kv_rotate)
+ * q, k, q_out, k_out: [tokens][q_heads or k_heads][head_dim] of `type`, head_dim
+ * even and at most 512; either side may have no heads.  Weights [head_dim] of
+ * weight_type (`type` or fp32), NULL: ones.  The outputs may be the inputs (same
+ * strides), otherwise nothing may overlap.  Everything between is float32; the
+ * result is rounded once.  eps > 0.
+ *
+ * The gradient: from q_grad and k_grad, those of the outputs, g = the rotation
+ * turned back,
+ *   dw = sum over tokens and heads of g n,   dx = (g w - n sum(g w n) / head_dim) (sum x^2 / head_dim + eps)^-1/2
+ * into dq, dk (they may be q_grad and k_grad) and dq_weight, dk_weight (NULL:
+ * not wanted; of no tokens: 0), sums in float32 in an order that depends on the
+ * sizes alone.  workspace (if a weight's gradient is wanted): 256-byte aligned,
+ * contents free.
+ */
+esp_status esp_kv_norm_rotate(const esp_kv_rope *rope, int32_t type, int64_t tokens, int32_t head_dim, int32_t q_heads,
+                              int32_t k_heads, esp_kv_view q, esp_kv_view k, const void *q_weight, const void *k_weight,
+                              int32_t weight_type, const int32_t *positions, float eps, esp_kv_view q_out,
+                              esp_kv_view k_out, void *stream);
+esp_status esp_kv_norm_rotate_workspace(int64_t tokens, int32_t head_dim, int32_t q_heads, int32_t k_heads, size_t *bytes);
+esp_status esp_kv_norm_rotate_backward(const esp_kv_rope *rope, int32_t type, int64_t tokens, int32_t head_dim, int32_t q_heads,
+                                       int32_t k_heads, esp_kv_view q, esp_kv_view k, const void *q_weight, const void *k_weight,
+                                       int32_t weight_type, const int32_t *positions, float eps, esp_kv_view q_grad,
+                                       esp_kv_view k_grad, esp_kv_view dq, esp_kv_view dk, void *dq_weight, void *dk_weight,
+                                       void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Beam search's selection: for each of `groups` requests the `width` (1 to 64)
+ * largest of
+ *   scores[beam] + logits[beam][token] - ln sum exp logits[beam]
+ * over its beams (1 to 1024) and the vocabulary, the largest first, equal ones by
+ * beam and token.  logits [groups][beams][vocab], the last dimension contiguous,
+ * strides in elements; -inf: the token is not to be had.  The sums over a row are
+ * float32 within a lane, binary64 beyond; what is compared, and scores_out before
+ * its rounding, is binary64, one beam's tokens by their logits alone.  Beams whose
+ * score is not finite, and beams with a NaN or +inf among their logits, have no
+ * candidates.  ended (uint8 [groups][beams], NULL: none): such a beam goes on as it
+ * is, with token `pad` and its own score.  scores_out, parents and tokens are
+ * [groups][width]: the new score, the number group * beams + beam of the sequence
+ * that goes on (for esp_kv_reorder), its token; -inf, -1 and -1 where there are
+ * fewer candidates.  workspace: 256-byte aligned, contents free.
+ */
+esp_status esp_kv_select_beams_workspace(int32_t groups, int32_t beams, int32_t vocab, int32_t width, size_t *bytes);
+esp_status esp_kv_select_beams(int32_t type, int32_t groups, int32_t beams, int32_t vocab, int32_t width, const void *logits,
+                               int64_t group_stride, int64_t beam_stride, const float *scores, const uint8_t *ended,
+                               int32_t pad, float *scores_out, int32_t *parents, int32_t *tokens, void *workspace,
+                               size_t workspace_bytes, void *stream);
+
+/*
  * Writes new tokens into the cache.  Row b has the tokens
  * [offsets[b], offsets[b+1]) of k and v (type bf16 or fp16), which are the
  * last ones of sequence seqs[b] (NULL: b): its length has already grown

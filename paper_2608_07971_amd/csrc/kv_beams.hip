@@ -1,0 +1,346 @@
+// Beam search's selection: of every request the `width` largest of
+//   score[beam] + x[beam][token] - ln sum exp x[beam]
+// over its beams and the vocabulary, ties to the lower beam, then the lower token.
+#include "kv_internal.hpp"
+
+namespace esp_kv {
+
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kMostWidth = 64;              // a wavefront holds the best so far, one a lane
+constexpr int kEach = 8;                    // logits a lane takes at a time
+constexpr int kBatch = 64 * kEach, kFlight = 4;
+constexpr float kLog2e = 1.4426950408889634f;
+
+struct BeamArgs {
+    const void *logits;
+    int64_t group_stride, beam_stride;
+    const float *scores;
+    const uint8_t *ended;
+    int32_t groups, beams, vocab, width, pad, splits, span;      // span: tokens of a split
+    uint64_t *keys;                         // [row][split][width]: the best of each
+    double *sums;                           // [row][split]
+    float *tops;
+    float *out;
+    int32_t *parents, *tokens;
+};
+
+// A number's bits in an order that integers have; -0 as 0.
+__device__ __forceinline__ uint32_t ordered(float x) {
+    const uint32_t u = __float_as_uint(x + 0.0f);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float number(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u); }
+// Larger is better: the logit, then the lower token.
+__device__ __forceinline__ uint64_t key_of(float x, uint32_t token) { return uint64_t(ordered(x)) << 32 | ~token; }
+
+struct One {                                // a key of 64 bits
+    uint64_t k;
+    __device__ __forceinline__ bool operator>(const One &o) const { return k > o.k; }
+};
+struct Two {                                // the sum in binary64, then the lower place
+    uint64_t k, l;
+    __device__ __forceinline__ bool operator>(const Two &o) const { return k > o.k || (k == o.k && l > o.l); }
+};
+__device__ __forceinline__ One from_lane(One a, int lane) { return {uint64_t(__shfl(int64_t(a.k), lane))}; }
+__device__ __forceinline__ Two from_lane(Two a, int lane) { return {uint64_t(__shfl(int64_t(a.k), lane)), uint64_t(__shfl(int64_t(a.l), lane))}; }
+
+// Keys of the lanes from the largest on, by a bitonic network.
+template <typename K> __device__ __forceinline__ K exchange(K mine, int lane, int with, bool larger) {
+    const K other = from_lane(mine, lane ^ with);
+    return (other > mine) == larger ? other : mine;
+}
+template <typename K> __device__ __forceinline__ K sorted(K mine, int lane) {
+#pragma unroll
+    for (int n = 2; n <= 64; n <<= 1)
+#pragma unroll
+        for (int j = n / 2; j; j >>= 1) mine = exchange(mine, lane, j, ((lane & j) == 0) == ((lane & n) == 0));
+    return mine;
+}
+// The 64 largest of two sorted sets.
+template <typename K> __device__ __forceinline__ K merged(K best, K more, int lane) {
+    more = from_lane(more, 63 - lane);
+    best = more > best ? more : best;
+#pragma unroll
+    for (int j = 32; j; j >>= 1) best = exchange(best, lane, j, (lane & j) == 0);
+    return best;
+}
+
+__device__ __forceinline__ void wave_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// The best keys that a wavefront has seen.  What passes the `width`-th of them
+// waits in LDS until there are 64 to be sorted in.
+template <typename K> struct Best {
+    K best, least;                          // least: the width-th
+    K *queue;                               // [128]
+    int lane, width, waiting;
+    __device__ __forceinline__ void start(K first, K *q, int w) {
+        lane = threadIdx.x & 63;
+        queue = q;
+        width = w;
+        waiting = 0;
+        best = sorted(first, lane);
+        least = from_lane(best, width - 1);
+    }
+    __device__ __forceinline__ void join(K more) {
+        best = merged(best, sorted(more, lane), lane);
+        least = from_lane(best, width - 1);
+    }
+    __device__ __forceinline__ void offer(K k, bool there) {
+        there = there && k > least;
+        const uint64_t who = __ballot(there);
+        if (!who) return;
+        if (there) queue[waiting + __builtin_amdgcn_mbcnt_hi(uint32_t(who >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(who), 0))] = k;
+        waiting += __popcll(who);
+        if (waiting < 64) return;
+        wave_fence();
+        const K now = queue[lane], rest = queue[64 + lane];
+        wave_fence();
+        queue[lane] = rest;
+        waiting -= 64;
+        join(now);
+    }
+    __device__ __forceinline__ void finish() {
+        wave_fence();
+        if (waiting) join(lane < waiting ? queue[lane] : K{});
+    }
+};
+
+// Running sum of exp(x - top).
+struct Sum {
+    float top, sum;
+    __device__ __forceinline__ static float off(float top) { return top == -INFINITY ? 0.0f : top; }
+    template <int N> __device__ __forceinline__ void add(const float (&x)[N], float most) {
+        const float to = fmaxf(top, most), by = off(to);
+        float s = sum * __builtin_amdgcn_exp2f((top - by) * kLog2e);
+#pragma unroll
+        for (int j = 0; j < N; j++) s += __builtin_amdgcn_exp2f((x[j] - by) * kLog2e);
+        top = to;
+        sum = s;
+    }
+};
+
+template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) Eight {
+    T x[kEach];
+};
+
+// A workgroup a split of a beam's vocabulary.
+template <typename T> __global__ __launch_bounds__(kThreads) void k_beam_rows(BeamArgs a) {
+    __shared__ One lds[kWaves][128];
+    __shared__ float tops[kWaves];
+    __shared__ double sums[kWaves];
+    const int row = blockIdx.x / a.splits, split = blockIdx.x - row * a.splits;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const float score = a.scores[row];
+    if (!(fabsf(score) < INFINITY) || (a.ended && a.ended[row])) return;        // k_beam_join does not ask for it
+    const int group = row / a.beams;
+    const T *x = static_cast<const T *>(a.logits) + group * a.group_stride + (row - group * a.beams) * a.beam_stride;
+    const int64_t from = int64_t(split) * a.span, to = min(int64_t(a.vocab), from + a.span);
+
+    Best<One> best;
+    Sum sum{-INFINITY, 0.0f};
+    bool first = true;
+    for (int64_t at = from + wave * kBatch; at < to; at += kWaves * kBatch * kFlight) {
+        float v[kFlight][kEach];
+#pragma unroll
+        for (int f = 0; f < kFlight; f++) {
+            const int64_t i = at + f * (kWaves * kBatch) + lane * kEach;
+            if (i + kEach <= to) {
+                const Eight<T> e = *reinterpret_cast<const Eight<T> *>(x + i);
+#pragma unroll
+                for (int j = 0; j < kEach; j++) v[f][j] = float(e.x[j]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < kEach; j++) v[f][j] = i + j < to ? float(x[i + j]) : -INFINITY;
+            }
+        }
+#pragma unroll
+        for (int f = 0; f < kFlight; f++) {
+            const uint32_t i = uint32_t(at + f * (kWaves * kBatch) + lane * kEach);
+            float most = v[f][0];
+#pragma unroll
+            for (int j = 1; j < kEach; j++) most = fmaxf(most, v[f][j]);
+            sum.add(v[f], most);
+            uint64_t own = 0;
+            if (first) {                    // starts with each lane's largest
+#pragma unroll
+                for (int j = 0; j < kEach; j++) own = max(own, key_of(v[f][j], i + j));
+                best.start(One{own}, lds[wave], a.width);
+            }
+            if (first || __any(most > number(uint32_t(best.least.k >> 32)))) {
+#pragma unroll
+                for (int j = 0; j < kEach; j++) {
+                    const One k{key_of(v[f][j], i + j)};
+                    best.offer(k, k.k != own);
+                }
+            }
+            first = false;
+        }
+    }
+    if (first) best.start(One{0}, lds[wave], a.width);           // nothing for this wavefront
+    best.finish();
+    // over the wavefront, then over the workgroup, in binary64
+    float top = sum.top;
+#pragma unroll
+    for (int m = 32; m; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
+    double total = double(sum.sum) * double(__builtin_amdgcn_exp2f((sum.top - Sum::off(top)) * kLog2e));
+#pragma unroll
+    for (int m = 32; m; m >>= 1) total += __shfl_xor(total, m);
+    wave_fence();
+    lds[wave][lane] = best.best;
+    if (lane == 0) {
+        tops[wave] = top;
+        sums[wave] = total;
+    }
+    __syncthreads();
+    if (wave) return;
+    One all = best.best;
+#pragma unroll
+    for (int w = 1; w < kWaves; w++) all = merged(all, lds[w][lane], lane);
+    if (lane < a.width) a.keys[int64_t(blockIdx.x) * a.width + lane] = all.k;
+    if (lane == 0) {
+#pragma unroll
+        for (int w = 1; w < kWaves; w++) top = fmaxf(top, tops[w]);
+        total = 0.0;
+#pragma unroll
+        for (int w = 0; w < kWaves; w++) total += sums[w] * double(__builtin_amdgcn_exp2f((tops[w] - Sum::off(top)) * kLog2e));
+        a.tops[blockIdx.x] = top;
+        a.sums[blockIdx.x] = total;
+    }
+}
+
+__device__ __forceinline__ uint64_t ordered(double x) {
+    const uint64_t u = uint64_t(__double_as_longlong(x + 0.0));
+    return u >> 63 ? ~u : u | uint64_t(1) << 63;
+}
+__device__ __forceinline__ double number(uint64_t u) { return __longlong_as_double(int64_t(u >> 63 ? u & ~(uint64_t(1) << 63) : ~u)); }
+
+// A wavefront a request: beams' sums over their splits, then the best of what they left.
+__global__ __launch_bounds__(64) void k_beam_join(BeamArgs a) {
+    __shared__ Two queue[128];
+    extern __shared__ double lse[];         // [beams]; NaN: no candidates
+    const int group = blockIdx.x, lane = threadIdx.x;
+    for (int b = lane; b < a.beams; b += 64) {
+        const int row = group * a.beams + b;
+        double l = NAN;
+        if (a.ended && a.ended[row]) {
+            l = 0.0;
+        } else if (fabsf(a.scores[row]) < INFINITY) {
+            float top = -INFINITY;
+            for (int i = 0; i < a.splits; i++) top = fmaxf(top, a.tops[int64_t(row) * a.splits + i]);
+            double sum = 0.0;
+            for (int i = 0; i < a.splits; i++) {
+                const int64_t at = int64_t(row) * a.splits + i;
+                sum += a.sums[at] * exp2((double(a.tops[at]) - Sum::off(top)) * 1.4426950408889634074);
+            }
+            l = double(top) + log(sum);
+        }
+        lse[b] = l;
+    }
+    __syncthreads();
+    // the lists' first ones before their second
+    const int lists = a.beams * a.splits;
+    const int64_t all = int64_t(lists) * a.width;
+    Best<Two> best;
+    for (int64_t i0 = 0; i0 < all; i0 += 64) {
+        Two k{0, 0};
+        if (i0 + lane < all) {
+            const int rank = int((i0 + lane) / lists), list = int(i0 + lane - int64_t(rank) * lists), beam = list / a.splits;
+            const int row = group * a.beams + beam;
+            const double s = double(a.scores[row]);
+            double total = NAN;
+            uint32_t token = 0;
+            if (a.ended && a.ended[row]) {
+                token = uint32_t(a.pad);
+                if (rank == 0 && list == beam * a.splits) total = s;
+            } else if (fabs(s) < INFINITY) {
+                const uint64_t held = a.keys[(int64_t(row) * a.splits + (list - beam * a.splits)) * a.width + rank];
+                token = ~uint32_t(held);
+                if (held) total = s + (double(number(uint32_t(held >> 32))) - lse[beam]);
+            }
+            if (fabs(total) < INFINITY) k = {ordered(total), ~(uint64_t(beam) << 32 | token)};
+        }
+        if (i0 == 0) best.start(k, queue, a.width);
+        else best.offer(k, k.k != 0);
+    }
+    best.finish();
+    if (lane < a.width) {
+        const bool there = best.best.k != 0;
+        const uint64_t place = ~best.best.l;
+        const int64_t at = int64_t(group) * a.width + lane;
+        a.out[at] = there ? float(number(best.best.k)) : -INFINITY;
+        a.parents[at] = there ? group * a.beams + int(place >> 32) : -1;
+        a.tokens[at] = there ? int(uint32_t(place)) : -1;
+    }
+}
+
+}  // namespace esp_kv
+
+using namespace esp_kv;
+
+namespace {
+
+constexpr int kMostBeams = 1024;
+constexpr int64_t kMostRows = 1 << 23;      // a launch's threads are numbered in 32 bits
+
+esp_status check(int32_t groups, int32_t beams, int32_t vocab, int32_t width) {
+    if (groups < 0 || beams < 1 || beams > kMostBeams || vocab < 1 || width < 1 || width > kMostWidth) return ESP_ERR_SHAPE;
+    return int64_t(groups) * beams > kMostRows ? ESP_ERR_SHAPE : ESP_OK;
+}
+
+// Splits of a beam's vocabulary: enough workgroups for the GPU, none of less than a turn.
+void lay_out(BeamArgs &a) {
+    const int64_t rows = int64_t(a.groups) * a.beams, turn = kWaves * kBatch;
+    const int64_t most = (a.vocab + turn - 1) / turn;
+    int64_t splits = rows ? 1024 / rows : 1;
+    splits = splits < 1 ? 1 : splits > 16 ? 16 : splits;
+    splits = splits > most ? most : splits;
+    a.span = int32_t(((a.vocab + splits - 1) / splits + turn - 1) / turn * turn);
+    a.splits = int32_t((int64_t(a.vocab) + a.span - 1) / a.span);
+}
+size_t bytes_of(const BeamArgs &a) {
+    const size_t n = size_t(a.groups) * a.beams * a.splits;
+    return n * (a.width * sizeof(uint64_t) + sizeof(double) + sizeof(float));
+}
+
+}  // namespace
+
+extern "C" esp_status esp_kv_select_beams_workspace(int32_t groups, int32_t beams, int32_t vocab, int32_t width, size_t *bytes) {
+    if (!bytes) return ESP_ERR_INVALID_ARG;
+    if (esp_status e = check(groups, beams, vocab, width)) return e;
+    BeamArgs a{};
+    a.groups = groups;
+    a.beams = beams;
+    a.vocab = vocab;
+    a.width = width;
+    lay_out(a);
+    *bytes = bytes_of(a);
+    return ESP_OK;
+}
+
+extern "C" esp_status esp_kv_select_beams(int32_t type, int32_t groups, int32_t beams, int32_t vocab, int32_t width, const void *logits,
+                                          int64_t group_stride, int64_t beam_stride, const float *scores, const uint8_t *ended,
+                                          int32_t pad, float *scores_out, int32_t *parents, int32_t *tokens, void *workspace,
+                                          size_t workspace_bytes, void *stream) {
+    if (type < ESP_KV_BF16 || type > ESP_KV_FP32) return ESP_ERR_INVALID_ARG;
+    if (esp_status e = check(groups, beams, vocab, width)) return e;
+    if (ended && (pad < 0 || pad >= vocab)) return ESP_ERR_INVALID_ARG;
+    if (groups == 0) return ESP_OK;
+    if (!logits || !scores || !scores_out || !parents || !tokens) return ESP_ERR_INVALID_ARG;
+    BeamArgs a{logits, group_stride, beam_stride, scores, ended, groups, beams, vocab, width, pad, 0, 0, nullptr, nullptr, nullptr, scores_out, parents, tokens};
+    lay_out(a);
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < bytes_of(a)) return ESP_ERR_WORKSPACE;
+    const size_t n = size_t(groups) * beams * a.splits;
+    a.keys = static_cast<uint64_t *>(workspace);
+    a.sums = reinterpret_cast<double *>(a.keys + n * width);
+    a.tops = reinterpret_cast<float *>(a.sums + n);
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    const unsigned blocks = unsigned(n);
+    if (type == ESP_KV_BF16) k_beam_rows<__bf16><<<blocks, kThreads, 0, s>>>(a);
+    else if (type == ESP_KV_FP16) k_beam_rows<_Float16><<<blocks, kThreads, 0, s>>>(a);
+    else k_beam_rows<float><<<blocks, kThreads, 0, s>>>(a);
+    k_beam_join<<<unsigned(groups), 64, size_t(beams) * sizeof(double), s>>>(a);
+    return launched();
+}

@@ -50,6 +50,11 @@ _P, _I, _L, _V, _Z = C.c_void_p, C.c_int32, C.c_int64, esp_kv_view, C.POINTER(C.
 _SIGS = {
     "esp_kv_rope_turns": [_I, C.c_double, _I, C.c_double, _I, _P, C.POINTER(C.c_float)],
     "esp_kv_rotate": [_P, _I, _L, _I, _I, _V, _P, _I, _V, _P],
+    "esp_kv_norm_rotate": [_P, _I, _L, _I, _I, _I, _V, _V, _P, _P, _I, _P, C.c_float, _V, _V, _P],
+    "esp_kv_norm_rotate_workspace": [_L, _I, _I, _I, _Z],
+    "esp_kv_norm_rotate_backward": [_P, _I, _L, _I, _I, _I, _V, _V, _P, _P, _I, _P, C.c_float, _V, _V, _V, _V, _P, _P, _P, C.c_size_t, _P],
+    "esp_kv_select_beams_workspace": [_I, _I, _I, _I, _Z],
+    "esp_kv_select_beams": [_I, _I, _I, _I, _I, _P, _L, _L, _P, _P, _I, _P, _P, _P, _P, C.c_size_t, _P],
     "esp_kv_append": [_P, _I, _I, _I, _L, _P, _P, _V, _V, _P, _I, _V, _V, _P],
     "esp_kv_gather": [_P, _I, _I, _I, _L, _P, _P, _P, _P, _P, _P],
     "esp_kv_attend_workspace": [_P, _I, _L, _I, _I, _I, _Z],
@@ -96,7 +101,9 @@ def _on_stream(call):
     given is noted at the tensors that it is to read, so that the allocator keeps those that the caller drops."""
     @functools.wraps(call)
     def entry(first, *args, stream=None, **more):
-        index = first.index
+        index = first.device.index if isinstance(first, torch.Tensor) else first.index
+        if index is None and isinstance(first, torch.Tensor):
+            raise ValueError("a tensor on the GPU expected: there is no CPU path")
         if stream is None and _current_device() == index:
             return call(first, *args, s=_raw_stream(index), **more)
         if stream is None:
@@ -192,15 +199,14 @@ class _NoGradient(torch.autograd.Function):
     """A result that depends on tensors that require gradients, through what has none: backward() says so."""
 
     @staticmethod
-    def forward(ctx, what, source, result):
-        ctx.what = what
+    def forward(ctx, what, source, result, why="the cache holds its tokens rounded to 8 bits"):
+        ctx.what, ctx.why = what, why
         ctx.mark_dirty(result)
         return result
 
     @staticmethod
     def backward(ctx, grad):
-        raise RuntimeError(f"{ctx.what} has no gradient: the cache holds its tokens rounded to 8 bits. Detach its inputs, or "
-                           "call it under torch.no_grad()")
+        raise RuntimeError(f"{ctx.what} has no gradient: {ctx.why}. Detach its inputs, or call it under torch.no_grad()")
 
 
 def _turn(rope, x, positions, inverse, out, s: int) -> torch.Tensor:
@@ -217,6 +223,139 @@ def _turn(rope, x, positions, inverse, out, s: int) -> torch.Tensor:
     _check(lib().esp_kv_rotate(rope.ptr, kind, T, H, D, _view(x, T, H, D, "x", x.device), _ints(positions, T, "positions", x.device),
                                1 if inverse else 0, _view(out, T, H, D, "out", x.device), s), "esp_kv_rotate")
     return out
+
+
+def _accumulators(tensors, capture):
+    """What adds up the gradients of the leaves among tensors, and whether another graph than this capture's holds one of
+    these: autograd would then go to the stream of that graph in a captured backward pass, which ends the process."""
+    nodes, older = [], False
+    for x in tensors:
+        if x is not None and x.requires_grad and x.is_leaf:
+            probe, node = object(), torch.autograd.graph.get_gradient_edge(x).node
+            node.metadata["esp_probe"] = probe
+            del node                            # goes unless a graph holds it
+            node = torch.autograd.graph.get_gradient_edge(x).node
+            if node.metadata.pop("esp_probe", None) is not probe:
+                node.metadata["esp_capture"] = capture
+            elif node.metadata.get("esp_capture") != capture:
+                older = True
+            nodes.append(node)
+    return nodes, older
+
+
+def _weights(q_weight, k_weight, x, dim: int):
+    """Kind and addresses of the norms' weights."""
+    given = [w for w in (q_weight, k_weight) if w is not None]
+    for w in given:
+        if w.shape != (dim,) or w.device != x.device or not w.is_contiguous() or w.dtype not in (x.dtype, torch.float32) or w.dtype != given[0].dtype:
+            raise ValueError(f"weights: contiguous [{dim}] on {x.device} expected, both of the type of q and k or both float32")
+    kind = _TYPES[given[0].dtype if given else x.dtype]
+    return kind, *(None if w is None else w.data_ptr() for w in (q_weight, k_weight))
+
+
+@_on_stream
+def norm_rotate(rope: Rope, q: torch.Tensor, k: torch.Tensor, q_weight, k_weight, positions: torch.Tensor, eps: float = 1e-6, *, s: int):
+    """(q, k) [tokens, heads, head_dim], each head divided by the root of its mean square (plus eps), times its weight
+    [head_dim] (the type of q and k or float32; None: ones), turned by positions (int32 [tokens]).  Has its gradient, of
+    the weights too.  Either may have no heads.  stream: the current one, unless given."""
+    if torch.is_grad_enabled() and any(x is not None and x.requires_grad for x in (q, k, q_weight, k_weight)):
+        capture = _capture(s)
+        nodes, older = ((), False) if capture is None else _accumulators((q, k, q_weight, k_weight), capture)
+        result = _Normed.apply(q, k, q_weight, k_weight, rope, positions, eps, older, s)
+        del nodes                               # until here: the graph holds them now
+        return result
+    return _norm(rope, q, k, q_weight, k_weight, positions, eps, s)
+
+
+def _sides(rope, q, k):
+    kind = _TYPES.get(q.dtype)
+    if kind is None or k.dtype != q.dtype or q.dim() != 3 or k.dim() != 3 or q.device != rope.device:
+        raise ValueError(f"q and k: bfloat16, float16 or float32 tensors [tokens, heads, head_dim] on {rope.device} expected, of one type")
+    (T, Hq, D), Hk = q.shape, k.shape[1]
+    if D != rope.head_dim:
+        raise ValueError(f"q and k: heads of {rope.head_dim} elements expected")
+    return kind, T, D, Hq, Hk, _view(q, T, Hq, D, "q", q.device), _view(k, T, Hk, D, "k", q.device)
+
+
+def _like(x):
+    return torch.empty_like(x) if x.is_contiguous() else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+
+
+def _norm(rope, q, k, q_weight, k_weight, positions, eps, s: int):
+    kind, T, D, Hq, Hk, vq, vk = _sides(rope, q, k)
+    weight, wq, wk = _weights(q_weight, k_weight, q, D)
+    oq, ok = _like(q), _like(k)
+    _check(lib().esp_kv_norm_rotate(rope.ptr, kind, T, D, Hq, Hk, vq, vk, wq, wk, weight, _ints(positions, T, "positions", q.device), eps,
+                                    esp_kv_view(oq.data_ptr(), Hq * D, D), esp_kv_view(ok.data_ptr(), Hk * D, D), s), "esp_kv_norm_rotate")
+    return oq, ok
+
+
+class _Normed(torch.autograd.Function):
+    """norm_rotate with its gradient."""
+
+    @staticmethod
+    def forward(ctx, q, k, q_weight, k_weight, rope, positions, eps, older, s):
+        ctx.rope, ctx.eps, ctx.older = rope, eps, older
+        ctx.save_for_backward(q, k, q_weight, k_weight, positions)
+        return _norm(rope, q, k, q_weight, k_weight, positions, eps, s)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, gq, gk):
+        if ctx.older:
+            raise RuntimeError("norm_rotate: a captured backward pass of leaves that a graph from before the capture holds, too. Drop "
+                               "that graph before the capture")
+        return _norm_back(ctx.rope, *ctx.saved_tensors, ctx.eps, gq, gk, ctx.needs_input_grad[2:4])
+
+
+@_on_stream
+def _norm_back(rope, q, k, q_weight, k_weight, positions, eps, gq, gk, wanted, *, s: int):
+    kind, T, D, Hq, Hk, vq, vk = _sides(rope, q, k)
+    weight, wq, wk = _weights(q_weight, k_weight, q, D)
+    gq, gk = (g if g.stride(-1) == 1 or D == 1 else g.contiguous() for g in (gq, gk))
+    dq, dk = _like(q), _like(k)
+    dwq, dwk = (torch.empty_like(w) if w is not None and want else None for w, want in zip((q_weight, k_weight), wanted))
+    work, size = None, 0
+    if dwq is not None or dwk is not None:
+        n = C.c_size_t(0)
+        _check(lib().esp_kv_norm_rotate_workspace(T, D, Hq, Hk, C.byref(n)), "esp_kv_norm_rotate_workspace")
+        work, size = torch.empty(n.value, dtype=torch.uint8, device=q.device), n.value
+    _check(lib().esp_kv_norm_rotate_backward(
+        rope.ptr, kind, T, D, Hq, Hk, vq, vk, wq, wk, weight, _ints(positions, T, "positions", q.device), eps,
+        _view(gq, T, Hq, D, "q", q.device), _view(gk, T, Hk, D, "k", q.device), esp_kv_view(dq.data_ptr(), Hq * D, D),
+        esp_kv_view(dk.data_ptr(), Hk * D, D), None if dwq is None else dwq.data_ptr(), None if dwk is None else dwk.data_ptr(),
+        None if work is None else work.data_ptr(), size, s), "esp_kv_norm_rotate_backward")
+    return dq, dk, dwq, dwk, None, None, None, None, None
+
+
+@_on_stream
+def select_beams(logits: torch.Tensor, scores: torch.Tensor, width: int, ended: Optional[torch.Tensor] = None, pad: int = 0, *, s: int):
+    """(scores, parents, tokens) [groups, width]: the best continuations of the beams of each request by score plus log
+    probability, from logits [groups, beams, vocab] and scores (float32 [groups, beams]), the best first, equal ones by
+    beam and token.  parents number the sequences group * beams + beam, as PagedCache.reorder takes them; -1 (and a score
+    of -inf) where there are fewer.  ended (bool [groups, beams]): beams that go on as they are, with token pad.  No
+    gradient: backward() raises.  stream: the current one, unless given."""
+    kind = _TYPES.get(logits.dtype)
+    if kind is None or logits.dim() != 3 or (logits.shape[2] > 1 and logits.stride(2) != 1):
+        raise ValueError("logits: bfloat16, float16 or float32 [groups, beams, vocab] expected, the last dimension contiguous")
+    (G, B, V), dev = logits.shape, logits.device
+    if scores.shape != (G, B) or scores.dtype != torch.float32 or scores.device != dev or not scores.is_contiguous():
+        raise ValueError(f"scores: contiguous float32 [{G}, {B}] on {dev} expected")
+    if ended is not None and (ended.shape != (G, B) or ended.dtype != torch.bool or ended.device != dev or not ended.is_contiguous()):
+        raise ValueError(f"ended: contiguous bool [{G}, {B}] on {dev} expected")
+    n = C.c_size_t(0)
+    _check(lib().esp_kv_select_beams_workspace(G, B, V, width, C.byref(n)), "esp_kv_select_beams_workspace")
+    out = torch.empty((G, width), dtype=torch.float32, device=dev)
+    both = torch.empty((2, G, width), dtype=torch.int32, device=dev)
+    parents, tokens = both[0], both[1]
+    work = torch.empty(max(n.value, 1), dtype=torch.uint8, device=dev)
+    _check(lib().esp_kv_select_beams(kind, G, B, V, width, logits.data_ptr(), logits.stride(0), logits.stride(1), scores.data_ptr(),
+                                     None if ended is None else ended.data_ptr(), pad, out.data_ptr(), parents.data_ptr(),
+                                     tokens.data_ptr(), work.data_ptr(), n.value, s), "esp_kv_select_beams")
+    source = next((x for x in (logits, scores) if x.requires_grad), None) if torch.is_grad_enabled() else None
+    if source is not None:
+        out = _NoGradient.apply("select_beams", source, out, "it selects")
+    return out, parents, tokens
 
 
 class PagedCache:

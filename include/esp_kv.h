@@ -5,8 +5,11 @@
  * The price loop gives an offline-inference job a configuration: a number of
  * sequences and a number of bytes of GPU memory for its cache.  The calls
  * below are that cache: pages that grow, shrink, fork and move to a smaller
- * budget (resize, fork, compact), writing new tokens with rotary positions in
- * 8 bits (append), and attention over what is held (attend).
+ * budget (resize, fork, reorder, compact), writing new tokens with rotary positions
+ * in 8 bits (append), attention over what is held (attend), and the weight that
+ * tokens get from it, by which a sequence is cut (weigh, evict).  Beside it stand
+ * what such a job does to queries, keys and logits: norms with the rotation
+ * (norm_rotate, with its gradient) and beam search's selection (select_beams).
  *
  * Layout.  A page holds page_tokens tokens of every layer and key/value head.
  * The pool is page-major, so a pool whose last pages are empty can be cut:
@@ -198,7 +201,23 @@ esp_status esp_kv_attend(const esp_kv_cache *cache, int32_t layer, int32_t type,
                          int32_t window, int32_t max_new, int32_t max_length, esp_kv_view out, float *lse,
                          void *workspace, size_t workspace_bytes, void *stream);
 
-/* Bytes that resize, fork (of n children; as many for any n up to sequences) and compact need; 256-byte aligned, contents free. */
+/*
+ * The attention weight that cached tokens got from the call's queries, added to
+ * what they had: for every row's sequence and key head h
+ *   mass[t] = decay * mass[t] + sum exp(scale * q . k_t - lse[q])
+ * over the row's queries that see token t (esp_kv_attend's rules, arguments and
+ * bounds) and the query heads of h; with the lse that attend left these are its
+ * softmax weights.  The row's own new tokens begin at 0.  mass: float32
+ * [layers][sequences][kv_heads][table_width * page_tokens], contiguous; places from
+ * a sequence's length on, and sequences of rows that have no tokens or are left
+ * out, stay as they were.  A query whose lse is -inf adds nothing.  Sums are float32.
+ */
+esp_status esp_kv_weigh(const esp_kv_cache *cache, int32_t layer, int32_t type, int32_t rows, int64_t tokens,
+                        const int32_t *offsets, const int32_t *seqs, int32_t q_heads, esp_kv_view q, const float *lse,
+                        float scale, int32_t window, float decay, int32_t max_new, int32_t max_length, float *mass,
+                        void *stream);
+
+/* Bytes that resize, fork (of n children; as many for any n up to sequences), reorder and compact need; 256-byte aligned, contents free. */
 esp_status esp_kv_pages_workspace(const esp_kv_cache *cache, int32_t n, size_t *bytes);
 
 /*
@@ -219,6 +238,37 @@ esp_status esp_kv_resize(const esp_kv_cache *cache, const int32_t *lengths, void
  */
 esp_status esp_kv_fork(const esp_kv_cache *cache, int32_t n, const int32_t *parents, const int32_t *children,
                        void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * All sequences at once: sequence i goes on as sequence parents[i] was before
+ * the call (int32 [sequences]; -1: it ends), any of them any number of times, as
+ * esp_kv_select_beams leaves them.  Full pages are shared.  A partly filled last
+ * page stays with the parent if it goes on as itself, else with the first that goes
+ * on as it, and is copied for the others to the lowest pages that are free then, in
+ * order of i.  With a parent that is no sequence (ESP_ERR_INVALID_ARG) or too few
+ * free pages (ESP_ERR_RANGE) nothing changes.
+ */
+esp_status esp_kv_reorder(const esp_kv_cache *cache, const int32_t *parents, void *workspace, size_t workspace_bytes,
+                          void *stream);
+
+/*
+ * Cuts every sequence that is longer than keep[s] (int32 [sequences], >= 0) to
+ * keep[s] tokens.  Each layer and key head chooses its own: the last `recent` (at
+ * most keep[s]), then those of the largest mass (esp_kv_weigh), equal ones by the
+ * lower place, NaN last.  They move together in their order, their masses with them;
+ * masses from keep[s] on, and codes past
+ * the new end in its page, stay as they were.  What attention and positions make of
+ * a token's new place is the caller's: keys stay turned as they were written.  A
+ * block's scale is the largest of the blocks that its tokens come from, and codes of
+ * smaller ones are rounded once more.  A page that other sequences share is left to
+ * them for the lowest free page, in order of sequence and slot; pages past the new
+ * end lose an owner.  With too few free pages (ESP_ERR_RANGE), a negative keep, a
+ * length out of range or a page that is missing (ESP_ERR_SHAPE) nothing changes.
+ * workspace: 256-byte aligned, contents free.
+ */
+esp_status esp_kv_evict_workspace(const esp_kv_cache *cache, size_t *bytes);
+esp_status esp_kv_evict(const esp_kv_cache *cache, const int32_t *keep, int32_t recent, float *mass, void *workspace,
+                        size_t workspace_bytes, void *stream);
 
 /*
  * Empties the pages from `limit` on (limit < 0: from the number of live pages

@@ -1,0 +1,372 @@
+// Eviction by accumulated attention weight: of a sequence that is cut, every
+// layer and key head keeps its own tokens, the last `recent` and those of the
+// largest weight, which move together in their order.
+//   1  entries whose page is shared, and free pages, are marked; what is wrong is noted
+//   2  these entries get pages of their own, pages past the new end go
+//   3  a workgroup a layer, sequence and head finds the least weight that stays, marks
+//      the tokens in a bit mask and moves their weights together
+//   4  a workgroup a layer, sequence, head and side moves the codes
+// A token never moves to a higher place, so both moves go through a row once, in place:
+// what a stretch of new places takes comes from there or from further on.
+#include "kv_pages.hpp"
+
+namespace esp_kv {
+
+struct EvictArgs {
+    Cache c;
+    const int32_t *keep;
+    float *mass;
+    uint64_t *kept;                         // [layer][sequence][head][words]: tokens that stay
+    int32_t recent, words;
+};
+
+__device__ __forceinline__ int pages_of(const Cache &c, int tokens) { return int((uint32_t(tokens) + c.tokens - 1) >> c.shift); }
+
+// Workgroups [0, entries.blocks): entries; the rest: pages.
+__global__ __launch_bounds__(kThreads) void k_evict_mark(Cache c, const int32_t *keep, Work w) {
+    __shared__ int lds[4];
+    const int b = blockIdx.x;
+    if (b >= w.entries.blocks) {
+        mark(w.pages, b - w.entries.blocks, w.page_mask, w.page_sum, lds, [&](int64_t p) { return c.refs[p] == 0; });
+        return;
+    }
+    int bad = 0;
+    mark(w.entries, b, w.need_mask, w.need_sum, lds, [&](int64_t i) {
+        const int seq = int(uint32_t(i) / uint32_t(c.width)), slot = int(uint32_t(i) - uint32_t(seq) * uint32_t(c.width));
+        const int32_t m = c.lengths[seq], k = keep[seq], p = c.table[i];
+        const bool ok = k >= 0 && m >= 0 && m <= int64_t(c.width) << c.shift, cut = ok && m > k;
+        const bool page = p >= 0 && p < c.pages;
+        bad |= !ok || p < -1 || p >= c.pages || (cut && slot < pages_of(c, m) && !page);
+        w.rows[i] = p;
+        if (slot == 0) w.row_lengths[seq] = cut ? m : -1;
+        return cut && slot < pages_of(c, k) && page && c.refs[p] > 1;
+    });
+    bad = block_sum(bad, lds);
+    if (threadIdx.x == 0) w.bad[b] = bad;
+}
+
+__global__ __launch_bounds__(kThreads) void k_evict_take(Cache c, const int32_t *keep, Work w) {
+    __shared__ int lds[4], free_at[kMaxBlocks + 1], need_at[kMaxBlocks + 1];
+    int bad = 0;
+    for (int b = threadIdx.x; b < w.entries.blocks; b += kThreads) bad |= w.bad[b];
+    bad = block_sum(bad, lds);
+    prefix(w.page_sum, w.pages.blocks, free_at, lds);
+    prefix(w.need_sum, w.entries.blocks, need_at, lds);
+    const bool go = !bad && free_at[w.pages.blocks] >= need_at[w.entries.blocks];
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        *w.count = go;
+        if (!go) record(c, bad ? ESP_ERR_SHAPE : ESP_ERR_RANGE);
+    }
+    if (!go) return;
+    ranked(w.entries, blockIdx.x, w.need_mask, need_at[blockIdx.x], w.need_mask, 0, [&](int64_t i, bool need, int rank, bool, int) {
+        const int seq = int(uint32_t(i) / uint32_t(c.width)), slot = int(uint32_t(i) - uint32_t(seq) * uint32_t(c.width));
+        if (w.row_lengths[seq] < 0) return;
+        const int32_t p = w.rows[i];
+        if (need) {
+            const int to = select(w, [&](int b) { return free_at[b]; }, 0, rank);
+            if (to >= 0) {
+                c.refs[to] = 1;
+                c.table[i] = to;
+                atomicAdd(c.refs + p, -1);
+            }
+        } else if (slot >= pages_of(c, keep[seq]) && p >= 0) {
+            c.table[i] = -1;
+            atomicAdd(c.refs + p, -1);
+        }
+        if (slot == 0) c.lengths[seq] = keep[seq];
+    });
+}
+
+// A weight's place in the order of all: NaN below everything, -0 as 0.
+__device__ __forceinline__ uint32_t order_of(float x) {
+    const uint32_t u = __float_as_uint(x + 0.0f);
+    return x != x ? 0 : u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+struct Place {
+    int layer, seq, head;
+};
+__device__ __forceinline__ Place place_of(const Cache &c, int i) {
+    const int head = i % c.heads, rest = i / c.heads;
+    return {rest / c.sequences, rest % c.sequences, head};
+}
+
+// The want-th largest weight by its bits, eight at a time from the top; then one pass over
+// the tokens in order, equal ones by the lower place.
+__global__ __launch_bounds__(kThreads) void k_evict_select(EvictArgs a, Work w) {
+    __shared__ int counts[256], at[4], ties[4], picked[2];
+    const Cache &c = a.c;
+    const Place p = place_of(c, blockIdx.x);
+    const int length = w.row_lengths[p.seq];
+    if (!*w.count || length < 0) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int keep = a.keep[p.seq], recent = min(a.recent, keep), older = length - recent;
+    float *mass = a.mass + int64_t(blockIdx.x) * (int64_t(c.width) << c.shift);
+    uint64_t *kept = a.kept + int64_t(blockIdx.x) * a.words;
+
+    uint32_t least = ~0u;                   // of those that stay
+    int want = keep - recent;               // and how many equal to it do
+    if (want > 0) {
+        uint32_t known = 0;
+        least = 0;
+        for (int shift = 24; shift >= 0; shift -= 8) {
+            counts[tid] = 0;
+            __syncthreads();
+            for (int t = tid; t < older; t += kThreads) {
+                const uint32_t u = order_of(mass[t]);
+                if ((u & known) == least) atomicAdd(counts + ((u >> shift) & 255), 1);
+            }
+            __syncthreads();
+            if (wave == 0) {                // four digits a lane, from the largest
+                int own[4], sum = 0;
+#pragma unroll
+                for (int k = 0; k < 4; k++) sum += own[k] = counts[255 - 4 * lane - k];
+                int before = sum;
+#pragma unroll
+                for (int m = 1; m < 64; m <<= 1) {
+                    const int v = __shfl_up(before, m);
+                    before += lane >= m ? v : 0;
+                }
+                before -= sum;
+#pragma unroll
+                for (int k = 0; k < 4; k++) {
+                    if (want > before && want <= before + own[k]) {
+                        picked[0] = 255 - 4 * lane - k;
+                        picked[1] = want - before;
+                    }
+                    before += own[k];
+                }
+            }
+            __syncthreads();
+            least |= uint32_t(picked[0]) << shift;
+            known |= 255u << shift;
+            want = picked[1];
+            __syncthreads();
+        }
+    }
+    int to = 0, equal = 0;                  // tokens that stay, and those equal to `least`, so far
+    for (int t0 = 0; t0 < length; t0 += kThreads) {
+        const int t = t0 + tid;
+        const float x = t < length ? mass[t] : 0.0f;
+        const uint32_t u = order_of(x);
+        const bool tie = t < older && u == least;
+        const uint64_t same = __ballot(tie);
+        if (lane == 0) ties[wave] = __popcll(same);
+        __syncthreads();
+        int rank = equal + lanes_below(same);
+        for (int k = 0; k < 4; k++) {
+            rank += k < wave ? ties[k] : 0;
+            equal += ties[k];
+        }
+        const bool stays = t < length && (t >= older || u > least || (tie && rank < want));
+        const uint64_t who = __ballot(stays);
+        if (lane == 0) {
+            at[wave] = __popcll(who);
+            if (t < length) kept[t / 64] = who;
+        }
+        __syncthreads();
+        int place = to + lanes_below(who);
+        for (int k = 0; k < 4; k++) {
+            place += k < wave ? at[k] : 0;
+            to += at[k];
+        }
+        if (stays) mass[place] = x;
+        __syncthreads();
+    }
+}
+
+constexpr int kTurn = 64;                   // tokens moved at a time: whole pages
+constexpr int kStretch = 4096;              // tokens whose mask is read at a time
+
+struct Moved {
+    int64_t from;                           // block of the old page
+    int32_t in_page;
+    float by;                               // the old scale over the new
+};
+
+__device__ __forceinline__ uint32_t code2(float x, float y) { return __builtin_amdgcn_cvt_pk_fp8_f32(x, y, 0, false); }
+__device__ __forceinline__ uint32_t rescaled(uint32_t w, float b0, float b1, float b2, float b3) {
+    const half2 a = codes<false>(w, static_cast<half2 *>(nullptr)), b = codes<true>(w, static_cast<half2 *>(nullptr));
+    return code2(float(a[0]) * b0, float(a[1]) * b1) | code2(float(b[0]) * b2, float(b[1]) * b3) << 16;
+}
+
+template <int Dim, int Page> __global__ __launch_bounds__(kThreads) void k_evict_move(EvictArgs a, Work w) {
+    __shared__ int list[kStretch + kTurn];
+    __shared__ Moved moved[kTurn];
+    const Cache &c = a.c;
+    const int item = blockIdx.x >> 1, values = blockIdx.x & 1;
+    const Place p = place_of(c, item);
+    const int length = w.row_lengths[p.seq];
+    if (!*w.count || length < 0) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const uint64_t *kept = a.kept + int64_t(item) * a.words;
+    const int32_t *old = w.rows + int64_t(p.seq) * c.width, *table = c.table + int64_t(p.seq) * c.width;
+    uint8_t *pool = values ? c.v : c.k;
+
+    // tokens list[from, from + n) to places [done, done + n)
+    auto turn = [&](int from, int n, int done) {
+        if (wave == 0) {
+            const int src = list[from + min(lane, n - 1)];
+            const int32_t page = old[src / Page];
+            const float was = lane < n ? *c.block_scale(page, p.layer, values, p.head) : 0.0f;
+            float now = was;
+#pragma unroll
+            for (int m = Page / 2; m; m >>= 1) now = fmaxf(now, __shfl_xor(now, m));
+            moved[lane] = {c.block(page, p.layer, p.head), src % Page, now > 0.0f ? was / now : 1.0f};
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            if (lane % Page == 0 && lane < n) *c.block_scale(table[(done + lane) / Page], p.layer, values, p.head) = now;
+        }
+        __syncthreads();
+        if (!values) {
+            constexpr int kChunks = Dim / 16, kUnits = kTurn * kChunks / kThreads;
+            uint4v x[kUnits];
+#pragma unroll
+            for (int i = 0; i < kUnits; i++) {
+                const int u = tid + i * kThreads, t = min(u / kChunks, n - 1);
+                x[i] = *reinterpret_cast<const uint4v *>(pool + moved[t].from + moved[t].in_page * Dim + u % kChunks * 16);
+            }
+#pragma unroll
+            for (int i = 0; i < kUnits; i++) {
+                const float by = moved[min((tid + i * kThreads) / kChunks, n - 1)].by;
+                if (by != 1.0f)
+#pragma unroll
+                    for (int k = 0; k < 4; k++) x[i][k] = rescaled(x[i][k], by, by, by, by);
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < kUnits; i++) {
+                const int u = tid + i * kThreads, t = u / kChunks;
+                if (t < n) {
+                    const int at = done + t;
+                    *reinterpret_cast<uint4v *>(pool + c.block(table[at / Page], p.layer, p.head) + at % Page * Dim + u % kChunks * 16) = x[i];
+                }
+            }
+        } else {
+            constexpr int kUnits = kTurn / 16 * Dim / kThreads;  // sixteen tokens of a dimension
+            uint4v x[kUnits];
+#pragma unroll
+            for (int i = 0; i < kUnits; i++) {
+                const int u = tid + i * kThreads, d = u % Dim, t = u / Dim * 16;
+#pragma unroll
+                for (int k = 0; k < 4; k++) {
+                    uint32_t b[4];
+                    float by[4];
+#pragma unroll
+                    for (int j = 0; j < 4; j++) {
+                        const Moved &m = moved[min(t + 4 * k + j, n - 1)];
+                        b[j] = pool[m.from + d * Page + m.in_page];
+                        by[j] = m.by;
+                    }
+                    uint32_t word = b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24;
+                    if (by[0] != 1.0f || by[1] != 1.0f || by[2] != 1.0f || by[3] != 1.0f) word = rescaled(word, by[0], by[1], by[2], by[3]);
+                    x[i][k] = word;
+                }
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < kUnits; i++) {
+                const int u = tid + i * kThreads, d = u % Dim, t = u / Dim * 16;
+                if (t < n) {
+                    const int at = done + t;
+                    uint4v *to = reinterpret_cast<uint4v *>(pool + c.block(table[at / Page], p.layer, p.head) + d * Page + at % Page);
+                    if (t + 16 > n) {       // past the end: as it was
+                        const uint4v was = *to;
+#pragma unroll
+                        for (int k = 0; k < 4; k++) {
+                            const int left = n - t - 4 * k;
+                            const uint32_t own = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
+                            x[i][k] = (x[i][k] & own) | (was[k] & ~own);
+                        }
+                    }
+                    *to = x[i];
+                }
+            }
+        }
+        __syncthreads();
+    };
+
+    int held = 0, done = 0;
+    const int words = (length + 63) / 64, keep = a.keep[p.seq];
+    for (int x0 = 0; x0 < words; x0 += 64) {
+        const uint64_t m = x0 + lane < words ? kept[x0 + lane] : 0;
+        int before = __popcll(m);
+        const int own = before;
+#pragma unroll
+        for (int k = 1; k < 64; k <<= 1) {
+            const int v = __shfl_up(before, k);
+            before += lane >= k ? v : 0;
+        }
+        const int all = __shfl(before, 63);
+        before -= own;
+        for (int x = wave; x < 64; x += 4) {
+            const uint64_t n = __shfl(m, x);
+            const int at = held + __shfl(before, x) + lanes_below(n);
+            if (bit_of(n, lane)) list[at] = (x0 + x) * 64 + lane;
+        }
+        held += all;
+        __syncthreads();
+        int from = 0;
+        for (; held - from >= kTurn && done + kTurn <= keep; from += kTurn, done += kTurn) turn(from, kTurn, done);
+        if (x0 + 64 >= words || held - from >= keep - done) {    // keep tokens, whatever the masses did meanwhile
+            if (min(held - from, keep - done) > 0) turn(from, min(held - from, keep - done), done);
+            return;
+        }
+        const int rest = held - from, next = tid < rest ? list[from + tid] : 0;
+        __syncthreads();
+        if (tid < rest) list[tid] = next;
+        __syncthreads();
+        held = rest;
+    }
+}
+
+}  // namespace esp_kv
+
+using namespace esp_kv;
+
+namespace {
+
+constexpr int64_t kMostBlocks = ((int64_t(1) << 32) - kThreads) / kThreads;    // a launch's threads are numbered in 32 bits
+
+int64_t words_of(const esp_kv_cache *c) { return (int64_t(c->table_width) * c->page_tokens + 63) / 64; }
+int64_t items_of(const esp_kv_cache *c) { return int64_t(c->layers) * c->kv_heads * c->sequences; }
+
+template <int Dim> void move(const EvictArgs &a, const Work &w, unsigned blocks, hipStream_t s) {
+    switch (a.c.tokens) {
+    case 16: k_evict_move<Dim, 16><<<blocks, kThreads, 0, s>>>(a, w); break;
+    case 32: k_evict_move<Dim, 32><<<blocks, kThreads, 0, s>>>(a, w); break;
+    default: k_evict_move<Dim, 64><<<blocks, kThreads, 0, s>>>(a, w); break;
+    }
+}
+
+}  // namespace
+
+extern "C" esp_status esp_kv_evict_workspace(const esp_kv_cache *cache, size_t *bytes) {
+    if (esp_status e = check_cache(cache)) return e;
+    if (!bytes) return ESP_ERR_INVALID_ARG;
+    if (2 * items_of(cache) > kMostBlocks) return ESP_ERR_SHAPE;
+    Work w;
+    *bytes = lay_out(cache, nullptr, w) + size_t(items_of(cache)) * words_of(cache) * sizeof(uint64_t);
+    return ESP_OK;
+}
+
+extern "C" esp_status esp_kv_evict(const esp_kv_cache *cache, const int32_t *keep, int32_t recent, float *mass, void *workspace,
+                                   size_t workspace_bytes, void *stream) {
+    size_t need = 0;
+    if (esp_status e = esp_kv_evict_workspace(cache, &need)) return e;
+    if (!keep || !mass) return ESP_ERR_INVALID_ARG;
+    if (recent < 0) return ESP_ERR_SHAPE;
+    Work w;
+    if (esp_status e = work_of(cache, workspace, workspace_bytes, w)) return e;
+    if (workspace_bytes < need) return ESP_ERR_WORKSPACE;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    const Cache c = cache_of(cache);
+    const size_t before = need - size_t(items_of(cache)) * words_of(cache) * sizeof(uint64_t);
+    const EvictArgs a{c, keep, mass, reinterpret_cast<uint64_t *>(static_cast<char *>(workspace) + before), recent, int32_t(words_of(cache))};
+    k_evict_mark<<<w.entries.blocks + w.pages.blocks, kThreads, 0, s>>>(c, keep, w);
+    k_evict_take<<<w.entries.blocks, kThreads, 0, s>>>(c, keep, w);
+    const unsigned items = unsigned(items_of(cache));
+    k_evict_select<<<items, kThreads, 0, s>>>(a, w);
+    if (c.dim == 64) move<64>(a, w, 2 * items, s);
+    else move<128>(a, w, 2 * items, s);
+    return launched();
+}

@@ -468,6 +468,7 @@ extern "C" esp_status esp_kv_norm_rotate_backward(const esp_kv_rope *rope, int32
                                                   void *workspace, size_t workspace_bytes, void *stream) {
     if (esp_status e = check(rope, type, tokens, head_dim, q_heads, k_heads, weight_type, eps)) return e;
     if (tokens == 0) q_heads = k_heads = 0;                        // the weights' gradients are 0
+    if (q_heads + k_heads == 0 && !dq_weight && !dk_weight) return ESP_OK;
     if (q_heads + k_heads && !positions) return ESP_ERR_INVALID_ARG;
     if ((q_heads && (!q.data || !q_grad.data || !dq.data)) || (k_heads && (!k.data || !k_grad.data || !dk.data))) return ESP_ERR_INVALID_ARG;
     const int size = type == ESP_KV_FP32 ? 4 : 2;

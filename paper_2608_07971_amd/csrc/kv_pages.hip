@@ -1,4 +1,4 @@
-// Page operations of the paged 8-bit cache: resize, fork, compact.
+// Page operations of the paged 8-bit cache: resize, fork, reorder, compact.
 //
 // All choices are by index (the lowest free page, in order of sequence and
 // slot), so results do not depend on the order of atomics.  An operation is
@@ -13,186 +13,9 @@
 //      not suffice, takes step 1 back
 // (One workgroup doing all of it took 170 us for 256 sequences of up to 256
 // pages in a pool of 65,536; the launches of a step 3-5 us each.)
-#include "kv_internal.hpp"
-
-#include <type_traits>
+#include "kv_pages.hpp"
 
 namespace esp_kv {
-
-constexpr int kThreads = 256;
-constexpr int kCopyThreads = 256;
-constexpr int kMaxBlocks = 1024;            // blocks of pages, and of entries: added up by every workgroup
-
-// Pages or table entries [0, n) in at most kMaxBlocks blocks of `words` mask words.
-struct Blocks {
-    int64_t n;
-    int32_t words, blocks;
-    static Blocks of(int64_t n, int least) {
-        const int64_t all = (n + 63) / 64, per = (all + kMaxBlocks - 1) / kMaxBlocks;
-        Blocks b{n, int32_t(per > least ? per : least), 0};
-        b.blocks = int32_t((all + b.words - 1) / b.words);
-        return b;
-    }
-};
-
-struct Work {
-    Blocks pages, entries;
-    uint64_t *page_mask;                    // free (or, compact: live) pages
-    uint64_t *need_mask, *split_mask;       // entries that take a page; of these, entries that copy one
-    int32_t *page_sum, *need_sum, *split_sum, *bad;
-    int32_t *count;                         // copies to make
-    int2 *copies;                           // from, to
-    int32_t *goes;                          // [pages] new places
-    bool at_once;                           // pages are copied by the workgroup that finds them
-};
-
-__device__ __forceinline__ int lanes_below(uint64_t mask) {
-    return __builtin_amdgcn_mbcnt_hi(uint32_t(mask >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(mask), 0));
-}
-
-// Sum of x over the workgroup.
-__device__ __forceinline__ int block_sum(int x, int *lds) {
-#pragma unroll
-    for (int m = 32; m; m >>= 1) x += __shfl_xor(x, m);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
-    __syncthreads();
-    return lds[0] + lds[1] + lds[2] + lds[3];
-}
-
-// Exclusive prefix of n <= kMaxBlocks values into at[0 .. n], all threads.
-__device__ __forceinline__ void prefix(const int32_t *values, int n, int *at, int *lds) {
-    int x[4], sum = 0;
-#pragma unroll
-    for (int k = 0; k < 4; k++) {
-        const int i = threadIdx.x * 4 + k;
-        x[k] = i < n ? values[i] : 0;
-    }
-#pragma unroll
-    for (int k = 0; k < 4; k++) sum += x[k];
-    int before = sum;
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-        const int v = __shfl_up(before, m);
-        before += int(threadIdx.x & 63) >= m ? v : 0;
-    }
-    __syncthreads();
-    if ((threadIdx.x & 63) == 63) lds[threadIdx.x >> 6] = before;
-    __syncthreads();
-    before -= sum;
-    for (int w = 0; w < int(threadIdx.x >> 6); w++) before += lds[w];
-#pragma unroll
-    for (int k = 0; k < 4; k++) {
-        const int i = threadIdx.x * 4 + k;
-        if (i <= n) at[i] = before;
-        before += x[k];
-    }
-    if (threadIdx.x == kThreads - 1 && n == kMaxBlocks) at[n] = before;
-    __syncthreads();
-}
-
-// Place of the set bit that r others precede.
-__device__ __forceinline__ int nth_bit(uint64_t m, int r) {
-    int at = 0;
-#pragma unroll
-    for (int w = 32; w; w >>= 1) {
-        const int below = __popcll(m & ((uint64_t(1) << w) - 1));
-        const bool past = r >= below;
-        r -= past ? below : 0;
-        at += past ? w : 0;
-        m >>= past ? w : 0;
-    }
-    return at;
-}
-
-// The page of rank r among those whose bit is set (flip 0) or clear (flip ~0);
-// at(b): how many there are before block b.
-template <typename At> __device__ int select(const Work &w, At at, uint64_t flip, int r) {
-    int lo = 0, hi = w.pages.blocks - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (at(mid) <= r) lo = mid;
-        else hi = mid - 1;
-    }
-    r -= at(lo);
-    const int64_t words = (w.pages.n + 63) / 64, from = int64_t(lo) * w.pages.words;
-    for (int x = 0; x < w.pages.words; x += 4) {
-        uint64_t m[4];
-#pragma unroll
-        for (int k = 0; k < 4; k++) m[k] = x + k < w.pages.words && from + x + k < words ? w.page_mask[from + x + k] ^ flip : 0;
-#pragma unroll
-        for (int k = 0; k < 4; k++) {
-            const int held = __popcll(m[k]);
-            if (r < held) return int((from + x + k) * 64 + nth_bit(m[k], r));
-            r -= held;
-        }
-    }
-    return -1;
-}
-
-// A workgroup copies a page: keys, values and scales of all layers.
-__device__ __forceinline__ void copy_page(const Cache &c, int32_t from, int32_t to) {
-    const int64_t vectors = int64_t(c.layers) * c.heads * c.tokens * c.dim / 16;
-    const int scales = c.layers * 2 * c.heads;
-#pragma unroll
-    for (int side = 0; side < 2; side++) {
-        uint4v *pool = reinterpret_cast<uint4v *>(side ? c.v : c.k);
-        for (int64_t at = threadIdx.x; at < vectors; at += kThreads * 4) {
-            uint4v x[4];
-#pragma unroll
-            for (int j = 0; j < 4; j++)
-                if (at + j * kThreads < vectors) x[j] = pool[from * vectors + at + j * kThreads];
-#pragma unroll
-            for (int j = 0; j < 4; j++)
-                if (at + j * kThreads < vectors) pool[to * vectors + at + j * kThreads] = x[j];
-        }
-    }
-    for (int i = threadIdx.x; i < scales; i += kThreads) c.scale[int64_t(to) * scales + i] = c.scale[int64_t(from) * scales + i];
-}
-
-// Marks the items of block `block` that `has` holds for: four wavefronts, a word each at a time.
-template <typename Has> __device__ __forceinline__ void mark(const Blocks &b, int block, uint64_t *mask, int32_t *sum, int *lds, Has has) {
-    const int64_t words = (b.n + 63) / 64, from = int64_t(block) * b.words, to = min(words, from + b.words);
-    int mine = 0;
-    for (int64_t x = from + (threadIdx.x >> 6); x < to; x += 4) {
-        const int64_t i = x * 64 + (threadIdx.x & 63);
-        const uint64_t m = __ballot(i < b.n && has(i));
-        if ((threadIdx.x & 63) == 0) {
-            mask[x] = m;
-            mine += __popcll(m);
-        }
-    }
-    mine = block_sum(mine, lds);
-    if (threadIdx.x == 0) sum[block] = mine;
-}
-
-// Calls use(i, held, rank, held2, rank2) for every item of a block: whether its
-// bit is set in each of two masks, and how many set bits come before it, from
-// `before` and `before2` at the block's start.
-template <typename Use>
-__device__ __forceinline__ void ranked(const Blocks &b, int block, const uint64_t *mask, int before, const uint64_t *mask2, int before2, Use use) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t words = (b.n + 63) / 64, from = int64_t(block) * b.words, to = min(words, from + b.words);
-    for (int64_t x0 = from; x0 < to; x0 += 64) {                 // a word a lane
-        const uint64_t m = x0 + lane < to ? mask[x0 + lane] : 0, m2 = x0 + lane < to ? mask2[x0 + lane] : 0;
-        int at = __popcll(m), at2 = __popcll(m2);
-        const int own = at, own2 = at2;
-#pragma unroll
-        for (int s = 1; s < 64; s <<= 1) {
-            const int v = __shfl_up(at, s), v2 = __shfl_up(at2, s);
-            at += lane >= s ? v : 0;
-            at2 += lane >= s ? v2 : 0;
-        }
-        for (int x = wave; x < 64 && x0 + x < to; x += 4) {      // an item a lane
-            const uint64_t n = __shfl(m, x), n2 = __shfl(m2, x);
-            const int r = before + __shfl(at - own, x), r2 = before2 + __shfl(at2 - own2, x);
-            const int64_t i = (x0 + x) * 64 + lane;
-            if (i < b.n) use(i, bool(n >> lane & 1), r + lanes_below(n), bool(n2 >> lane & 1), r2 + lanes_below(n2));
-        }
-        before += __shfl(at, 63);
-        before2 += __shfl(at2, 63);
-    }
-}
 
 // ---------------------------------------------------------------------------
 // Resize: table entries by blocks
@@ -398,6 +221,98 @@ __global__ __launch_bounds__(kThreads) void k_fork_take(Cache c, int n, const in
 }
 
 // ---------------------------------------------------------------------------
+// Reorder: a workgroup a sequence; every row is put together aside before any is written
+// ---------------------------------------------------------------------------
+
+constexpr int kInvalid = 1, kWrong = 2, kCopies = 4;
+
+__global__ __launch_bounds__(kThreads) void k_reorder_drop(Cache c, const int32_t *parents, Work w) {
+    __shared__ int lds[4];
+    const int i = blockIdx.x, parent = parents[i];
+    const bool there = parent >= 0 && parent < c.sequences;
+    // the partly filled page stays with the parent itself, or else with the first that goes on with it
+    int earlier = 0;
+    for (int j = threadIdx.x; j < i; j += kThreads) earlier |= parents[j] == parent;
+    earlier = block_sum(earlier, lds);
+    int wrong = 0, length = 0, part = -1;
+    bool copies = false;
+    if (there) {
+        length = c.lengths[parent];
+        wrong = length < 0 || length > int64_t(c.width) << c.shift;
+        if (!wrong && (length & (c.tokens - 1))) {
+            part = length >> c.shift;
+            wrong |= c.table[int64_t(parent) * c.width + part] < 0;
+            copies = parents[parent] == parent ? parent != i : earlier != 0;
+        }
+    }
+    for (int x = threadIdx.x; x < c.width; x += kThreads) {
+        const int32_t p = there ? c.table[int64_t(parent) * c.width + x] : -1, k = c.table[int64_t(i) * c.width + x];
+        const bool ok = p >= -1 && p < c.pages;
+        wrong |= !ok || k < -1 || k >= c.pages;
+        if (k >= 0 && k < c.pages) atomicAdd(c.refs + k, -1);
+        if (p >= 0 && ok && !(copies && x == part)) atomicAdd(c.refs + p, 1);
+        w.rows[int64_t(i) * c.width + x] = ok ? p : -1;
+    }
+    wrong = block_sum(wrong, lds);
+    if (threadIdx.x == 0) {
+        w.row_lengths[i] = length;
+        w.bad[i] = (parent < -1 || parent >= c.sequences ? kInvalid : 0) | (wrong ? kWrong : 0) | (copies ? kCopies : 0);
+    }
+}
+
+__global__ __launch_bounds__(kThreads) void k_reorder_take(Cache c, Work w) {
+    __shared__ int lds[4], free_at[kMaxBlocks + 1];
+    const int i = blockIdx.x;
+    int invalid = 0, wrong = 0, need = 0, rank = 0;
+    for (int j = threadIdx.x; j < c.sequences; j += kThreads) {
+        const int b = w.bad[j], one = b / kCopies;
+        invalid |= b & kInvalid;
+        wrong |= b & kWrong;
+        need += one;
+        rank += j < i ? one : 0;
+    }
+    invalid = block_sum(invalid, lds);
+    wrong = block_sum(wrong, lds);
+    need = block_sum(need, lds);
+    rank = block_sum(rank, lds);
+    prefix(w.page_sum, w.pages.blocks, free_at, lds);
+    const int length = w.row_lengths[i], part = w.bad[i] & kCopies ? length >> c.shift : -1;
+    if (invalid || wrong || free_at[w.pages.blocks] < need) {
+        for (int x = threadIdx.x; x < c.width; x += kThreads) {
+            const int32_t p = w.rows[int64_t(i) * c.width + x], k = c.table[int64_t(i) * c.width + x];
+            if (p >= 0 && x != part) atomicAdd(c.refs + p, -1);
+            if (k >= 0 && k < c.pages) atomicAdd(c.refs + k, 1);
+        }
+        if (i == 0 && threadIdx.x == 0) {
+            *w.count = 0;
+            record(c, invalid ? ESP_ERR_INVALID_ARG : wrong ? ESP_ERR_SHAPE : ESP_ERR_RANGE);
+        }
+        return;
+    }
+    if (threadIdx.x == 0) lds[0] = lds[1] = -1;
+    __syncthreads();
+    for (int x = threadIdx.x; x < c.width; x += kThreads) {
+        int32_t p = w.rows[int64_t(i) * c.width + x];
+        if (x == part) {
+            const int to = select(w, [&](int b) { return free_at[b]; }, 0, rank);
+            if (to >= 0) {
+                w.copies[rank] = make_int2(p, to);
+                c.refs[to] = 1;
+                lds[0] = p;
+                lds[1] = to;
+            }
+            p = to;
+        }
+        c.table[int64_t(i) * c.width + x] = p;
+    }
+    if (threadIdx.x == 0) c.lengths[i] = length;
+    if (i == 0 && threadIdx.x == 0) *w.count = need;
+    if (!w.at_once) return;
+    __syncthreads();
+    if (lds[1] >= 0) copy_page(c, lds[0], lds[1]);
+}
+
+// ---------------------------------------------------------------------------
 // Compact
 // ---------------------------------------------------------------------------
 
@@ -520,32 +435,7 @@ constexpr int64_t kAtOnce = 128 << 10;
 // 845 / 70.
 constexpr int64_t kResizeCopies = 16, kResizeBytes = 64 << 10;
 
-// Lays the work out behind `p`; returns its bytes.
-size_t lay_out(const esp_kv_cache *c, char *p, Work &w) {
-    w.pages = Blocks::of(c->pages, 4);
-    w.entries = Blocks::of(int64_t(c->sequences) * c->table_width, 16);
-    char *at = p;
-    auto take = [&](auto *&to, size_t n) {
-        to = reinterpret_cast<std::remove_reference_t<decltype(to)>>(at);
-        at += (n * sizeof(*to) + 255) / 256 * 256;
-    };
-    take(w.count, 1);
-    take(w.page_mask, (size_t(w.pages.n) + 63) / 64);
-    take(w.need_mask, (size_t(w.entries.n) + 63) / 64);
-    take(w.split_mask, (size_t(w.entries.n) + 63) / 64);
-    take(w.page_sum, kMaxBlocks);
-    take(w.need_sum, kMaxBlocks);
-    take(w.split_sum, kMaxBlocks);
-    take(w.bad, size_t(c->sequences) > size_t(kMaxBlocks) ? size_t(c->sequences) : size_t(kMaxBlocks));
-    take(w.copies, size_t(c->pages));
-    take(w.goes, size_t(c->pages));
-    w.at_once = false;
-    return size_t(at - p);
-}
-esp_status work_of(const esp_kv_cache *c, void *workspace, size_t bytes, Work &w) {
-    const size_t need = lay_out(c, static_cast<char *>(workspace), w);
-    return workspace && (reinterpret_cast<uintptr_t>(workspace) & 255) == 0 && bytes >= need ? ESP_OK : ESP_ERR_WORKSPACE;
-}
+constexpr int32_t kMostSequences = (1 << 24) - 1;                              // a launch's threads are numbered in 32 bits
 int64_t page_bytes(const esp_kv_cache *c) { return 2 * int64_t(c->layers) * c->kv_heads * c->page_tokens * c->head_dim; }
 // Copies that one workgroup of resize may have to make: one a sequence of its entries.
 int64_t copies_of(const esp_kv_cache *c, const Work &w) {
@@ -600,6 +490,22 @@ extern "C" esp_status esp_kv_fork(const esp_kv_cache *cache, int32_t n, const in
     k_mark_free<<<w.pages.blocks, kThreads, 0, s>>>(c, w);
     k_fork_take<<<n, kThreads, 0, s>>>(c, n, parents, children, w);
     if (!w.at_once) k_copy<<<copy_blocks(cache, n), kCopyThreads, 0, s>>>(c, w.count, w.copies, nullptr, nullptr);
+    return launched();
+}
+
+extern "C" esp_status esp_kv_reorder(const esp_kv_cache *cache, const int32_t *parents, void *workspace, size_t workspace_bytes, void *stream) {
+    if (esp_status e = check_cache(cache)) return e;
+    if (!parents) return ESP_ERR_INVALID_ARG;
+    if (cache->sequences > kMostSequences) return ESP_ERR_SHAPE;
+    Work w;
+    if (esp_status e = work_of(cache, workspace, workspace_bytes, w)) return e;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    const Cache c = cache_of(cache);
+    w.at_once = page_bytes(cache) <= kAtOnce;
+    k_reorder_drop<<<cache->sequences, kThreads, 0, s>>>(c, parents, w);
+    k_mark_free<<<w.pages.blocks, kThreads, 0, s>>>(c, w);
+    k_reorder_take<<<cache->sequences, kThreads, 0, s>>>(c, w);
+    if (!w.at_once) k_copy<<<copy_blocks(cache, cache->sequences), kCopyThreads, 0, s>>>(c, w.count, w.copies, nullptr, nullptr);
     return launched();
 }
 

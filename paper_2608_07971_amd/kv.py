@@ -7,7 +7,11 @@ and `PagedCache` own the tensors.  A step of an offline-inference job:
     q = cache.append(layer, k, v, offsets, rope=rope, q=q)
     out, lse = cache.attend(layer, q, offsets, max_new=1)
 
-`fork`, `resize` and `compact` make a changed batch or memory budget real.
+`norm_rotate` (norms of queries and keys with the rotation, with its gradient)
+comes before `append` without a rope, `weigh` and `evict` (the attention weight
+that tokens got, and cutting sequences by it) after `attend`, `select_beams` and
+`reorder` after the logits.
+`fork`, `reorder`, `resize` and `compact` make a changed batch or memory budget real.
 There is no CPU fallback.
 """
 from __future__ import annotations
@@ -59,9 +63,13 @@ _SIGS = {
     "esp_kv_gather": [_P, _I, _I, _I, _L, _P, _P, _P, _P, _P, _P],
     "esp_kv_attend_workspace": [_P, _I, _L, _I, _I, _I, _Z],
     "esp_kv_attend": [_P, _I, _I, _I, _L, _P, _P, _I, _V, C.c_float, _I, _I, _I, _V, _P, _P, C.c_size_t, _P],
+    "esp_kv_weigh": [_P, _I, _I, _I, _L, _P, _P, _I, _V, _P, C.c_float, _I, C.c_float, _I, _I, _P, _P],
+    "esp_kv_evict_workspace": [_P, _Z],
+    "esp_kv_evict": [_P, _P, _I, _P, _P, C.c_size_t, _P],
     "esp_kv_pages_workspace": [_P, _I, _Z],
     "esp_kv_resize": [_P, _P, _P, C.c_size_t, _P],
     "esp_kv_fork": [_P, _I, _P, _P, _P, C.c_size_t, _P],
+    "esp_kv_reorder": [_P, _P, _P, C.c_size_t, _P],
     "esp_kv_compact": [_P, _I, _P, _P, _P, _P, C.c_size_t, _P],
     "esp_kv_device_status": [_P, _P],
 }
@@ -395,7 +403,7 @@ class PagedCache:
         self.pages, self.layers, self.kv_heads, self.page_tokens, self.head_dim = P, L, H, T, D
         self.sequences, self.table_width = table.shape
         self._work, self._graph_work, self._sizes = {}, (None, {}), {}
-        self._scale, self._pages_bytes = D ** -0.5, None
+        self._scale, self._pages_bytes, self._evict_bytes = D ** -0.5, None, None
         self._source = None                     # requires gradients once tokens were appended that do
         # kernels and captured graphs take the addresses by value: the tensors stay for the cache's life
         self.c = esp_kv_cache(self.pages, self.layers, self.kv_heads, self.page_tokens, self.head_dim, self.sequences,
@@ -521,6 +529,33 @@ class PagedCache:
             return self._results("attend", q, out)[0], None
         return self._results("attend", q, out, stats)
 
+    @property
+    def mass_shape(self) -> tuple:
+        """Shape of the float32 tensor that `weigh` adds to and `evict` reads, of zeros at first."""
+        return self.layers, self.sequences, self.kv_heads, self.table_width * self.page_tokens
+
+    def _mass(self, mass) -> int:
+        if mass.shape != self.mass_shape or mass.dtype != torch.float32 or mass.device != self.device or not mass.is_contiguous() or mass.requires_grad:
+            raise ValueError(f"mass: contiguous float32 {list(self.mass_shape)} on {self.device} expected, without a gradient")
+        return mass.data_ptr()
+
+    @_on_stream
+    def weigh(self, layer: int, q, lse, offsets, mass, scale: Optional[float] = None, window: int = 0, decay: float = 1.0,
+              max_new: Optional[int] = None, max_length: Optional[int] = None, seqs=None, *, s: int) -> None:
+        """Adds to mass (float32 of mass_shape) the attention weight that the cached tokens got from q, whose lse `attend`
+        returned; what a token had from before counts decay times.  The other arguments as `attend` takes them.  Not part
+        of any gradient."""
+        kind = _TYPES.get(q.dtype)
+        if kind is None or kind == FP32 or q.dim() != 3:
+            raise ValueError("q: bfloat16 or float16 [tokens, q_heads, head_dim] expected")
+        T, H, _ = q.shape
+        if lse.shape != (T, H) or lse.dtype != torch.float32 or lse.device != self.device or not lse.is_contiguous():
+            raise ValueError(f"lse: contiguous float32 [{T}, {H}] on {self.device} expected")
+        rows, off, sq = self._rows(offsets, seqs)
+        _check(lib().esp_kv_weigh(self.ptr, layer, kind, rows, T, off, sq, H, _view(q, T, H, self.head_dim, "q", self.device), lse.data_ptr(),
+                                  self._scale if scale is None else scale, window, decay, T if max_new is None else max_new,
+                                  self.table_width * self.page_tokens if max_length is None else max_length, self._mass(mass), s), "esp_kv_weigh")
+
     def _pages_work(self, stream: int) -> torch.Tensor:
         if self._pages_bytes is None:
             z = C.c_size_t(0)
@@ -542,6 +577,25 @@ class PagedCache:
         w = self._pages_work(s)
         _check(lib().esp_kv_fork(self.ptr, n, _ints(parents, n, "parents", self.device), _ints(children, n, "children", self.device),
                                  w.data_ptr(), w.numel(), s), "esp_kv_fork")
+
+    @_on_stream
+    def reorder(self, parents, *, s: int) -> None:
+        """Every sequence i goes on as parents[i] was (int32 [sequences]; -1: it ends), as select_beams leaves them."""
+        w = self._pages_work(s)
+        _check(lib().esp_kv_reorder(self.ptr, _ints(parents, self.sequences, "parents", self.device), w.data_ptr(), w.numel(), s),
+               "esp_kv_reorder")
+
+    @_on_stream
+    def evict(self, keep, mass, recent: int = 0, *, s: int) -> None:
+        """Cuts sequences that are longer than keep (int32 [sequences]): each layer and head keeps its last `recent` tokens
+        and those of the largest mass, moved together in their order, their masses too."""
+        if self._evict_bytes is None:
+            z = C.c_size_t(0)
+            _check(lib().esp_kv_evict_workspace(self.ptr, C.byref(z)), "esp_kv_evict_workspace")
+            self._evict_bytes = z.value
+        w = self._workspace("evict", self._evict_bytes, s)
+        _check(lib().esp_kv_evict(self.ptr, _ints(keep, self.sequences, "keep", self.device), recent, self._mass(mass), w.data_ptr(), w.numel(), s),
+               "esp_kv_evict")
 
     @_on_stream
     def compact(self, limit: Optional[int] = None, *, s: int):

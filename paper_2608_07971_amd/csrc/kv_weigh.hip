@@ -8,7 +8,10 @@ namespace esp_kv {
 typedef float float16v __attribute__((ext_vector_type(16)));
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
+constexpr int kGroups = 2;                  // of four wavefronts each, that take turns with the queries
+constexpr int kSubs = 2;
 constexpr int kRows = 32;                   // (token, query head) rows of a matrix tile
+constexpr int kStep = kGroups * kSubs * kRows;
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct View {
@@ -55,60 +58,129 @@ __device__ __forceinline__ int wave_sum(int x) {
     return x;
 }
 
-// A wavefront has kCols times 32 cached tokens, which stay in registers as the
-// columns of the products; the queries that see them go by, 32 rows at a time,
-// through LDS for all four wavefronts.  So a token's sum is its lane's own, and
-// no two workgroups add to the same place.
-template <typename T, int Dim, int Page, int kCols> __global__ __launch_bounds__(kThreads) void k_weigh(WeighArgs a) {
+// The key head's tiles of kTile tokens in order of rows, cut into even shares.  Finds the
+// first of share `share` of `shares`, and how many it has.
+struct Found {
+    int row, tile, count;
+};
+template <int kTile> __device__ __forceinline__ Found find_share(const WeighArgs &a, int share, int shares, bool note) {
+    const int lane = threadIdx.x & 63, rows = a.rows.rows;
+    auto tiles_of = [&](int b, bool n) { return b < rows ? (usable(a, b, n).length + kTile - 1) / kTile : 0; };
+    int all = 0, held[4];
+#pragma unroll
+    for (int k = 0; k < 4; k++) all += held[k] = tiles_of(64 * k + lane, note);   // the first 256 are kept
+    for (int b = 256; b < rows; b += 256)
+#pragma unroll
+        for (int k = 0; k < 4; k++) all += tiles_of(b + 64 * k + lane, note);
+    all = wave_sum(all);
+    const int each = int((int64_t(all) + shares - 1) / shares);
+    const int64_t begin = int64_t(share) * each;
+    Found f{-1, 0, int(min(int64_t(each), max(int64_t(0), all - begin)))};
+    if (f.count == 0) return f;
+    for (int b0 = 0, before = 0; b0 < rows; b0 += 256) {
+        if (b0)
+#pragma unroll
+            for (int k = 0; k < 4; k++) held[k] = tiles_of(b0 + 64 * k + lane, false);
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            int at = held[k];
+#pragma unroll
+            for (int m = 1; m < 64; m <<= 1) {
+                const int v = __shfl_up(at, m);
+                at += lane >= m ? v : 0;
+            }
+            at += before;                   // tiles up to this row's last
+            const uint64_t past = __ballot(begin < at);
+            if (past) {
+                const int l = __builtin_ctzll(past);
+                f.row = b0 + 64 * k + l;
+                f.tile = int(begin) - __shfl(at - held[k], l);
+                return f;
+            }
+            before = __shfl(at, 63);
+        }
+    }
+    return f;                               // lengths that changed under the call
+}
+
+// Row r of a sequence's (token, query head) rows, going on by the same number each time.
+struct Walker {
+    int token, head;
+    __device__ __forceinline__ Walker() {}
+    __device__ __forceinline__ Walker(int r, int group) : token(r / group), head(r - token * group) {}
+    // whether the head came round
+    __device__ __forceinline__ bool on(int tokens, int heads, int group) {
+        token += tokens;
+        head += heads;
+        const bool round = head >= group;
+        if (round) {
+            head -= group;
+            token++;
+        }
+        return round;
+    }
+};
+
+// Eight elements at any alignment.
+template <typename T> __device__ __forceinline__ typename Pack<T>::v8 load8(const T *p, bool wide) {
+    typename Pack<T>::v8 x;
+    if (wide) x = *reinterpret_cast<const typename Pack<T>::v8 *>(p);
+    else
+#pragma unroll
+        for (int e = 0; e < 8; e++) x[e] = p[e];
+    return x;
+}
+
+// A token's keys as one lane of each half holds them: half h's steps 2 i and 2 i + 1 are
+// elements 32 i + 16 h and on, so that codes are loaded sixteen at a time.
+template <typename T, int Dim> struct Keys {
     typedef typename Pack<T>::v8 V8;
     typedef typename Pack<T>::v2 V2;
-    constexpr int kSteps = Dim / 16, kTile = kWaves * 32 * kCols, kRowBytes = Dim * 2;
-    constexpr int kChunks = kRows * Dim / 8 / kThreads;          // 16-byte chunks of a tile of queries a thread stages
-    __shared__ __align__(16) uint8_t queries[2][kRows * kRowBytes];
-    __shared__ __align__(16) float lses[2][kRows];
-    __shared__ __align__(16) int places[2][kRows];
-    __shared__ int sums[kWaves], found[2];
+    uint4v w[Dim / 32];
+    __device__ __forceinline__ void load(const uint8_t *token, int half) {
+#pragma unroll
+        for (int s = 0; s < Dim / 32; s++) w[s] = *reinterpret_cast<const uint4v *>(token + 32 * s + 16 * half);
+    }
+    __device__ __forceinline__ V8 step(int s) const { return codes8<V8, V2>(w[s / 2][s % 2 * 2], w[s / 2][s % 2 * 2 + 1]); }
+};
+
+__device__ __forceinline__ float weight(float product, float scale, float lse) {
+    return __builtin_amdgcn_exp2f(__builtin_fmaf(product, scale, -lse) * kLog2e);
+}
+
+// Many queries.  A wavefront has 32 cached tokens, which stay in registers as the columns
+// of the products; the queries that see them go by, through LDS, kStep rows at a time, of
+// which each group of four wavefronts takes kSubs times 32.  So a token's sum is its lanes'
+// own, and no two workgroups add to the same place.
+template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads * kGroups, 4) void k_weigh(WeighArgs a) {
+    typedef typename Pack<T>::v8 V8;
+    constexpr int kSteps = Dim / 16, kTile = kWaves * 32, kRowBytes = Dim * 2, kAll = kThreads * kGroups;
+    constexpr int kPass = kAll / (Dim / 8), kPasses = kStep / kPass;      // rows that the threads load at once, 16 bytes each
+    __shared__ __align__(16) uint8_t queries[2][kStep * kRowBytes];
+    __shared__ __align__(16) float lses[2][kStep];
+    __shared__ __align__(16) int places[2][kStep];
+    __shared__ float sums[kGroups][kTile];
 
     const Cache &c = a.c;
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5;
-    const int head = blockIdx.x / a.shares, share = blockIdx.x - head * a.shares;
+    const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5;
+    const int number = __builtin_amdgcn_readfirstlane(tid >> 6), wave = number % kWaves, team = number / kWaves;
+    const int share = blockIdx.x / c.heads, head = blockIdx.x - share * c.heads;
+    const Found f = find_share<kTile>(a, share, a.shares, blockIdx.x == 0 && tid < 64);
+    int b = __builtin_amdgcn_readfirstlane(f.row), tile = __builtin_amdgcn_readfirstlane(f.tile);
+    if (b < 0) return;
 
-    // the head's tiles in order of rows: this workgroup's share of them
-    auto tiles_of = [&](int b, bool note) { return b < a.rows.rows ? (usable(a, b, note).length + kTile - 1) / kTile : 0; };
-    int all = 0;
-    for (int b = tid; b < a.rows.rows; b += kThreads) all += tiles_of(b, blockIdx.x == 0);
-    all = wave_sum(all);
-    if (lane == 0) sums[wave] = all;
-    __syncthreads();
-    all = sums[0] + sums[1] + sums[2] + sums[3];
-    const int each = (all + a.shares - 1) / a.shares, begin = share * each, end = min(all, begin + each);
-    if (begin >= end) return;
-    if (tid == 0) found[0] = -1;
-    for (int b0 = 0, before = 0; before <= begin && b0 < a.rows.rows; b0 += kThreads) {
-        const int own = tiles_of(b0 + tid, false);
-        int at = own;
-#pragma unroll
-        for (int m = 1; m < 64; m <<= 1) {
-            const int v = __shfl_up(at, m);
-            at += lane >= m ? v : 0;
-        }
-        __syncthreads();
-        if (lane == 63) sums[wave] = at;
-        __syncthreads();
-        for (int w = 0; w < wave; w++) at += sums[w];
-        at += before;                       // tiles up to this row's last
-        if (begin < at && begin >= at - own) {
-            found[0] = b0 + tid;
-            found[1] = begin - (at - own);
-        }
-        before += sums[0] + sums[1] + sums[2] + sums[3];
-    }
-    __syncthreads();
-    int b = __builtin_amdgcn_readfirstlane(found[0]), tile = __builtin_amdgcn_readfirstlane(found[1]);
-    if (b < 0) return;                      // lengths that changed under the call
-
+    // a 16-byte chunk's place in its row of LDS is turned by the row, so that the rows that a
+    // matrix step reads at once lie in different banks
     auto turn = [](int row) { return Dim == 128 ? row & 15 : (row >> 1) & 7; };
-    for (int left = end - begin; left > 0; left--, tile++) {
+    const int chunk = (tid % (Dim / 8)) ^ turn(tid / (Dim / 8));
+    uint32_t query_at[kSteps];
+#pragma unroll
+    for (int i = 0; i < kSteps; i++)
+        query_at[i] = (team * (kSubs * kRows) + col) * kRowBytes + (((i / 2 * 4 + 2 * half + i % 2) ^ turn(col)) << 4);
+    const int tokens_on = kPass / a.group, heads_on = kPass - tokens_on * a.group;
+    const int64_t ahead = tokens_on * a.q.token + heads_on * a.q.head, round = a.q.token - a.group * a.q.head;
+
+    for (int left = __builtin_amdgcn_readfirstlane(f.count); left > 0; left--, tile++) {
         Row row = usable(a, b, false);
         while (tile * kTile >= row.length) {
             if (++b >= a.rows.rows) return;
@@ -117,129 +189,240 @@ template <typename T, int Dim, int Page, int kCols> __global__ __launch_bounds__
         }
         const int p0 = row.length - row.n, n_rows = row.n * a.group, t0 = tile * kTile;
         // rows that may see a token of the tile
-        const int t1 = min(row.length, t0 + kTile) - 1;
-        int r_from = max(0, t0 - p0) * a.group / kRows * kRows, r_to = n_rows;
+        const int t1 = min(row.length, t0 + kTile) - 1, w0 = t0 + wave * 32, t = w0 + col;
+        const int r_from = max(0, t0 - p0) * a.group / kRows * kRows;
+        int r_to = n_rows;
         if (a.window > 0) r_to = int(min(int64_t(n_rows), max(int64_t(0), int64_t(t1) + a.window - p0) * a.group));
 
-        int page[kCols];
-        float ks[kCols], sum[kCols];
-        V8 k[kCols][kSteps];
-#pragma unroll
-        for (int j = 0; j < kCols; j++) {
-            const int t = t0 + (wave * kCols + j) * 32 + col;
-            page[j] = t < row.length ? c.table[int64_t(row.seq) * c.width + t / Page] : -1;
-            if (t < row.length && (page[j] < 0 || page[j] >= c.pages)) {
-                record(c, ESP_ERR_SHAPE);
-                page[j] = -1;
-            }
-            sum[j] = 0.0f;
+        int page = t < row.length ? c.table[int64_t(row.seq) * c.width + t / Page] : -1;
+        if (t < row.length && (page < 0 || page >= c.pages)) {
+            record(c, ESP_ERR_SHAPE);
+            page = -1;
         }
+        float sum = 0.0f;
         if (r_from < r_to) {
+            const float ks = *c.block_scale(max(page, 0), a.layer, 0, head) * a.scale;
+            V8 k[kSteps];
+            {
+                Keys<T, Dim> codes;
+                codes.load(c.k + c.block(max(page, 0), a.layer, head) + t % Page * Dim, half);
 #pragma unroll
-            for (int j = 0; j < kCols; j++) {
-                const int t = t0 + (wave * kCols + j) * 32 + col, p = max(page[j], 0);
-                const uint8_t *from = c.k + c.block(p, a.layer, head) + t % Page * Dim + 16 * half;
-                ks[j] = *c.block_scale(p, a.layer, 0, head) * a.scale;
-                uint4v w[kSteps / 2];
-#pragma unroll
-                for (int s = 0; s < kSteps / 2; s++) w[s] = *reinterpret_cast<const uint4v *>(from + 32 * s);
-#pragma unroll
-                for (int s = 0; s < kSteps / 2; s++) {
-                    k[j][2 * s] = codes8<V8, V2>(w[s][0], w[s][1]);
-                    k[j][2 * s + 1] = codes8<V8, V2>(w[s][2], w[s][3]);
-                }
+                for (int s = 0; s < kSteps; s++) k[s] = codes.step(s);
             }
-            // a tile of queries on its way: through registers into LDS
-            V8 next[kChunks];
+            // rows that are not there are read as the last one
+            Walker at(r_from + tid / (Dim / 8), a.group);
+            const T *base = static_cast<const T *>(a.q.data) + int64_t(row.first) * a.q.token + int64_t(head) * a.group * a.q.head + chunk * 8;
+            const T *from = base + at.token * a.q.token + at.head * a.q.head, *last_row = base + (row.n - 1) * a.q.token;
+            int own_row = r_from + (tid & (kStep - 1));
             float next_lse = 0.0f;
             int next_place = -1;
-            auto load = [&](int r0) {
+            auto load = [&](int buffer) {
 #pragma unroll
-                for (int i = 0; i < kChunks; i++) {
-                    const int u = tid + i * kThreads, r = r0 + u / (Dim / 8), d = u % (Dim / 8) * 8;
-                    V8 x{};
-                    if (r < n_rows) {
-                        const int token = r / a.group, h = head * a.group + r - token * a.group;
-                        const T *src = static_cast<const T *>(a.q.data) + int64_t(row.first + token) * a.q.token + int64_t(h) * a.q.head + d;
-                        if (a.wide) x = *reinterpret_cast<const V8 *>(src);
-                        else
-#pragma unroll
-                            for (int e = 0; e < 8; e++) x[e] = src[e];
+                for (int i = 0; i < kPasses; i++) {
+                    const T *src = at.token < row.n ? from : last_row;
+                    uint8_t *to = &queries[buffer][(i * kAll + number * 64) * 16];
+                    if (a.wide) {
+                        __builtin_amdgcn_global_load_lds(reinterpret_cast<const __attribute__((address_space(1))) void *>(reinterpret_cast<uintptr_t>(src)),
+                                                         (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+                    } else {
+                        *reinterpret_cast<V8 *>(to + lane * 16) = load8<T>(src, false);
                     }
-                    next[i] = x;
+                    from += ahead;
+                    if (at.on(tokens_on, heads_on, a.group)) from += round;
                 }
-                if (tid < kRows) {
-                    const int r = r0 + tid, token = r / a.group;
+                if (tid < kStep) {
                     next_lse = INFINITY;
                     next_place = -1;
-                    if (r < n_rows) {
-                        const float l = a.lse[int64_t(row.first + token) * a.q_heads + head * a.group + r - token * a.group];
+                    if (own_row < n_rows) {
+                        const Walker w(own_row, a.group);
+                        const float l = a.lse[int64_t(row.first + w.token) * a.q_heads + head * a.group + w.head];
                         next_lse = l == -INFINITY ? INFINITY : l;            // it sees nothing
-                        next_place = p0 + token;
+                        next_place = p0 + w.token;
                     }
+                    own_row += kStep;
                 }
             };
-            load(r_from);
-            for (int r0 = r_from; r0 < r_to; r0 += kRows) {
-                const int buffer = (r0 / kRows) & 1;
-#pragma unroll
-                for (int i = 0; i < kChunks; i++) {
-                    const int u = tid + i * kThreads, r = u / (Dim / 8), chunk = u % (Dim / 8);
-                    *reinterpret_cast<V8 *>(&queries[buffer][r * kRowBytes + ((chunk ^ turn(r)) << 4)]) = next[i];
-                }
-                if (tid < kRows) {
+            auto put = [&](int buffer) {
+                if (tid < kStep) {
                     lses[buffer][tid] = next_lse;
                     places[buffer][tid] = next_place;
                 }
-                __syncthreads();
-                if (r0 + kRows < r_to) load(r0 + kRows);
-                float16v s[kCols];
+                __builtin_amdgcn_s_waitcnt(0x0f70);              // the queries have come in
+            };
+            auto products = [&](int buffer, int sub, float16v &s) {
+                V8 q[kSteps];
 #pragma unroll
-                for (int j = 0; j < kCols; j++)
+                for (int i = 0; i < kSteps; i++) q[i] = *reinterpret_cast<const V8 *>(&queries[buffer][query_at[i] + sub * kRows * kRowBytes]);
+                __builtin_amdgcn_sched_barrier(0);               // all reads on their way before the first product waits
 #pragma unroll
-                    for (int i = 0; i < 16; i++) s[j][i] = 0.0f;
-                // half h's steps 2 i and 2 i + 1: elements 32 i + 16 h and on, as the keys were loaded
+                for (int i = 0; i < 16; i++) s[i] = 0.0f;
 #pragma unroll
-                for (int i = 0; i < kSteps; i++) {
-                    const int chunk = i / 2 * 4 + 2 * half + i % 2;
-                    const V8 q = *reinterpret_cast<const V8 *>(&queries[buffer][col * kRowBytes + ((chunk ^ turn(col)) << 4)]);
+                for (int i = 0; i < kSteps; i++) s = product32(q[i], k[i], s);
+            };
+            // s[4 y + x]: row 8 y + 4 half + x
+            auto add = [&](int buffer, int sub, const float16v &s) {
+                const float *lse = &lses[buffer][(team * kSubs + sub) * kRows + 4 * half];
+                float e[16];
 #pragma unroll
-                    for (int j = 0; j < kCols; j++) s[j] = product32(q, k[j][i], s[j]);
+                for (int y = 0; y < 4; y++) {
+                    const float4v l = *reinterpret_cast<const float4v *>(lse + 8 * y);
+#pragma unroll
+                    for (int x = 0; x < 4; x++) e[4 * y + x] = __builtin_fmaf(s[4 * y + x], ks, -l[x]);
                 }
-                const int first = p0 + r0 / a.group, last = p0 + min(r0 + kRows, n_rows) / a.group;
-                const int w0 = t0 + wave * kCols * 32, w1 = w0 + kCols * 32 - 1;
-                const bool whole = r0 + kRows <= n_rows && w1 <= first && (a.window <= 0 || w0 > last - a.window);
+                __builtin_amdgcn_sched_barrier(0);               // each step for all of them, so that none waits for itself
 #pragma unroll
-                for (int y = 0; y < 4; y++) {            // s[4 y + x]: row 8 y + 4 half + x
-                    const float4v l = *reinterpret_cast<const float4v *>(&lses[buffer][8 * y + 4 * half]);
-                    if (whole) {
+                for (int i = 0; i < 16; i++) e[i] *= kLog2e;
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                        for (int j = 0; j < kCols; j++)
+                for (int i = 0; i < 16; i++) e[i] = __builtin_amdgcn_exp2f(e[i]);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                            for (int x = 0; x < 4; x++) sum[j] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[j][4 * y + x], ks[j], -l[x]) * kLog2e);
-                    } else {
-                        const int *at = &places[buffer][8 * y + 4 * half];
+                for (int m = 8; m; m >>= 1)
 #pragma unroll
-                        for (int j = 0; j < kCols; j++) {
-                            const int t = w0 + j * 32 + col;
+                    for (int i = 0; i < m; i++) e[i] += e[i + m];
+                sum += e[0];
+            };
+            auto add_seen = [&](int buffer, int sub, const float16v &s) {
+                const int r = (team * kSubs + sub) * kRows + 4 * half;
 #pragma unroll
-                            for (int x = 0; x < 4; x++) {
-                                const bool seen = t <= at[x] && (a.window <= 0 || t > at[x] - a.window);
-                                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j][4 * y + x], ks[j], -l[x]) * kLog2e);
-                                sum[j] += seen ? e : 0.0f;
-                            }
-                        }
+                for (int y = 0; y < 4; y++)
+#pragma unroll
+                    for (int x = 0; x < 4; x++) {
+                        const int p = places[buffer][r + 8 * y + x];
+                        const float e = weight(s[4 * y + x], ks, lses[buffer][r + 8 * y + x]);
+                        sum += t <= p && (a.window <= 0 || t > p - a.window) ? e : 0.0f;
+                    }
+            };
+            Walker seen(r_from + team * kSubs * kRows, a.group);
+            const int seen_tokens = kStep / a.group, seen_heads = kStep - seen_tokens * a.group, spread = kSubs * kRows / a.group + 1;
+            load(0);
+            put(0);
+            __syncthreads();
+            int buffer = 0;
+            for (int r0 = r_from; r0 < r_to; r0 += kStep, buffer ^= 1) {
+                const bool more = r0 + kStep < r_to;
+                if (more) load(buffer ^ 1);
+                const int own0 = r0 + team * kSubs * kRows, first = p0 + seen.token, last = first + spread;
+                seen.on(seen_tokens, seen_heads, a.group);
+                if (own0 + kSubs * kRows <= n_rows && w0 + 31 <= first && (a.window <= 0 || w0 > last - a.window)) {
+#pragma unroll
+                    for (int i = 0; i < kSubs; i++) {
+                        float16v s;
+                        products(buffer, i, s);
+                        add(buffer, i, s);
+                    }
+                } else {
+                    for (int i = 0; i < kSubs && own0 + i * kRows < r_to; i++) {
+                        float16v s;
+                        products(buffer, i, s);
+                        add_seen(buffer, i, s);
                     }
                 }
+                if (more) put(buffer ^ 1);
+                __syncthreads();
             }
-            __syncthreads();                // the next tile's queries go into the same places
         }
-        float *mass = a.mass + ((int64_t(a.layer) * c.sequences + row.seq) * c.heads + head) * (int64_t(c.width) * Page);
+        sum += __shfl_xor(sum, 32);
+        if (half == 0) sums[team][wave * 32 + col] = sum;
+        __syncthreads();
+        if (team == 0 && half == 0 && page >= 0) {
 #pragma unroll
-        for (int j = 0; j < kCols; j++) {
-            const int t = t0 + (wave * kCols + j) * 32 + col;
-            const float got = sum[j] + __shfl_xor(sum[j], 32);
-            if (half == 0 && t < row.length && page[j] >= 0) mass[t] = t < p0 ? __builtin_fmaf(mass[t], a.decay, got) : got;
+            for (int g = 1; g < kGroups; g++) sum += sums[g][wave * 32 + col];
+            float *mass = a.mass + ((int64_t(a.layer) * c.sequences + row.seq) * c.heads + head) * (int64_t(c.width) * Page) + t;
+            *mass = t < p0 ? __builtin_fmaf(*mass, a.decay, sum) : sum;
+        }
+        __syncthreads();                    // the next tile's sums go into the same places
+    }
+}
+
+// Few queries, at most 32 rows a sequence and key head: they stay in registers while a
+// wavefront goes through its share of the tokens, 32 at a time, the next ones' codes and
+// the pages after these on their way.
+template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 3) void k_weigh_few(WeighArgs a) {
+    typedef typename Pack<T>::v8 V8;
+    constexpr int kSteps = Dim / 16, kTile = 32;
+    const Cache &c = a.c;
+    const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+    const int unit = __builtin_amdgcn_readfirstlane(blockIdx.x * kWaves + (threadIdx.x >> 6));
+    const int share = unit / c.heads, head = unit - share * c.heads;
+    if (share >= a.shares) return;
+    const Found f = find_share<kTile>(a, share, a.shares, unit == 0);
+    int b = __builtin_amdgcn_readfirstlane(f.row), tile = __builtin_amdgcn_readfirstlane(f.tile), left = __builtin_amdgcn_readfirstlane(f.count);
+    if (b < 0) return;
+    for (; left > 0; b++, tile = 0) {
+        if (b >= a.rows.rows) return;
+        const Row row = usable(a, b, false);
+        const int p0 = row.length - row.n, n_rows = row.n * a.group, end = min(tile + left, (row.length + kTile - 1) / kTile);
+        if (tile >= end) continue;
+        left -= end - tile;
+        // the rows of this lane's products: 8 y + 4 half + x
+        V8 q[kSteps];
+        {
+            const Walker w(min(col, n_rows - 1), a.group);
+            const T *from = static_cast<const T *>(a.q.data) + int64_t(row.first + w.token) * a.q.token + int64_t(head * a.group + w.head) * a.q.head + 16 * half;
+#pragma unroll
+            for (int s = 0; s < kSteps; s++) q[s] = load8<T>(from + s / 2 * 32 + s % 2 * 8, a.wide);
+        }
+        float lse[16];
+#pragma unroll
+        for (int y = 0; y < 4; y++)
+#pragma unroll
+            for (int x = 0; x < 4; x++) {
+                const int r = 8 * y + 4 * half + x;
+                lse[4 * y + x] = INFINITY;
+                if (r < n_rows) {
+                    const Walker w(r, a.group);
+                    const float l = a.lse[int64_t(row.first + w.token) * a.q_heads + head * a.group + w.head];
+                    lse[4 * y + x] = l == -INFINITY ? INFINITY : l;          // it sees nothing
+                }
+            }
+        const int32_t *table = c.table + int64_t(row.seq) * c.width;
+        float *mass = a.mass + ((int64_t(a.layer) * c.sequences + row.seq) * c.heads + head) * (int64_t(c.width) * Page);
+        auto page_of = [&](int i) {
+            const int t = i * kTile + col;
+            return i < end && t < row.length ? table[t / Page] : -1;
+        };
+        struct Tile {
+            Keys<T, Dim> codes;
+            float ks, mass;
+            bool there;
+        };
+        auto load = [&](Tile &x, int i, int page) {
+            const int t = i * kTile + col;
+            x.there = uint32_t(page) < uint32_t(c.pages);
+            if (!x.there && i < end && t < row.length) record(c, ESP_ERR_SHAPE);
+            const int p = x.there ? page : 0;
+            x.codes.load(c.k + c.block(p, a.layer, head) + t % Page * Dim, half);
+            x.ks = *c.block_scale(p, a.layer, 0, head) * a.scale;
+            x.mass = x.there && t < p0 ? mass[t] : 0.0f;
+        };
+        Tile now, next;
+        int page = page_of(tile + 1);
+        load(now, tile, page_of(tile));
+        for (; tile < end; tile++) {
+            load(next, tile + 1, page);
+            page = page_of(tile + 2);
+            float16v s;
+#pragma unroll
+            for (int i = 0; i < 16; i++) s[i] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kSteps; i++) s = product32(q[i], now.codes.step(i), s);
+            const int t = tile * kTile + col;
+            // whether all rows that there are see all of the tile
+            const bool whole = tile * kTile + kTile - 1 <= p0 && (a.window <= 0 || tile * kTile > p0 + row.n - 1 - a.window);
+            float sum = 0.0f;
+#pragma unroll
+            for (int y = 0; y < 4; y++)
+                if (8 * y < n_rows)
+#pragma unroll
+                    for (int x = 0; x < 4; x++) {
+                        const float e = weight(s[4 * y + x], now.ks, lse[4 * y + x]);
+                        const int r = 8 * y + 4 * half + x, p = whole ? 0 : p0 + r / a.group;
+                        sum += r < n_rows && (whole || (t <= p && (a.window <= 0 || t > p - a.window))) ? e : 0.0f;
+                    }
+            sum += __shfl_xor(sum, 32);
+            if (half == 0 && now.there) mass[t] = t < p0 ? __builtin_fmaf(now.mass, a.decay, sum) : sum;
+            now = next;
         }
     }
 }
@@ -250,18 +433,22 @@ using namespace esp_kv;
 
 namespace {
 
-constexpr int64_t kMostBlocks = ((int64_t(1) << 32) - kThreads) / kThreads;    // a launch's threads are numbered in 32 bits
+constexpr int kFewWaves = 3072;
+constexpr int64_t kMostBlocks = ((int64_t(1) << 32) - 1) / (kThreads * kGroups);  // a launch's threads are numbered in 32 bits
 
-template <typename T, int Dim, int kCols> void launch(const WeighArgs &a, unsigned blocks, hipStream_t s) {
+template <typename T, int Dim, int Page> void launch(const WeighArgs &a, bool many, unsigned blocks, hipStream_t s) {
+    if (many) k_weigh<T, Dim, Page><<<blocks, kThreads * kGroups, 0, s>>>(a);
+    else k_weigh_few<T, Dim, Page><<<blocks, kThreads, 0, s>>>(a);
+}
+template <typename T, int Dim> void launch(const WeighArgs &a, bool many, unsigned blocks, hipStream_t s) {
     switch (a.c.tokens) {
-    case 16: k_weigh<T, Dim, 16, kCols><<<blocks, kThreads, 0, s>>>(a); break;
-    case 32: k_weigh<T, Dim, 32, kCols><<<blocks, kThreads, 0, s>>>(a); break;
-    default: k_weigh<T, Dim, 64, kCols><<<blocks, kThreads, 0, s>>>(a); break;
+    case 16: launch<T, Dim, 16>(a, many, blocks, s); break;
+    case 32: launch<T, Dim, 32>(a, many, blocks, s); break;
+    default: launch<T, Dim, 64>(a, many, blocks, s); break;
     }
 }
 template <typename T> void launch(const WeighArgs &a, bool many, unsigned blocks, hipStream_t s) {
-    if (a.c.dim == 64) many ? launch<T, 64, 2>(a, blocks, s) : launch<T, 64, 1>(a, blocks, s);
-    else many ? launch<T, 128, 2>(a, blocks, s) : launch<T, 128, 1>(a, blocks, s);
+    a.c.dim == 64 ? launch<T, 64>(a, many, blocks, s) : launch<T, 128>(a, many, blocks, s);
 }
 
 }  // namespace
@@ -280,15 +467,17 @@ extern "C" esp_status esp_kv_weigh(const esp_kv_cache *cache, int32_t layer, int
     const int32_t group = q_heads / cache->kv_heads;
     if (tokens * group > INT32_MAX - kRows) return ESP_ERR_SHAPE;
     const bool many = int64_t(max_new) * group > kRows;
-    const int64_t tile = kWaves * 32 * (many ? 2 : 1), most = rows * ((int64_t(max_length) + tile - 1) / tile);
+    // shares of a head's tiles: one each where queries are many; else as many as the GPU holds wavefronts
+    const int64_t tile = many ? kWaves * 32 : 32, most = rows * ((int64_t(max_length) + tile - 1) / tile);
     if (most > INT32_MAX) return ESP_ERR_SHAPE;
-    const int64_t fill = (many ? 16384 : 4096) / cache->kv_heads + 1, shares = most < fill ? most : fill;
-    if (shares * cache->kv_heads > kMostBlocks) return ESP_ERR_SHAPE;
+    const int64_t fill = (many ? 16384 : kFewWaves) / cache->kv_heads + 1, shares = most < fill ? most : fill;
+    const int64_t workers = shares * cache->kv_heads, count = many ? workers : (workers + kWaves - 1) / kWaves;
+    if (count > kMostBlocks) return ESP_ERR_SHAPE;
     const bool wide = (reinterpret_cast<uintptr_t>(q.data) & 15) == 0 && q.token_stride % 8 == 0 && q.head_stride % 8 == 0;
     const WeighArgs a{cache_of(cache), Rows{offsets, seqs, rows, tokens}, View{q.data, q.token_stride, q.head_stride}, lse, mass, scale, decay,
                       layer, q_heads, group, window, max_new, max_length, int32_t(shares), wide};
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    const unsigned blocks = unsigned(shares * cache->kv_heads);
+    const unsigned blocks = unsigned(count);
     if (type == ESP_KV_BF16) launch<__bf16>(a, many, blocks, s);
     else launch<_Float16>(a, many, blocks, s);
     return launched();

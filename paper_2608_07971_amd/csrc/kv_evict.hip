@@ -178,10 +178,12 @@ __global__ __launch_bounds__(kThreads) void k_evict_select(EvictArgs a, Work w) 
 constexpr int kTurn = 64;                   // tokens moved at a time: whole pages
 constexpr int kStretch = 4096;              // tokens whose mask is read at a time
 
-struct Moved {
-    int64_t from;                           // block of the old page
-    int32_t in_page;
-    float by;                               // the old scale over the new
+// Where the tokens of a turn come from.
+struct Sources {
+    int64_t from[kTurn];                    // block of the old page
+    int32_t in_page[kTurn];
+    float by[kTurn];                        // the old scale over the new
+    int32_t rescale;                        // whether any of these is not 1
 };
 
 __device__ __forceinline__ uint32_t code2(float x, float y) { return __builtin_amdgcn_cvt_pk_fp8_f32(x, y, 0, false); }
@@ -190,99 +192,124 @@ __device__ __forceinline__ uint32_t rescaled(uint32_t w, float b0, float b1, flo
     return code2(float(a[0]) * b0, float(a[1]) * b1) | code2(float(b[0]) * b2, float(b[1]) * b3) << 16;
 }
 
+// Keys: sixteen bytes a thread.  Values, whose tokens lie innermost: a lane has a dimension,
+// and takes the sixteen tokens of a group that stand together there at once; which of their
+// bytes go where is the same for all lanes, so that a byte is a permutation whose selector
+// lies in a scalar register.
 template <int Dim, int Page> __global__ __launch_bounds__(kThreads) void k_evict_move(EvictArgs a, Work w) {
     __shared__ int list[kStretch + kTurn];
-    __shared__ Moved moved[kTurn];
+    __shared__ Sources sources[2];
     const Cache &c = a.c;
     const int item = blockIdx.x >> 1, values = blockIdx.x & 1;
     const Place p = place_of(c, item);
     const int length = w.row_lengths[p.seq];
     if (!*w.count || length < 0) return;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint64_t *kept = a.kept + int64_t(item) * a.words;
     const int32_t *old = w.rows + int64_t(p.seq) * c.width, *table = c.table + int64_t(p.seq) * c.width;
     uint8_t *pool = values ? c.v : c.k;
 
-    // tokens list[from, from + n) to places [done, done + n)
-    auto turn = [&](int from, int n, int done) {
-        if (wave == 0) {
-            const int src = list[from + min(lane, n - 1)];
-            const int32_t page = old[src / Page];
-            const float was = lane < n ? *c.block_scale(page, p.layer, values, p.head) : 0.0f;
-            float now = was;
+    // A wavefront finds the sources of tokens list[from, from + n), which go to places
+    // [done, done + n), and leaves their new pages' scales there: no later token comes
+    // from these pages.
+    auto look = [&](int from, int n, int done, Sources &to) {
+        const int src = list[from + min(lane, n - 1)];
+        const int32_t page = old[src / Page];
+        const float was = lane < n ? *c.block_scale(page, p.layer, values, p.head) : 0.0f;
+        float now = was;
 #pragma unroll
-            for (int m = Page / 2; m; m >>= 1) now = fmaxf(now, __shfl_xor(now, m));
-            moved[lane] = {c.block(page, p.layer, p.head), src % Page, now > 0.0f ? was / now : 1.0f};
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            if (lane % Page == 0 && lane < n) *c.block_scale(table[(done + lane) / Page], p.layer, values, p.head) = now;
+        for (int m = Page / 2; m; m >>= 1) now = fmaxf(now, __shfl_xor(now, m));
+        const float by = now > 0.0f ? was / now : 1.0f;
+        to.from[lane] = c.block(page, p.layer, p.head);
+        to.in_page[lane] = src % Page;
+        to.by[lane] = by;
+        const bool any = __any(lane < n && by != 1.0f);
+        if (lane == 0) to.rescale = any;
+        if (lane % Page == 0 && lane < n) *c.block_scale(table[(done + lane) / Page], p.layer, values, p.head) = now;
+    };
+    auto move_keys = [&](int n, int done, const Sources &m) {
+        constexpr int kChunks = Dim / 16, kUnits = kTurn * kChunks / kThreads;
+        uint4v x[kUnits];
+#pragma unroll
+        for (int i = 0; i < kUnits; i++) {
+            const int u = tid + i * kThreads, t = min(u / kChunks, n - 1);
+            x[i] = *reinterpret_cast<const uint4v *>(pool + m.from[t] + m.in_page[t] * Dim + u % kChunks * 16);
         }
-        __syncthreads();
-        if (!values) {
-            constexpr int kChunks = Dim / 16, kUnits = kTurn * kChunks / kThreads;
-            uint4v x[kUnits];
+        if (m.rescale)
 #pragma unroll
             for (int i = 0; i < kUnits; i++) {
-                const int u = tid + i * kThreads, t = min(u / kChunks, n - 1);
-                x[i] = *reinterpret_cast<const uint4v *>(pool + moved[t].from + moved[t].in_page * Dim + u % kChunks * 16);
+                const float by = m.by[min((tid + i * kThreads) / kChunks, n - 1)];
+#pragma unroll
+                for (int k = 0; k < 4; k++) x[i][k] = by != 1.0f ? rescaled(x[i][k], by, by, by, by) : x[i][k];
             }
+        __syncthreads();                    // all of them are read before any place is written
 #pragma unroll
-            for (int i = 0; i < kUnits; i++) {
-                const float by = moved[min((tid + i * kThreads) / kChunks, n - 1)].by;
-                if (by != 1.0f)
+        for (int i = 0; i < kUnits; i++) {
+            const int u = tid + i * kThreads, t = u / kChunks, at = done + t;
+            if (t < n) *reinterpret_cast<uint4v *>(pool + c.block(table[at / Page], p.layer, p.head) + at % Page * Dim + u % kChunks * 16) = x[i];
+        }
+    };
+    auto move_values = [&](int n, int done, int from, const Sources &m) {
+        constexpr int kHalves = Dim / 64, kOwn = kTurn * kHalves / 4;     // tokens of a wavefront
+        const int d = wave % kHalves * 64 + lane, t0 = wave / kHalves * kOwn, own = min(kOwn, n - t0);
+        uint4v x[kOwn / 16];
+        if (own > 0) {
+            const int src = list[from + t0 + min(lane, own - 1)];
+            // group of sixteen tokens of the old pages that a lane's token is in; the first of each
+            const int before = __shfl_up(src, 1);
+            uint64_t firsts = __ballot(lane < own && lane > 0 && src >> 4 != before >> 4);
+            auto load = [&](int t) {        // the group of token t
+                const int s = __builtin_amdgcn_readlane(src, t);
+                const int64_t block = m.from[t0 + t];
+                return *reinterpret_cast<const uint4v *>(pool + block + d * Page + (s % Page & ~15));
+            };
+            uint4v now = load(0), next = now;
+            int turns = firsts ? __builtin_ctzll(firsts) : 64;   // the token that the next group begins with
+            if (turns < 64) next = load(turns);
 #pragma unroll
-                    for (int k = 0; k < 4; k++) x[i][k] = rescaled(x[i][k], by, by, by, by);
-            }
-            __syncthreads();
+            for (int i = 0; i < kOwn; i += 4) {
+                uint32_t word = 0;
 #pragma unroll
-            for (int i = 0; i < kUnits; i++) {
-                const int u = tid + i * kThreads, t = u / kChunks;
-                if (t < n) {
-                    const int at = done + t;
-                    *reinterpret_cast<uint4v *>(pool + c.block(table[at / Page], p.layer, p.head) + at % Page * Dim + u % kChunks * 16) = x[i];
+                for (int j = 0; j < 4; j++) {
+                    const int t = i + j;
+                    if (t < own) {
+                        if (t == turns) {
+                            now = next;
+                            firsts &= firsts - 1;
+                            turns = firsts ? __builtin_ctzll(firsts) : 64;
+                            if (turns < 64) next = load(turns);
+                        }
+                        const uint32_t s = uint32_t(__builtin_amdgcn_readlane(src, t)) & 15, none = 0x0c0c0c0cu;
+                        const uint32_t pick = (none & ~(255u << (8 * j))) | (s & 7) << (8 * j);
+                        word |= __builtin_amdgcn_perm(now[1], now[0], s < 8 ? pick : none) | __builtin_amdgcn_perm(now[3], now[2], s < 8 ? none : pick);
+                    }
                 }
+                x[i / 16][i / 4 % 4] = word;
             }
-        } else {
-            constexpr int kUnits = kTurn / 16 * Dim / kThreads;  // sixteen tokens of a dimension
-            uint4v x[kUnits];
+            if (m.rescale)
 #pragma unroll
-            for (int i = 0; i < kUnits; i++) {
-                const int u = tid + i * kThreads, d = u % Dim, t = u / Dim * 16;
+                for (int i = 0; i < kOwn; i += 4) {
+                    const float *by = &m.by[t0 + i];
+                    x[i / 16][i / 4 % 4] = rescaled(x[i / 16][i / 4 % 4], by[0], by[1], by[2], by[3]);
+                }
+        }
+        __syncthreads();                    // all of them are read before any place is written
+#pragma unroll
+        for (int i = 0; i < kOwn; i += 16) {
+            const int left = own - i, at = done + t0 + i;
+            if (left <= 0) break;
+            uint4v *to = reinterpret_cast<uint4v *>(pool + c.block(table[at / Page], p.layer, p.head) + d * Page + at % Page);
+            if (left < 16) {                // past the end: as it was
+                const uint4v was = *to;
 #pragma unroll
                 for (int k = 0; k < 4; k++) {
-                    uint32_t b[4];
-                    float by[4];
-#pragma unroll
-                    for (int j = 0; j < 4; j++) {
-                        const Moved &m = moved[min(t + 4 * k + j, n - 1)];
-                        b[j] = pool[m.from + d * Page + m.in_page];
-                        by[j] = m.by;
-                    }
-                    uint32_t word = b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24;
-                    if (by[0] != 1.0f || by[1] != 1.0f || by[2] != 1.0f || by[3] != 1.0f) word = rescaled(word, by[0], by[1], by[2], by[3]);
-                    x[i][k] = word;
+                    const int more = left - 4 * k;
+                    const uint32_t mine = more >= 4 ? ~0u : more <= 0 ? 0u : (1u << (8 * more)) - 1;
+                    x[i / 16][k] = (x[i / 16][k] & mine) | (was[k] & ~mine);
                 }
             }
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < kUnits; i++) {
-                const int u = tid + i * kThreads, d = u % Dim, t = u / Dim * 16;
-                if (t < n) {
-                    const int at = done + t;
-                    uint4v *to = reinterpret_cast<uint4v *>(pool + c.block(table[at / Page], p.layer, p.head) + d * Page + at % Page);
-                    if (t + 16 > n) {       // past the end: as it was
-                        const uint4v was = *to;
-#pragma unroll
-                        for (int k = 0; k < 4; k++) {
-                            const int left = n - t - 4 * k;
-                            const uint32_t own = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
-                            x[i][k] = (x[i][k] & own) | (was[k] & ~own);
-                        }
-                    }
-                    *to = x[i];
-                }
-            }
+            *to = x[i / 16];
         }
-        __syncthreads();
     };
 
     int held = 0, done = 0;
@@ -303,14 +330,28 @@ template <int Dim, int Page> __global__ __launch_bounds__(kThreads) void k_evict
             const int at = held + __shfl(before, x) + lanes_below(n);
             if (bit_of(n, lane)) list[at] = (x0 + x) * 64 + lane;
         }
-        held += all;
+        held = __builtin_amdgcn_readfirstlane(held + all);
         __syncthreads();
-        int from = 0;
-        for (; held - from >= kTurn && done + kTurn <= keep; from += kTurn, done += kTurn) turn(from, kTurn, done);
-        if (x0 + 64 >= words || held - from >= keep - done) {    // keep tokens, whatever the masses did meanwhile
-            if (min(held - from, keep - done) > 0) turn(from, min(held - from, keep - done), done);
-            return;
+        // tokens of a turn: whole ones, and what is left at the end of all; keep tokens in all, whatever the masses did meanwhile
+        auto size = [&](int from, int done) {
+            const int n = min(held - from, keep - done);
+            return n >= kTurn ? kTurn : x0 + 64 >= words || n == keep - done ? n : 0;
+        };
+        int from = 0, slot = 0, n = size(0, done);
+        if (n > 0 && wave == 0) look(0, n, done, sources[0]);
+        __syncthreads();
+        while (n > 0) {
+            const int more = size(from + n, done + n);
+            if (more > 0 && wave == 0) look(from + n, more, done + n, sources[slot ^ 1]);
+            if (values) move_values(n, done, from, sources[slot]);
+            else move_keys(n, done, sources[slot]);
+            __syncthreads();
+            from += n;
+            done += n;
+            n = more;
+            slot ^= 1;
         }
+        if (done >= keep) return;
         const int rest = held - from, next = tid < rest ? list[from + tid] : 0;
         __syncthreads();
         if (tid < rest) list[tid] = next;

@@ -91,6 +91,8 @@ __device__ __forceinline__ Place place_of(const Cache &c, int i) {
     return {rest / c.sequences, rest % c.sequences, head};
 }
 
+constexpr int kHeld = 16;                   // weights a thread: rows of up to 4,096 tokens are read once
+
 // The want-th largest weight by its bits, eight at a time from the top; then one pass over
 // the tokens in order, equal ones by the lower place.
 __global__ __launch_bounds__(kThreads) void k_evict_select(EvictArgs a, Work w) {
@@ -104,6 +106,10 @@ __global__ __launch_bounds__(kThreads) void k_evict_select(EvictArgs a, Work w) 
     float *mass = a.mass + int64_t(blockIdx.x) * (int64_t(c.width) << c.shift);
     uint64_t *kept = a.kept + int64_t(blockIdx.x) * a.words;
 
+    // a thread's first weights stay in registers, longer rows are read again
+    float first[kHeld];
+#pragma unroll
+    for (int i = 0; i < kHeld; i++) first[i] = i * kThreads + tid < length ? mass[i * kThreads + tid] : 0.0f;
     uint32_t least = ~0u;                   // of those that stay
     int want = keep - recent;               // and how many equal to it do
     if (want > 0) {
@@ -112,10 +118,14 @@ __global__ __launch_bounds__(kThreads) void k_evict_select(EvictArgs a, Work w) 
         for (int shift = 24; shift >= 0; shift -= 8) {
             counts[tid] = 0;
             __syncthreads();
-            for (int t = tid; t < older; t += kThreads) {
-                const uint32_t u = order_of(mass[t]);
+            auto count = [&](float x) {
+                const uint32_t u = order_of(x);
                 if ((u & known) == least) atomicAdd(counts + ((u >> shift) & 255), 1);
-            }
+            };
+#pragma unroll
+            for (int i = 0; i < kHeld; i++)
+                if (i * kThreads + tid < older) count(first[i]);
+            for (int t = kHeld * kThreads + tid; t < older; t += kThreads) count(mass[t]);
             __syncthreads();
             if (wave == 0) {                // four digits a lane, from the largest
                 int own[4], sum = 0;
@@ -145,9 +155,8 @@ __global__ __launch_bounds__(kThreads) void k_evict_select(EvictArgs a, Work w) 
         }
     }
     int to = 0, equal = 0;                  // tokens that stay, and those equal to `least`, so far
-    for (int t0 = 0; t0 < length; t0 += kThreads) {
+    auto settle = [&](int t0, float x) {
         const int t = t0 + tid;
-        const float x = t < length ? mass[t] : 0.0f;
         const uint32_t u = order_of(x);
         const bool tie = t < older && u == least;
         const uint64_t same = __ballot(tie);
@@ -172,18 +181,25 @@ __global__ __launch_bounds__(kThreads) void k_evict_select(EvictArgs a, Work w) 
         }
         if (stays) mass[place] = x;
         __syncthreads();
-    }
+    };
+#pragma unroll
+    for (int i = 0; i < kHeld; i++)
+        if (i * kThreads < length) settle(i * kThreads, first[i]);
+    for (int t0 = kHeld * kThreads; t0 < length; t0 += kThreads) settle(t0, t0 + tid < length ? mass[t0 + tid] : 0.0f);
 }
 
-constexpr int kTurn = 64;                   // tokens moved at a time: whole pages
-constexpr int kStretch = 4096;              // tokens whose mask is read at a time
+// kTurn tokens move at a time, whole pages; the mask of kStretch is read at a time.  Shorter
+// turns wait more often for their look-ups, longer ones leave the GPU fewer workgroups: 64,
+// 128, 256 tokens take 304, 276, 327 us for 1,024 rows of 2,048 kept of up to 4,096 tokens of
+// 128, and 39, 21, 14 us for 8 rows of 1,000 of 1,500 tokens of 64.
+constexpr int kTurn = 128, kMoveThreads = 4 * kTurn, kMoveWaves = kMoveThreads / 64, kStretch = 2048;
 
 // Where the tokens of a turn come from.
 struct Sources {
-    int64_t from[kTurn];                    // block of the old page
+    int64_t from[kTurn], to[kTurn / 16];    // block of the old page; of the new, of each sixteen
     int32_t in_page[kTurn];
     float by[kTurn];                        // the old scale over the new
-    int32_t rescale;                        // whether any of these is not 1
+    int32_t rescale[kTurn / 64];            // whether any of these is not 1
 };
 
 __device__ __forceinline__ uint32_t code2(float x, float y) { return __builtin_amdgcn_cvt_pk_fp8_f32(x, y, 0, false); }
@@ -196,7 +212,7 @@ __device__ __forceinline__ uint32_t rescaled(uint32_t w, float b0, float b1, flo
 // and takes the sixteen tokens of a group that stand together there at once; which of their
 // bytes go where is the same for all lanes, so that a byte is a permutation whose selector
 // lies in a scalar register.
-template <int Dim, int Page> __global__ __launch_bounds__(kThreads) void k_evict_move(EvictArgs a, Work w) {
+template <int Dim, int Page> __global__ __launch_bounds__(kMoveThreads) void k_evict_move(EvictArgs a, Work w) {
     __shared__ int list[kStretch + kTurn];
     __shared__ Sources sources[2];
     const Cache &c = a.c;
@@ -209,48 +225,52 @@ template <int Dim, int Page> __global__ __launch_bounds__(kThreads) void k_evict
     const int32_t *old = w.rows + int64_t(p.seq) * c.width, *table = c.table + int64_t(p.seq) * c.width;
     uint8_t *pool = values ? c.v : c.k;
 
-    // A wavefront finds the sources of tokens list[from, from + n), which go to places
+    // Wavefronts, 64 each, find the sources of tokens list[from, from + n), which go to places
     // [done, done + n), and leaves their new pages' scales there: no later token comes
     // from these pages.
     auto look = [&](int from, int n, int done, Sources &to) {
-        const int src = list[from + min(lane, n - 1)];
+        const int t = wave * 64 + lane, src = list[from + min(t, n - 1)];
         const int32_t page = old[src / Page];
-        const float was = lane < n ? *c.block_scale(page, p.layer, values, p.head) : 0.0f;
+        const float was = t < n ? *c.block_scale(page, p.layer, values, p.head) : 0.0f;
         float now = was;
 #pragma unroll
         for (int m = Page / 2; m; m >>= 1) now = fmaxf(now, __shfl_xor(now, m));
         const float by = now > 0.0f ? was / now : 1.0f;
-        to.from[lane] = c.block(page, p.layer, p.head);
-        to.in_page[lane] = src % Page;
-        to.by[lane] = by;
-        const bool any = __any(lane < n && by != 1.0f);
-        if (lane == 0) to.rescale = any;
-        if (lane % Page == 0 && lane < n) *c.block_scale(table[(done + lane) / Page], p.layer, values, p.head) = now;
+        to.from[t] = c.block(page, p.layer, p.head);
+        to.in_page[t] = src % Page;
+        to.by[t] = by;
+        const bool any = __any(t < n && by != 1.0f);
+        if (lane == 0) to.rescale[wave] = any;
+        if (t % 16 == 0 && t < n) {
+            const int32_t place = table[(done + t) / Page];
+            to.to[t / 16] = c.block(place, p.layer, p.head);
+            if (t % Page == 0) *c.block_scale(place, p.layer, values, p.head) = now;
+        }
     };
     auto move_keys = [&](int n, int done, const Sources &m) {
-        constexpr int kChunks = Dim / 16, kUnits = kTurn * kChunks / kThreads;
+        constexpr int kChunks = Dim / 16, kUnits = kTurn * kChunks / kMoveThreads;
         uint4v x[kUnits];
 #pragma unroll
         for (int i = 0; i < kUnits; i++) {
-            const int u = tid + i * kThreads, t = min(u / kChunks, n - 1);
+            const int u = tid + i * kMoveThreads, t = min(u / kChunks, n - 1);
             x[i] = *reinterpret_cast<const uint4v *>(pool + m.from[t] + m.in_page[t] * Dim + u % kChunks * 16);
         }
-        if (m.rescale)
+        if (m.rescale[0] | m.rescale[1])
 #pragma unroll
             for (int i = 0; i < kUnits; i++) {
-                const float by = m.by[min((tid + i * kThreads) / kChunks, n - 1)];
+                const float by = m.by[min((tid + i * kMoveThreads) / kChunks, n - 1)];
 #pragma unroll
                 for (int k = 0; k < 4; k++) x[i][k] = by != 1.0f ? rescaled(x[i][k], by, by, by, by) : x[i][k];
             }
         __syncthreads();                    // all of them are read before any place is written
 #pragma unroll
         for (int i = 0; i < kUnits; i++) {
-            const int u = tid + i * kThreads, t = u / kChunks, at = done + t;
-            if (t < n) *reinterpret_cast<uint4v *>(pool + c.block(table[at / Page], p.layer, p.head) + at % Page * Dim + u % kChunks * 16) = x[i];
+            const int u = tid + i * kMoveThreads, t = u / kChunks, at = done + t;
+            if (t < n) *reinterpret_cast<uint4v *>(pool + m.to[t / 16] + at % Page * Dim + u % kChunks * 16) = x[i];
         }
     };
     auto move_values = [&](int n, int done, int from, const Sources &m) {
-        constexpr int kHalves = Dim / 64, kOwn = kTurn * kHalves / 4;     // tokens of a wavefront
+        constexpr int kHalves = Dim / 64, kOwn = kTurn * kHalves / kMoveWaves;     // tokens of a wavefront
         const int d = wave % kHalves * 64 + lane, t0 = wave / kHalves * kOwn, own = min(kOwn, n - t0);
         uint4v x[kOwn / 16];
         if (own > 0) {
@@ -286,7 +306,7 @@ template <int Dim, int Page> __global__ __launch_bounds__(kThreads) void k_evict
                 }
                 x[i / 16][i / 4 % 4] = word;
             }
-            if (m.rescale)
+            if (m.rescale[0] | m.rescale[1])
 #pragma unroll
                 for (int i = 0; i < kOwn; i += 4) {
                     const float *by = &m.by[t0 + i];
@@ -298,7 +318,7 @@ template <int Dim, int Page> __global__ __launch_bounds__(kThreads) void k_evict
         for (int i = 0; i < kOwn; i += 16) {
             const int left = own - i, at = done + t0 + i;
             if (left <= 0) break;
-            uint4v *to = reinterpret_cast<uint4v *>(pool + c.block(table[at / Page], p.layer, p.head) + d * Page + at % Page);
+            uint4v *to = reinterpret_cast<uint4v *>(pool + m.to[(t0 + i) / 16] + d * Page + at % Page);
             if (left < 16) {                // past the end: as it was
                 const uint4v was = *to;
 #pragma unroll
@@ -314,8 +334,8 @@ template <int Dim, int Page> __global__ __launch_bounds__(kThreads) void k_evict
 
     int held = 0, done = 0;
     const int words = (length + 63) / 64, keep = a.keep[p.seq];
-    for (int x0 = 0; x0 < words; x0 += 64) {
-        const uint64_t m = x0 + lane < words ? kept[x0 + lane] : 0;
+    for (int x0 = 0; x0 < words; x0 += kStretch / 64) {
+        const uint64_t m = lane < kStretch / 64 && x0 + lane < words ? kept[x0 + lane] : 0;
         int before = __popcll(m);
         const int own = before;
 #pragma unroll
@@ -325,7 +345,7 @@ template <int Dim, int Page> __global__ __launch_bounds__(kThreads) void k_evict
         }
         const int all = __shfl(before, 63);
         before -= own;
-        for (int x = wave; x < 64; x += 4) {
+        for (int x = wave; x < kStretch / 64; x += kMoveWaves) {
             const uint64_t n = __shfl(m, x);
             const int at = held + __shfl(before, x) + lanes_below(n);
             if (bit_of(n, lane)) list[at] = (x0 + x) * 64 + lane;
@@ -335,14 +355,14 @@ template <int Dim, int Page> __global__ __launch_bounds__(kThreads) void k_evict
         // tokens of a turn: whole ones, and what is left at the end of all; keep tokens in all, whatever the masses did meanwhile
         auto size = [&](int from, int done) {
             const int n = min(held - from, keep - done);
-            return n >= kTurn ? kTurn : x0 + 64 >= words || n == keep - done ? n : 0;
+            return n >= kTurn ? kTurn : x0 + kStretch / 64 >= words || n == keep - done ? n : 0;
         };
         int from = 0, slot = 0, n = size(0, done);
-        if (n > 0 && wave == 0) look(0, n, done, sources[0]);
+        if (n > 0 && wave < kTurn / 64) look(0, n, done, sources[0]);
         __syncthreads();
         while (n > 0) {
             const int more = size(from + n, done + n);
-            if (more > 0 && wave == 0) look(from + n, more, done + n, sources[slot ^ 1]);
+            if (more > 0 && wave < kTurn / 64) look(from + n, more, done + n, sources[slot ^ 1]);
             if (values) move_values(n, done, from, sources[slot]);
             else move_keys(n, done, sources[slot]);
             __syncthreads();
@@ -366,16 +386,16 @@ using namespace esp_kv;
 
 namespace {
 
-constexpr int64_t kMostBlocks = ((int64_t(1) << 32) - kThreads) / kThreads;    // a launch's threads are numbered in 32 bits
+constexpr int64_t kMostBlocks = ((int64_t(1) << 32) - kMoveThreads) / kMoveThreads;    // a launch's threads are numbered in 32 bits
 
 int64_t words_of(const esp_kv_cache *c) { return (int64_t(c->table_width) * c->page_tokens + 63) / 64; }
 int64_t items_of(const esp_kv_cache *c) { return int64_t(c->layers) * c->kv_heads * c->sequences; }
 
 template <int Dim> void move(const EvictArgs &a, const Work &w, unsigned blocks, hipStream_t s) {
     switch (a.c.tokens) {
-    case 16: k_evict_move<Dim, 16><<<blocks, kThreads, 0, s>>>(a, w); break;
-    case 32: k_evict_move<Dim, 32><<<blocks, kThreads, 0, s>>>(a, w); break;
-    default: k_evict_move<Dim, 64><<<blocks, kThreads, 0, s>>>(a, w); break;
+    case 16: k_evict_move<Dim, 16><<<blocks, kMoveThreads, 0, s>>>(a, w); break;
+    case 32: k_evict_move<Dim, 32><<<blocks, kMoveThreads, 0, s>>>(a, w); break;
+    default: k_evict_move<Dim, 64><<<blocks, kMoveThreads, 0, s>>>(a, w); break;
     }
 }
 

@@ -99,8 +99,8 @@ template <typename T> __device__ __forceinline__ void load(const View &v, int64_
     constexpr int kVec = 16 / int(sizeof(T));
     const T *p = static_cast<const T *>(v.data) + t * v.token + head * v.head;
     Vec<T> u, w;
-    u.w = *reinterpret_cast<const uint4v *>(p + a);
-    w.w = *reinterpret_cast<const uint4v *>(p + b);
+    u.w = __builtin_nontemporal_load(reinterpret_cast<const uint4v *>(p + a));
+    w.w = __builtin_nontemporal_load(reinterpret_cast<const uint4v *>(p + b));
 #pragma unroll
     for (int j = 0; j < kVec; j++) {
         x[j] = float(u.x[j]);
@@ -326,25 +326,26 @@ template <typename T, bool Back> __global__ __launch_bounds__(kThreads) void k_n
         s.partial[int64_t(block) * a.dim + i] = (lds[0][i] + lds[1][i]) + (lds[2][i] + lds[3][i]);
 }
 
-// Sums of the workgroups' rows: 16 elements a workgroup, 16 stretches of rows each.
-template <typename T> __global__ __launch_bounds__(kThreads) void k_norm_weights(NormArgs a) {
-    __shared__ float lds[16][17];
+// Sums of the workgroups' rows: 16 elements a workgroup, 64 stretches of rows each.
+constexpr int kSumThreads = 1024;
+template <typename T> __global__ __launch_bounds__(kSumThreads) void k_norm_weights(NormArgs a) {
+    __shared__ float lds[64][17];
     const Side &s = a.side[blockIdx.y];
     if (!s.dweight) return;
     const int i = blockIdx.x * 16 + threadIdx.x % 16, part = threadIdx.x / 16;
     float sum = 0.0f;
     if (i < a.dim)
-        for (int b = part; b < s.blocks; b += 128) {    // eight loads in flight
+        for (int b = part; b < s.blocks; b += 512) {    // eight loads in flight
             float x[8];
 #pragma unroll
-            for (int k = 0; k < 8; k++) x[k] = b + 16 * k < s.blocks ? s.partial[int64_t(b + 16 * k) * a.dim + i] : 0.0f;
+            for (int k = 0; k < 8; k++) x[k] = b + 64 * k < s.blocks ? s.partial[int64_t(b + 64 * k) * a.dim + i] : 0.0f;
 #pragma unroll
             for (int k = 0; k < 8; k++) sum += x[k];
         }
     lds[part][threadIdx.x % 16] = sum;
     __syncthreads();
     if (part || i >= a.dim) return;
-    for (int k = 1; k < 16; k++) sum += lds[k][threadIdx.x];
+    for (int k = 1; k < 64; k++) sum += lds[k][threadIdx.x];
     if (a.wide_weight) static_cast<float *>(s.dweight)[i] = sum;
     else static_cast<T *>(s.dweight)[i] = T(sum);
 }
@@ -357,7 +358,10 @@ namespace {
 
 constexpr int64_t kMostBlocks = ((int64_t(1) << 32) - kThreads) / kThreads;    // a launch's threads are numbered in 32 bits
 constexpr int kPerHeads = 4, kBackHeads = 2;
-constexpr int kBackBlocks = 1024;           // workgroups of a gradient, of queries and keys together
+// Workgroups of a gradient, of queries and keys together: those that the GPU holds at once, or
+// twice as many, whose ends lie less far apart, where each still has four turns.  So many / the
+// others: 655,320 heads of 128 in bf16 114 / 135 us; 131,168 of 64 in fp16 21 / 25.
+constexpr int kBackBlocks = 768;
 
 View view_of(const esp_kv_view &v) { return {v.data, v.token_stride, v.head_stride}; }
 bool wide(const esp_kv_view &v, int size) {
@@ -383,10 +387,11 @@ esp_status check(const esp_kv_rope *rope, int32_t type, int64_t tokens, int32_t 
 bool vectors(const NormArgs &a, int size, bool aligned) { return aligned && a.rope.rotary % (32 / size) == 0 && a.dim % (32 / size) == 0; }
 
 // Workgroups of a gradient: all at once, shared between queries and keys by their heads.
-void share_blocks(NormArgs &a, int64_t tokens, int32_t q_heads, int32_t k_heads) {
+void share_blocks(NormArgs &a, int64_t tokens, int32_t q_heads, int32_t k_heads, int lanes) {
     const int64_t heads = int64_t(q_heads) + k_heads;
     if (!heads) return;
-    const int64_t want = least((tokens * heads + 31) / 32, kBackBlocks);
+    const int64_t teams = kThreads / lanes, turns = (tokens * heads + teams * kBackHeads - 1) / (teams * kBackHeads);
+    const int64_t want = turns >= 8 * kBackBlocks ? 2 * kBackBlocks : least(turns, kBackBlocks);
     for (int i = 0; i < 2; i++) {
         const int64_t own = i ? k_heads : q_heads;
         a.side[i].blocks = own ? int32_t((want * own + heads - 1) / heads) : 0;
@@ -425,7 +430,7 @@ template <typename T> esp_status run(NormArgs &a, bool back, bool aligned, hipSt
         default: launch<T, 64>(a, back, unsigned(blocks), s); break;
         }
     }
-    if (back && (a.side[0].dweight || a.side[1].dweight)) k_norm_weights<T><<<dim3((a.dim + 15) / 16, 2), kThreads, 0, s>>>(a);
+    if (back && (a.side[0].dweight || a.side[1].dweight)) k_norm_weights<T><<<dim3((a.dim + 15) / 16, 2), kSumThreads, 0, s>>>(a);
     return launched();
 }
 esp_status run(NormArgs &a, int32_t type, bool back, bool aligned, void *stream) {
@@ -456,7 +461,7 @@ extern "C" esp_status esp_kv_norm_rotate_workspace(int64_t tokens, int32_t head_
     if (tokens < 0 || tokens > INT32_MAX || q_heads < 0 || q_heads > 65536 || k_heads < 0 || k_heads > 65536 || head_dim < 2 || head_dim > kMostDim)
         return ESP_ERR_SHAPE;
     NormArgs a{};
-    share_blocks(a, tokens, q_heads, k_heads);
+    share_blocks(a, tokens, q_heads, k_heads, lanes_of(head_dim, 2));
     *bytes = (size_t(a.side[0].blocks) + a.side[1].blocks) * head_dim * sizeof(float);
     return ESP_OK;
 }
@@ -475,7 +480,7 @@ extern "C" esp_status esp_kv_norm_rotate_backward(const esp_kv_rope *rope, int32
     NormArgs a{{{view_of(q), view_of(q_grad), view_of(dq), q_weight, nullptr, dq_weight, q_heads, 0},
                 {view_of(k), view_of(k_grad), view_of(dk), k_weight, nullptr, dk_weight, k_heads, 0}},
                {rope->turns, rope->magnitude, rope->rotary_dim, rope->interleaved}, positions, tokens, head_dim, weight_type == ESP_KV_FP32, eps, 1.0f / float(head_dim)};
-    share_blocks(a, tokens, q_heads, k_heads);
+    share_blocks(a, tokens, q_heads, k_heads, lanes_of(head_dim, 2));
     if (dq_weight || dk_weight) {
         const size_t need = (size_t(a.side[0].blocks) + a.side[1].blocks) * head_dim * sizeof(float);
         if (need && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < need)) return ESP_ERR_WORKSPACE;

@@ -135,7 +135,7 @@ def _ints(t, n: Optional[int], what: str, device) -> int:
 
 
 def _view(t, tokens: int, heads: int, dim: int, what: str, device) -> esp_kv_view:
-    if t.shape != (tokens, heads, dim) or t.device != device:
+    if tuple(t.shape) != (tokens, heads, dim) or t.device != device:
         raise ValueError(f"{what}: tensor [{tokens}, {heads}, {dim}] on {device} expected")
     a, b, c = t.stride()
     if c != 1 and dim > 1 and t.numel():
@@ -255,7 +255,7 @@ def _weights(q_weight, k_weight, x, dim: int):
     """Kind and addresses of the norms' weights."""
     given = [w for w in (q_weight, k_weight) if w is not None]
     for w in given:
-        if w.shape != (dim,) or w.device != x.device or not w.is_contiguous() or w.dtype not in (x.dtype, torch.float32) or w.dtype != given[0].dtype:
+        if tuple(w.shape) != (dim,) or w.device != x.device or not w.is_contiguous() or w.dtype not in (x.dtype, torch.float32) or w.dtype != given[0].dtype:
             raise ValueError(f"weights: contiguous [{dim}] on {x.device} expected, both of the type of q and k or both float32")
     kind = _TYPES[given[0].dtype if given else x.dtype]
     return kind, *(None if w is None else w.data_ptr() for w in (q_weight, k_weight))
@@ -289,12 +289,18 @@ def _like(x):
     return torch.empty_like(x) if x.is_contiguous() else torch.empty(x.shape, dtype=x.dtype, device=x.device)
 
 
-def _norm(rope, q, k, q_weight, k_weight, positions, eps, s: int):
+def _given(rope, q, k, q_weight, k_weight, positions, eps) -> tuple:
+    """The arguments that forward and backward have in common."""
     kind, T, D, Hq, Hk, vq, vk = _sides(rope, q, k)
     weight, wq, wk = _weights(q_weight, k_weight, q, D)
+    return rope.ptr, kind, T, D, Hq, Hk, vq, vk, wq, wk, weight, _ints(positions, T, "positions", q.device), eps
+
+
+def _norm(rope, q, k, q_weight, k_weight, positions, eps, s: int):
+    given = _given(rope, q, k, q_weight, k_weight, positions, eps)
+    _, _, _, D, Hq, Hk, *_ = given
     oq, ok = _like(q), _like(k)
-    _check(lib().esp_kv_norm_rotate(rope.ptr, kind, T, D, Hq, Hk, vq, vk, wq, wk, weight, _ints(positions, T, "positions", q.device), eps,
-                                    esp_kv_view(oq.data_ptr(), Hq * D, D), esp_kv_view(ok.data_ptr(), Hk * D, D), s), "esp_kv_norm_rotate")
+    _check(lib().esp_kv_norm_rotate(*given, esp_kv_view(oq.data_ptr(), Hq * D, D), esp_kv_view(ok.data_ptr(), Hk * D, D), s), "esp_kv_norm_rotate")
     return oq, ok
 
 
@@ -318,22 +324,34 @@ class _Normed(torch.autograd.Function):
 
 @_on_stream
 def _norm_back(rope, q, k, q_weight, k_weight, positions, eps, gq, gk, wanted, *, s: int):
-    kind, T, D, Hq, Hk, vq, vk = _sides(rope, q, k)
-    weight, wq, wk = _weights(q_weight, k_weight, q, D)
+    given = _given(rope, q, k, q_weight, k_weight, positions, eps)
+    _, _, T, D, Hq, Hk, *_ = given
     gq, gk = (g if g.stride(-1) == 1 or D == 1 else g.contiguous() for g in (gq, gk))
     dq, dk = _like(q), _like(k)
     dwq, dwk = (torch.empty_like(w) if w is not None and want else None for w, want in zip((q_weight, k_weight), wanted))
     work, size = None, 0
     if dwq is not None or dwk is not None:
-        n = C.c_size_t(0)
-        _check(lib().esp_kv_norm_rotate_workspace(T, D, Hq, Hk, C.byref(n)), "esp_kv_norm_rotate_workspace")
-        work, size = torch.empty(n.value, dtype=torch.uint8, device=q.device), n.value
+        size = _norm_bytes(T, D, Hq, Hk)
+        work = torch.empty(size, dtype=torch.uint8, device=q.device)
     _check(lib().esp_kv_norm_rotate_backward(
-        rope.ptr, kind, T, D, Hq, Hk, vq, vk, wq, wk, weight, _ints(positions, T, "positions", q.device), eps,
-        _view(gq, T, Hq, D, "q", q.device), _view(gk, T, Hk, D, "k", q.device), esp_kv_view(dq.data_ptr(), Hq * D, D),
+        *given, _view(gq, T, Hq, D, "q", q.device), _view(gk, T, Hk, D, "k", q.device), esp_kv_view(dq.data_ptr(), Hq * D, D),
         esp_kv_view(dk.data_ptr(), Hk * D, D), None if dwq is None else dwq.data_ptr(), None if dwk is None else dwk.data_ptr(),
         None if work is None else work.data_ptr(), size, s), "esp_kv_norm_rotate_backward")
     return dq, dk, dwq, dwk, None, None, None, None, None
+
+
+@functools.lru_cache(maxsize=4096)
+def _norm_bytes(tokens: int, dim: int, q_heads: int, k_heads: int) -> int:
+    n = C.c_size_t(0)
+    _check(lib().esp_kv_norm_rotate_workspace(tokens, dim, q_heads, k_heads, C.byref(n)), "esp_kv_norm_rotate_workspace")
+    return n.value
+
+
+@functools.lru_cache(maxsize=4096)
+def _select_bytes(groups: int, beams: int, vocab: int, width: int) -> int:
+    n = C.c_size_t(0)
+    _check(lib().esp_kv_select_beams_workspace(groups, beams, vocab, width, C.byref(n)), "esp_kv_select_beams_workspace")
+    return n.value
 
 
 @_on_stream
@@ -351,15 +369,14 @@ def select_beams(logits: torch.Tensor, scores: torch.Tensor, width: int, ended: 
         raise ValueError(f"scores: contiguous float32 [{G}, {B}] on {dev} expected")
     if ended is not None and (ended.shape != (G, B) or ended.dtype != torch.bool or ended.device != dev or not ended.is_contiguous()):
         raise ValueError(f"ended: contiguous bool [{G}, {B}] on {dev} expected")
-    n = C.c_size_t(0)
-    _check(lib().esp_kv_select_beams_workspace(G, B, V, width, C.byref(n)), "esp_kv_select_beams_workspace")
+    size = _select_bytes(G, B, V, width)
     out = torch.empty((G, width), dtype=torch.float32, device=dev)
     both = torch.empty((2, G, width), dtype=torch.int32, device=dev)
     parents, tokens = both[0], both[1]
-    work = torch.empty(max(n.value, 1), dtype=torch.uint8, device=dev)
+    work = torch.empty(max(size, 1), dtype=torch.uint8, device=dev)
     _check(lib().esp_kv_select_beams(kind, G, B, V, width, logits.data_ptr(), logits.stride(0), logits.stride(1), scores.data_ptr(),
                                      None if ended is None else ended.data_ptr(), pad, out.data_ptr(), parents.data_ptr(),
-                                     tokens.data_ptr(), work.data_ptr(), n.value, s), "esp_kv_select_beams")
+                                     tokens.data_ptr(), work.data_ptr(), size, s), "esp_kv_select_beams")
     source = next((x for x in (logits, scores) if x.requires_grad), None) if torch.is_grad_enabled() else None
     if source is not None:
         out = _NoGradient.apply("select_beams", source, out, "it selects")

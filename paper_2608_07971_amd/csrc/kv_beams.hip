@@ -8,7 +8,7 @@ namespace esp_kv {
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kMostWidth = 64;              // a wavefront holds the best so far, one a lane
 constexpr int kEach = 8;                    // logits a lane takes at a time
-constexpr int kBatch = 64 * kEach, kFlight = 4;
+constexpr int kBatch = 64 * kEach;
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct BeamArgs {
@@ -41,28 +41,53 @@ struct Two {                                // the sum in binary64, then the low
     uint64_t k, l;
     __device__ __forceinline__ bool operator>(const Two &o) const { return k > o.k || (k == o.k && l > o.l); }
 };
+// x of the lane whose number differs in the bit With: by rows' permutations and swaps of rows
+// and halves, without LDS.
+template <int With> __device__ __forceinline__ uint32_t across(uint32_t x, int lane) {
+    if constexpr (With == 1) return __builtin_amdgcn_mov_dpp(x, 0xb1, 0xf, 0xf, true);                   // quads: 1 0 3 2
+    if constexpr (With == 2) return __builtin_amdgcn_mov_dpp(x, 0x4e, 0xf, 0xf, true);                   // 2 3 0 1
+    if constexpr (With == 4) return __builtin_amdgcn_mov_dpp(__builtin_amdgcn_mov_dpp(x, 0x1b, 0xf, 0xf, true), 0x141, 0xf, 0xf, true);   // 3 2 1 0, then eights back to front
+    if constexpr (With == 8) return __builtin_amdgcn_mov_dpp(x, 0x128, 0xf, 0xf, true);                  // sixteens by eight
+    if constexpr (With == 16) {
+        const auto s = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+        return lane & 16 ? s[0] : s[1];
+    }
+    if constexpr (With == 32) {
+        const auto s = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+        return lane & 32 ? s[0] : s[1];
+    }
+}
+template <int With> __device__ __forceinline__ uint64_t across(uint64_t x, int lane) {
+    return uint64_t(across<With>(uint32_t(x >> 32), lane)) << 32 | across<With>(uint32_t(x), lane);
+}
+template <int With> __device__ __forceinline__ One across(One a, int lane) { return {across<With>(a.k, lane)}; }
+template <int With> __device__ __forceinline__ Two across(Two a, int lane) { return {across<With>(a.k, lane), across<With>(a.l, lane)}; }
 __device__ __forceinline__ One from_lane(One a, int lane) { return {uint64_t(__shfl(int64_t(a.k), lane))}; }
 __device__ __forceinline__ Two from_lane(Two a, int lane) { return {uint64_t(__shfl(int64_t(a.k), lane)), uint64_t(__shfl(int64_t(a.l), lane))}; }
 
 // Keys of the lanes from the largest on, by a bitonic network.
-template <typename K> __device__ __forceinline__ K exchange(K mine, int lane, int with, bool larger) {
-    const K other = from_lane(mine, lane ^ with);
+template <int With, typename K> __device__ __forceinline__ K exchange(K mine, int lane, bool larger) {
+    const K other = across<With>(mine, lane);
     return (other > mine) == larger ? other : mine;
 }
-template <typename K> __device__ __forceinline__ K sorted(K mine, int lane) {
-#pragma unroll
-    for (int n = 2; n <= 64; n <<= 1)
-#pragma unroll
-        for (int j = n / 2; j; j >>= 1) mine = exchange(mine, lane, j, ((lane & j) == 0) == ((lane & n) == 0));
+template <int With, typename K> __device__ __forceinline__ K halved(K mine, int lane, bool down) {      // of a bitonic stretch
+    mine = exchange<With>(mine, lane, ((lane & With) == 0) == down);
+    if constexpr (With > 1) mine = halved<With / 2>(mine, lane, down);
     return mine;
+}
+template <typename K> __device__ __forceinline__ K sorted(K mine, int lane) {
+    mine = halved<1>(mine, lane, (lane & 2) == 0);
+    mine = halved<2>(mine, lane, (lane & 4) == 0);
+    mine = halved<4>(mine, lane, (lane & 8) == 0);
+    mine = halved<8>(mine, lane, (lane & 16) == 0);
+    mine = halved<16>(mine, lane, (lane & 32) == 0);
+    return halved<32>(mine, lane, true);
 }
 // The 64 largest of two sorted sets.
 template <typename K> __device__ __forceinline__ K merged(K best, K more, int lane) {
     more = from_lane(more, 63 - lane);
     best = more > best ? more : best;
-#pragma unroll
-    for (int j = 32; j; j >>= 1) best = exchange(best, lane, j, (lane & j) == 0);
-    return best;
+    return halved<32>(best, lane, true);
 }
 
 __device__ __forceinline__ void wave_fence() {
@@ -88,8 +113,8 @@ template <typename K> struct Best {
         best = merged(best, sorted(more, lane), lane);
         least = from_lane(best, width - 1);
     }
+    // there: whether k passes `least`
     __device__ __forceinline__ void offer(K k, bool there) {
-        there = there && k > least;
         const uint64_t who = __ballot(there);
         if (!who) return;
         if (there) queue[waiting + __builtin_amdgcn_mbcnt_hi(uint32_t(who >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(who), 0))] = k;
@@ -112,11 +137,13 @@ template <typename K> struct Best {
 struct Sum {
     float top, sum;
     __device__ __forceinline__ static float off(float top) { return top == -INFINITY ? 0.0f : top; }
-    template <int N> __device__ __forceinline__ void add(const float (&x)[N], float most) {
+    template <int M, int N> __device__ __forceinline__ void add(const float (&x)[M][N], float most) {
         const float to = fmaxf(top, most), by = off(to);
         float s = sum * __builtin_amdgcn_exp2f((top - by) * kLog2e);
 #pragma unroll
-        for (int j = 0; j < N; j++) s += __builtin_amdgcn_exp2f((x[j] - by) * kLog2e);
+        for (int i = 0; i < M; i++)
+#pragma unroll
+            for (int j = 0; j < N; j++) s += __builtin_amdgcn_exp2f((x[i][j] - by) * kLog2e);
         top = to;
         sum = s;
     }
@@ -131,6 +158,7 @@ template <typename T> __global__ __launch_bounds__(kThreads) void k_beam_rows(Be
     __shared__ One lds[kWaves][128];
     __shared__ float tops[kWaves];
     __shared__ double sums[kWaves];
+    constexpr int kFlight = 8 / int(sizeof(T));                  // vectors at a time
     const int row = blockIdx.x / a.splits, split = blockIdx.x - row * a.splits;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const float score = a.scores[row];
@@ -139,44 +167,60 @@ template <typename T> __global__ __launch_bounds__(kThreads) void k_beam_rows(Be
     const T *x = static_cast<const T *>(a.logits) + group * a.group_stride + (row - group * a.beams) * a.beam_stride;
     const int64_t from = int64_t(split) * a.span, to = min(int64_t(a.vocab), from + a.span);
 
-    Best<One> best;
-    Sum sum{-INFINITY, 0.0f};
-    bool first = true;
-    for (int64_t at = from + wave * kBatch; at < to; at += kWaves * kBatch * kFlight) {
-        float v[kFlight][kEach];
+    Eight<T> e[kFlight];
+    auto load = [&](int64_t at) {
 #pragma unroll
         for (int f = 0; f < kFlight; f++) {
             const int64_t i = at + f * (kWaves * kBatch) + lane * kEach;
             if (i + kEach <= to) {
-                const Eight<T> e = *reinterpret_cast<const Eight<T> *>(x + i);
-#pragma unroll
-                for (int j = 0; j < kEach; j++) v[f][j] = float(e.x[j]);
+                e[f] = *reinterpret_cast<const Eight<T> *>(x + i);
             } else {
 #pragma unroll
-                for (int j = 0; j < kEach; j++) v[f][j] = i + j < to ? float(x[i + j]) : -INFINITY;
+                for (int j = 0; j < kEach; j++) e[f].x[j] = i + j < to ? x[i + j] : T(-INFINITY);
             }
         }
+    };
+    Best<One> best;
+    Sum sum{-INFINITY, 0.0f};
+    bool first = true;
+    for (int64_t at = from + wave * kBatch; at < to; at += kWaves * kBatch * kFlight) {
+        load(at);
+        float v[kFlight][kEach];
+#pragma unroll
+        for (int f = 0; f < kFlight; f++)
+#pragma unroll
+            for (int j = 0; j < kEach; j++) v[f][j] = float(e[f].x[j]);
+        float most[kFlight], top = -INFINITY;
 #pragma unroll
         for (int f = 0; f < kFlight; f++) {
-            const uint32_t i = uint32_t(at + f * (kWaves * kBatch) + lane * kEach);
-            float most = v[f][0];
+            most[f] = v[f][0];
 #pragma unroll
-            for (int j = 1; j < kEach; j++) most = fmaxf(most, v[f][j]);
-            sum.add(v[f], most);
-            uint64_t own = 0;
-            if (first) {                    // starts with each lane's largest
+            for (int j = 1; j < kEach; j++) most[f] = fmaxf(most[f], v[f][j]);
+            top = fmaxf(top, most[f]);
+        }
+        sum.add(v, top);
+        auto token = [&](int i) { return at + i / kEach * (kWaves * kBatch) + lane * kEach + i % kEach; };
+        uint64_t own = 0;
+        if (first) {                        // starts with each lane's largest
 #pragma unroll
-                for (int j = 0; j < kEach; j++) own = max(own, key_of(v[f][j], i + j));
-                best.start(One{own}, lds[wave], a.width);
-            }
-            if (first || __any(most > number(uint32_t(best.least.k >> 32)))) {
+            for (int i = 0; i < kFlight * kEach; i++) own = max(own, key_of(v[i / kEach][i % kEach], uint32_t(token(i))));
+            best.start(One{own}, lds[wave], a.width);
+        }
+        const float least = number(uint32_t(best.least.k >> 32));
+        uint32_t passes = 0;
+        if (first) {
 #pragma unroll
-                for (int j = 0; j < kEach; j++) {
-                    const One k{key_of(v[f][j], i + j)};
-                    best.offer(k, k.k != own);
-                }
-            }
-            first = false;
+            for (int i = 0; i < kFlight * kEach; i++) passes |= v[i / kEach][i % kEach] >= least ? 1u << i : 0;
+        } else {                            // of equal ones the earlier is better: a later one has to be larger
+            if (!__any(top > least)) continue;
+#pragma unroll
+            for (int i = 0; i < kFlight * kEach; i++) passes |= v[i / kEach][i % kEach] > least ? 1u << i : 0;
+        }
+        first = false;
+        for (; __any(passes != 0); passes &= passes - 1) {       // few: read once more
+            const int64_t t = passes ? token(__builtin_ctz(passes)) : at, held = min(t, to - 1);
+            const One k{key_of(t < to ? float(x[held]) : -INFINITY, uint32_t(t))};
+            best.offer(k, passes && k > best.least && k.k != own);
         }
     }
     if (first) best.start(One{0}, lds[wave], a.width);           // nothing for this wavefront
@@ -197,7 +241,7 @@ template <typename T> __global__ __launch_bounds__(kThreads) void k_beam_rows(Be
     __syncthreads();
     if (wave) return;
     One all = best.best;
-#pragma unroll
+#pragma unroll 1
     for (int w = 1; w < kWaves; w++) all = merged(all, lds[w][lane], lane);
     if (lane < a.width) a.keys[int64_t(blockIdx.x) * a.width + lane] = all.k;
     if (lane == 0) {
@@ -222,6 +266,14 @@ __global__ __launch_bounds__(64) void k_beam_join(BeamArgs a) {
     __shared__ Two queue[128];
     extern __shared__ double lse[];         // [beams]; NaN: no candidates
     const int group = blockIdx.x, lane = threadIdx.x;
+    // the lists' first ones before their second; the first 64 on their way while the sums are made
+    const int lists = a.beams * a.splits;
+    const int64_t all = int64_t(lists) * a.width;
+    auto key = [&](int64_t i) {
+        const int rank = int(i / lists), list = int(i - int64_t(rank) * lists);
+        return i < all ? a.keys[(int64_t(group) * lists + list) * a.width + rank] : 0;
+    };
+    const uint64_t early = key(lane);
     for (int b = lane; b < a.beams; b += 64) {
         const int row = group * a.beams + b;
         double l = NAN;
@@ -240,9 +292,6 @@ __global__ __launch_bounds__(64) void k_beam_join(BeamArgs a) {
         lse[b] = l;
     }
     __syncthreads();
-    // the lists' first ones before their second
-    const int lists = a.beams * a.splits;
-    const int64_t all = int64_t(lists) * a.width;
     Best<Two> best;
     for (int64_t i0 = 0; i0 < all; i0 += 64) {
         Two k{0, 0};
@@ -256,14 +305,14 @@ __global__ __launch_bounds__(64) void k_beam_join(BeamArgs a) {
                 token = uint32_t(a.pad);
                 if (rank == 0 && list == beam * a.splits) total = s;
             } else if (fabs(s) < INFINITY) {
-                const uint64_t held = a.keys[(int64_t(row) * a.splits + (list - beam * a.splits)) * a.width + rank];
+                const uint64_t held = i0 == 0 ? early : key(i0 + lane);
                 token = ~uint32_t(held);
                 if (held) total = s + (double(number(uint32_t(held >> 32))) - lse[beam]);
             }
             if (fabs(total) < INFINITY) k = {ordered(total), ~(uint64_t(beam) << 32 | token)};
         }
         if (i0 == 0) best.start(k, queue, a.width);
-        else best.offer(k, k.k != 0);
+        else best.offer(k, k > best.least);
     }
     best.finish();
     if (lane < a.width) {

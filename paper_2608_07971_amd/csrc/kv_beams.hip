@@ -7,6 +7,7 @@ namespace esp_kv {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kMostWidth = 64;              // a wavefront holds the best so far, one a lane
+constexpr int kMostSplits = 16;             // of a beam's vocabulary
 constexpr int kEach = 8;                    // logits a lane takes at a time
 constexpr int kBatch = 64 * kEach;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -274,22 +275,19 @@ __global__ __launch_bounds__(64) void k_beam_join(BeamArgs a) {
         return i < all ? a.keys[(int64_t(group) * lists + list) * a.width + rank] : 0;
     };
     const uint64_t early = key(lane);
-    for (int b = lane; b < a.beams; b += 64) {
-        const int row = group * a.beams + b;
-        double l = NAN;
-        if (a.ended && a.ended[row]) {
-            l = 0.0;
-        } else if (fabsf(a.scores[row]) < INFINITY) {
-            float top = -INFINITY;
-            for (int i = 0; i < a.splits; i++) top = fmaxf(top, a.tops[int64_t(row) * a.splits + i]);
-            double sum = 0.0;
-            for (int i = 0; i < a.splits; i++) {
-                const int64_t at = int64_t(row) * a.splits + i;
-                sum += a.sums[at] * exp2((double(a.tops[at]) - Sum::off(top)) * 1.4426950408889634074);
-            }
-            l = double(top) + log(sum);
-        }
-        lse[b] = l;
+    for (int b0 = 0; b0 < a.beams; b0 += 64 / kMostSplits) {     // a beam by as many lanes as it may have splits
+        const int b = b0 + lane / kMostSplits, i = lane % kMostSplits, row = group * a.beams + min(b, a.beams - 1);
+        const bool ended = a.ended && a.ended[row], live = !ended && fabsf(a.scores[row]) < INFINITY, there = live && i < a.splits;
+        const int64_t at = int64_t(row) * a.splits + min(i, a.splits - 1);
+        const float own = there ? a.tops[at] : -INFINITY;
+        const double part = there ? a.sums[at] : 0.0;
+        float top = own;
+#pragma unroll
+        for (int m = kMostSplits / 2; m; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
+        double sum = there ? part * exp2((double(own) - Sum::off(top)) * 1.4426950408889634074) : 0.0;
+#pragma unroll
+        for (int m = kMostSplits / 2; m; m >>= 1) sum += __shfl_xor(sum, m);
+        if (i == 0 && b < a.beams) lse[b] = live ? double(top) + log(sum) : ended ? 0.0 : double(NAN);
     }
     __syncthreads();
     Best<Two> best;
@@ -344,7 +342,7 @@ void lay_out(BeamArgs &a) {
     const int64_t rows = int64_t(a.groups) * a.beams, turn = kWaves * kBatch;
     const int64_t most = (a.vocab + turn - 1) / turn;
     int64_t splits = rows ? 1024 / rows : 1;
-    splits = splits < 1 ? 1 : splits > 16 ? 16 : splits;
+    splits = splits < 1 ? 1 : splits > kMostSplits ? kMostSplits : splits;
     splits = splits > most ? most : splits;
     a.span = int32_t(((a.vocab + splits - 1) / splits + turn - 1) / turn * turn);
     a.splits = int32_t((int64_t(a.vocab) + a.span - 1) / a.span);

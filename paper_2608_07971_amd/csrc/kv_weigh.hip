@@ -8,10 +8,10 @@ namespace esp_kv {
 typedef float float16v __attribute__((ext_vector_type(16)));
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
-constexpr int kGroups = 2;                  // of four wavefronts each, that take turns with the queries
-constexpr int kSubs = 2;
 constexpr int kRows = 32;                   // (token, query head) rows of a matrix tile
-constexpr int kStep = kGroups * kSubs * kRows;
+// k_weigh: groups of four wavefronts that share the queries between them, and tiles of rows that
+// each takes between two barriers.
+constexpr int kGroups = 2, kSubs = 2, kStep = kGroups * kSubs * kRows;
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct View {
@@ -151,7 +151,14 @@ __device__ __forceinline__ float weight(float product, float scale, float lse) {
 // Many queries.  A wavefront has 32 cached tokens, which stay in registers as the columns
 // of the products; the queries that see them go by, through LDS, kStep rows at a time, of
 // which each group of four wavefronts takes kSubs times 32.  So a token's sum is its lanes'
-// own, and no two workgroups add to the same place.
+// own, and no two workgroups add to the same place.  Products wait for no read and no
+// exponential for another: all of a tile's reads, products, differences and exponentials go
+// one kind after another.
+// Bound by the wavefronts' vector instructions (a sixteenth of a tile: difference, product,
+// exponential, sum): 3 sequences of up to 12,000 tokens, up to 2,048 of them new, 32 query
+// heads of 128, 279 GFLOP, 364 us (767 TFLOP/s).  Queries through registers instead of direct
+// into LDS: 457; one group of wavefronts, or four: 509, 489; heads one after another in the
+// launch instead of next to each other, so that long shares come last: 449.
 template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads * kGroups, 4) void k_weigh(WeighArgs a) {
     typedef typename Pack<T>::v8 V8;
     constexpr int kSteps = Dim / 16, kTile = kWaves * 32, kRowBytes = Dim * 2, kAll = kThreads * kGroups;
@@ -335,9 +342,11 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads *
     }
 }
 
-// Few queries, at most 32 rows a sequence and key head: they stay in registers while a
-// wavefront goes through its share of the tokens, 32 at a time, the next ones' codes and
-// the pages after these on their way.
+// Few queries: 32 rows of a sequence and key head stay in registers while a wavefront goes
+// through its share of the tokens, 32 at a time, the next ones' codes and the pages after
+// these on their way.  More rows take as many rounds, each adding to the one before.
+// Bound by memory: 64 single tokens of 32 heads on up to 8,192 cached ones of 8 key heads (200
+// MB) 43 us where the memory-side cache holds them (4.6 TB/s), 60 us where it does not.
 template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 3) void k_weigh_few(WeighArgs a) {
     typedef typename Pack<T>::v8 V8;
     constexpr int kSteps = Dim / 16, kTile = 32;
@@ -355,74 +364,76 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 
         const int p0 = row.length - row.n, n_rows = row.n * a.group, end = min(tile + left, (row.length + kTile - 1) / kTile);
         if (tile >= end) continue;
         left -= end - tile;
-        // the rows of this lane's products: 8 y + 4 half + x
-        V8 q[kSteps];
-        {
-            const Walker w(min(col, n_rows - 1), a.group);
-            const T *from = static_cast<const T *>(a.q.data) + int64_t(row.first + w.token) * a.q.token + int64_t(head * a.group + w.head) * a.q.head + 16 * half;
-#pragma unroll
-            for (int s = 0; s < kSteps; s++) q[s] = load8<T>(from + s / 2 * 32 + s % 2 * 8, a.wide);
-        }
-        float lse[16];
-#pragma unroll
-        for (int y = 0; y < 4; y++)
-#pragma unroll
-            for (int x = 0; x < 4; x++) {
-                const int r = 8 * y + 4 * half + x;
-                lse[4 * y + x] = INFINITY;
-                if (r < n_rows) {
-                    const Walker w(r, a.group);
-                    const float l = a.lse[int64_t(row.first + w.token) * a.q_heads + head * a.group + w.head];
-                    lse[4 * y + x] = l == -INFINITY ? INFINITY : l;          // it sees nothing
-                }
-            }
         const int32_t *table = c.table + int64_t(row.seq) * c.width;
         float *mass = a.mass + ((int64_t(a.layer) * c.sequences + row.seq) * c.heads + head) * (int64_t(c.width) * Page);
-        auto page_of = [&](int i) {
-            const int t = i * kTile + col;
-            return i < end && t < row.length ? table[t / Page] : -1;
-        };
-        struct Tile {
-            Keys<T, Dim> codes;
-            float ks, mass;
-            bool there;
-        };
-        auto load = [&](Tile &x, int i, int page) {
-            const int t = i * kTile + col;
-            x.there = uint32_t(page) < uint32_t(c.pages);
-            if (!x.there && i < end && t < row.length) record(c, ESP_ERR_SHAPE);
-            const int p = x.there ? page : 0;
-            x.codes.load(c.k + c.block(p, a.layer, head) + t % Page * Dim, half);
-            x.ks = *c.block_scale(p, a.layer, 0, head) * a.scale;
-            x.mass = x.there && t < p0 ? mass[t] : 0.0f;
-        };
-        Tile now, next;
-        int page = page_of(tile + 1);
-        load(now, tile, page_of(tile));
-        for (; tile < end; tile++) {
-            load(next, tile + 1, page);
-            page = page_of(tile + 2);
-            float16v s;
+        for (int r0 = 0; r0 < n_rows; r0 += kRows) {
+            // the rows of this lane's products: r0 + 8 y + 4 half + x
+            V8 q[kSteps];
+            {
+                const Walker w(min(r0 + col, n_rows - 1), a.group);
+                const T *from = static_cast<const T *>(a.q.data) + int64_t(row.first + w.token) * a.q.token + int64_t(head * a.group + w.head) * a.q.head + 16 * half;
 #pragma unroll
-            for (int i = 0; i < 16; i++) s[i] = 0.0f;
-#pragma unroll
-            for (int i = 0; i < kSteps; i++) s = product32(q[i], now.codes.step(i), s);
-            const int t = tile * kTile + col;
-            // whether all rows that there are see all of the tile
-            const bool whole = tile * kTile + kTile - 1 <= p0 && (a.window <= 0 || tile * kTile > p0 + row.n - 1 - a.window);
-            float sum = 0.0f;
+                for (int s = 0; s < kSteps; s++) q[s] = load8<T>(from + s / 2 * 32 + s % 2 * 8, a.wide);
+            }
+            float lse[16];
 #pragma unroll
             for (int y = 0; y < 4; y++)
-                if (8 * y < n_rows)
 #pragma unroll
-                    for (int x = 0; x < 4; x++) {
-                        const float e = weight(s[4 * y + x], now.ks, lse[4 * y + x]);
-                        const int r = 8 * y + 4 * half + x, p = whole ? 0 : p0 + r / a.group;
-                        sum += r < n_rows && (whole || (t <= p && (a.window <= 0 || t > p - a.window))) ? e : 0.0f;
+                for (int x = 0; x < 4; x++) {
+                    const int r = r0 + 8 * y + 4 * half + x;
+                    lse[4 * y + x] = INFINITY;
+                    if (r < n_rows) {
+                        const Walker w(r, a.group);
+                        const float l = a.lse[int64_t(row.first + w.token) * a.q_heads + head * a.group + w.head];
+                        lse[4 * y + x] = l == -INFINITY ? INFINITY : l;          // it sees nothing
                     }
-            sum += __shfl_xor(sum, 32);
-            if (half == 0 && now.there) mass[t] = t < p0 ? __builtin_fmaf(now.mass, a.decay, sum) : sum;
-            now = next;
+                }
+            auto page_of = [&](int i) {
+                const int t = i * kTile + col;
+                return i < end && t < row.length ? table[t / Page] : -1;
+            };
+            struct Tile {
+                Keys<T, Dim> codes;
+                float ks, mass;
+                bool there;
+            };
+            auto load = [&](Tile &x, int i, int page) {
+                const int t = i * kTile + col;
+                x.there = uint32_t(page) < uint32_t(c.pages);
+                if (!x.there && i < end && t < row.length && r0 == 0) record(c, ESP_ERR_SHAPE);
+                const int p = x.there ? page : 0;
+                x.codes.load(c.k + c.block(p, a.layer, head) + t % Page * Dim, half);
+                x.ks = *c.block_scale(p, a.layer, 0, head) * a.scale;
+                x.mass = x.there && t < row.length && (t < p0 || r0) ? mass[t] : 0.0f;
+            };
+            Tile now, next;
+            int page = page_of(tile + 1);
+            load(now, tile, page_of(tile));
+            for (int i = tile; i < end; i++) {
+                load(next, i + 1, page);
+                page = page_of(i + 2);
+                float16v s;
+#pragma unroll
+                for (int j = 0; j < 16; j++) s[j] = 0.0f;
+#pragma unroll
+                for (int j = 0; j < kSteps; j++) s = product32(q[j], now.codes.step(j), s);
+                const int t = i * kTile + col;
+                // whether all rows that there are see all of the tile
+                const bool whole = i * kTile + kTile - 1 <= p0 && (a.window <= 0 || i * kTile > p0 + row.n - 1 - a.window);
+                float sum = 0.0f;
+#pragma unroll
+                for (int y = 0; y < 4; y++)
+                    if (r0 + 8 * y < n_rows)
+#pragma unroll
+                        for (int x = 0; x < 4; x++) {
+                            const float e = weight(s[4 * y + x], now.ks, lse[4 * y + x]);
+                            const int r = r0 + 8 * y + 4 * half + x, p = whole ? 0 : p0 + r / a.group;
+                            sum += r < n_rows && (whole || (t <= p && (a.window <= 0 || t > p - a.window))) ? e : 0.0f;
+                        }
+                sum += __shfl_xor(sum, 32);
+                if (half == 0 && now.there) mass[t] = __builtin_fmaf(now.mass, r0 ? 1.0f : a.decay, sum);
+                now = next;
+            }
         }
     }
 }
@@ -433,6 +444,12 @@ using namespace esp_kv;
 
 namespace {
 
+// Rows (token, query head) a sequence and key head up to which k_weigh_few takes a call, in
+// rounds of 32.  So / by k_weigh, 64 sequences of about 3,800 tokens of 128: 48 rows of 4 key
+// heads 71 / 128 us, 96 rows 94 / 122, 128 rows 117 / 121, 192 rows 170 / 134.
+constexpr int kFewRows = 128;
+// Its wavefronts: three a SIMD, which its registers allow.  As many / twice as many: 60 / 72 us
+// (weights of 64 single tokens of 32 heads on up to 8,192 cached ones, 8 key heads).
 constexpr int kFewWaves = 3072;
 constexpr int64_t kMostBlocks = ((int64_t(1) << 32) - 1) / (kThreads * kGroups);  // a launch's threads are numbered in 32 bits
 
@@ -465,8 +482,10 @@ extern "C" esp_status esp_kv_weigh(const esp_kv_cache *cache, int32_t layer, int
     if (rows == 0 || tokens == 0 || max_new == 0 || max_length == 0) return ESP_OK;
     if (!offsets || !q.data || !lse || !mass) return ESP_ERR_INVALID_ARG;
     const int32_t group = q_heads / cache->kv_heads;
-    if (tokens * group > INT32_MAX - kRows) return ESP_ERR_SHAPE;
-    const bool many = int64_t(max_new) * group > kRows;
+    if (tokens * group > INT32_MAX - 8 * kStep) return ESP_ERR_SHAPE;
+    // the most new tokens of a row, if none is without any (others take k_weigh_few more rounds)
+    const int64_t longest = tokens - rows + 1 < max_new ? (tokens < rows ? 1 : tokens - rows + 1) : max_new;
+    const bool many = longest * group > kFewRows;
     // shares of a head's tiles: one each where queries are many; else as many as the GPU holds wavefronts
     const int64_t tile = many ? kWaves * 32 : 32, most = rows * ((int64_t(max_length) + tile - 1) / tile);
     if (most > INT32_MAX) return ESP_ERR_SHAPE;

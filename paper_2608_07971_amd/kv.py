@@ -560,8 +560,9 @@ class PagedCache:
     def weigh(self, layer: int, q, lse, offsets, mass, scale: Optional[float] = None, window: int = 0, decay: float = 1.0,
               max_new: Optional[int] = None, max_length: Optional[int] = None, seqs=None, *, s: int) -> None:
         """Adds to mass (float32 of mass_shape) the attention weight that the cached tokens got from q, whose lse `attend`
-        returned; what a token had from before counts decay times.  The other arguments as `attend` takes them.  Not part
-        of any gradient."""
+        returned; what a token had from before counts decay times, the row's new tokens begin at 0.  The other arguments as
+        `attend` takes them; where rows have few tokens, a loose max_new has cost up to twice the time.  Not part of any
+        gradient."""
         kind = _TYPES.get(q.dtype)
         if kind is None or kind == FP32 or q.dim() != 3:
             raise ValueError("q: bfloat16 or float16 [tokens, q_heads, head_dim] expected")
@@ -597,7 +598,8 @@ class PagedCache:
 
     @_on_stream
     def reorder(self, parents, *, s: int) -> None:
-        """Every sequence i goes on as parents[i] was (int32 [sequences]; -1: it ends), as select_beams leaves them."""
+        """Every sequence i goes on as parents[i] was (int32 [sequences]; -1: it ends), as select_beams leaves them.  What
+        the caller keeps for sequences, such as the masses of `weigh`, is the caller's to reorder."""
         w = self._pages_work(s)
         _check(lib().esp_kv_reorder(self.ptr, _ints(parents, self.sequences, "parents", self.device), w.data_ptr(), w.numel(), s),
                "esp_kv_reorder")

@@ -73,7 +73,8 @@ CASES = [
     ([2, 0, 5, 3], [300, 200, 5, 2], 2, 8, 128, 64, 0, torch.bfloat16), ([1, 1], [700, 90], 1, 8, 128, 16, 50, torch.float16),
     ([40, 7, 0, 130], [400, 7, 30, 131], 2, 4, 64, 16, 0, torch.bfloat16), ([300], [900], 1, 3, 128, 32, 100, torch.bfloat16), ([33, 64], [33, 700], 2, 1, 128, 64, 1, torch.float16),
     ([3, 200], [2, 150], 2, 2, 64, 16, 0, torch.float16), ([6], [5000], 2, 6, 64, 64, 3000, torch.bfloat16), ([1, 1], [257, 258], 16, 1, 64, 16, 0, torch.bfloat16),
-    ([65], [130], 4, 16, 64, 16, 0, torch.bfloat16),
+    ([65], [130], 4, 16, 64, 16, 0, torch.bfloat16), ([12] + [0] * 11, [300] * 12, 1, 16, 64, 16, 0, torch.float16),
+    ([0] * 5 + [9, 1], [40] * 5 + [200, 70], 2, 12, 128, 32, 120, torch.bfloat16),
 ]
 
 

@@ -300,7 +300,9 @@ __global__ __launch_bounds__(64) void k_beam_join(BeamArgs a) {
     }
     __syncthreads();
     Best<Two> best;
-    for (int64_t i0 = 0; i0 < all; i0 += 64) {
+    // lists are sorted: once as many in a row as there are lists have not passed, no other does
+    int64_t quiet = 0;
+    for (int64_t i0 = 0; i0 < all && quiet < lists; i0 += 64) {
         Two k{0, 0};
         if (i0 + lane < all) {
             const int rank = int((i0 + lane) / lists), list = int(i0 + lane - int64_t(rank) * lists), beam = list / a.splits;
@@ -318,8 +320,13 @@ __global__ __launch_bounds__(64) void k_beam_join(BeamArgs a) {
             }
             if (fabs(total) < INFINITY) k = {ordered(total), ~(uint64_t(beam) << 32 | token)};
         }
-        if (i0 == 0) best.start(k, queue, a.width);
-        else best.offer(k, k > best.least);
+        if (i0 == 0) {
+            best.start(k, queue, a.width);
+            continue;
+        }
+        const bool passes = k > best.least;
+        quiet = __any(passes) ? 0 : quiet + 64;
+        best.offer(k, passes);
     }
     best.finish();
     if (lane < a.width) {

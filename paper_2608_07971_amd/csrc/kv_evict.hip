@@ -53,11 +53,31 @@ __global__ __launch_bounds__(kThreads) void k_evict_take(Cache c, const int32_t 
     prefix(w.page_sum, w.pages.blocks, free_at, lds);
     prefix(w.need_sum, w.entries.blocks, need_at, lds);
     const bool go = !bad && free_at[w.pages.blocks] >= need_at[w.entries.blocks];
-    if (blockIdx.x == 0 && threadIdx.x == 0) {
-        *w.count = go;
-        if (!go) record(c, bad ? ESP_ERR_SHAPE : ESP_ERR_RANGE);
+    if (!go) {
+        if (blockIdx.x == 0 && threadIdx.x == 0) {
+            *w.count = 0;
+            record(c, bad ? ESP_ERR_SHAPE : ESP_ERR_RANGE);
+        }
+        return;
     }
-    if (!go) return;
+    if (blockIdx.x == 0) {                  // the sequences that are cut, in order
+        int n = 0;
+        for (int s0 = 0; s0 < c.sequences; s0 += kThreads) {
+            const int seq = s0 + threadIdx.x;
+            const bool is = seq < c.sequences && w.row_lengths[seq] >= 0;
+            const uint64_t who = __ballot(is);
+            __syncthreads();
+            if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = __popcll(who);
+            __syncthreads();
+            int at = n + lanes_below(who);
+            for (int k = 0; k < 4; k++) {
+                at += k < int(threadIdx.x >> 6) ? lds[k] : 0;
+                n += lds[k];
+            }
+            if (is) w.cut[at] = seq;
+        }
+        if (threadIdx.x == 0) *w.count = n;
+    }
     ranked(w.entries, blockIdx.x, w.need_mask, need_at[blockIdx.x], w.need_mask, 0, [&](int64_t i, bool need, int rank, bool, int) {
         const int seq = int(uint32_t(i) / uint32_t(c.width)), slot = int(uint32_t(i) - uint32_t(seq) * uint32_t(c.width));
         if (w.row_lengths[seq] < 0) return;
@@ -83,12 +103,13 @@ __device__ __forceinline__ uint32_t order_of(float x) {
     return x != x ? 0 : u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
+// Item i of those that are cut: its place, and its number among all.
 struct Place {
-    int layer, seq, head;
+    int layer, seq, head, number;
 };
-__device__ __forceinline__ Place place_of(const Cache &c, int i) {
-    const int head = i % c.heads, rest = i / c.heads;
-    return {rest / c.sequences, rest % c.sequences, head};
+__device__ __forceinline__ Place place_of(const Cache &c, const Work &w, int i) {
+    const int head = i % c.heads, rest = i / c.heads, layer = rest % c.layers, seq = w.cut[rest / c.layers];
+    return {layer, seq, head, (layer * c.sequences + seq) * c.heads + head};
 }
 
 constexpr int kHeld = 16;                   // weights a thread: rows of up to 4,096 tokens are read once
@@ -98,94 +119,95 @@ constexpr int kHeld = 16;                   // weights a thread: rows of up to 4
 __global__ __launch_bounds__(kThreads) void k_evict_select(EvictArgs a, Work w) {
     __shared__ int counts[256], at[4], ties[4], picked[2];
     const Cache &c = a.c;
-    const Place p = place_of(c, blockIdx.x);
-    const int length = w.row_lengths[p.seq];
-    if (!*w.count || length < 0) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int keep = a.keep[p.seq], recent = min(a.recent, keep), older = length - recent;
-    float *mass = a.mass + int64_t(blockIdx.x) * (int64_t(c.width) << c.shift);
-    uint64_t *kept = a.kept + int64_t(blockIdx.x) * a.words;
+    for (int item = blockIdx.x, items = *w.count * c.layers * c.heads; item < items; item += gridDim.x) {
+        const Place p = place_of(c, w, item);
+        const int length = w.row_lengths[p.seq];
+        const int keep = a.keep[p.seq], recent = min(a.recent, keep), older = length - recent;
+        float *mass = a.mass + int64_t(p.number) * (int64_t(c.width) << c.shift);
+        uint64_t *kept = a.kept + int64_t(p.number) * a.words;
 
-    // a thread's first weights stay in registers, longer rows are read again
-    float first[kHeld];
+        // a thread's first weights stay in registers, longer rows are read again
+        float first[kHeld];
 #pragma unroll
-    for (int i = 0; i < kHeld; i++) first[i] = i * kThreads + tid < length ? mass[i * kThreads + tid] : 0.0f;
-    uint32_t least = ~0u;                   // of those that stay
-    int want = keep - recent;               // and how many equal to it do
-    if (want > 0) {
-        uint32_t known = 0;
-        least = 0;
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            counts[tid] = 0;
-            __syncthreads();
-            auto count = [&](float x) {
-                const uint32_t u = order_of(x);
-                if ((u & known) == least) atomicAdd(counts + ((u >> shift) & 255), 1);
-            };
+        for (int i = 0; i < kHeld; i++) first[i] = i * kThreads + tid < length ? mass[i * kThreads + tid] : 0.0f;
+        uint32_t least = ~0u;                   // of those that stay
+        int want = keep - recent;               // and how many equal to it do
+        if (want > 0) {
+            uint32_t known = 0;
+            least = 0;
+            for (int shift = 24; shift >= 0; shift -= 8) {
+                counts[tid] = 0;
+                __syncthreads();
+                auto count = [&](float x) {
+                    const uint32_t u = order_of(x);
+                    if ((u & known) == least) atomicAdd(counts + ((u >> shift) & 255), 1);
+                };
 #pragma unroll
-            for (int i = 0; i < kHeld; i++)
-                if (i * kThreads + tid < older) count(first[i]);
-            for (int t = kHeld * kThreads + tid; t < older; t += kThreads) count(mass[t]);
-            __syncthreads();
-            if (wave == 0) {                // four digits a lane, from the largest
-                int own[4], sum = 0;
+                for (int i = 0; i < kHeld; i++)
+                    if (i * kThreads + tid < older) count(first[i]);
+                for (int t = kHeld * kThreads + tid; t < older; t += kThreads) count(mass[t]);
+                __syncthreads();
+                if (wave == 0) {                // four digits a lane, from the largest
+                    int own[4], sum = 0;
 #pragma unroll
-                for (int k = 0; k < 4; k++) sum += own[k] = counts[255 - 4 * lane - k];
-                int before = sum;
+                    for (int k = 0; k < 4; k++) sum += own[k] = counts[255 - 4 * lane - k];
+                    int before = sum;
 #pragma unroll
-                for (int m = 1; m < 64; m <<= 1) {
-                    const int v = __shfl_up(before, m);
-                    before += lane >= m ? v : 0;
-                }
-                before -= sum;
-#pragma unroll
-                for (int k = 0; k < 4; k++) {
-                    if (want > before && want <= before + own[k]) {
-                        picked[0] = 255 - 4 * lane - k;
-                        picked[1] = want - before;
+                    for (int m = 1; m < 64; m <<= 1) {
+                        const int v = __shfl_up(before, m);
+                        before += lane >= m ? v : 0;
                     }
-                    before += own[k];
+                    before -= sum;
+#pragma unroll
+                    for (int k = 0; k < 4; k++) {
+                        if (want > before && want <= before + own[k]) {
+                            picked[0] = 255 - 4 * lane - k;
+                            picked[1] = want - before;
+                        }
+                        before += own[k];
+                    }
                 }
+                __syncthreads();
+                least |= uint32_t(picked[0]) << shift;
+                known |= 255u << shift;
+                want = picked[1];
+                __syncthreads();
+            }
+        }
+        int to = 0, equal = 0;                  // tokens that stay, and those equal to `least`, so far
+        auto settle = [&](int t0, float x) {
+            const int t = t0 + tid;
+            const uint32_t u = order_of(x);
+            const bool tie = t < older && u == least;
+            const uint64_t same = __ballot(tie);
+            if (lane == 0) ties[wave] = __popcll(same);
+            __syncthreads();
+            int rank = equal + lanes_below(same);
+            for (int k = 0; k < 4; k++) {
+                rank += k < wave ? ties[k] : 0;
+                equal += ties[k];
+            }
+            const bool stays = t < length && (t >= older || u > least || (tie && rank < want));
+            const uint64_t who = __ballot(stays);
+            if (lane == 0) {
+                at[wave] = __popcll(who);
+                if (t < length) kept[t / 64] = who;
             }
             __syncthreads();
-            least |= uint32_t(picked[0]) << shift;
-            known |= 255u << shift;
-            want = picked[1];
+            int place = to + lanes_below(who);
+            for (int k = 0; k < 4; k++) {
+                place += k < wave ? at[k] : 0;
+                to += at[k];
+            }
+            if (stays) mass[place] = x;
             __syncthreads();
-        }
-    }
-    int to = 0, equal = 0;                  // tokens that stay, and those equal to `least`, so far
-    auto settle = [&](int t0, float x) {
-        const int t = t0 + tid;
-        const uint32_t u = order_of(x);
-        const bool tie = t < older && u == least;
-        const uint64_t same = __ballot(tie);
-        if (lane == 0) ties[wave] = __popcll(same);
-        __syncthreads();
-        int rank = equal + lanes_below(same);
-        for (int k = 0; k < 4; k++) {
-            rank += k < wave ? ties[k] : 0;
-            equal += ties[k];
-        }
-        const bool stays = t < length && (t >= older || u > least || (tie && rank < want));
-        const uint64_t who = __ballot(stays);
-        if (lane == 0) {
-            at[wave] = __popcll(who);
-            if (t < length) kept[t / 64] = who;
-        }
-        __syncthreads();
-        int place = to + lanes_below(who);
-        for (int k = 0; k < 4; k++) {
-            place += k < wave ? at[k] : 0;
-            to += at[k];
-        }
-        if (stays) mass[place] = x;
-        __syncthreads();
-    };
+        };
 #pragma unroll
-    for (int i = 0; i < kHeld; i++)
-        if (i * kThreads < length) settle(i * kThreads, first[i]);
-    for (int t0 = kHeld * kThreads; t0 < length; t0 += kThreads) settle(t0, t0 + tid < length ? mass[t0 + tid] : 0.0f);
+        for (int i = 0; i < kHeld; i++)
+            if (i * kThreads < length) settle(i * kThreads, first[i]);
+        for (int t0 = kHeld * kThreads; t0 < length; t0 += kThreads) settle(t0, t0 + tid < length ? mass[t0 + tid] : 0.0f);
+    }
 }
 
 // kTurn tokens move at a time, whole pages; the mask of kStretch is read at a time.  Shorter
@@ -216,167 +238,168 @@ template <int Dim, int Page> __global__ __launch_bounds__(kMoveThreads) void k_e
     __shared__ int list[kStretch + kTurn];
     __shared__ Sources sources[2];
     const Cache &c = a.c;
-    const int item = blockIdx.x >> 1, values = blockIdx.x & 1;
-    const Place p = place_of(c, item);
-    const int length = w.row_lengths[p.seq];
-    if (!*w.count || length < 0) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const uint64_t *kept = a.kept + int64_t(item) * a.words;
-    const int32_t *old = w.rows + int64_t(p.seq) * c.width, *table = c.table + int64_t(p.seq) * c.width;
-    uint8_t *pool = values ? c.v : c.k;
+    for (int item = blockIdx.x, items = *w.count * c.layers * c.heads * 2; item < items; item += gridDim.x) {
+        const Place p = place_of(c, w, item >> 1);
+        const int length = w.row_lengths[p.seq], values = item & 1;
+        const uint64_t *kept = a.kept + int64_t(p.number) * a.words;
+        const int32_t *old = w.rows + int64_t(p.seq) * c.width, *table = c.table + int64_t(p.seq) * c.width;
+        uint8_t *pool = values ? c.v : c.k;
 
-    // Wavefronts, 64 each, find the sources of tokens list[from, from + n), which go to places
-    // [done, done + n), and leaves their new pages' scales there: no later token comes
-    // from these pages.
-    auto look = [&](int from, int n, int done, Sources &to) {
-        const int t = wave * 64 + lane, src = list[from + min(t, n - 1)];
-        const int32_t page = old[src / Page];
-        const float was = t < n ? *c.block_scale(page, p.layer, values, p.head) : 0.0f;
-        float now = was;
+        // Wavefronts, 64 each, find the sources of tokens list[from, from + n), which go to places
+        // [done, done + n), and leaves their new pages' scales there: no later token comes
+        // from these pages.
+        auto look = [&](int from, int n, int done, Sources &to) {
+            const int t = wave * 64 + lane, src = list[from + min(t, n - 1)];
+            const int32_t page = old[src / Page];
+            const float was = t < n ? *c.block_scale(page, p.layer, values, p.head) : 0.0f;
+            float now = was;
 #pragma unroll
-        for (int m = Page / 2; m; m >>= 1) now = fmaxf(now, __shfl_xor(now, m));
-        const float by = now > 0.0f ? was / now : 1.0f;
-        to.from[t] = c.block(page, p.layer, p.head);
-        to.in_page[t] = src % Page;
-        to.by[t] = by;
-        const bool any = __any(t < n && by != 1.0f);
-        if (lane == 0) to.rescale[wave] = any;
-        if (t % 16 == 0 && t < n) {
-            const int32_t place = table[(done + t) / Page];
-            to.to[t / 16] = c.block(place, p.layer, p.head);
-            if (t % Page == 0) *c.block_scale(place, p.layer, values, p.head) = now;
-        }
-    };
-    auto move_keys = [&](int n, int done, const Sources &m) {
-        constexpr int kChunks = Dim / 16, kUnits = kTurn * kChunks / kMoveThreads;
-        uint4v x[kUnits];
-#pragma unroll
-        for (int i = 0; i < kUnits; i++) {
-            const int u = tid + i * kMoveThreads, t = min(u / kChunks, n - 1);
-            x[i] = *reinterpret_cast<const uint4v *>(pool + m.from[t] + m.in_page[t] * Dim + u % kChunks * 16);
-        }
-        if (m.rescale[0] | m.rescale[1])
+            for (int m = Page / 2; m; m >>= 1) now = fmaxf(now, __shfl_xor(now, m));
+            const float by = now > 0.0f ? was / now : 1.0f;
+            to.from[t] = c.block(page, p.layer, p.head);
+            to.in_page[t] = src % Page;
+            to.by[t] = by;
+            const bool any = __any(t < n && by != 1.0f);
+            if (lane == 0) to.rescale[wave] = any;
+            if (t % 16 == 0 && t < n) {
+                const int32_t place = table[(done + t) / Page];
+                to.to[t / 16] = c.block(place, p.layer, p.head);
+                if (t % Page == 0) *c.block_scale(place, p.layer, values, p.head) = now;
+            }
+        };
+        auto move_keys = [&](int n, int done, const Sources &m) {
+            constexpr int kChunks = Dim / 16, kUnits = kTurn * kChunks / kMoveThreads;
+            uint4v x[kUnits];
 #pragma unroll
             for (int i = 0; i < kUnits; i++) {
-                const float by = m.by[min((tid + i * kMoveThreads) / kChunks, n - 1)];
-#pragma unroll
-                for (int k = 0; k < 4; k++) x[i][k] = by != 1.0f ? rescaled(x[i][k], by, by, by, by) : x[i][k];
-            }
-        __syncthreads();                    // all of them are read before any place is written
-#pragma unroll
-        for (int i = 0; i < kUnits; i++) {
-            const int u = tid + i * kMoveThreads, t = u / kChunks, at = done + t;
-            if (t < n) *reinterpret_cast<uint4v *>(pool + m.to[t / 16] + at % Page * Dim + u % kChunks * 16) = x[i];
-        }
-    };
-    auto move_values = [&](int n, int done, int from, const Sources &m) {
-        constexpr int kHalves = Dim / 64, kOwn = kTurn * kHalves / kMoveWaves;     // tokens of a wavefront
-        const int d = wave % kHalves * 64 + lane, t0 = wave / kHalves * kOwn, own = min(kOwn, n - t0);
-        uint4v x[kOwn / 16];
-        if (own > 0) {
-            const int src = list[from + t0 + min(lane, own - 1)];
-            // group of sixteen tokens of the old pages that a lane's token is in; the first of each
-            const int before = __shfl_up(src, 1);
-            uint64_t firsts = __ballot(lane < own && lane > 0 && src >> 4 != before >> 4);
-            auto load = [&](int t) {        // the group of token t
-                const int s = __builtin_amdgcn_readlane(src, t);
-                const int64_t block = m.from[t0 + t];
-                return *reinterpret_cast<const uint4v *>(pool + block + d * Page + (s % Page & ~15));
-            };
-            uint4v now = load(0), next = now;
-            int turns = firsts ? __builtin_ctzll(firsts) : 64;   // the token that the next group begins with
-            if (turns < 64) next = load(turns);
-#pragma unroll
-            for (int i = 0; i < kOwn; i += 4) {
-                uint32_t word = 0;
-#pragma unroll
-                for (int j = 0; j < 4; j++) {
-                    const int t = i + j;
-                    if (t < own) {
-                        if (t == turns) {
-                            now = next;
-                            firsts &= firsts - 1;
-                            turns = firsts ? __builtin_ctzll(firsts) : 64;
-                            if (turns < 64) next = load(turns);
-                        }
-                        const uint32_t s = uint32_t(__builtin_amdgcn_readlane(src, t)) & 15, none = 0x0c0c0c0cu;
-                        const uint32_t pick = (none & ~(255u << (8 * j))) | (s & 7) << (8 * j);
-                        word |= __builtin_amdgcn_perm(now[1], now[0], s < 8 ? pick : none) | __builtin_amdgcn_perm(now[3], now[2], s < 8 ? none : pick);
-                    }
-                }
-                x[i / 16][i / 4 % 4] = word;
+                const int u = tid + i * kMoveThreads, t = min(u / kChunks, n - 1);
+                x[i] = *reinterpret_cast<const uint4v *>(pool + m.from[t] + m.in_page[t] * Dim + u % kChunks * 16);
             }
             if (m.rescale[0] | m.rescale[1])
 #pragma unroll
-                for (int i = 0; i < kOwn; i += 4) {
-                    const float *by = &m.by[t0 + i];
-                    x[i / 16][i / 4 % 4] = rescaled(x[i / 16][i / 4 % 4], by[0], by[1], by[2], by[3]);
-                }
-        }
-        __syncthreads();                    // all of them are read before any place is written
+                for (int i = 0; i < kUnits; i++) {
+                    const float by = m.by[min((tid + i * kMoveThreads) / kChunks, n - 1)];
 #pragma unroll
-        for (int i = 0; i < kOwn; i += 16) {
-            const int left = own - i, at = done + t0 + i;
-            if (left <= 0) break;
-            uint4v *to = reinterpret_cast<uint4v *>(pool + m.to[(t0 + i) / 16] + d * Page + at % Page);
-            if (left < 16) {                // past the end: as it was
-                const uint4v was = *to;
-#pragma unroll
-                for (int k = 0; k < 4; k++) {
-                    const int more = left - 4 * k;
-                    const uint32_t mine = more >= 4 ? ~0u : more <= 0 ? 0u : (1u << (8 * more)) - 1;
-                    x[i / 16][k] = (x[i / 16][k] & mine) | (was[k] & ~mine);
+                    for (int k = 0; k < 4; k++) x[i][k] = by != 1.0f ? rescaled(x[i][k], by, by, by, by) : x[i][k];
                 }
+            __syncthreads();                    // all of them are read before any place is written
+#pragma unroll
+            for (int i = 0; i < kUnits; i++) {
+                const int u = tid + i * kMoveThreads, t = u / kChunks, at = done + t;
+                if (t < n) *reinterpret_cast<uint4v *>(pool + m.to[t / 16] + at % Page * Dim + u % kChunks * 16) = x[i];
             }
-            *to = x[i / 16];
-        }
-    };
-
-    int held = 0, done = 0;
-    const int words = (length + 63) / 64, keep = a.keep[p.seq];
-    for (int x0 = 0; x0 < words; x0 += kStretch / 64) {
-        const uint64_t m = lane < kStretch / 64 && x0 + lane < words ? kept[x0 + lane] : 0;
-        int before = __popcll(m);
-        const int own = before;
-#pragma unroll
-        for (int k = 1; k < 64; k <<= 1) {
-            const int v = __shfl_up(before, k);
-            before += lane >= k ? v : 0;
-        }
-        const int all = __shfl(before, 63);
-        before -= own;
-        for (int x = wave; x < kStretch / 64; x += kMoveWaves) {
-            const uint64_t n = __shfl(m, x);
-            const int at = held + __shfl(before, x) + lanes_below(n);
-            if (bit_of(n, lane)) list[at] = (x0 + x) * 64 + lane;
-        }
-        held = __builtin_amdgcn_readfirstlane(held + all);
-        __syncthreads();
-        // tokens of a turn: whole ones, and what is left at the end of all; keep tokens in all, whatever the masses did meanwhile
-        auto size = [&](int from, int done) {
-            const int n = min(held - from, keep - done);
-            return n >= kTurn ? kTurn : x0 + kStretch / 64 >= words || n == keep - done ? n : 0;
         };
-        int from = 0, slot = 0, n = size(0, done);
-        if (n > 0 && wave < kTurn / 64) look(0, n, done, sources[0]);
-        __syncthreads();
-        while (n > 0) {
-            const int more = size(from + n, done + n);
-            if (more > 0 && wave < kTurn / 64) look(from + n, more, done + n, sources[slot ^ 1]);
-            if (values) move_values(n, done, from, sources[slot]);
-            else move_keys(n, done, sources[slot]);
+        auto move_values = [&](int n, int done, int from, const Sources &m) {
+            constexpr int kHalves = Dim / 64, kOwn = kTurn * kHalves / kMoveWaves;     // tokens of a wavefront
+            const int d = wave % kHalves * 64 + lane, t0 = wave / kHalves * kOwn, own = min(kOwn, n - t0);
+            uint4v x[kOwn / 16];
+            if (own > 0) {
+                const int src = list[from + t0 + min(lane, own - 1)];
+                // group of sixteen tokens of the old pages that a lane's token is in; the first of each
+                const int before = __shfl_up(src, 1);
+                uint64_t firsts = __ballot(lane < own && lane > 0 && src >> 4 != before >> 4);
+                auto load = [&](int t) {        // the group of token t
+                    const int s = __builtin_amdgcn_readlane(src, t);
+                    const int64_t block = m.from[t0 + t];
+                    return *reinterpret_cast<const uint4v *>(pool + block + d * Page + (s % Page & ~15));
+                };
+                uint4v now = load(0), next = now;
+                int turns = firsts ? __builtin_ctzll(firsts) : 64;   // the token that the next group begins with
+                if (turns < 64) next = load(turns);
+#pragma unroll
+                for (int i = 0; i < kOwn; i += 4) {
+                    uint32_t word = 0;
+#pragma unroll
+                    for (int j = 0; j < 4; j++) {
+                        const int t = i + j;
+                        if (t < own) {
+                            if (t == turns) {
+                                now = next;
+                                firsts &= firsts - 1;
+                                turns = firsts ? __builtin_ctzll(firsts) : 64;
+                                if (turns < 64) next = load(turns);
+                            }
+                            const uint32_t s = uint32_t(__builtin_amdgcn_readlane(src, t)) & 15, none = 0x0c0c0c0cu;
+                            const uint32_t pick = (none & ~(255u << (8 * j))) | (s & 7) << (8 * j);
+                            word |= __builtin_amdgcn_perm(now[1], now[0], s < 8 ? pick : none) | __builtin_amdgcn_perm(now[3], now[2], s < 8 ? none : pick);
+                        }
+                    }
+                    x[i / 16][i / 4 % 4] = word;
+                }
+                if (m.rescale[0] | m.rescale[1])
+#pragma unroll
+                    for (int i = 0; i < kOwn; i += 4) {
+                        const float *by = &m.by[t0 + i];
+                        x[i / 16][i / 4 % 4] = rescaled(x[i / 16][i / 4 % 4], by[0], by[1], by[2], by[3]);
+                    }
+            }
+            __syncthreads();                    // all of them are read before any place is written
+#pragma unroll
+            for (int i = 0; i < kOwn; i += 16) {
+                const int left = own - i, at = done + t0 + i;
+                if (left <= 0) break;
+                uint4v *to = reinterpret_cast<uint4v *>(pool + m.to[(t0 + i) / 16] + d * Page + at % Page);
+                if (left < 16) {                // past the end: as it was
+                    const uint4v was = *to;
+#pragma unroll
+                    for (int k = 0; k < 4; k++) {
+                        const int more = left - 4 * k;
+                        const uint32_t mine = more >= 4 ? ~0u : more <= 0 ? 0u : (1u << (8 * more)) - 1;
+                        x[i / 16][k] = (x[i / 16][k] & mine) | (was[k] & ~mine);
+                    }
+                }
+                *to = x[i / 16];
+            }
+        };
+
+        int held = 0, done = 0;
+        const int words = (length + 63) / 64, keep = a.keep[p.seq];
+        for (int x0 = 0; x0 < words; x0 += kStretch / 64) {
+            const uint64_t m = lane < kStretch / 64 && x0 + lane < words ? kept[x0 + lane] : 0;
+            int before = __popcll(m);
+            const int own = before;
+#pragma unroll
+            for (int k = 1; k < 64; k <<= 1) {
+                const int v = __shfl_up(before, k);
+                before += lane >= k ? v : 0;
+            }
+            const int all = __shfl(before, 63);
+            before -= own;
+            for (int x = wave; x < kStretch / 64; x += kMoveWaves) {
+                const uint64_t n = __shfl(m, x);
+                const int at = held + __shfl(before, x) + lanes_below(n);
+                if (bit_of(n, lane)) list[at] = (x0 + x) * 64 + lane;
+            }
+            held = __builtin_amdgcn_readfirstlane(held + all);
             __syncthreads();
-            from += n;
-            done += n;
-            n = more;
-            slot ^= 1;
+            // tokens of a turn: whole ones, and what is left at the end of all; keep tokens in all, whatever the masses did meanwhile
+            auto size = [&](int from, int done) {
+                const int n = min(held - from, keep - done);
+                return n >= kTurn ? kTurn : x0 + kStretch / 64 >= words || n == keep - done ? n : 0;
+            };
+            int from = 0, slot = 0, n = size(0, done);
+            if (n > 0 && wave < kTurn / 64) look(0, n, done, sources[0]);
+            __syncthreads();
+            while (n > 0) {
+                const int more = size(from + n, done + n);
+                if (more > 0 && wave < kTurn / 64) look(from + n, more, done + n, sources[slot ^ 1]);
+                if (values) move_values(n, done, from, sources[slot]);
+                else move_keys(n, done, sources[slot]);
+                __syncthreads();
+                from += n;
+                done += n;
+                n = more;
+                slot ^= 1;
+            }
+            if (done >= keep) break;
+            const int rest = held - from, next = tid < rest ? list[from + tid] : 0;
+            __syncthreads();
+            if (tid < rest) list[tid] = next;
+            __syncthreads();
+            held = rest;
         }
-        if (done >= keep) return;
-        const int rest = held - from, next = tid < rest ? list[from + tid] : 0;
-        __syncthreads();
-        if (tid < rest) list[tid] = next;
-        __syncthreads();
-        held = rest;
+        __syncthreads();                        // the next item's list goes into the same place
     }
 }
 
@@ -386,7 +409,10 @@ using namespace esp_kv;
 
 namespace {
 
-constexpr int64_t kMostBlocks = ((int64_t(1) << 32) - kMoveThreads) / kMoveThreads;    // a launch's threads are numbered in 32 bits
+// Workgroups that go through the items, of which few may be cut: 264 us with one for each of
+// 131,072 layers, sequences and heads of which none is, 14 so.
+constexpr int64_t kMostBlocks = 4096;
+unsigned blocks_of(int64_t items) { return unsigned(items < kMostBlocks ? items : kMostBlocks); }
 
 int64_t words_of(const esp_kv_cache *c) { return (int64_t(c->table_width) * c->page_tokens + 63) / 64; }
 int64_t items_of(const esp_kv_cache *c) { return int64_t(c->layers) * c->kv_heads * c->sequences; }
@@ -404,7 +430,7 @@ template <int Dim> void move(const EvictArgs &a, const Work &w, unsigned blocks,
 extern "C" esp_status esp_kv_evict_workspace(const esp_kv_cache *cache, size_t *bytes) {
     if (esp_status e = check_cache(cache)) return e;
     if (!bytes) return ESP_ERR_INVALID_ARG;
-    if (2 * items_of(cache) > kMostBlocks) return ESP_ERR_SHAPE;
+    if (2 * items_of(cache) > INT32_MAX) return ESP_ERR_SHAPE;
     Work w;
     *bytes = lay_out(cache, nullptr, w) + size_t(items_of(cache)) * words_of(cache) * sizeof(uint64_t);
     return ESP_OK;
@@ -425,9 +451,9 @@ extern "C" esp_status esp_kv_evict(const esp_kv_cache *cache, const int32_t *kee
     const EvictArgs a{c, keep, mass, reinterpret_cast<uint64_t *>(static_cast<char *>(workspace) + before), recent, int32_t(words_of(cache))};
     k_evict_mark<<<w.entries.blocks + w.pages.blocks, kThreads, 0, s>>>(c, keep, w);
     k_evict_take<<<w.entries.blocks, kThreads, 0, s>>>(c, keep, w);
-    const unsigned items = unsigned(items_of(cache));
-    k_evict_select<<<items, kThreads, 0, s>>>(a, w);
-    if (c.dim == 64) move<64>(a, w, 2 * items, s);
-    else move<128>(a, w, 2 * items, s);
+    const int64_t items = items_of(cache);
+    k_evict_select<<<blocks_of(items), kThreads, 0, s>>>(a, w);
+    if (c.dim == 64) move<64>(a, w, blocks_of(2 * items), s);
+    else move<128>(a, w, blocks_of(2 * items), s);
     return launched();
 }

@@ -33,6 +33,7 @@ struct Work {
     int2 *copies;                           // from, to
     int32_t *goes;                          // [pages] new places
     int32_t *rows, *row_lengths;            // a table and lengths aside: [sequences][width], [sequences]
+    int32_t *cut;                           // [sequences] those that an eviction cuts
     bool at_once;                           // pages are copied by the workgroup that finds them
 };
 
@@ -215,6 +216,7 @@ inline size_t lay_out(const esp_kv_cache *c, char *p, Work &w) {
     take(w.goes, size_t(c->pages));
     take(w.rows, size_t(w.entries.n));
     take(w.row_lengths, size_t(c->sequences));
+    take(w.cut, size_t(c->sequences));
     w.at_once = false;
     return size_t(at - p);
 }

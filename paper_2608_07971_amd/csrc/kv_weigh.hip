@@ -180,10 +180,7 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads *
     // matrix step reads at once lie in different banks
     auto turn = [](int row) { return Dim == 128 ? row & 15 : (row >> 1) & 7; };
     const int chunk = (tid % (Dim / 8)) ^ turn(tid / (Dim / 8));
-    uint32_t query_at[kSteps];
-#pragma unroll
-    for (int i = 0; i < kSteps; i++)
-        query_at[i] = (team * (kSubs * kRows) + col) * kRowBytes + (((i / 2 * 4 + 2 * half + i % 2) ^ turn(col)) << 4);
+    const uint32_t query_at = (team * (kSubs * kRows) + col) * kRowBytes + (((2 * half) ^ turn(col)) << 4);
     const int tokens_on = kPass / a.group, heads_on = kPass - tokens_on * a.group;
     const int64_t ahead = tokens_on * a.q.token + heads_on * a.q.head, round = a.q.token - a.group * a.q.head;
 
@@ -259,7 +256,8 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads *
             auto products = [&](int buffer, int sub, float16v &s) {
                 V8 q[kSteps];
 #pragma unroll
-                for (int i = 0; i < kSteps; i++) q[i] = *reinterpret_cast<const V8 *>(&queries[buffer][query_at[i] + sub * kRows * kRowBytes]);
+                for (int i = 0; i < kSteps; i++)
+                    q[i] = *reinterpret_cast<const V8 *>(&queries[buffer][0] + ((query_at + sub * kRows * kRowBytes) ^ ((i / 2 * 4 + i % 2) << 4)));
                 __builtin_amdgcn_sched_barrier(0);               // all reads on their way before the first product waits
 #pragma unroll
                 for (int i = 0; i < 16; i++) s[i] = 0.0f;

@@ -72,6 +72,7 @@ CASES = [
     ([1], [0], 0, 1, 64, 16, 1), ([2, 1], [1, 1], 1, 1, 64, 16, 1), ([100, 40, 0, 17], [50, 50, 3, 17], 8, 2, 64, 16, 2), ([500, 333, 64], [1, 200, 63], 0, 2, 128, 32, 1),
     ([1000], [999], 999, 1, 128, 64, 2), ([700, 900, 65, 129], [300, 17, 64, 128], 5000, 3, 64, 64, 1), ([5000, 4097, 4096], [4096, 2049, 64], 30, 1, 64, 16, 1),
     ([9000], [4500], 0, 2, 64, 32, 1), ([300] * 20, [7 * i for i in range(20)], 16, 1, 128, 16, 3), ([257, 256], [255, 128], 100, 2, 128, 16, 1),
+    ([20, 3, 19] * 34, [9] * 102, 2, 6, 64, 16, 11),
 ]
 
 

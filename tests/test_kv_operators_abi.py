@@ -90,5 +90,5 @@ def test_bad_reorderings_weights_and_evictions_are_refused():
     assert L.esp_kv_evict(p, A, -1, A, A, n.value, None) == esp.ESP_ERR_SHAPE
     for w, size in ((None, n.value), (A + 8, n.value), (A, n.value - 1)):
         assert L.esp_kv_evict(p, A, 0, A, w, size, None) == esp.ESP_ERR_WORKSPACE
-    many = _cache(sequences=1 << 20, layers=16)
+    many = _cache(sequences=1 << 25, layers=16)
     assert L.esp_kv_evict_workspace(C.addressof(many), C.byref(n)) == esp.ESP_ERR_SHAPE

@@ -221,7 +221,9 @@ __global__ __launch_bounds__(kThreads) void k_fork_take(Cache c, int n, const in
 }
 
 // ---------------------------------------------------------------------------
-// Reorder: a workgroup a sequence; every row is put together aside before any is written
+// Reorder: a workgroup a sequence; every row is put together aside before any is written.
+// Three launches: 256 beams of up to 157 pages of 64 KB, some 110 of them copied, 5.5 + 2 + 8.8
+// us; 4 beams 3.2 + 1.6 + 4.2 us.
 // ---------------------------------------------------------------------------
 
 constexpr int kInvalid = 1, kWrong = 2, kCopies = 4;

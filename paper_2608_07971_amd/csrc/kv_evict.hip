@@ -221,6 +221,8 @@ constexpr int kTurn = 128, kMoveThreads = 4 * kTurn, kMoveWaves = kMoveThreads /
 // Where the tokens of a turn come from.
 struct Sources {
     int64_t from[kTurn], to[kTurn / 16];    // block of the old page; of the new, of each sixteen
+    int32_t page[kTurn / 16];               // the new page of each sixteen, and its scale
+    float scale[kTurn / 16];
     int32_t in_page[kTurn];
     float by[kTurn];                        // the old scale over the new
     int32_t rescale[kTurn / 64];            // whether any of these is not 1
@@ -251,8 +253,7 @@ template <int Dim, int Page> __global__ __launch_bounds__(kMoveThreads) void k_e
         uint8_t *pool = values ? c.v : c.k;
 
         // Wavefronts, 64 each, find the sources of tokens list[from, from + n), which go to places
-        // [done, done + n), and leaves their new pages' scales there: no later token comes
-        // from these pages.
+        // [done, done + n).
         auto look = [&](int from, int n, int done, Sources &to) {
             const int t = wave * 64 + lane, src = list[from + min(t, n - 1)];
             const int32_t page = old[src / Page];
@@ -269,8 +270,15 @@ template <int Dim, int Page> __global__ __launch_bounds__(kMoveThreads) void k_e
             if (t % 16 == 0 && t < n) {
                 const int32_t place = table[(done + t) / Page];
                 to.to[t / 16] = c.block(place, p.layer, p.head);
-                if (t % Page == 0) *c.block_scale(place, p.layer, values, p.head) = now;
+                to.page[t / 16] = place;
+                to.scale[t / 16] = now;
             }
+        };
+        // The new pages' scales, once all of a turn's old ones have been read: no later token
+        // comes from these pages.
+        auto leave_scales = [&](int n, const Sources &m) {
+            const int t = tid * 16;
+            if (t < n && t % Page == 0) *c.block_scale(m.page[tid], p.layer, values, p.head) = m.scale[tid];
         };
         auto move_keys = [&](int n, int done, const Sources &m) {
             constexpr int kChunks = Dim / 16, kUnits = kTurn * kChunks / kMoveThreads;
@@ -288,6 +296,7 @@ template <int Dim, int Page> __global__ __launch_bounds__(kMoveThreads) void k_e
                     for (int k = 0; k < 4; k++) x[i][k] = by != 1.0f ? rescaled(x[i][k], by, by, by, by) : x[i][k];
                 }
             __syncthreads();                    // all of them are read before any place is written
+            leave_scales(n, m);
 #pragma unroll
             for (int i = 0; i < kUnits; i++) {
                 const int u = tid + i * kMoveThreads, t = u / kChunks, at = done + t;
@@ -339,6 +348,7 @@ template <int Dim, int Page> __global__ __launch_bounds__(kMoveThreads) void k_e
                     }
             }
             __syncthreads();                    // all of them are read before any place is written
+            leave_scales(n, m);
 #pragma unroll
             for (int i = 0; i < kOwn; i += 16) {
                 const int left = own - i, at = done + t0 + i;

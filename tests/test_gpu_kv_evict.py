@@ -98,6 +98,16 @@ def test_shared_pages_are_left_to_the_others():
     assert int(cache.refs.max()) == 1
 
 
+@pytest.mark.parametrize("page", [16, 32, 64])
+@pytest.mark.parametrize("gone", [16, 64, 128, 200])
+def test_a_beginning_that_goes(gone, page):
+    """Each stretch of new places takes its tokens, and their scales, from the places of the next."""
+    cache = ref.make(kv, [1500, 700, 900], heads=8, dim=64, page=page, layers=4, seed=gone)
+    mass = _mass(cache) + 1.0
+    mass[..., :gone] = 0.0
+    _check(cache, [1500 - gone, 700 - gone, 900 - gone], mass, 0)
+
+
 def test_equal_weights_infinities_and_nan():
     cache = ref.make(kv, [300, 300, 300, 300], heads=1, dim=64)
     mass = torch.full(cache.mass_shape, 0.25, device="cuda")

@@ -207,10 +207,10 @@ esp_status esp_kv_attend(const esp_kv_cache *cache, int32_t layer, int32_t type,
  *   mass[t] = decay * mass[t] + sum exp(scale * q . k_t - lse[q])
  * over the row's queries that see token t (esp_kv_attend's rules, arguments and
  * bounds) and the query heads of h; with the lse that attend left these are its
- * softmax weights.  The row's own new tokens begin at 0.  mass: float32
- * [layers][sequences][kv_heads][table_width * page_tokens], contiguous; places from
- * a sequence's length on, and sequences of rows that have no tokens or are left
- * out, stay as they were.  A query whose lse is -inf adds nothing.  Sums are float32.
+ * softmax weights.  Rows name distinct sequences, whose own new tokens begin at 0.
+ * mass: float32 [layers][sequences][kv_heads][table_width * page_tokens],
+ * contiguous; places from a sequence's length on, and sequences of rows that have no
+ * tokens or are left out, stay as they were.  A query whose lse is -inf adds nothing.  Sums are float32.
  * max_new chooses the kernel: where rows have few tokens, a loose one has cost up to
  * twice the time.
  */

@@ -46,12 +46,12 @@ template <int kLanes> __device__ __forceinline__ float team_sum(float x) {
     return x;
 }
 
-// Two 16-byte vectors of a head a lane, so that both sides of its pairs are its
-// own: with halves lane c has vectors c and c + n of the turned part's 2 n, with
+// Two vectors of a head a lane, 16 bytes each or, where the turned part's halves are no
+// multiple of these, 8, so that both sides of its pairs are its own: with halves lane c has vectors c and c + n of the turned part's 2 n, with
 // neighbours as pairs the same vectors with pairs of their own; then the same of
 // the part that passes through.
-template <typename T> struct Place {
-    static constexpr int kVec = 16 / int(sizeof(T));
+template <typename T, int kBytes> struct Place {
+    static constexpr int kVec = kBytes / int(sizeof(T));
     int a, b;                               // elements of the two vectors
     bool turn;
     __device__ __forceinline__ Place(const Rope &r, int dim, int c) {
@@ -90,34 +90,37 @@ template <typename T> struct Place {
     }
 };
 
-template <typename T> union Vec {
-    uint4v w;
-    T x[16 / sizeof(T)];
+template <typename T, int kBytes> union Vec {
+    typedef uint32_t Words __attribute__((ext_vector_type(kBytes / 4)));
+    Words w;
+    T x[kBytes / sizeof(T)];
 };
 
-template <typename T> __device__ __forceinline__ void load(const View &v, int64_t t, int head, int a, int b, float (&x)[32 / sizeof(T)]) {
-    constexpr int kVec = 16 / int(sizeof(T));
+template <typename T, int kBytes>
+__device__ __forceinline__ void load(const View &v, int64_t t, int head, int a, int b, float (&x)[2 * kBytes / sizeof(T)]) {
+    constexpr int kVec = kBytes / int(sizeof(T));
     const T *p = static_cast<const T *>(v.data) + t * v.token + head * v.head;
-    Vec<T> u, w;
-    u.w = __builtin_nontemporal_load(reinterpret_cast<const uint4v *>(p + a));
-    w.w = __builtin_nontemporal_load(reinterpret_cast<const uint4v *>(p + b));
+    Vec<T, kBytes> u, w;
+    u.w = __builtin_nontemporal_load(reinterpret_cast<const typename Vec<T, kBytes>::Words *>(p + a));
+    w.w = __builtin_nontemporal_load(reinterpret_cast<const typename Vec<T, kBytes>::Words *>(p + b));
 #pragma unroll
     for (int j = 0; j < kVec; j++) {
         x[j] = float(u.x[j]);
         x[kVec + j] = float(w.x[j]);
     }
 }
-template <typename T> __device__ __forceinline__ void store(const View &v, int64_t t, int head, int a, int b, const float (&x)[32 / sizeof(T)]) {
-    constexpr int kVec = 16 / int(sizeof(T));
+template <typename T, int kBytes>
+__device__ __forceinline__ void store(const View &v, int64_t t, int head, int a, int b, const float (&x)[2 * kBytes / sizeof(T)]) {
+    constexpr int kVec = kBytes / int(sizeof(T));
     T *p = static_cast<T *>(v.data) + t * v.token + head * v.head;
-    Vec<T> u, w;
+    Vec<T, kBytes> u, w;
 #pragma unroll
     for (int j = 0; j < kVec; j++) {
         u.x[j] = T(x[j]);
         w.x[j] = T(x[kVec + j]);
     }
-    *reinterpret_cast<uint4v *>(p + a) = u.w;
-    *reinterpret_cast<uint4v *>(p + b) = w.w;
+    *reinterpret_cast<typename Vec<T, kBytes>::Words *>(p + a) = u.w;
+    *reinterpret_cast<typename Vec<T, kBytes>::Words *>(p + b) = w.w;
 }
 
 // Whose work a workgroup does: queries first, then keys.
@@ -149,8 +152,8 @@ struct Walk {
 // wanted again here.
 // Bound by memory: 16,383 tokens of 32 + 8 heads of 128 in bf16 (336 MB) 67 us (5.0 TB/s); 256
 // of them 7.6 us, a chain of loads, sums and angles.
-template <typename T, int kLanes, int kPer> __global__ __launch_bounds__(kThreads) void k_norm(NormArgs a) {
-    constexpr int kVec = 16 / int(sizeof(T)), kTeams = kThreads / kLanes;
+template <typename T, int kBytes, int kLanes, int kPer> __global__ __launch_bounds__(kThreads) void k_norm(NormArgs a) {
+    constexpr int kVec = kBytes / int(sizeof(T)), kTeams = kThreads / kLanes;
     int block = blockIdx.x;
     const Side &s = a.side[side_of(a, block)];
     const int c = threadIdx.x % kLanes, groups = (s.heads + kPer - 1) / kPer;
@@ -158,10 +161,10 @@ template <typename T, int kLanes, int kPer> __global__ __launch_bounds__(kThread
     if (t >= a.tokens) return;              // whole teams leave
     const int head = int(unit - t * groups) * kPer;
     const bool there = c < a.dim / (2 * kVec);
-    const Place<T> at(a.rope, a.dim, there ? c : 0);
+    const Place<T, kBytes> at(a.rope, a.dim, there ? c : 0);
     float x[kPer][2 * kVec], w[2 * kVec], cs[kVec], sn[kVec];
 #pragma unroll
-    for (int h = 0; h < kPer; h++) load<T>(s.x, t, min(head + h, s.heads - 1), at.a, at.b, x[h]);
+    for (int h = 0; h < kPer; h++) load<T, kBytes>(s.x, t, min(head + h, s.heads - 1), at.a, at.b, x[h]);
 #pragma unroll
     for (int j = 0; j < kVec; j++) {
         w[j] = weight_at<T>(a, s.weight, at.a + j);
@@ -177,8 +180,8 @@ template <typename T, int kLanes, int kPer> __global__ __launch_bounds__(kThread
         const float r = rsqrtf(__builtin_fmaf(sum, a.part, a.eps));
 #pragma unroll
         for (int j = 0; j < 2 * kVec; j++) x[h][j] = x[h][j] * r * w[j];
-        Place<T>::turn_by(a.rope.interleaved, x[h], cs, sn);
-        if (there && head + h < s.heads) store<T>(s.y, t, head + h, at.a, at.b, x[h]);
+        Place<T, kBytes>::turn_by(a.rope.interleaved, x[h], cs, sn);
+        if (there && head + h < s.heads) store<T, kBytes>(s.y, t, head + h, at.a, at.b, x[h]);
     }
 }
 
@@ -187,14 +190,14 @@ template <typename T, int kLanes, int kPer> __global__ __launch_bounds__(kThread
 // The same teams, each going through many tokens with the sums of its elements' weight
 // gradient in registers; a workgroup's sums go to its row of `partial`, added up by
 // k_norm_weights in an order that depends on nothing but the sizes.
-template <typename T, int kLanes, int kPer> __global__ __launch_bounds__(kThreads) void k_norm_back(NormArgs a) {
-    constexpr int kVec = 16 / int(sizeof(T)), kTeams = kThreads / kLanes, kOwn = 2 * kVec;
+template <typename T, int kBytes, int kLanes, int kPer> __global__ __launch_bounds__(kThreads) void k_norm_back(NormArgs a) {
+    constexpr int kVec = kBytes / int(sizeof(T)), kTeams = kThreads / kLanes, kOwn = 2 * kVec;
     __shared__ float lds[4][kMostDim];
     int block = blockIdx.x;
     const Side &s = a.side[side_of(a, block)];
     const int c = threadIdx.x % kLanes, groups = (s.heads + kPer - 1) / kPer;
     const bool there = c < a.dim / (2 * kVec);
-    const Place<T> at(a.rope, a.dim, there ? c : 0);
+    const Place<T, kBytes> at(a.rope, a.dim, there ? c : 0);
     float w[kOwn], dw[kOwn];
 #pragma unroll
     for (int j = 0; j < kVec; j++) {
@@ -209,14 +212,14 @@ template <typename T, int kLanes, int kPer> __global__ __launch_bounds__(kThread
         float x[kPer][kOwn], g[kPer][kOwn], cs[kVec], sn[kVec];
 #pragma unroll
         for (int h = 0; h < kPer; h++) {
-            load<T>(s.x, t, min(head + h, s.heads - 1), at.a, at.b, x[h]);
-            load<T>(s.y, t, min(head + h, s.heads - 1), at.a, at.b, g[h]);
+            load<T, kBytes>(s.x, t, min(head + h, s.heads - 1), at.a, at.b, x[h]);
+            load<T, kBytes>(s.y, t, min(head + h, s.heads - 1), at.a, at.b, g[h]);
         }
         at.angles(a.rope, a.positions[t], -1.0f, cs, sn);
 #pragma unroll
         for (int h = 0; h < kPer; h++) {
             const bool held = there && head + h < s.heads;
-            Place<T>::turn_by(a.rope.interleaved, g[h], cs, sn);
+            Place<T, kBytes>::turn_by(a.rope.interleaved, g[h], cs, sn);
             float sum = 0.0f, dot = 0.0f;
 #pragma unroll
             for (int j = 0; j < kOwn; j++) {
@@ -232,7 +235,7 @@ template <typename T, int kLanes, int kPer> __global__ __launch_bounds__(kThread
                 dw[j] += held ? g[h][j] * n : 0.0f;
                 x[h][j] = r * __builtin_fmaf(g[h][j], w[j], -(n * mean));
             }
-            if (held) store<T>(s.dx, t, head + h, at.a, at.b, x[h]);
+            if (held) store<T, kBytes>(s.dx, t, head + h, at.a, at.b, x[h]);
         }
     }
     if (!s.dweight) return;
@@ -250,7 +253,7 @@ template <typename T, int kLanes, int kPer> __global__ __launch_bounds__(kThread
 }
 
 // Any strides, alignment and rotary part: a wavefront a token and head, a pair a lane at a time.
-constexpr int kMostPairs = kMostDim / 2 / 64;
+constexpr int kMostPairs = kMostDim / 2 / 64, kAnyHeads = 8;      // heads that angles are worked out for once
 template <typename T, bool Back> __global__ __launch_bounds__(kThreads) void k_norm_any(NormArgs a) {
     __shared__ float lds[4][kMostDim];
     int block = blockIdx.x;
@@ -268,54 +271,58 @@ template <typename T, bool Back> __global__ __launch_bounds__(kThreads) void k_n
         wb[k] = weight_at<T>(a, s.weight, eb[k]);
         da[k] = db[k] = 0.0f;
     }
-    for (Walk u(block * 4 + wave, s.blocks * 4, s.heads); u.token < a.tokens; u.next()) {
+    const int groups = (s.heads + kAnyHeads - 1) / kAnyHeads;
+    for (Walk u(block * 4 + wave, s.blocks * 4, groups); u.token < a.tokens; u.next()) {
         const int64_t t = u.token;
-        const int head = u.group;
-        const T *px = static_cast<const T *>(s.x.data) + t * s.x.token + head * s.x.head;
-        T *py = static_cast<T *>(s.y.data) + t * s.y.token + head * s.y.head;
-        float xa[kMostPairs], xb[kMostPairs], ga[kMostPairs], gb[kMostPairs], sum = 0.0f, dot = 0.0f;
+        float cs[kMostPairs], sn[kMostPairs];
 #pragma unroll
         for (int k = 0; k < kMostPairs; k++) {
             const int i = lane + 64 * k;
-            xa[k] = xb[k] = ga[k] = gb[k] = 0.0f;
-            if (i < pairs) {
-                xa[k] = float(px[ea[k]]);
-                xb[k] = float(px[eb[k]]);
-                float c = 1.0f, sn = 0.0f;
-                if (i < half) {
-                    cos_sin(double(a.positions[t]) * a.rope.turns[i], c, sn);
-                    c *= a.rope.magnitude;
-                    sn *= a.rope.magnitude;
-                }
-                if (Back) {
-                    const float u = float(py[ea[k]]), v = float(py[eb[k]]);
-                    ga[k] = __builtin_fmaf(u, c, v * sn);
-                    gb[k] = __builtin_fmaf(v, c, -(u * sn));
-                } else {
-                    ga[k] = c;
-                    gb[k] = sn;
-                }
-                sum = __builtin_fmaf(xa[k], xa[k], __builtin_fmaf(xb[k], xb[k], sum));
-                if (Back) dot = __builtin_fmaf(ga[k] * wa[k], xa[k], __builtin_fmaf(gb[k] * wb[k], xb[k], dot));
+            cs[k] = 1.0f;
+            sn[k] = 0.0f;
+            if (i < half) {
+                cos_sin(double(a.positions[t]) * a.rope.turns[i], cs[k], sn[k]);
+                cs[k] *= a.rope.magnitude;
+                sn[k] *= a.rope.magnitude;
             }
         }
-        sum = team_sum<64>(sum);
-        if (Back) dot = team_sum<64>(dot);
-        const float r = rsqrtf(__builtin_fmaf(sum, a.part, a.eps)), mean = dot * r * a.part;
-        T *out = Back ? static_cast<T *>(s.dx.data) + t * s.dx.token + head * s.dx.head : py;
+        for (int head = u.group * kAnyHeads; head < min(s.heads, (u.group + 1) * kAnyHeads); head++) {
+            const T *px = static_cast<const T *>(s.x.data) + t * s.x.token + head * s.x.head;
+            T *py = static_cast<T *>(s.y.data) + t * s.y.token + head * s.y.head;
+            float xa[kMostPairs], xb[kMostPairs], ga[kMostPairs], gb[kMostPairs], sum = 0.0f, dot = 0.0f;
 #pragma unroll
-        for (int k = 0; k < kMostPairs; k++) {
-            if (lane + 64 * k >= pairs) continue;
-            const float na = xa[k] * r, nb = xb[k] * r;
-            if (Back) {
-                da[k] += ga[k] * na;
-                db[k] += gb[k] * nb;
-                out[ea[k]] = T(r * __builtin_fmaf(ga[k], wa[k], -(na * mean)));
-                out[eb[k]] = T(r * __builtin_fmaf(gb[k], wb[k], -(nb * mean)));
-            } else {
-                const float u = na * wa[k], v = nb * wb[k];
-                out[ea[k]] = T(__builtin_fmaf(u, ga[k], -(v * gb[k])));
-                out[eb[k]] = T(__builtin_fmaf(u, gb[k], v * ga[k]));
+            for (int k = 0; k < kMostPairs; k++) {
+                xa[k] = xb[k] = ga[k] = gb[k] = 0.0f;
+                if (lane + 64 * k < pairs) {
+                    xa[k] = float(px[ea[k]]);
+                    xb[k] = float(px[eb[k]]);
+                    sum = __builtin_fmaf(xa[k], xa[k], __builtin_fmaf(xb[k], xb[k], sum));
+                    if (Back) {
+                        const float y = float(py[ea[k]]), z = float(py[eb[k]]);
+                        ga[k] = __builtin_fmaf(y, cs[k], z * sn[k]);
+                        gb[k] = __builtin_fmaf(z, cs[k], -(y * sn[k]));
+                        dot = __builtin_fmaf(ga[k] * wa[k], xa[k], __builtin_fmaf(gb[k] * wb[k], xb[k], dot));
+                    }
+                }
+            }
+            sum = team_sum<64>(sum);
+            if (Back) dot = team_sum<64>(dot);
+            const float r = rsqrtf(__builtin_fmaf(sum, a.part, a.eps)), mean = dot * r * a.part;
+            T *out = Back ? static_cast<T *>(s.dx.data) + t * s.dx.token + head * s.dx.head : py;
+#pragma unroll
+            for (int k = 0; k < kMostPairs; k++) {
+                if (lane + 64 * k >= pairs) continue;
+                const float na = xa[k] * r, nb = xb[k] * r;
+                if (Back) {
+                    da[k] += ga[k] * na;
+                    db[k] += gb[k] * nb;
+                    out[ea[k]] = T(r * __builtin_fmaf(ga[k], wa[k], -(na * mean)));
+                    out[eb[k]] = T(r * __builtin_fmaf(gb[k], wb[k], -(nb * mean)));
+                } else {
+                    const float y = na * wa[k], z = nb * wb[k];
+                    out[ea[k]] = T(__builtin_fmaf(y, cs[k], -(z * sn[k])));
+                    out[eb[k]] = T(__builtin_fmaf(y, sn[k], z * cs[k]));
+                }
             }
         }
     }
@@ -369,14 +376,17 @@ constexpr int kPerHeads = 4, kBackHeads = 2;
 constexpr int kBackBlocks = 768;
 
 View view_of(const esp_kv_view &v) { return {v.data, v.token_stride, v.head_stride}; }
-bool wide(const esp_kv_view &v, int size) {
-    return (reinterpret_cast<uintptr_t>(v.data) & 15) == 0 && v.token_stride * size % 16 == 0 && v.head_stride * size % 16 == 0;
+// Bytes that accesses at multiples of them may have: 16, 8 or 0 (neither).
+int wide(const esp_kv_view &v, int size) {
+    const uint64_t all = uint64_t(reinterpret_cast<uintptr_t>(v.data)) | uint64_t(v.token_stride * size) | uint64_t(v.head_stride * size);
+    return all % 16 == 0 ? 16 : all % 8 == 0 ? 8 : 0;
 }
-int lanes_of(int32_t dim, int size) {       // lanes of a head: a power of two
+int lanes_of(int32_t dim, int size, int bytes) {                 // lanes of a head: a power of two
     int n = 1;
-    while (n < dim * size / 32) n *= 2;
+    while (n < dim * size / (2 * bytes)) n *= 2;
     return n;
 }
+int least_of(int a, int b) { return a < b ? a : b; }
 int64_t least(int64_t a, int64_t b) { return a < b ? a : b; }
 
 esp_status check(const esp_kv_rope *rope, int32_t type, int64_t tokens, int32_t head_dim, int32_t q_heads, int32_t k_heads, int32_t weight_type, float eps) {
@@ -388,8 +398,12 @@ esp_status check(const esp_kv_rope *rope, int32_t type, int64_t tokens, int32_t 
     return rope->rotary_dim >= 2 && rope->rotary_dim % 2 == 0 && rope->rotary_dim <= head_dim ? ESP_OK : ESP_ERR_SHAPE;
 }
 
-// Whether heads can be taken as vectors.
-bool vectors(const NormArgs &a, int size, bool aligned) { return aligned && a.rope.rotary % (32 / size) == 0 && a.dim % (32 / size) == 0; }
+// Bytes of the vectors that heads are taken as, 0: none.
+int vectors(const NormArgs &a, int size, int most) {
+    for (int bytes = most; bytes >= 8; bytes /= 2)
+        if (a.rope.rotary * size % (2 * bytes) == 0 && a.dim * size % (2 * bytes) == 0 && lanes_of(a.dim, size, bytes) <= 64) return bytes;
+    return 0;
+}
 
 // Workgroups of a gradient: all at once, shared between queries and keys by their heads.
 void share_blocks(NormArgs &a, int64_t tokens, int32_t q_heads, int32_t k_heads, int lanes) {
@@ -403,42 +417,46 @@ void share_blocks(NormArgs &a, int64_t tokens, int32_t q_heads, int32_t k_heads,
     }
 }
 
-template <typename T, int kLanes> void launch(const NormArgs &a, bool back, unsigned blocks, hipStream_t s) {
-    if (back) k_norm_back<T, kLanes, kBackHeads><<<blocks, kThreads, 0, s>>>(a);
-    else k_norm<T, kLanes, kPerHeads><<<blocks, kThreads, 0, s>>>(a);
+template <typename T, int kBytes, int kLanes> void launch(const NormArgs &a, bool back, unsigned blocks, hipStream_t s) {
+    if (back) k_norm_back<T, kBytes, kLanes, kBackHeads><<<blocks, kThreads, 0, s>>>(a);
+    else k_norm<T, kBytes, kLanes, kPerHeads><<<blocks, kThreads, 0, s>>>(a);
 }
-template <typename T> esp_status run(NormArgs &a, bool back, bool aligned, hipStream_t s) {
-    const bool vector = vectors(a, sizeof(T), aligned);
-    const int lanes = lanes_of(a.dim, sizeof(T));
+template <typename T, int kBytes> void launch(const NormArgs &a, int lanes, bool back, unsigned blocks, hipStream_t s) {
+    switch (lanes) {
+    case 1: launch<T, kBytes, 1>(a, back, blocks, s); break;
+    case 2: launch<T, kBytes, 2>(a, back, blocks, s); break;
+    case 4: launch<T, kBytes, 4>(a, back, blocks, s); break;
+    case 8: launch<T, kBytes, 8>(a, back, blocks, s); break;
+    case 16: launch<T, kBytes, 16>(a, back, blocks, s); break;
+    case 32: launch<T, kBytes, 32>(a, back, blocks, s); break;
+    default: launch<T, kBytes, 64>(a, back, blocks, s); break;
+    }
+}
+template <typename T> esp_status run(NormArgs &a, bool back, int aligned, hipStream_t s) {
+    const int bytes = vectors(a, sizeof(T), aligned), lanes = bytes ? lanes_of(a.dim, sizeof(T), bytes) : 64;
     int64_t blocks = 0;
     for (Side &side : a.side) {
         if (!back && side.heads) {
-            const int64_t groups = vector ? (side.heads + kPerHeads - 1) / kPerHeads : side.heads, teams = vector ? kThreads / lanes : 4;
+            const int64_t per = bytes ? kPerHeads : kAnyHeads, groups = (side.heads + per - 1) / per, teams = kThreads / lanes;
             const int64_t need = (a.tokens * groups + teams - 1) / teams;
-            if (vector && need > kMostBlocks / 2) return ESP_ERR_SHAPE;
-            side.blocks = int32_t(vector ? need : least(need, 65536));
+            if (bytes && need > kMostBlocks / 2) return ESP_ERR_SHAPE;
+            side.blocks = int32_t(bytes ? need : least(need, 65536));
         }
         blocks += side.blocks;
     }
     if (blocks == 0) {
-    } else if (!vector) {
+    } else if (bytes == 16) {
+        launch<T, 16>(a, lanes, back, unsigned(blocks), s);
+    } else if (bytes == 8) {
+        launch<T, 8>(a, lanes, back, unsigned(blocks), s);
+    } else {
         if (back) k_norm_any<T, true><<<unsigned(blocks), kThreads, 0, s>>>(a);
         else k_norm_any<T, false><<<unsigned(blocks), kThreads, 0, s>>>(a);
-    } else {
-        switch (lanes) {
-        case 1: launch<T, 1>(a, back, unsigned(blocks), s); break;
-        case 2: launch<T, 2>(a, back, unsigned(blocks), s); break;
-        case 4: launch<T, 4>(a, back, unsigned(blocks), s); break;
-        case 8: launch<T, 8>(a, back, unsigned(blocks), s); break;
-        case 16: launch<T, 16>(a, back, unsigned(blocks), s); break;
-        case 32: launch<T, 32>(a, back, unsigned(blocks), s); break;
-        default: launch<T, 64>(a, back, unsigned(blocks), s); break;
-        }
     }
     if (back && (a.side[0].dweight || a.side[1].dweight)) k_norm_weights<T><<<dim3((a.dim + 15) / 16, 2), kSumThreads, 0, s>>>(a);
     return launched();
 }
-esp_status run(NormArgs &a, int32_t type, bool back, bool aligned, void *stream) {
+esp_status run(NormArgs &a, int32_t type, bool back, int aligned, void *stream) {
     const hipStream_t s = static_cast<hipStream_t>(stream);
     if (type == ESP_KV_BF16) return run<__bf16>(a, back, aligned, s);
     if (type == ESP_KV_FP16) return run<_Float16>(a, back, aligned, s);
@@ -457,7 +475,7 @@ extern "C" esp_status esp_kv_norm_rotate(const esp_kv_rope *rope, int32_t type, 
     const int size = type == ESP_KV_FP32 ? 4 : 2;
     NormArgs a{{{view_of(q), view_of(q_out), {}, q_weight, nullptr, nullptr, q_heads, 0}, {view_of(k), view_of(k_out), {}, k_weight, nullptr, nullptr, k_heads, 0}},
                {rope->turns, rope->magnitude, rope->rotary_dim, rope->interleaved}, positions, tokens, head_dim, weight_type == ESP_KV_FP32, eps, 1.0f / float(head_dim)};
-    const bool aligned = (!q_heads || (wide(q, size) && wide(q_out, size))) && (!k_heads || (wide(k, size) && wide(k_out, size)));
+    const int aligned = least_of(q_heads ? least_of(wide(q, size), wide(q_out, size)) : 16, k_heads ? least_of(wide(k, size), wide(k_out, size)) : 16);
     return run(a, type, false, aligned, stream);
 }
 
@@ -466,7 +484,7 @@ extern "C" esp_status esp_kv_norm_rotate_workspace(int64_t tokens, int32_t head_
     if (tokens < 0 || tokens > INT32_MAX || q_heads < 0 || q_heads > 65536 || k_heads < 0 || k_heads > 65536 || head_dim < 2 || head_dim > kMostDim)
         return ESP_ERR_SHAPE;
     NormArgs a{};
-    share_blocks(a, tokens, q_heads, k_heads, lanes_of(head_dim, 2));
+    share_blocks(a, tokens, q_heads, k_heads, lanes_of(head_dim, 2, 16));
     *bytes = (size_t(a.side[0].blocks) + a.side[1].blocks) * head_dim * sizeof(float);
     return ESP_OK;
 }
@@ -485,7 +503,7 @@ extern "C" esp_status esp_kv_norm_rotate_backward(const esp_kv_rope *rope, int32
     NormArgs a{{{view_of(q), view_of(q_grad), view_of(dq), q_weight, nullptr, dq_weight, q_heads, 0},
                 {view_of(k), view_of(k_grad), view_of(dk), k_weight, nullptr, dk_weight, k_heads, 0}},
                {rope->turns, rope->magnitude, rope->rotary_dim, rope->interleaved}, positions, tokens, head_dim, weight_type == ESP_KV_FP32, eps, 1.0f / float(head_dim)};
-    share_blocks(a, tokens, q_heads, k_heads, lanes_of(head_dim, 2));
+    share_blocks(a, tokens, q_heads, k_heads, lanes_of(head_dim, 2, 16));
     if (dq_weight || dk_weight) {
         const size_t need = (size_t(a.side[0].blocks) + a.side[1].blocks) * head_dim * sizeof(float);
         if (need && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < need)) return ESP_ERR_WORKSPACE;
@@ -493,7 +511,7 @@ extern "C" esp_status esp_kv_norm_rotate_backward(const esp_kv_rope *rope, int32
         a.side[0].partial = p;
         a.side[1].partial = p + size_t(a.side[0].blocks) * head_dim;
     }
-    const bool aligned = (!q_heads || (wide(q, size) && wide(q_grad, size) && wide(dq, size))) &&
-                         (!k_heads || (wide(k, size) && wide(k_grad, size) && wide(dk, size)));
+    auto both = [&](const esp_kv_view &x, const esp_kv_view &g, const esp_kv_view &d) { return least_of(wide(x, size), least_of(wide(g, size), wide(d, size))); };
+    const int aligned = least_of(q_heads ? both(q, q_grad, dq) : 16, k_heads ? both(k, k_grad, dk) : 16);
     return run(a, type, true, aligned, stream);
 }

@@ -233,9 +233,9 @@ def _turn(rope, x, positions, inverse, out, s: int) -> torch.Tensor:
     return out
 
 
-def _accumulators(tensors, capture):
-    """What adds up the gradients of the leaves among tensors, and whether another graph than this capture's holds one of
-    these: autograd would then go to the stream of that graph in a captured backward pass, which ends the process."""
+def _accumulators(tensors, stream: int):
+    """What adds up the gradients of the leaves among tensors, and whether a graph that was not captured on this stream
+    holds one of these: autograd would then go to that graph's stream in a captured backward pass, which ends the process."""
     nodes, older = [], False
     for x in tensors:
         if x is not None and x.requires_grad and x.is_leaf:
@@ -244,8 +244,8 @@ def _accumulators(tensors, capture):
             del node                            # goes unless a graph holds it
             node = torch.autograd.graph.get_gradient_edge(x).node
             if node.metadata.pop("esp_probe", None) is not probe:
-                node.metadata["esp_capture"] = capture
-            elif node.metadata.get("esp_capture") != capture:
+                node.metadata["esp_stream"] = stream
+            elif node.metadata.get("esp_stream") != stream:
                 older = True
             nodes.append(node)
     return nodes, older
@@ -267,8 +267,8 @@ def norm_rotate(rope: Rope, q: torch.Tensor, k: torch.Tensor, q_weight, k_weight
     [head_dim] (the type of q and k or float32; None: ones), turned by positions (int32 [tokens]).  Has its gradient, of
     the weights too.  Either may have no heads.  stream: the current one, unless given."""
     if torch.is_grad_enabled() and any(x is not None and x.requires_grad for x in (q, k, q_weight, k_weight)):
-        capture = _capture(s)
-        nodes, older = ((), False) if capture is None else _accumulators((q, k, q_weight, k_weight), capture)
+        capturing = torch.cuda.is_current_stream_capturing()
+        nodes, older = _accumulators((q, k, q_weight, k_weight), s) if capturing else ((), False)
         result = _Normed.apply(q, k, q_weight, k_weight, rope, positions, eps, older, s)
         del nodes                               # until here: the graph holds them now
         return result

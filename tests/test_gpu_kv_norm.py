@@ -94,7 +94,8 @@ CASES = [
     (50, 3, 4, 512, 128, False, "none", torch.float16, None), (23, 4, 4, 64, 32, False, "none", torch.float32, None),
     (31, 3, 2, 66, 66, True, "none", torch.float16, torch.float16), (29, 1, 2, 258, 130, False, "ntk", torch.float32, torch.float32),
     (12, 5, 1, 2, 2, False, "none", torch.float32, torch.float32), (64, 1, 6, 16, 16, True, "none", torch.bfloat16, torch.float32),
-    (40, 6, 1, 32, 16, False, "none", torch.float16, torch.float16), (2, 3, 3, 500, 500, False, "none", torch.bfloat16, torch.bfloat16),
+    (200, 9, 5, 24, 8, False, "none", torch.bfloat16, torch.float32), (60, 2, 3, 512, 508, False, "none", torch.float16, torch.float16),
+    (77, 3, 2, 120, 60, True, "none", torch.float32, torch.float32), (40, 6, 1, 32, 16, False, "none", torch.float16, torch.float16), (2, 3, 3, 500, 500, False, "none", torch.bfloat16, torch.bfloat16),
 ]
 
 
@@ -118,9 +119,10 @@ def test_strides(dtype):
     fused = _randn(3, 50, 12, 64, dtype=dtype)                   # queries, keys and values of one product
     wide = _randn(4, 50, 7, 65, dtype=dtype)                     # rows of 65: not 16-byte aligned
     one = _randn(5, 1, 7, 64, dtype=dtype)
+    eights = _randn(7, 50, 9, 64 + 8 // one.element_size(), dtype=dtype)[..., 8 // one.element_size():]     # places at multiples of 8 bytes
     w = (1.0 + 0.1 * _randn(6, 64)).to(dtype)
     for q, k in ((fused[:, :8], fused[:, 8:10]), (wide[..., 1:], wide[:, 2:5, :64]), (one.expand(50, 7, 64), wide[:, :1, 1:].expand(50, 3, 64)),
-                 (wide.transpose(0, 1).contiguous().transpose(0, 1)[..., :64], fused[:, 10:])):
+                 (wide.transpose(0, 1).contiguous().transpose(0, 1)[..., :64], fused[:, 10:]), (eights[:, :5], fused[:, :2]), (eights[:, 5:], eights[:, :1])):
         _say(f"norm strides {q.stride()} {k.stride()} {dtype}")
         q, k = q.detach(), k.detach()
         gq, gk = (torch.randn(*x.shape[:2], 128, device="cuda").to(dtype)[..., 64:] for x in (q, k))
@@ -231,6 +233,18 @@ def test_a_training_step_in_a_graph():
         torch.cuda.synchronize()
         want = step()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+    _say("another capture while the first one's results live")
+    second = torch.cuda.CUDAGraph()
+    y = None
+    with torch.cuda.graph(second):
+        y = kv.norm_rotate(rope, q, k, qw, kw, pos)
+    third = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(third):
+        again = step()
+    third.replay()
+    torch.cuda.synchronize()
+    assert y[0].grad_fn is not None and all(torch.equal(a, b) for a, b in zip(again, want))
+    del y
     _say("a captured backward pass beside an eager graph of the same leaves")
     lives = kv.norm_rotate(rope, q, k, qw, kw, pos)
     torch.cuda.synchronize()

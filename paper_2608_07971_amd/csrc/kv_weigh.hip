@@ -31,6 +31,8 @@ struct WeighArgs {
 
 __device__ __forceinline__ float16v product32(half8 x, half8 y, float16v z) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(x, y, z, 0, 0, 0); }
 __device__ __forceinline__ float16v product32(bhalf8 x, bhalf8 y, float16v z) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, z, 0, 0, 0); }
+__device__ __forceinline__ float4v product16(half8 x, half8 y, float4v z) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(x, y, z, 0, 0, 0); }
+__device__ __forceinline__ float4v product16(bhalf8 x, bhalf8 y, float4v z) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, z, 0, 0, 0); }
 template <typename T> struct Pack;
 template <> struct Pack<_Float16> { typedef half8 v8; typedef half2 v2; };
 template <> struct Pack<__bf16> { typedef bhalf8 v8; typedef bhalf2 v2; };
@@ -340,16 +342,21 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads *
     }
 }
 
-// Few queries: 32 rows of a sequence and key head stay in registers while a wavefront goes
-// through its share of the tokens, 32 at a time, the next ones' codes and the pages after
-// these on their way.  More rows take as many rounds, each adding to the one before.
+// Few queries: kBlocks times 16 rows of a sequence and key head stay in registers while a
+// wavefront goes through its share of the tokens, 64 at a time, sixteen a column block of the
+// products; the next ones' codes and the pages after these are on their way.  A block's tokens
+// lie in one page, so its place and scale are the wavefront's.  More rows take as many rounds,
+// each adding to the one before.
 // Bound by memory: 64 single tokens of 32 heads on up to 8,192 cached ones of 8 key heads (200
-// MB) 43 us where the memory-side cache holds them (4.6 TB/s), 60 us where it does not.
-template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 3) void k_weigh_few(WeighArgs a) {
+// MB) 43 us where the memory-side cache holds them (4.6 TB/s), 54 us where it does not (60 with
+// products of 32 by 32, whose registers leave three wavefronts a SIMD and 32 tokens a turn).
+template <typename T, int Dim, int Page, int kBlocks>
+__global__ __launch_bounds__(kThreads, kBlocks == 1 ? 4 : 3) void k_weigh_few(WeighArgs a) {
     typedef typename Pack<T>::v8 V8;
-    constexpr int kSteps = Dim / 16, kTile = 32;
+    typedef typename Pack<T>::v2 V2;
+    constexpr int kSteps = Dim / 32, kTile = 64, kRound = 16 * kBlocks;
     const Cache &c = a.c;
-    const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+    const int lane = threadIdx.x & 63, col = lane & 15, quarter = lane >> 4;
     const int unit = __builtin_amdgcn_readfirstlane(blockIdx.x * kWaves + (threadIdx.x >> 6));
     const int share = unit / c.heads, head = unit - share * c.heads;
     if (share >= a.shares) return;
@@ -358,51 +365,58 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 
     if (b < 0) return;
     for (; left > 0; b++, tile = 0) {
         if (b >= a.rows.rows) return;
-        const Row row = usable(a, b, false);
+        Row row = usable(a, b, false);
+        row.n = __builtin_amdgcn_readfirstlane(row.n);
+        row.length = __builtin_amdgcn_readfirstlane(row.length);
         const int p0 = row.length - row.n, n_rows = row.n * a.group, end = min(tile + left, (row.length + kTile - 1) / kTile);
         if (tile >= end) continue;
         left -= end - tile;
         const int32_t *table = c.table + int64_t(row.seq) * c.width;
         float *mass = a.mass + ((int64_t(a.layer) * c.sequences + row.seq) * c.heads + head) * (int64_t(c.width) * Page);
-        for (int r0 = 0; r0 < n_rows; r0 += kRows) {
-            // the rows of this lane's products: r0 + 8 y + 4 half + x
-            V8 q[kSteps];
-            {
-                const Walker w(min(r0 + col, n_rows - 1), a.group);
-                const T *from = static_cast<const T *>(a.q.data) + int64_t(row.first + w.token) * a.q.token + int64_t(head * a.group + w.head) * a.q.head + 16 * half;
+        for (int r0 = 0; r0 < n_rows; r0 += kRound) {
+            // quarter g's elements of steps 2 i and 2 i + 1: 64 i + 16 g and on, as the codes are loaded
+            V8 q[kBlocks][kSteps];
+            float lse[kBlocks][4];          // of rows r0 + 16 y + 4 quarter + x
 #pragma unroll
-                for (int s = 0; s < kSteps; s++) q[s] = load8<T>(from + s / 2 * 32 + s % 2 * 8, a.wide);
-            }
-            float lse[16];
+            for (int y = 0; y < kBlocks; y++) {
+                const Walker w(min(r0 + 16 * y + col, n_rows - 1), a.group);
+                const T *from = static_cast<const T *>(a.q.data) + int64_t(row.first + w.token) * a.q.token + int64_t(head * a.group + w.head) * a.q.head;
 #pragma unroll
-            for (int y = 0; y < 4; y++)
+                for (int s = 0; s < kSteps; s++) q[y][s] = load8<T>(from + s / 2 * 64 + 16 * quarter + s % 2 * 8, a.wide);
 #pragma unroll
                 for (int x = 0; x < 4; x++) {
-                    const int r = r0 + 8 * y + 4 * half + x;
-                    lse[4 * y + x] = INFINITY;
+                    const int r = r0 + 16 * y + 4 * quarter + x;
+                    lse[y][x] = INFINITY;
                     if (r < n_rows) {
-                        const Walker w(r, a.group);
-                        const float l = a.lse[int64_t(row.first + w.token) * a.q_heads + head * a.group + w.head];
-                        lse[4 * y + x] = l == -INFINITY ? INFINITY : l;          // it sees nothing
+                        const Walker v(r, a.group);
+                        const float l = a.lse[int64_t(row.first + v.token) * a.q_heads + head * a.group + v.head];
+                        lse[y][x] = l == -INFINITY ? INFINITY : l;           // it sees nothing
                     }
                 }
+            }
             auto page_of = [&](int i) {
-                const int t = i * kTile + col;
+                const int t = i * kTile + lane;
                 return i < end && t < row.length ? table[t / Page] : -1;
             };
             struct Tile {
-                Keys<T, Dim> codes;
-                float ks, mass;
+                uint4v codes[4][Dim / 64];
+                float scale, mass;          // of the lane's own token
                 bool there;
             };
             auto load = [&](Tile &x, int i, int page) {
-                const int t = i * kTile + col;
+                const int t = i * kTile + lane;
                 x.there = uint32_t(page) < uint32_t(c.pages);
                 if (!x.there && i < end && t < row.length && r0 == 0) record(c, ESP_ERR_SHAPE);
-                const int p = x.there ? page : 0;
-                x.codes.load(c.k + c.block(p, a.layer, head) + t % Page * Dim, half);
-                x.ks = *c.block_scale(p, a.layer, 0, head) * a.scale;
-                x.mass = x.there && t < row.length && (t < p0 || r0) ? mass[t] : 0.0f;
+                page = x.there ? page : 0;
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    const uint8_t *block = c.k + c.block(__builtin_amdgcn_readlane(page, 16 * j), a.layer, head);
+                    const uint32_t at = uint32_t((16 * j + col) % Page * Dim + 16 * quarter);
+#pragma unroll
+                    for (int s = 0; s < Dim / 64; s++) x.codes[j][s] = *reinterpret_cast<const uint4v *>(block + (at + 64 * s));
+                }
+                x.scale = *c.block_scale(page, a.layer, 0, head) * a.scale;
+                x.mass = x.there && (t < p0 || r0) ? mass[t] : 0.0f;
             };
             Tile now, next;
             int page = page_of(tile + 1);
@@ -410,26 +424,37 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads, 
             for (int i = tile; i < end; i++) {
                 load(next, i + 1, page);
                 page = page_of(i + 2);
-                float16v s;
-#pragma unroll
-                for (int j = 0; j < 16; j++) s[j] = 0.0f;
-#pragma unroll
-                for (int j = 0; j < kSteps; j++) s = product32(q[j], now.codes.step(j), s);
-                const int t = i * kTile + col;
                 // whether all rows that there are see all of the tile
                 const bool whole = i * kTile + kTile - 1 <= p0 && (a.window <= 0 || i * kTile > p0 + row.n - 1 - a.window);
-                float sum = 0.0f;
+                float own = 0.0f;
 #pragma unroll
-                for (int y = 0; y < 4; y++)
-                    if (r0 + 8 * y < n_rows)
+                for (int j = 0; j < 4; j++) {
+                    float4v s[kBlocks];
+#pragma unroll
+                    for (int y = 0; y < kBlocks; y++) s[y] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int k = 0; k < kSteps; k++) {
+                        const uint4v w = now.codes[j][k / 2];
+                        const V8 key = codes8<V8, V2>(w[k % 2 * 2], w[k % 2 * 2 + 1]);
+#pragma unroll
+                        for (int y = 0; y < kBlocks; y++) s[y] = product16(q[y][k], key, s[y]);
+                    }
+                    const float ks = __uint_as_float(uint32_t(__builtin_amdgcn_readlane(__float_as_uint(now.scale), 16 * j)));
+                    const int t = i * kTile + 16 * j + col;
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int y = 0; y < kBlocks; y++)
 #pragma unroll
                         for (int x = 0; x < 4; x++) {
-                            const float e = weight(s[4 * y + x], now.ks, lse[4 * y + x]);
-                            const int r = r0 + 8 * y + 4 * half + x, p = whole ? 0 : p0 + r / a.group;
+                            const float e = weight(s[y][x], ks, lse[y][x]);
+                            const int r = r0 + 16 * y + 4 * quarter + x, p = whole ? 0 : p0 + r / a.group;
                             sum += r < n_rows && (whole || (t <= p && (a.window <= 0 || t > p - a.window))) ? e : 0.0f;
                         }
-                sum += __shfl_xor(sum, 32);
-                if (half == 0 && now.there) mass[t] = __builtin_fmaf(now.mass, r0 ? 1.0f : a.decay, sum);
+                    sum += __shfl_xor(sum, 16);
+                    sum += __shfl_xor(sum, 32);
+                    own = quarter == j ? sum : own;
+                }
+                if (now.there) mass[i * kTile + lane] = __builtin_fmaf(now.mass, r0 ? 1.0f : a.decay, own);
                 now = next;
             }
         }
@@ -443,27 +468,29 @@ using namespace esp_kv;
 namespace {
 
 // Rows (token, query head) a sequence and key head up to which k_weigh_few takes a call, in
-// rounds of 32.  So / by k_weigh, 64 sequences of about 3,800 tokens of 128: 48 rows of 4 key
-// heads 71 / 128 us, 96 rows 94 / 122, 128 rows 117 / 121, 192 rows 170 / 134.
+// rounds of 16 or 32.  So / by k_weigh, 64 sequences of about 3,800 tokens of 128: 48 rows of 4
+// key heads 68 / 128 us, 96 rows 89 / 122, 128 rows 106 / 121, 192 rows 160 / 134.
 constexpr int kFewRows = 128;
-// Its wavefronts: three a SIMD, which its registers allow.  As many / twice as many: 60 / 72 us
-// (weights of 64 single tokens of 32 heads on up to 8,192 cached ones, 8 key heads).
-constexpr int kFewWaves = 3072;
+// Its wavefronts, as many as its registers allow at once: three a SIMD for rounds of 32 rows, four
+// for 16.  2,048 / 4,096 / 8,192 of the latter: 59 / 54 / 55 us (weights of 64 single tokens of
+// 32 heads on up to 8,192 cached ones, 8 key heads).
+constexpr int kFewWaves = 3072, kFewestWaves = 4096;
 constexpr int64_t kMostBlocks = ((int64_t(1) << 32) - 1) / (kThreads * kGroups);  // a launch's threads are numbered in 32 bits
 
-template <typename T, int Dim, int Page> void launch(const WeighArgs &a, bool many, unsigned blocks, hipStream_t s) {
-    if (many) k_weigh<T, Dim, Page><<<blocks, kThreads * kGroups, 0, s>>>(a);
-    else k_weigh_few<T, Dim, Page><<<blocks, kThreads, 0, s>>>(a);
+template <typename T, int Dim, int Page> void launch(const WeighArgs &a, int rows, unsigned blocks, hipStream_t s) {
+    if (rows > kFewRows) k_weigh<T, Dim, Page><<<blocks, kThreads * kGroups, 0, s>>>(a);
+    else if (rows > 16) k_weigh_few<T, Dim, Page, 2><<<blocks, kThreads, 0, s>>>(a);
+    else k_weigh_few<T, Dim, Page, 1><<<blocks, kThreads, 0, s>>>(a);
 }
-template <typename T, int Dim> void launch(const WeighArgs &a, bool many, unsigned blocks, hipStream_t s) {
+template <typename T, int Dim> void launch(const WeighArgs &a, int rows, unsigned blocks, hipStream_t s) {
     switch (a.c.tokens) {
-    case 16: launch<T, Dim, 16>(a, many, blocks, s); break;
-    case 32: launch<T, Dim, 32>(a, many, blocks, s); break;
-    default: launch<T, Dim, 64>(a, many, blocks, s); break;
+    case 16: launch<T, Dim, 16>(a, rows, blocks, s); break;
+    case 32: launch<T, Dim, 32>(a, rows, blocks, s); break;
+    default: launch<T, Dim, 64>(a, rows, blocks, s); break;
     }
 }
-template <typename T> void launch(const WeighArgs &a, bool many, unsigned blocks, hipStream_t s) {
-    a.c.dim == 64 ? launch<T, 64>(a, many, blocks, s) : launch<T, 128>(a, many, blocks, s);
+template <typename T> void launch(const WeighArgs &a, int rows, unsigned blocks, hipStream_t s) {
+    a.c.dim == 64 ? launch<T, 64>(a, rows, blocks, s) : launch<T, 128>(a, rows, blocks, s);
 }
 
 }  // namespace
@@ -483,11 +510,12 @@ extern "C" esp_status esp_kv_weigh(const esp_kv_cache *cache, int32_t layer, int
     if (tokens * group > INT32_MAX - 8 * kStep) return ESP_ERR_SHAPE;
     // the most new tokens of a row, if none is without any (others take k_weigh_few more rounds)
     const int64_t longest = tokens - rows + 1 < max_new ? (tokens < rows ? 1 : tokens - rows + 1) : max_new;
-    const bool many = longest * group > kFewRows;
+    const int32_t most_rows = int32_t(longest * group < INT32_MAX ? longest * group : INT32_MAX);
+    const bool many = most_rows > kFewRows;
     // shares of a head's tiles: one each where queries are many; else as many as the GPU holds wavefronts
-    const int64_t tile = many ? kWaves * 32 : 32, most = rows * ((int64_t(max_length) + tile - 1) / tile);
+    const int64_t tile = many ? kWaves * 32 : 64, most = rows * ((int64_t(max_length) + tile - 1) / tile);
     if (most > INT32_MAX) return ESP_ERR_SHAPE;
-    const int64_t fill = (many ? 16384 : kFewWaves) / cache->kv_heads + 1, shares = most < fill ? most : fill;
+    const int64_t fill = (many ? 16384 : most_rows > 16 ? kFewWaves : kFewestWaves) / cache->kv_heads + 1, shares = most < fill ? most : fill;
     const int64_t workers = shares * cache->kv_heads, count = many ? workers : (workers + kWaves - 1) / kWaves;
     if (count > kMostBlocks) return ESP_ERR_SHAPE;
     const bool wide = (reinterpret_cast<uintptr_t>(q.data) & 15) == 0 && q.token_stride % 8 == 0 && q.head_stride % 8 == 0;
@@ -495,7 +523,7 @@ extern "C" esp_status esp_kv_weigh(const esp_kv_cache *cache, int32_t layer, int
                       layer, q_heads, group, window, max_new, max_length, int32_t(shares), wide};
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const unsigned blocks = unsigned(count);
-    if (type == ESP_KV_BF16) launch<__bf16>(a, many, blocks, s);
-    else launch<_Float16>(a, many, blocks, s);
+    if (type == ESP_KV_BF16) launch<__bf16>(a, most_rows, blocks, s);
+    else launch<_Float16>(a, most_rows, blocks, s);
     return launched();
 }

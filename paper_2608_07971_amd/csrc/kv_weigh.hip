@@ -133,8 +133,8 @@ template <typename T> __device__ __forceinline__ typename Pack<T>::v8 load8(cons
     return x;
 }
 
-// A token's keys as one lane of each half holds them: half h's steps 2 i and 2 i + 1 are
-// elements 32 i + 16 h and on, so that codes are loaded sixteen at a time.
+// A token's keys as one lane of each half holds them for k_weigh: half h's steps 2 i and 2 i + 1
+// are elements 32 i + 16 h and on, so that codes are loaded sixteen at a time.
 template <typename T, int Dim> struct Keys {
     typedef typename Pack<T>::v8 V8;
     typedef typename Pack<T>::v2 V2;
@@ -474,7 +474,7 @@ constexpr int kFewRows = 128;
 // Its wavefronts, as many as its registers allow at once: three a SIMD for rounds of 32 rows, four
 // for 16.  2,048 / 4,096 / 8,192 of the latter: 59 / 54 / 55 us (weights of 64 single tokens of
 // 32 heads on up to 8,192 cached ones, 8 key heads).
-constexpr int kFewWaves = 3072, kFewestWaves = 4096;
+constexpr int kUnits = 1024, kFewWaves = 3 * kUnits, kFewestWaves = 4 * kUnits;           // kUnits: the GPU's SIMDs
 constexpr int64_t kMostBlocks = ((int64_t(1) << 32) - 1) / (kThreads * kGroups);  // a launch's threads are numbered in 32 bits
 
 template <typename T, int Dim, int Page> void launch(const WeighArgs &a, int rows, unsigned blocks, hipStream_t s) {

@@ -607,7 +607,8 @@ class PagedCache:
     @_on_stream
     def evict(self, keep, mass, recent: int = 0, *, s: int) -> None:
         """Cuts sequences that are longer than keep (int32 [sequences]): each layer and head keeps its last `recent` tokens
-        and those of the largest mass, moved together in their order, their masses too."""
+        and those of the largest mass, moved together in their order, their masses too.  Scratch, kept like that of the
+        other calls: a bit for every mass."""
         if self._evict_bytes is None:
             z = C.c_size_t(0)
             _check(lib().esp_kv_evict_workspace(self.ptr, C.byref(z)), "esp_kv_evict_workspace")

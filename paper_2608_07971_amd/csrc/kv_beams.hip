@@ -271,21 +271,21 @@ __device__ __forceinline__ uint64_t ordered(double x) {
 }
 __device__ __forceinline__ double number(uint64_t u) { return __longlong_as_double(int64_t(u >> 63 ? u & ~(uint64_t(1) << 63) : ~u)); }
 
-// A wavefront a request (64 of 8 beams 6.6 us, one of 4 beams in 16 splits 5.2 us): beams' sums over their splits, then the best of what they left.
-__global__ __launch_bounds__(64) void k_beam_join(BeamArgs a) {
+// A workgroup a request (64 of 8 beams 6.1 us, one of 4 beams in 16 splits 4.2 us): beams' sums over
+// their splits, then, by one wavefront, the best of what they left.
+__global__ __launch_bounds__(kThreads) void k_beam_join(BeamArgs a) {
     __shared__ Two queue[128];
     extern __shared__ double lse[];         // [beams]; NaN: no candidates
-    const int group = blockIdx.x, lane = threadIdx.x;
+    const int group = blockIdx.x, lane = threadIdx.x & 63;
     // the lists' first ones before their second; the first 64 on their way while the sums are made
-    const int lists = a.beams * a.splits;
-    const int64_t all = int64_t(lists) * a.width;
-    auto key = [&](int64_t i) {
-        const int rank = int(i / lists), list = int(i - int64_t(rank) * lists);
+    const uint32_t lists = a.beams * a.splits, all = lists * a.width;          // at most 2^20
+    auto key = [&](uint32_t i) {
+        const uint32_t rank = i / lists, list = i - rank * lists;
         return i < all ? a.keys[(int64_t(group) * lists + list) * a.width + rank] : 0;
     };
     const uint64_t early = key(lane);
-    for (int b0 = 0; b0 < a.beams; b0 += 64 / kMostSplits) {     // a beam by as many lanes as it may have splits
-        const int b = b0 + lane / kMostSplits, i = lane % kMostSplits, row = group * a.beams + min(b, a.beams - 1);
+    for (int b0 = 0; b0 < a.beams; b0 += kThreads / kMostSplits) {             // a beam by as many lanes as it may have splits
+        const int b = b0 + threadIdx.x / kMostSplits, i = threadIdx.x % kMostSplits, row = group * a.beams + min(b, a.beams - 1);
         const bool ended = a.ended && a.ended[row], live = !ended && fabsf(a.scores[row]) < INFINITY, there = live && i < a.splits;
         const int64_t at = int64_t(row) * a.splits + min(i, a.splits - 1);
         const float own = there ? a.tops[at] : -INFINITY;
@@ -299,13 +299,14 @@ __global__ __launch_bounds__(64) void k_beam_join(BeamArgs a) {
         if (i == 0 && b < a.beams) lse[b] = live ? double(top) + log(sum) : ended ? 0.0 : double(NAN);
     }
     __syncthreads();
+    if (threadIdx.x >= 64) return;          // the rest is one wavefront's
     Best<Two> best;
     // lists are sorted: once as many in a row as there are lists have not passed, no other does
-    int64_t quiet = 0;
-    for (int64_t i0 = 0; i0 < all && quiet < lists; i0 += 64) {
+    uint32_t quiet = 0;
+    for (uint32_t i0 = 0; i0 < all && quiet < lists; i0 += 64) {
         Two k{0, 0};
         if (i0 + lane < all) {
-            const int rank = int((i0 + lane) / lists), list = int(i0 + lane - int64_t(rank) * lists), beam = list / a.splits;
+            const uint32_t rank = (i0 + lane) / lists, list = i0 + lane - rank * lists, beam = list / uint32_t(a.splits);
             const int row = group * a.beams + beam;
             const double s = double(a.scores[row]);
             double total = NAN;
@@ -405,6 +406,6 @@ extern "C" esp_status esp_kv_select_beams(int32_t type, int32_t groups, int32_t 
     if (type == ESP_KV_BF16) k_beam_rows<__bf16><<<blocks, kThreads, 0, s>>>(a);
     else if (type == ESP_KV_FP16) k_beam_rows<_Float16><<<blocks, kThreads, 0, s>>>(a);
     else k_beam_rows<float><<<blocks, kThreads, 0, s>>>(a);
-    k_beam_join<<<unsigned(groups), 64, size_t(beams) * sizeof(double), s>>>(a);
+    k_beam_join<<<unsigned(groups), kThreads, size_t(beams) * sizeof(double), s>>>(a);
     return launched();
 }

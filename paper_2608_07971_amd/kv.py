@@ -314,12 +314,17 @@ class _Normed(torch.autograd.Function):
         return _norm(rope, q, k, q_weight, k_weight, positions, eps, s)
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
     def backward(ctx, gq, gk):
         if ctx.older:
             raise RuntimeError("norm_rotate: a captured backward pass of leaves that a graph from before the capture holds, too. Drop "
                                "that graph before the capture")
-        return _norm_back(ctx.rope, *ctx.saved_tensors, ctx.eps, gq, gk, ctx.needs_input_grad[2:4])
+        saved = ctx.saved_tensors
+        grads = _norm_back(ctx.rope, *saved, ctx.eps, gq, gk, ctx.needs_input_grad[2:4])
+        if torch.is_grad_enabled():             # a graph of the gradient is asked for
+            source = next((x for x in (*saved, gq, gk) if x is not None and x.requires_grad), None)
+            if source is not None:
+                grads = [None if g is None else _NoGradient.apply("norm_rotate's gradient", source, g, "it is not made twice") for g in grads]
+        return *grads, None, None, None, None, None
 
 
 @_on_stream
@@ -337,7 +342,7 @@ def _norm_back(rope, q, k, q_weight, k_weight, positions, eps, gq, gk, wanted, *
         *given, _view(gq, T, Hq, D, "q", q.device), _view(gk, T, Hk, D, "k", q.device), esp_kv_view(dq.data_ptr(), Hq * D, D),
         esp_kv_view(dk.data_ptr(), Hk * D, D), None if dwq is None else dwq.data_ptr(), None if dwk is None else dwk.data_ptr(),
         None if work is None else work.data_ptr(), size, s), "esp_kv_norm_rotate_backward")
-    return dq, dk, dwq, dwk, None, None, None, None, None
+    return dq, dk, dwq, dwk
 
 
 @functools.lru_cache(maxsize=4096)

@@ -199,10 +199,12 @@ def test_no_tokens_no_heads_and_parts_of_the_gradient():
     yq, yk = kv.norm_rotate(rope, q, q, w, w, pos)
     dq, dw = torch.autograd.grad((yq, yk), (q, w), (g, g))
     assert torch.equal(dw, all_of[1] + all_of[1]) and torch.equal(dq, all_of[0] + all_of[0])
-    with pytest.raises(RuntimeError):
-        yq, _ = kv.norm_rotate(rope, q, k, w, None, pos)
-        first, = torch.autograd.grad(yq, q, g.clone().requires_grad_(), create_graph=True)
-        first.sum().backward()                                    # no gradient of the gradient
+    yq, _ = kv.norm_rotate(rope, q, k, w, None, pos)
+    first, second = torch.autograd.grad(yq, (q, w), g.clone().requires_grad_(), create_graph=True)
+    assert torch.equal(first, all_of[0]) and torch.equal(second, all_of[1])
+    for lost in (first, second):
+        with pytest.raises(RuntimeError, match="no gradient"):
+            lost.sum().backward()                                 # of the gradient there is none
 
 
 def test_a_training_step_in_a_graph():

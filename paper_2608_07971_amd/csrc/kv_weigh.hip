@@ -169,6 +169,8 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads *
     __shared__ __align__(16) float lses[2][kStep];
     __shared__ __align__(16) int places[2][kStep];
     __shared__ float sums[kGroups][kTile];
+    __shared__ bool counts[2][kGroups];     // whether all of a group's rows of a step do
+    static_assert(kSubs * kRows == 64, "a group's rows of a step are one wavefront's");
 
     const Cache &c = a.c;
     const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5;
@@ -241,9 +243,8 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads *
                     next_place = -1;
                     if (own_row < n_rows) {
                         const Walker w(own_row, a.group);
-                        const float l = a.lse[int64_t(row.first + w.token) * a.q_heads + head * a.group + w.head];
-                        next_lse = l == -INFINITY ? INFINITY : l;            // it sees nothing
-                        next_place = p0 + w.token;
+                        next_lse = a.lse[int64_t(row.first + w.token) * a.q_heads + head * a.group + w.head];
+                        next_place = next_lse == -INFINITY ? -1 : p0 + w.token;     // -1: sees nothing, whatever the query holds
                     }
                     own_row += kStep;
                 }
@@ -252,6 +253,8 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads *
                 if (tid < kStep) {
                     lses[buffer][tid] = next_lse;
                     places[buffer][tid] = next_place;
+                    const bool all = __all(next_place >= 0);
+                    if (lane == 0) counts[buffer][number] = all;
                 }
                 __builtin_amdgcn_s_waitcnt(0x0f70);              // the queries have come in
             };
@@ -311,7 +314,7 @@ template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads *
                 if (more) load(buffer ^ 1);
                 const int own0 = r0 + team * kSubs * kRows, first = p0 + seen.token, last = first + spread;
                 seen.on(seen_tokens, seen_heads, a.group);
-                if (own0 + kSubs * kRows <= n_rows && w0 + 31 <= first && (a.window <= 0 || w0 > last - a.window)) {
+                if (counts[buffer][team] && w0 + 31 <= first && (a.window <= 0 || w0 > last - a.window)) {
 #pragma unroll
                     for (int i = 0; i < kSubs; i++) {
                         float16v s;
@@ -390,7 +393,7 @@ __global__ __launch_bounds__(kThreads, kBlocks == 1 ? 4 : 3) void k_weigh_few(We
                     if (r < n_rows) {
                         const Walker v(r, a.group);
                         const float l = a.lse[int64_t(row.first + v.token) * a.q_heads + head * a.group + v.head];
-                        lse[y][x] = l == -INFINITY ? INFINITY : l;           // it sees nothing
+                        lse[y][x] = l == -INFINITY ? INFINITY : l;           // infinity: sees nothing, whatever the query holds
                     }
                 }
             }
@@ -448,7 +451,7 @@ __global__ __launch_bounds__(kThreads, kBlocks == 1 ? 4 : 3) void k_weigh_few(We
                         for (int x = 0; x < 4; x++) {
                             const float e = weight(s[y][x], ks, lse[y][x]);
                             const int r = r0 + 16 * y + 4 * quarter + x, p = whole ? 0 : p0 + r / a.group;
-                            sum += r < n_rows && (whole || (t <= p && (a.window <= 0 || t > p - a.window))) ? e : 0.0f;
+                            sum += lse[y][x] != INFINITY && (whole || (t <= p && (a.window <= 0 || t > p - a.window))) ? e : 0.0f;
                         }
                     sum += __shfl_xor(sum, 16);
                     sum += __shfl_xor(sum, 32);

@@ -141,6 +141,22 @@ def test_queries_that_see_nothing_and_infinities():
     assert bool(mass[0, 0, 0, :97].isinf().all()) and not mass[0, 0, 0, 97:100].any()
 
 
+@pytest.mark.parametrize("new,lengths,group,page,window", [([1, 3], [500, 3], 4, 16, 0), ([20, 9], [800, 200], 2, 32, 150), ([300], [900], 3, 16, 0),
+                                                           ([150, 200], [1100, 200], 2, 64, 400)])
+def test_padded_queries_hold_anything(new, lengths, group, page, window):
+    """A query whose lse is -inf adds nothing, whatever it holds itself."""
+    _say(f"weigh with padded queries {new} of {lengths}, group {group}, window {window}")
+    cache = ref.make(kv, lengths, heads=2, dim=64, page=page)
+    q = _randn(8, sum(new), 2 * group, 64)
+    _, lse = cache.attend(0, q, ref.offsets(new), window=window)
+    for i, x in ((0, float("nan")), (sum(new) // 2, float("inf")), (sum(new) - 1, -float("inf"))):
+        q[i, 1::2], lse[i, 1::2] = x, -float("inf")
+    q[-1, 0, 5], lse[-1, 0] = float("nan"), -float("inf")
+    _check(cache, q, new, window, lse=lse, decay=0.5)
+    lse.fill_(-float("inf"))
+    _check(cache, torch.full_like(q, float("nan")), new, window, lse=lse, decay=0.5)
+
+
 def test_wrong_rows_and_pages_are_left_out():
     cache = ref.make(kv, [100, 60, 20], heads=1, dim=64, width=8)
     q, lse = _randn(6, 3, 2, 64), torch.zeros(3, 2, device="cuda")

@@ -73,8 +73,10 @@ template <typename T, int kBytes> struct Place {
             }
         }
     }
-    // x: the first vector's elements, then the second's
-    static __device__ __forceinline__ void turn_by(bool interleaved, float (&x)[2 * kVec], const float (&cs)[kVec], const float (&sn)[kVec]) {
+    // x: the first vector's elements, then the second's.  What passes through is left alone: a sine
+    // of 0 would make NaN of an infinity's partner.
+    __device__ __forceinline__ void turn_by(bool interleaved, float (&x)[2 * kVec], const float (&cs)[kVec], const float (&sn)[kVec]) const {
+        if (!turn) return;
         auto pair = [](float &u, float &v, float c, float s) {
             const float fu = u, fv = v;
             u = __builtin_fmaf(fu, c, -(fv * s));
@@ -180,7 +182,7 @@ template <typename T, int kBytes, int kLanes, int kPer> __global__ __launch_boun
         const float r = rsqrtf(__builtin_fmaf(sum, a.part, a.eps));
 #pragma unroll
         for (int j = 0; j < 2 * kVec; j++) x[h][j] = x[h][j] * r * w[j];
-        Place<T, kBytes>::turn_by(a.rope.interleaved, x[h], cs, sn);
+        at.turn_by(a.rope.interleaved, x[h], cs, sn);
         if (there && head + h < s.heads) store<T, kBytes>(s.y, t, head + h, at.a, at.b, x[h]);
     }
 }
@@ -219,7 +221,7 @@ template <typename T, int kBytes, int kLanes, int kPer> __global__ __launch_boun
 #pragma unroll
         for (int h = 0; h < kPer; h++) {
             const bool held = there && head + h < s.heads;
-            Place<T, kBytes>::turn_by(a.rope.interleaved, g[h], cs, sn);
+            at.turn_by(a.rope.interleaved, g[h], cs, sn);
             float sum = 0.0f, dot = 0.0f;
 #pragma unroll
             for (int j = 0; j < kOwn; j++) {
@@ -299,8 +301,9 @@ template <typename T, bool Back> __global__ __launch_bounds__(kThreads) void k_n
                     sum = __builtin_fmaf(xa[k], xa[k], __builtin_fmaf(xb[k], xb[k], sum));
                     if (Back) {
                         const float y = float(py[ea[k]]), z = float(py[eb[k]]);
-                        ga[k] = __builtin_fmaf(y, cs[k], z * sn[k]);
-                        gb[k] = __builtin_fmaf(z, cs[k], -(y * sn[k]));
+                        const bool turn = lane + 64 * k < half;
+                        ga[k] = turn ? __builtin_fmaf(y, cs[k], z * sn[k]) : y;
+                        gb[k] = turn ? __builtin_fmaf(z, cs[k], -(y * sn[k])) : z;
                         dot = __builtin_fmaf(ga[k] * wa[k], xa[k], __builtin_fmaf(gb[k] * wb[k], xb[k], dot));
                     }
                 }
@@ -320,8 +323,9 @@ template <typename T, bool Back> __global__ __launch_bounds__(kThreads) void k_n
                     out[eb[k]] = T(r * __builtin_fmaf(gb[k], wb[k], -(nb * mean)));
                 } else {
                     const float y = na * wa[k], z = nb * wb[k];
-                    out[ea[k]] = T(__builtin_fmaf(y, cs[k], -(z * sn[k])));
-                    out[eb[k]] = T(__builtin_fmaf(y, sn[k], z * cs[k]));
+                    const bool turn = lane + 64 * k < half;
+                    out[ea[k]] = T(turn ? __builtin_fmaf(y, cs[k], -(z * sn[k])) : y);
+                    out[eb[k]] = T(turn ? __builtin_fmaf(y, sn[k], z * cs[k]) : z);
                 }
             }
         }

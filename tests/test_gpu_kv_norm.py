@@ -178,6 +178,30 @@ def test_rows_of_zeros_large_and_small_numbers():
     assert bad.nonzero().tolist() == [[3, 0], [4, 1]]
 
 
+@pytest.mark.parametrize("dim,rotary,interleaved,off,dtype", [(64, 32, False, 0, torch.bfloat16), (64, 32, True, 0, torch.float32), (128, 8, True, 0, torch.float16),
+                                                              (80, 40, False, 0, torch.bfloat16), (64, 30, False, 0, torch.float32), (64, 32, True, 1, torch.bfloat16)])
+def test_infinities_in_the_part_that_passes_through(dim, rotary, interleaved, off, dtype):
+    """They stay where they are: no element of that part has to do with another but through the norm."""
+    _say(f"norm, infinities behind {rotary} of {dim}, interleaved={interleaved}, {dtype}")
+    rope, pos = kv.Rope(dim, rotary, interleaved=interleaved), torch.arange(9, dtype=torch.int32, device="cuda")
+    place = lambda seed, heads: _randn(seed, 9, heads, dim + off, dtype=dtype)[..., off:]  # noqa: E731
+    q, k, gq, gk, w = place(1, 5), place(2, 1), place(3, 5), place(4, 1), torch.ones(dim, device="cuda")
+    for at in sorted({rotary, rotary + 1, dim // 2 + rotary // 2, dim - 1}):
+        big = w.clone()
+        big[at] = float("inf")
+        yq, yk = kv.norm_rotate(rope, q, k, big, big, pos)
+        rest = torch.arange(dim, device="cuda") != at
+        plain = kv.norm_rotate(rope, q, k, w, w, pos)
+        for y, one in ((yq, plain[0]), (yk, plain[1])):
+            assert bool(y[..., at].isinf().all()) and torch.equal(y[..., rest], one[..., rest])
+        x, mine = q.clone().requires_grad_(), w.clone().requires_grad_()
+        wide, turned = gq.clone(), kv.norm_rotate(rope, x, k, mine, None, pos)[0]
+        want, = torch.autograd.grad(turned, mine, gq, retain_graph=True)
+        wide[3, 2, at] = -float("inf")
+        got, = torch.autograd.grad(turned, mine, wide)
+        assert bool(got[at].isinf()) and torch.equal(got[rest], want[rest])
+
+
 def test_no_tokens_no_heads_and_parts_of_the_gradient():
     rope, pos = kv.Rope(64), torch.arange(5, dtype=torch.int32, device="cuda")
     none, w = torch.zeros(0, 3, 64, device="cuda", requires_grad=True), torch.ones(64, device="cuda", requires_grad=True)

@@ -121,12 +121,12 @@ esp_status esp_kv_norm_rotate_backward(const esp_kv_rope *rope, int32_t type, in
  * largest of
  *   scores[beam] + logits[beam][token] - ln sum exp logits[beam]
  * over its beams (1 to 1024) and the vocabulary, the largest first, equal ones by
- * beam and token.  logits [groups][beams][vocab], the last dimension contiguous,
- * strides in elements; -inf: the token is not to be had.  The sums over a row are
- * float32 within a lane, binary64 beyond; what is compared, and scores_out before
- * its rounding, is binary64, one beam's tokens by their logits alone.  Beams whose
- * score is not finite, and beams with a NaN or +inf among their logits, have no
- * candidates.  ended (uint8 [groups][beams], NULL: none): such a beam goes on as it
+ * beam, one beam's always by logit and then by token.  logits
+ * [groups][beams][vocab], the last dimension contiguous, strides in elements; -inf:
+ * the token is not to be had.  The sums over a row are float32 within a lane,
+ * binary64 beyond; what is compared across beams, and scores_out before its
+ * rounding, is binary64.  Beams whose score is not finite, and beams with a NaN or
+ * +inf among their logits, have no candidates.  ended (uint8 [groups][beams], NULL: none): such a beam goes on as it
  * is, with token `pad` and its own score.  scores_out, parents and tokens are
  * [groups][width]: the new score, the number group * beams + beam of the sequence
  * that goes on (for esp_kv_reorder), its token; -inf, -1 and -1 where there are

@@ -1,8 +1,9 @@
 // Beam search's selection: of every request the `width` largest of
 //   score[beam] + x[beam][token] - ln sum exp x[beam]
-// over its beams and the vocabulary, ties to the lower beam, then the lower token.
+// over its beams and the vocabulary, ties to the lower beam, then by its logits, then the lower
+// token.
 // Within a beam the order is that of the logits, so one pass finds its best while the sum
-// of exponentials runs along; a second launch, a wavefront a request, sums up the splits and
+// of exponentials runs along; a second launch, a workgroup a request, sums up the splits and
 // compares across beams in binary64.
 #include "kv_internal.hpp"
 
@@ -41,10 +42,15 @@ struct One {                                // a key of 64 bits
     uint64_t k;
     __device__ __forceinline__ bool operator>(const One &o) const { return k > o.k; }
 };
-struct Two {                                // the sum in binary64, then the lower place
+struct Two {                                // the sum in binary64, then the lower beam, then its own order (place_of)
     uint64_t k, l;
     __device__ __forceinline__ bool operator>(const Two &o) const { return k > o.k || (k == o.k && l > o.l); }
 };
+// A beam's order: the logit, then the earlier split and rank there, which is the lower token.
+constexpr int kMostBeams = 1024, kPlaces = kMostSplits * kMostWidth;
+__device__ __forceinline__ uint64_t place_of(uint32_t beam, uint32_t logit, uint32_t split, uint32_t rank) {
+    return (uint64_t(kMostBeams - 1 - beam) << 32 | logit) * kPlaces + (kPlaces - 1 - (split * kMostWidth + rank));
+}
 // x of the lane whose number differs in the bit With: by rows' permutations and swaps of rows
 // and halves, without LDS.
 template <int With> __device__ __forceinline__ uint32_t across(uint32_t x, int lane) {
@@ -301,7 +307,8 @@ __global__ __launch_bounds__(kThreads) void k_beam_join(BeamArgs a) {
     __syncthreads();
     if (threadIdx.x >= 64) return;          // the rest is one wavefront's
     Best<Two> best;
-    // lists are sorted: once as many in a row as there are lists have not passed, no other does
+    // lists are sorted in this order, too, where sums of a beam are equal but its logits are not: once
+    // as many in a row as there are lists have not passed, no other does
     uint32_t quiet = 0;
     for (uint32_t i0 = 0; i0 < all && quiet < lists; i0 += 64) {
         Two k{0, 0};
@@ -310,16 +317,15 @@ __global__ __launch_bounds__(kThreads) void k_beam_join(BeamArgs a) {
             const int row = group * a.beams + beam;
             const double s = double(a.scores[row]);
             double total = NAN;
-            uint32_t token = 0;
+            uint32_t logit = 0;
             if (a.ended && a.ended[row]) {
-                token = uint32_t(a.pad);
                 if (rank == 0 && list == beam * a.splits) total = s;
             } else if (fabs(s) < INFINITY) {
                 const uint64_t held = i0 == 0 ? early : key(i0 + lane);
-                token = ~uint32_t(held);
-                if (held) total = s + (double(number(uint32_t(held >> 32))) - lse[beam]);
+                logit = uint32_t(held >> 32);
+                if (held) total = s + (double(number(logit)) - lse[beam]);
             }
-            if (fabs(total) < INFINITY) k = {ordered(total), ~(uint64_t(beam) << 32 | token)};
+            if (fabs(total) < INFINITY) k = {ordered(total), place_of(beam, logit, list - beam * a.splits, rank)};
         }
         if (i0 == 0) {
             best.start(k, queue, a.width);
@@ -332,11 +338,15 @@ __global__ __launch_bounds__(kThreads) void k_beam_join(BeamArgs a) {
     best.finish();
     if (lane < a.width) {
         const bool there = best.best.k != 0;
-        const uint64_t place = ~best.best.l;
         const int64_t at = int64_t(group) * a.width + lane;
+        const uint32_t beam = kMostBeams - 1 - uint32_t(best.best.l / kPlaces >> 32), place = kPlaces - 1 - uint32_t(best.best.l % kPlaces);
+        const int row = there ? group * a.beams + int(beam) : -1;
+        int token = there ? a.pad : -1;
+        if (there && !(a.ended && a.ended[row]))
+            token = int(~uint32_t(a.keys[(int64_t(row) * a.splits + place / kMostWidth) * a.width + place % kMostWidth]));
         a.out[at] = there ? float(number(best.best.k)) : -INFINITY;
-        a.parents[at] = there ? group * a.beams + int(place >> 32) : -1;
-        a.tokens[at] = there ? int(uint32_t(place)) : -1;
+        a.parents[at] = row;
+        a.tokens[at] = token;
     }
 }
 
@@ -346,7 +356,7 @@ using namespace esp_kv;
 
 namespace {
 
-constexpr int kMostBeams = 1024, kMostVocab = 1 << 30;
+constexpr int kMostVocab = 1 << 30;
 constexpr int64_t kMostRows = 1 << 23;      // a launch's threads are numbered in 32 bits
 
 esp_status check(int32_t groups, int32_t beams, int32_t vocab, int32_t width) {

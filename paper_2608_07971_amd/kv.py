@@ -363,7 +363,7 @@ def _select_bytes(groups: int, beams: int, vocab: int, width: int) -> int:
 def select_beams(logits: torch.Tensor, scores: torch.Tensor, width: int, ended: Optional[torch.Tensor] = None, pad: int = 0, *, s: int):
     """(scores, parents, tokens) [groups, width]: the best continuations of the beams of each request by score plus log
     probability, from logits [groups, beams, vocab] and scores (float32 [groups, beams]), the best first, equal ones by
-    beam and token.  parents number the sequences group * beams + beam, as PagedCache.reorder takes them; -1 (and a score
+    beam, one beam's always by logit and then by token.  parents number the sequences group * beams + beam, as PagedCache.reorder takes them; -1 (and a score
     of -inf) where there are fewer.  ended (bool [groups, beams]): beams that go on as they are, with token pad.  No
     gradient: backward() raises.  stream: the current one, unless given."""
     kind = _TYPES.get(logits.dtype)

@@ -120,6 +120,30 @@ def test_ties_go_to_the_lower_beam_then_the_lower_token(vocab):
             assert tokens[g, :len(want)].tolist() == [t for _, t in want] and parents[g, :len(want)].tolist() == [g * B + b for b, _ in want]
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("vocab", [2, 300, 20000])
+def test_logits_whose_sums_round_to_the_same(vocab, dtype):
+    """One beam's tokens go by their logits, also where these differ by less than their sums in binary64 can show."""
+    _say(f"select, sums that are equal and logits that are not, {vocab} {dtype}")
+    B, gen = 3, torch.Generator().manual_seed(vocab)
+    small = (torch.rand(2, B, vocab, generator=gen) * 1e-20).to(dtype).cuda()     # beside a sum of logarithms above 0.6
+    small[:, :, 0] = 0.0
+    scores = torch.tensor([[-1.0, -1.0, -3.0], [-2.0, -2.5, -2.0]], device="cuda")
+    x = small.double().cpu().numpy()
+    totals = forms.beam_totals(x, scores.cpu().numpy(), None, 0)
+    assert (totals == totals[..., :1]).all()
+    for width in (1, 2, 7, 64):
+        _, parents, tokens = _check(small, scores, width)
+        n = min(width, B * vocab)
+        for g in range(2):
+            # beams of equal rows of sums: the better score, then the lower beam; sums of rows differ by 1e-20 at most
+            best = np.lexsort((np.arange(B), -totals[g, :, 0]))
+            want = [(g * B + b, t) for b in best for t in np.lexsort((np.arange(vocab), -x[g, b]))[:width]][:n]
+            assert [*zip(parents[g, :n].tolist(), tokens[g, :n].tolist())] == want
+        first = kv.select_beams(small, scores, 1)
+        assert torch.equal(first[2].cpu(), torch.tensor(tokens[:, :1]))
+
+
 def test_logits_in_any_order_and_at_any_place():
     V, W = 30011, 16
     up = torch.linspace(-9, 9, V).expand(1, 3, V)

@@ -21,6 +21,7 @@ import functools
 from typing import Optional
 
 import torch
+from torch.autograd import forward_ad
 
 from . import ESP_OK, EspError, lib as _base_lib
 
@@ -106,9 +107,13 @@ def _check(code: int, where: str) -> None:
 def _on_stream(call):
     """call(..., s): with the handle of the stream that the work goes to, on its device, so that what the call
     allocates belongs to that stream.  The current stream of the current device costs no context.  A stream that is
-    given is noted at the tensors that it is to read, so that the allocator keeps those that the caller drops."""
+    given is noted at the tensors that it is to read, so that the allocator keeps those that the caller drops.
+    None has a forward-mode derivative: a tangent would be lost, and is refused."""
     @functools.wraps(call)
     def entry(first, *args, stream=None, **more):
+        if forward_ad._current_level >= 0 and any(isinstance(x, torch.Tensor) and forward_ad.unpack_dual(x).tangent is not None
+                                                  for x in (first, *args, *more.values())):
+            raise RuntimeError(f"{call.__qualname__} has no forward-mode derivative: call it on tensors without a tangent")
         index = first.device.index if isinstance(first, torch.Tensor) else first.index
         if index is None and isinstance(first, torch.Tensor):
             raise ValueError("a tensor on the GPU expected: there is no CPU path")

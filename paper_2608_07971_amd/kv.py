@@ -26,6 +26,9 @@ from torch.autograd import forward_ad
 from . import ESP_OK, EspError, lib as _base_lib
 
 _raw_stream = torch._C._cuda_getCurrentRawStream
+# Kernels write by address, which autograd does not see: each call counts what it wrote, so that a graph that saved
+# such a tensor before raises in backward() instead of going on with other numbers.
+_written = torch.autograd.graph.increment_version
 _current_device = torch._C._cuda_getDevice
 
 BF16, FP16, FP32 = 0, 1, 2
@@ -184,7 +187,10 @@ def rotate(rope: Rope, x: torch.Tensor, positions: torch.Tensor, inverse: bool =
     what backward() does.  out may be x.  stream: the current one, unless given."""
     if torch.is_grad_enabled() and (x.requires_grad or (out is not None and out.requires_grad)):
         return _Turned.apply(x, None if out is x else out, out is x, rope, positions, inverse, s)
-    return _turn(rope, x, positions, inverse, out, s)
+    result = _turn(rope, x, positions, inverse, out, s)
+    if out is not None:
+        _written(out)
+    return result
 
 
 class _Turned(torch.autograd.Function):
@@ -427,6 +433,7 @@ class PagedCache:
         self.device, self.index = k.device, k.device.index
         self.status = torch.zeros(1, dtype=torch.int32, device=k.device)
         self.tensors = (k, v, scale, table, lengths, refs, self.status)
+        self._pool, self._all = (k, v, scale), (k, v, scale, table, lengths, refs)
         self.pages, self.layers, self.kv_heads, self.page_tokens, self.head_dim = P, L, H, T, D
         self.sequences, self.table_width = table.shape
         self._work, self._graph_work, self._sizes = {}, (None, {}), {}
@@ -499,6 +506,7 @@ class PagedCache:
             vq, vo = _view(q, T, heads, D, "q", dev), _view(out, T, heads, D, "q", dev)
         _check(lib().esp_kv_append(self.ptr, layer, kind, rows, T, off, sq, _view(k, T, H, D, "k", dev), _view(v, T, H, D, "v", dev),
                                    None if rope is None else rope.ptr, heads, vq, vo, s), "esp_kv_append")
+        _written(self._pool)
         if torch.is_grad_enabled() and (k.requires_grad or v.requires_grad) and self._source is None:
             self._source = torch.zeros((), requires_grad=True)
         return out if out is None or not q.requires_grad else self._results("append", q, out)[0]
@@ -543,6 +551,7 @@ class PagedCache:
             if len(self._sizes) >= 4096:
                 self._sizes.clear()
             size = self._sizes[shape] = n.value
+        given = out
         if out is None:
             out = torch.empty_like(q) if q.is_contiguous() else torch.empty(q.shape, dtype=q.dtype, device=self.device)
         elif out.dtype != q.dtype:
@@ -552,6 +561,8 @@ class PagedCache:
         _check(lib().esp_kv_attend(self.ptr, layer, kind, rows, T, off, sq, H, _view(q, T, H, self.head_dim, "q", self.device), scale,
                                    window, max_new, max_length, _view(out, T, H, self.head_dim, "out", self.device),
                                    None if stats is None else stats.data_ptr(), w.data_ptr(), w.numel(), s), "esp_kv_attend")
+        if given is not None:
+            _written(given)
         if stats is None:
             return self._results("attend", q, out)[0], None
         return self._results("attend", q, out, stats)
@@ -583,6 +594,7 @@ class PagedCache:
         _check(lib().esp_kv_weigh(self.ptr, layer, kind, rows, T, off, sq, H, _view(q, T, H, self.head_dim, "q", self.device), lse.data_ptr(),
                                   self._scale if scale is None else scale, window, decay, T if max_new is None else max_new,
                                   self.table_width * self.page_tokens if max_length is None else max_length, self._mass(mass), s), "esp_kv_weigh")
+        _written(mass)
 
     def _pages_work(self, stream: int) -> torch.Tensor:
         if self._pages_bytes is None:
@@ -597,6 +609,7 @@ class PagedCache:
         w = self._pages_work(s)
         _check(lib().esp_kv_resize(self.ptr, _ints(lengths, self.sequences, "lengths", self.device), w.data_ptr(), w.numel(), s),
                "esp_kv_resize")
+        _written(self._all)
 
     @_on_stream
     def fork(self, parents, children, *, s: int) -> None:
@@ -605,6 +618,7 @@ class PagedCache:
         w = self._pages_work(s)
         _check(lib().esp_kv_fork(self.ptr, n, _ints(parents, n, "parents", self.device), _ints(children, n, "children", self.device),
                                  w.data_ptr(), w.numel(), s), "esp_kv_fork")
+        _written(self._all)
 
     @_on_stream
     def reorder(self, parents, *, s: int) -> None:
@@ -613,6 +627,7 @@ class PagedCache:
         w = self._pages_work(s)
         _check(lib().esp_kv_reorder(self.ptr, _ints(parents, self.sequences, "parents", self.device), w.data_ptr(), w.numel(), s),
                "esp_kv_reorder")
+        _written(self._all)
 
     @_on_stream
     def evict(self, keep, mass, recent: int = 0, *, s: int) -> None:
@@ -626,6 +641,7 @@ class PagedCache:
         w = self._workspace("evict", self._evict_bytes, s)
         _check(lib().esp_kv_evict(self.ptr, _ints(keep, self.sequences, "keep", self.device), recent, self._mass(mass), w.data_ptr(), w.numel(), s),
                "esp_kv_evict")
+        _written((*self._all, mass))
 
     @_on_stream
     def compact(self, limit: Optional[int] = None, *, s: int):
@@ -637,6 +653,7 @@ class PagedCache:
         w = self._pages_work(s)
         _check(lib().esp_kv_compact(self.ptr, -1 if limit is None else limit, table.data_ptr(), refs.data_ptr(), live.data_ptr(),
                                     w.data_ptr(), w.numel(), s), "esp_kv_compact")
+        _written(self._pool)
         return table, refs, live
 
     @_on_stream

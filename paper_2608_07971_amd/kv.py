@@ -244,9 +244,48 @@ def _turn(rope, x, positions, inverse, out, s: int) -> torch.Tensor:
     return out
 
 
+class _Ask(torch.autograd.Function):
+    """Nothing of a tensor, and no gradient for it: its accumulator's turn comes without anything to add or to wait for."""
+
+    @staticmethod
+    def forward(ctx, x):
+        return x.new_empty(0)
+
+    @staticmethod
+    def backward(ctx, grad):
+        return None
+
+
+class _Told(Exception):
+    pass
+
+
+def _stream_of(node, leaf) -> Optional[int]:
+    """The stream that an accumulator of gradients belongs to, which is the one that was current when it was made: the
+    engine tells it by making it current for the accumulator, and is stopped there, before any work.  None: not known
+    (a leaf on the CPU; one with hooks, which would be called, too)."""
+    if not leaf.is_cuda or leaf._backward_hooks:
+        return None
+    told = []
+
+    def ask(grads):
+        told.append(_raw_stream(leaf.device.index))
+        raise _Told
+    hook = node.register_prehook(ask)
+    try:
+        with torch.enable_grad():
+            torch.autograd.backward(_Ask.apply(leaf), leaf.detach().new_empty(0))
+    except _Told:
+        pass
+    finally:
+        hook.remove()
+    return told[0] if told else None
+
+
 def _accumulators(tensors, stream: int):
-    """What adds up the gradients of the leaves among tensors, and whether a graph that was not captured on this stream
-    holds one of these: autograd would then go to that graph's stream in a captured backward pass, which ends the process."""
+    """What adds up the gradients of the leaves among tensors, and whether one of these belongs to another stream than this
+    one, because a graph that was made there holds it: autograd would go to that stream in a backward pass that is captured
+    on this one, which ends the process if it is none of the capture's."""
     nodes, older = [], False
     for x in tensors:
         if x is not None and x.requires_grad and x.is_leaf:
@@ -256,8 +295,9 @@ def _accumulators(tensors, stream: int):
             node = torch.autograd.graph.get_gradient_edge(x).node
             if node.metadata.pop("esp_probe", None) is not probe:
                 node.metadata["esp_stream"] = stream
-            elif node.metadata.get("esp_stream") != stream:
-                older = True
+            elif node.metadata.get("esp_stream") is None:
+                node.metadata["esp_stream"] = _stream_of(node, x)
+            older |= node.metadata["esp_stream"] != stream
             nodes.append(node)
     return nodes, older
 
@@ -327,8 +367,8 @@ class _Normed(torch.autograd.Function):
     @staticmethod
     def backward(ctx, gq, gk):
         if ctx.older:
-            raise RuntimeError("norm_rotate: a captured backward pass of leaves that a graph from before the capture holds, too. Drop "
-                               "that graph before the capture")
+            raise RuntimeError("norm_rotate: a captured backward pass of leaves whose gradients a graph from before the capture, or of "
+                               "another of its streams, adds up there (as is assumed of leaves with hooks). Drop that graph first")
         saved = ctx.saved_tensors
         grads = _norm_back(ctx.rope, *saved, ctx.eps, gq, gk, ctx.needs_input_grad[2:4])
         if torch.is_grad_enabled():             # a graph of the gradient is asked for

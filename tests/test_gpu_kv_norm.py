@@ -281,6 +281,59 @@ def test_a_training_step_in_a_graph():
     assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(lives, leaves, (gq, gk)), want[2:]))
 
 
+def _captured(leaves, step, **more):
+    """step's results from a graph and eagerly, for three sets of inputs."""
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, **more):
+        got = step()
+    for i in range(3):
+        _say(f"replay {i}")
+        with torch.no_grad():
+            for j, t in enumerate(leaves):
+                t.copy_(1.0 + 0.1 * _randn(20 * i + j, *t.shape))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, step()))
+
+
+def test_other_users_of_the_leaves_in_a_capture():
+    """A leaf that another operation of the same capture used first."""
+    rope, pos = kv.Rope(64), torch.arange(30, dtype=torch.int32, device="cuda")
+    q, k, w = (torch.ones(*n, device="cuda", requires_grad=True) for n in ((30, 4, 64), (30, 2, 64), (64,)))
+    grads = [_randn(i, *n) for i, n in enumerate(((30, 4, 64), (30, 2, 64), (64,), (30, 4, 64)))]
+
+    def step():
+        other = w * w, q * q
+        y = kv.norm_rotate(rope, q, k, w, w, pos)
+        return torch.autograd.grad((*y, *other), (q, k, w), grads)
+    step()
+    _captured((q, k, w), step)
+
+    def added():
+        for t in (q, k, w):
+            t.grad = None
+        other = w * w
+        y = kv.norm_rotate(rope, q, k, w, None, pos)
+        torch.autograd.backward((*y, other), grads[:3])
+        return [t.grad.clone() for t in (q, k, w)]
+    added()
+    _captured((q, k, w), added)
+
+
+def test_accumulators_that_were_made_on_the_stream_that_is_captured():
+    rope, pos, side = kv.Rope(64), torch.arange(9, dtype=torch.int32, device="cuda"), torch.cuda.Stream()
+    q, w = (torch.ones(*n, device="cuda", requires_grad=True) for n in ((9, 2, 64), (64,)))
+    g = _randn(1, 9, 2, 64)
+    with torch.cuda.stream(side):
+        kept = [q.view_as(q), w.view_as(w)]                       # hold them, as wrappers that keep accumulators do
+    torch.cuda.synchronize()
+    node = torch.autograd.graph.get_gradient_edge(w).node
+    assert kv._stream_of(node, w) == side.cuda_stream and q.grad is None
+    _captured((q, w), lambda: torch.autograd.grad(kv.norm_rotate(rope, q, q.detach(), w, None, pos)[0], (q, w), g), stream=side)
+    assert len(kept) == 2
+
+
 def test_another_stream():
     rope, pos, side = kv.Rope(64), torch.arange(50, dtype=torch.int32, device="cuda"), torch.cuda.Stream()
     q, k, w = _randn(8, 50, 4, 64).requires_grad_(), _randn(9, 50, 2, 64), torch.ones(64, device="cuda")

@@ -18,3 +18,25 @@ def test_leaves_of_an_older_graph_are_found():
     assert kv._accumulators((x,), 8)[1] is True                   # another stream's
     del mine
     assert kv._accumulators((x,), 8)[1] is False
+
+
+def test_the_stream_of_an_accumulator_decides(monkeypatch):
+    """Whichever call made it: a product recorded on the stream before is no older graph."""
+    x, asked = torch.ones(3, requires_grad=True), []
+    for told, older in ((7, False), (0, True), (9, True), (None, True)):
+        monkeypatch.setattr(kv, "_stream_of", lambda node, leaf: (asked.append(leaf), told)[1])
+        first = (x * x).sum()
+        nodes, found = kv._accumulators((x,), 7)
+        assert found is older and asked and asked[-1] is x
+        asked.clear()
+        assert kv._accumulators((x,), 7)[1] is older and bool(asked) is (told is None)      # once is enough
+        del first, nodes
+
+
+def test_asking_for_the_stream_leaves_the_leaf_alone():
+    x = torch.ones(3, requires_grad=True)
+    kept = x * 2
+    node = torch.autograd.graph.get_gradient_edge(x).node
+    assert kv._stream_of(node, x) is None and x.grad is None      # a leaf on the CPU has none
+    kept.sum().backward()
+    assert x.grad.tolist() == [2.0] * 3

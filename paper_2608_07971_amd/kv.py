@@ -186,7 +186,8 @@ def rotate(rope: Rope, x: torch.Tensor, positions: torch.Tensor, inverse: bool =
     """x [tokens, heads, head_dim] turned by positions (int32 [tokens]); inverse: turned back, which is the gradient, and
     what backward() does.  out may be x.  stream: the current one, unless given."""
     if torch.is_grad_enabled() and (x.requires_grad or (out is not None and out.requires_grad)):
-        return _Turned.apply(x, None if out is x else out, out is x, rope, positions, inverse, s)
+        with _Leaves(s, x, out) as older:
+            return _Turned.apply(x, None if out is x else out, out is x, rope, positions, inverse, older, s)
     result = _turn(rope, x, positions, inverse, out, s)
     if out is not None:
         _written(out)
@@ -197,21 +198,22 @@ class _Turned(torch.autograd.Function):
     """rotate with its gradient: the rotation times magnitude, transposed."""
 
     @staticmethod
-    def forward(ctx, x, out, in_place, rope, positions, inverse, s):
+    def forward(ctx, x, out, in_place, rope, positions, inverse, older, s):
         if in_place:
             out = x
         if out is not None:
             ctx.mark_dirty(out)
-        ctx.rope, ctx.inverse = rope, inverse
+        ctx.rope, ctx.inverse, ctx.older = rope, inverse, older
         ctx.save_for_backward(positions)
         return _turn(rope, x, positions, inverse, out, s)
 
     @staticmethod
     def backward(ctx, grad):
+        _refuse_older(ctx.older, "rotate")
         positions, = ctx.saved_tensors
         if grad.stride(-1) != 1:
             grad = grad.contiguous()
-        return rotate(ctx.rope, grad, positions, inverse=not ctx.inverse), None, None, None, None, None, None
+        return rotate(ctx.rope, grad, positions, inverse=not ctx.inverse), None, None, None, None, None, None, None
 
 
 class _NoGradient(torch.autograd.Function):
@@ -302,6 +304,25 @@ def _accumulators(tensors, stream: int):
     return nodes, older
 
 
+class _Leaves:
+    """In a capture: whether leaves among the tensors have accumulators of another stream.  Holds them until a graph does."""
+
+    def __init__(self, stream: int, *tensors):
+        self.nodes, self.older = _accumulators(tensors, stream) if torch.cuda.is_current_stream_capturing() else ((), False)
+
+    def __enter__(self) -> bool:
+        return self.older
+
+    def __exit__(self, *error) -> None:
+        self.nodes = ()
+
+
+def _refuse_older(older: bool, what: str) -> None:
+    if older:
+        raise RuntimeError(f"{what}: a captured backward pass of leaves whose gradients a graph from before the capture, or of another "
+                           "of its streams, adds up there (as is assumed of leaves with hooks). Drop that graph first")
+
+
 def _weights(q_weight, k_weight, x, dim: int):
     """Kind and addresses of the norms' weights."""
     given = [w for w in (q_weight, k_weight) if w is not None]
@@ -318,11 +339,8 @@ def norm_rotate(rope: Rope, q: torch.Tensor, k: torch.Tensor, q_weight, k_weight
     [head_dim] (the type of q and k or float32; None: ones), turned by positions (int32 [tokens]).  Has its gradient, of
     the weights too.  Either may have no heads.  stream: the current one, unless given."""
     if torch.is_grad_enabled() and any(x is not None and x.requires_grad for x in (q, k, q_weight, k_weight)):
-        capturing = torch.cuda.is_current_stream_capturing()
-        nodes, older = _accumulators((q, k, q_weight, k_weight), s) if capturing else ((), False)
-        result = _Normed.apply(q, k, q_weight, k_weight, rope, positions, eps, older, s)
-        del nodes                               # until here: the graph holds them now
-        return result
+        with _Leaves(s, q, k, q_weight, k_weight) as older:
+            return _Normed.apply(q, k, q_weight, k_weight, rope, positions, eps, older, s)
     return _norm(rope, q, k, q_weight, k_weight, positions, eps, s)
 
 
@@ -366,9 +384,7 @@ class _Normed(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, gq, gk):
-        if ctx.older:
-            raise RuntimeError("norm_rotate: a captured backward pass of leaves whose gradients a graph from before the capture, or of "
-                               "another of its streams, adds up there (as is assumed of leaves with hooks). Drop that graph first")
+        _refuse_older(ctx.older, "norm_rotate")
         saved = ctx.saved_tensors
         grads = _norm_back(ctx.rope, *saved, ctx.eps, gq, gk, ctx.needs_input_grad[2:4])
         if torch.is_grad_enabled():             # a graph of the gradient is asked for

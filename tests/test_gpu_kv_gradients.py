@@ -135,3 +135,35 @@ def test_the_cache_says_where_a_gradient_would_be_lost():
         with torch.no_grad():
             assert not any(t.requires_grad for t in calls(cache, kk, qq))
         assert cache.device_status() == 0
+
+
+def test_a_captured_step():
+    """Beside other users of its leaf in the capture; beside an eager graph of it the backward pass is refused."""
+    rope, pos = kv.Rope(64), torch.arange(7, dtype=torch.int32, device="cuda")
+    x, g = torch.zeros(7, 2, 64, device="cuda", requires_grad=True), _randn(1, 7, 2, 64)
+
+    def step():
+        other = x * x
+        return torch.autograd.grad((kv.rotate(rope, x, pos), other), x, (g, g))[0]
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for i in range(3):
+        _say(f"replay {i}")
+        with torch.no_grad():
+            x.copy_(_randn(i, 7, 2, 64))
+            g.copy_(_randn(10 + i, 7, 2, 64))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, step())
+    _say("a captured backward pass beside an eager graph of the same leaf")
+    lives = kv.rotate(rope, x, pos)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(torch.cuda.CUDAGraph()):
+        with pytest.raises(RuntimeError, match="before the capture"):
+            y = kv.rotate(rope, x, pos)                           # alone: a product would leave the capture's stream itself
+            torch.autograd.grad(y, x, g)
+    torch.cuda.synchronize()
+    assert bool((torch.autograd.grad(lives, x, g)[0] != 0).any())

@@ -1,4 +1,7 @@
 """Without a GPU: leaves whose accumulators a graph from before a capture holds are found."""
+import types
+
+import pytest
 import torch
 
 from paper_2608_07971_amd import kv
@@ -40,3 +43,15 @@ def test_asking_for_the_stream_leaves_the_leaf_alone():
     assert kv._stream_of(node, x) is None and x.grad is None      # a leaf on the CPU has none
     kept.sum().backward()
     assert x.grad.tolist() == [2.0] * 3
+
+
+def test_a_captured_rotation_of_an_older_graphs_leaf_has_no_backward(monkeypatch):
+    rope = types.SimpleNamespace(index=0)
+    monkeypatch.setattr(kv, "_turn", lambda rope, x, positions, inverse, out, s: x * 1)
+    x, pos = torch.ones(2, 1, 4, requires_grad=True), torch.zeros(2, dtype=torch.int32)
+    older = x * 2
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    y = kv.rotate.__wrapped__(rope, x, pos, s=7)
+    with pytest.raises(RuntimeError, match="before the capture"):
+        y.backward(torch.ones_like(y))
+    del older

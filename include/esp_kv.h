@@ -212,7 +212,8 @@ esp_status esp_kv_attend(const esp_kv_cache *cache, int32_t layer, int32_t type,
  * contiguous; places from a sequence's length on, and sequences of rows that have no
  * tokens or are left out, stay as they were.  A query whose lse is -inf adds nothing.  Sums are float32.
  * max_new chooses the kernel: where rows have few tokens, a loose one has cost up to
- * twice the time.
+ * twice the time.  With rows that have none among the others, each row's own count
+ * does, beside it, for one launch more.
  */
 esp_status esp_kv_weigh(const esp_kv_cache *cache, int32_t layer, int32_t type, int32_t rows, int64_t tokens,
                         const int32_t *offsets, const int32_t *seqs, int32_t q_heads, esp_kv_view q, const float *lse,

@@ -27,6 +27,7 @@ struct WeighArgs {
     float *mass;
     float scale, decay;
     int32_t layer, q_heads, group, window, max_new, max_length, shares, wide;
+    int32_t over, most;                     // sequences with more (token, query head) rows than `over`, and `most` of them, are this launch's
 };
 
 __device__ __forceinline__ float16v product32(half8 x, half8 y, float16v z) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(x, y, z, 0, 0, 0); }
@@ -50,7 +51,7 @@ __device__ __forceinline__ Row usable(const WeighArgs &a, int b, bool note) {
         if (note) record(a.c, ESP_ERR_SHAPE);
         return Row{};
     }
-    if (r.n == 0) r.length = 0;
+    if (r.n * a.group <= a.over || r.n * a.group > a.most) r.n = r.length = 0;
     return r;
 }
 
@@ -470,7 +471,7 @@ using namespace esp_kv;
 
 namespace {
 
-// Rows (token, query head) a sequence and key head up to which k_weigh_few takes a call, in
+// Rows (token, query head) a sequence and key head up to which k_weigh_few takes it, in
 // rounds of 16 or 32.  So / by k_weigh, 64 sequences of about 3,800 tokens of 128: 48 rows of 4
 // key heads 68 / 128 us, 96 rows 89 / 122, 128 rows 106 / 121, 192 rows 160 / 134.
 constexpr int kFewRows = 128;
@@ -478,22 +479,44 @@ constexpr int kFewRows = 128;
 // for 16.  2,048 / 4,096 / 8,192 of the latter: 59 / 54 / 55 us (weights of 64 single tokens of
 // 32 heads on up to 8,192 cached ones, 8 key heads).
 constexpr int kUnits = 1024, kFewWaves = 3 * kUnits, kFewestWaves = 4 * kUnits;           // kUnits: the GPU's SIMDs
-constexpr int64_t kMostBlocks = ((int64_t(1) << 32) - 1) / (kThreads * kGroups);  // a launch's threads are numbered in 32 bits
+// Workgroups of k_weigh, and of it where few sequences, if any, are its own: 64 single tokens whose
+// bound allows more take 94 us beside it, 91 alone (8 key heads, up to 8,040 tokens of 128).
+constexpr int kManyBlocks = 16384, kSomeBlocks = 1024;
 
-template <typename T, int Dim, int Page> void launch(const WeighArgs &a, int rows, unsigned blocks, hipStream_t s) {
-    if (rows > kFewRows) k_weigh<T, Dim, Page><<<blocks, kThreads * kGroups, 0, s>>>(a);
-    else if (rows > 16) k_weigh_few<T, Dim, Page, 2><<<blocks, kThreads, 0, s>>>(a);
+// How a sequence is weighed: by the most rows that it may have.
+enum Kind { kSixteens, kPairs, kMany };
+Kind kind_of(int64_t rows) { return rows <= 16 ? kSixteens : rows <= kFewRows ? kPairs : kMany; }
+constexpr int32_t kMostOf[] = {16, kFewRows, INT32_MAX};
+
+template <typename T, int Dim, int Page> void launch(const WeighArgs &a, Kind kind, unsigned blocks, hipStream_t s) {
+    if (kind == kMany) k_weigh<T, Dim, Page><<<blocks, kThreads * kGroups, 0, s>>>(a);
+    else if (kind == kPairs) k_weigh_few<T, Dim, Page, 2><<<blocks, kThreads, 0, s>>>(a);
     else k_weigh_few<T, Dim, Page, 1><<<blocks, kThreads, 0, s>>>(a);
 }
-template <typename T, int Dim> void launch(const WeighArgs &a, int rows, unsigned blocks, hipStream_t s) {
+template <typename T, int Dim> void launch(const WeighArgs &a, Kind kind, unsigned blocks, hipStream_t s) {
     switch (a.c.tokens) {
-    case 16: launch<T, Dim, 16>(a, rows, blocks, s); break;
-    case 32: launch<T, Dim, 32>(a, rows, blocks, s); break;
-    default: launch<T, Dim, 64>(a, rows, blocks, s); break;
+    case 16: launch<T, Dim, 16>(a, kind, blocks, s); break;
+    case 32: launch<T, Dim, 32>(a, kind, blocks, s); break;
+    default: launch<T, Dim, 64>(a, kind, blocks, s); break;
     }
 }
-template <typename T> void launch(const WeighArgs &a, int rows, unsigned blocks, hipStream_t s) {
-    a.c.dim == 64 ? launch<T, 64>(a, rows, blocks, s) : launch<T, 128>(a, rows, blocks, s);
+template <typename T> void launch(const WeighArgs &a, Kind kind, unsigned blocks, hipStream_t s) {
+    a.c.dim == 64 ? launch<T, 64>(a, kind, blocks, s) : launch<T, 128>(a, kind, blocks, s);
+}
+
+// The sequences of one kind; `alone`: no other launch has any.
+int64_t shares_of(const WeighArgs &a, Kind kind, bool alone) {
+    // shares of a head's tiles: one each where queries are many; else as many as the GPU holds wavefronts
+    const int64_t tile = kind == kMany ? kWaves * 32 : 64, most = a.rows.rows * ((int64_t(a.max_length) + tile - 1) / tile);
+    const int64_t fill = (kind == kMany ? alone ? kManyBlocks : kSomeBlocks : kind == kPairs ? kFewWaves : kFewestWaves) / a.c.heads + 1;
+    return most > INT32_MAX ? -1 : most < fill ? most : fill;
+}
+esp_status weigh(WeighArgs a, Kind kind, bool alone, int32_t type, hipStream_t s) {
+    a.shares = int32_t(shares_of(a, kind, alone));
+    const int64_t workers = int64_t(a.shares) * a.c.heads, count = kind == kMany ? workers : (workers + kWaves - 1) / kWaves;
+    if (type == ESP_KV_BF16) launch<__bf16>(a, kind, unsigned(count), s);
+    else launch<_Float16>(a, kind, unsigned(count), s);
+    return launched();
 }
 
 }  // namespace
@@ -511,22 +534,21 @@ extern "C" esp_status esp_kv_weigh(const esp_kv_cache *cache, int32_t layer, int
     if (!offsets || !q.data || !lse || !mass) return ESP_ERR_INVALID_ARG;
     const int32_t group = q_heads / cache->kv_heads;
     if (tokens * group > INT32_MAX - 8 * kStep) return ESP_ERR_SHAPE;
-    // the most new tokens of a row, if none is without any (others take k_weigh_few more rounds)
-    const int64_t longest = tokens - rows + 1 < max_new ? (tokens < rows ? 1 : tokens - rows + 1) : max_new;
-    const int32_t most_rows = int32_t(longest * group < INT32_MAX ? longest * group : INT32_MAX);
-    const bool many = most_rows > kFewRows;
-    // shares of a head's tiles: one each where queries are many; else as many as the GPU holds wavefronts
-    const int64_t tile = many ? kWaves * 32 : 64, most = rows * ((int64_t(max_length) + tile - 1) / tile);
-    if (most > INT32_MAX) return ESP_ERR_SHAPE;
-    const int64_t fill = (many ? 16384 : most_rows > 16 ? kFewWaves : kFewestWaves) / cache->kv_heads + 1, shares = most < fill ? most : fill;
-    const int64_t workers = shares * cache->kv_heads, count = many ? workers : (workers + kWaves - 1) / kWaves;
-    if (count > kMostBlocks) return ESP_ERR_SHAPE;
     const bool wide = (reinterpret_cast<uintptr_t>(q.data) & 15) == 0 && q.token_stride % 8 == 0 && q.head_stride % 8 == 0;
-    const WeighArgs a{cache_of(cache), Rows{offsets, seqs, rows, tokens}, View{q.data, q.token_stride, q.head_stride}, lse, mass, scale, decay,
-                      layer, q_heads, group, window, max_new, max_length, int32_t(shares), wide};
+    WeighArgs a{cache_of(cache), Rows{offsets, seqs, rows, tokens}, View{q.data, q.token_stride, q.head_stride}, lse, mass, scale, decay,
+                layer, q_heads, group, window, max_new, max_length, 0, wide, 0, INT32_MAX};
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    const unsigned blocks = unsigned(count);
-    if (type == ESP_KV_BF16) launch<__bf16>(a, most_rows, blocks, s);
-    else launch<_Float16>(a, most_rows, blocks, s);
-    return launched();
+    // what the caller allows a row, and the most that it has if no row is without any: where these are of
+    // different kinds, each row goes to the lesser kind if it is of that, else to the greater.  One row of
+    // 512 tokens among 511 empty ones, group 4, on 4,096: 52 us, 494 in the rounds of the lesser alone.
+    const int64_t even = tokens < rows ? 1 : tokens - rows + 1, longest = even < max_new ? even : max_new;
+    const Kind most = kind_of(int64_t(max_new) * group), least = kind_of(longest * group);
+    if (shares_of(a, least, true) < 0) return ESP_ERR_SHAPE;
+    if (least != most) {
+        a.most = kMostOf[least];
+        if (esp_status e = weigh(a, least, false, type, s)) return e;
+        a.over = a.most;
+        a.most = INT32_MAX;
+    }
+    return weigh(a, most, least == most, type, s);
 }

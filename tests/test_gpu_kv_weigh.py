@@ -89,6 +89,41 @@ def test_weigh(new, lengths, heads, group, dim, page, window, dtype, decay):
     assert torch.equal(first, again)                              # bounds change how, not what
 
 
+@pytest.mark.parametrize("heads,group,dtype", [(2, 4, torch.bfloat16), (1, 16, torch.float16)])
+def test_rows_of_every_kind_among_empty_ones(heads, group, dtype):
+    new = [0] * 140
+    new[3], new[4], new[40], new[77], new[139] = 1, 40, 5, 70, 8
+    g = np.random.default_rng(group)
+    lengths = [int(n + g.integers(0, 300)) for n in new]
+    cache = ref.make(kv, lengths, heads=heads, dim=64)
+    q, found = _randn(11, sum(new), heads * group, 64, dtype=dtype), []
+    for more in ({}, dict(max_new=70), dict(max_new=1000), dict(max_new=70, window=60)):
+        _say(f"weigh rows of every kind among empty ones, {heads} x {group}, {more}")
+        found.append(_check(cache, q, new, decay=0.5, **more))
+    assert torch.equal(found[0], found[1]) and torch.equal(found[0], found[2])
+    before = _mass(cache)
+    assert all(torch.equal(found[0][:, b], before[:, b]) for b in range(140) if new[b] == 0)
+
+
+def test_one_long_row_among_empty_ones_takes_what_it_takes():
+    """Its own kernel's time, not that of the rounds of single tokens (which is eight times as long)."""
+    H, G, n, length = 8, 4, 512, 4096
+    q, lse, times = _randn(12, n, H * G, 128), torch.full((n, H * G), 9.0, device="cuda"), []
+    for rows in (2, 512):
+        cache = ref.make(kv, [length] + [0] * (rows - 1), heads=H, dim=128)
+        offs, mass = ref.offsets([n] + [0] * (rows - 1)), torch.zeros(cache.mass_shape, device="cuda")
+        best = []
+        for _ in range(12):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            cache.weigh(0, q, lse, offs, mass, max_new=n)
+            b.record()
+            torch.cuda.synchronize()
+            best.append(a.elapsed_time(b))
+        times.append(min(best))
+    assert times[1] < 4 * times[0]
+
+
 def test_weights_add_up_to_one_a_query():
     cache = ref.make(kv, [500, 77], heads=2, dim=128)
     q, offs, mass = _randn(2, 5, 8, 128), ref.offsets([4, 1]), torch.zeros(1, 2, 2, cache.table_width * 16, device="cuda")

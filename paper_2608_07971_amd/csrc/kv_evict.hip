@@ -444,7 +444,8 @@ template <int Dim> void move(const EvictArgs &a, const Work &w, unsigned blocks,
 extern "C" esp_status esp_kv_evict_workspace(const esp_kv_cache *cache, size_t *bytes) {
     if (esp_status e = check_cache(cache)) return e;
     if (!bytes) return ESP_ERR_INVALID_ARG;
-    if (2 * items_of(cache) > INT32_MAX) return ESP_ERR_SHAPE;
+    // kernels count items, some launches' worth past the last, and a row's tokens, some turns past the last, in 32 bits
+    if (2 * items_of(cache) > INT32_MAX - (kMostBlocks - 1) || int64_t(cache->table_width) * cache->page_tokens > INT32_MAX - kStretch) return ESP_ERR_SHAPE;
     Work w;
     *bytes = lay_out(cache, nullptr, w) + size_t(items_of(cache)) * words_of(cache) * sizeof(uint64_t);
     return ESP_OK;

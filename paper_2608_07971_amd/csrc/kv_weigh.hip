@@ -534,6 +534,9 @@ extern "C" esp_status esp_kv_weigh(const esp_kv_cache *cache, int32_t layer, int
     if (!offsets || !q.data || !lse || !mass) return ESP_ERR_INVALID_ARG;
     const int32_t group = q_heads / cache->kv_heads;
     if (tokens * group > INT32_MAX - 8 * kStep) return ESP_ERR_SHAPE;
+    // tokens of a sequence are counted in 32 bits, some tiles past the last
+    const int64_t held = int64_t(cache->table_width) * cache->page_tokens, bound = max_length < held ? max_length : held;
+    if (bound > INT32_MAX - 8 * kStep) return ESP_ERR_SHAPE;
     const bool wide = (reinterpret_cast<uintptr_t>(q.data) & 15) == 0 && q.token_stride % 8 == 0 && q.head_stride % 8 == 0;
     WeighArgs a{cache_of(cache), Rows{offsets, seqs, rows, tokens}, View{q.data, q.token_stride, q.head_stride}, lse, mass, scale, decay,
                 layer, q_heads, group, window, max_new, max_length, 0, wide, 0, INT32_MAX};

@@ -92,3 +92,18 @@ def test_bad_reorderings_weights_and_evictions_are_refused():
         assert L.esp_kv_evict(p, A, 0, A, w, size, None) == esp.ESP_ERR_WORKSPACE
     many = _cache(sequences=1 << 25, layers=16)
     assert L.esp_kv_evict_workspace(C.addressof(many), C.byref(n)) == esp.ESP_ERR_SHAPE
+
+
+def test_counts_that_would_pass_32_bits_are_refused():
+    L, n, v = kv.lib(), C.c_size_t(0), _view()
+    for sequences, code in (((1 << 30) - (1 << 11), esp.ESP_OK), ((1 << 30) - (1 << 11) + 1, esp.ESP_ERR_SHAPE), ((1 << 30) - 1, esp.ESP_ERR_SHAPE)):
+        many = _cache(sequences=sequences, table_width=1, layers=1, kv_heads=1)       # keys and values: 2 items a sequence, 4,096 workgroups
+        assert L.esp_kv_evict_workspace(C.addressof(many), C.byref(n)) == code
+        if code:
+            assert L.esp_kv_evict(C.addressof(many), A, 0, A, A, 1 << 60, None) == code
+    for width, code in (((1 << 27) - 128 - 1, esp.ESP_OK), ((1 << 27) - 64, esp.ESP_ERR_SHAPE), ((1 << 27) - 1, esp.ESP_ERR_SHAPE)):
+        wide = _cache(sequences=1, table_width=width, page_tokens=16)
+        assert L.esp_kv_evict_workspace(C.addressof(wide), C.byref(n)) == code
+        if code:
+            for length in (16 * width, (1 << 31) - 1):
+                assert L.esp_kv_weigh(C.addressof(wide), 0, 0, 1, 1, A, None, 2, v, A, 0.1, 0, 1.0, 1, length, A, None) == code

@@ -59,6 +59,21 @@ def test_reorder_in_a_row(page, heads, dim, layers, sequences, width):
     assert not cache.refs.any() and not cache.lengths.any() and bool((cache.table == -1).all())
 
 
+@pytest.mark.parametrize("layers,heads,dim,page,sequences", [(9, 2, 64, 64, 6), (32, 2, 64, 32, 40), (17, 8, 128, 16, 5)])
+def test_pages_that_are_copied_by_a_launch_of_their_own(layers, heads, dim, page, sequences):
+    _say(f"reorder, pages of {2 * layers * heads * dim * page >> 10} KB, {sequences} sequences")
+    assert 2 * layers * heads * dim * page > 128 << 10
+    g = np.random.default_rng(layers)
+    lengths = [int(g.integers(0, 4 * page + 1)) for _ in range(sequences)]
+    cache = ref.make(kv, lengths, page=page, heads=heads, dim=dim, layers=layers, width=4, spare=sequences)
+    pages, first = forms.Pages(cache), _state(cache)
+    for parents in ([0] * sequences, list(range(sequences)), [int(x) for x in g.integers(-1, sequences, sequences)], [sequences - 1] * sequences, [sequences] * sequences):
+        ok = max(parents) < sequences and pages.reorder(parents)
+        cache.reorder(_dev(parents))
+        assert cache.device_status() == (0 if ok else esp.ESP_ERR_INVALID_ARG)
+        _same(cache, pages, first)
+
+
 def test_beams_write_apart_after_a_reordering():
     cache = ref.make(kv, [40, 40, 33, 5], heads=1, dim=64, pages=20, width=4)
     before = [cache.gather(0, _dev([0]), ref.offsets([n]), n, seqs=_dev([s]))[0] for s, n in enumerate((40, 40, 33, 5))]

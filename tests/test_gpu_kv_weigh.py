@@ -105,6 +105,28 @@ def test_rows_of_every_kind_among_empty_ones(heads, group, dtype):
     assert all(torch.equal(found[0][:, b], before[:, b]) for b in range(140) if new[b] == 0)
 
 
+@pytest.mark.parametrize("new,lengths,heads,group,dim,page,window,dtype", [
+    # shares of several tiles that go on in the next row: rounds of 16 rows, of 32, and many queries (beside few of them, and alone)
+    ([1] * 7, [2000, 130, 1, 0, 3001, 900, 2500], 32, 2, 64, 16, 0, torch.bfloat16), ([3, 2, 1, 3], [2222, 64, 1999, 3100], 32, 8, 64, 64, 1500, torch.float16),
+    ([20, 0, 17] + [0] * 60, [3100, 40, 2900] + [5] * 60, 32, 8, 64, 32, 0, torch.bfloat16), ([3, 130], [900, 9000], 256, 1, 64, 16, 400, torch.bfloat16),
+])
+def test_shares_of_several_tiles(new, lengths, heads, group, dim, page, window, dtype):
+    _say(f"weigh {new[:4]} of {lengths[:4]}, {heads} x {group} x {dim}, window {window}")
+    cache = ref.make(kv, lengths, heads=heads, dim=dim, page=page)
+    _check(cache, _randn(13, sum(new), heads * group, dim, dtype=dtype), new, window, decay=0.5, max_new=max(new), max_length=max(lengths))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("page", [16, 64])
+def test_many_queries_of_any_strides(dtype, page):
+    cache = ref.make(kv, [500, 190], heads=2, dim=128, page=page)
+    wide = _randn(14, 110, 9, 136, dtype=dtype)
+    for q in (wide[:, 1:7, :128], wide[:, 1:7, 3:131], wide[:, :6, 8:], wide.transpose(0, 1).contiguous().transpose(0, 1)[:, 2:8, 1:129], wide[:, :1, :128].expand(110, 6, 128)):
+        _say(f"weigh 60 + 50 queries of strides {q.stride()}, pages of {page}, {dtype}")
+        _check(cache, q, [60, 50], decay=0.5)
+        _check(cache, q, [50, 60], window=70)
+
+
 def test_one_long_row_among_empty_ones_takes_what_it_takes():
     """Its own kernel's time, not that of the rounds of single tokens (which is eight times as long)."""
     H, G, n, length = 8, 4, 512, 4096

@@ -271,6 +271,8 @@ def _stream_of(node, leaf) -> Optional[int]:
     told = []
 
     def ask(grads):
+        if grads[0] is not None:                # another thread's pass
+            return
         told.append(_raw_stream(leaf.device.index))
         raise _Told
     hook = node.register_prehook(ask)

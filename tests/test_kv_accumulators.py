@@ -55,3 +55,18 @@ def test_a_captured_rotation_of_an_older_graphs_leaf_has_no_backward(monkeypatch
     with pytest.raises(RuntimeError, match="before the capture"):
         y.backward(torch.ones_like(y))
     del older
+
+
+def test_asking_does_not_end_another_threads_pass(monkeypatch):
+    """The question is told from a pass that has a gradient to add."""
+    node, leaf = types.SimpleNamespace(hooks=[]), torch.ones(3, requires_grad=True)
+    node.register_prehook = lambda hook: (node.hooks.append(hook), types.SimpleNamespace(remove=lambda: node.hooks.remove(hook)))[1]
+    fake = types.SimpleNamespace(is_cuda=True, _backward_hooks=None, device=types.SimpleNamespace(index=0), detach=leaf.detach)
+    monkeypatch.setattr(kv, "_raw_stream", lambda index: 7)
+    monkeypatch.setattr(kv._Ask, "apply", lambda x: leaf)
+
+    def backward(root, grad):
+        assert node.hooks[0]((torch.ones(3),)) is None
+        node.hooks[0]((None,))
+    monkeypatch.setattr(torch.autograd, "backward", backward)
+    assert kv._stream_of(node, fake) == 7 and node.hooks == []

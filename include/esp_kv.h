@@ -102,7 +102,7 @@ esp_status esp_kv_rotate(const esp_kv_rope *rope, int32_t type, int64_t tokens, 
  *   dw = sum over tokens and heads of g n,   dx = (g w - n sum(g w n) / head_dim) (sum x^2 / head_dim + eps)^-1/2
  * into dq, dk (they may be q_grad and k_grad) and dq_weight, dk_weight (NULL:
  * not wanted; of no tokens: 0), sums in float32 in an order that depends on the
- * sizes alone.  workspace (if a weight's gradient is wanted): 256-byte aligned,
+ * sizes, types, strides and alignment of both sides, and on nothing else.  workspace (if a weight's gradient is wanted): 256-byte aligned,
  * contents free.
  */
 esp_status esp_kv_norm_rotate(const esp_kv_rope *rope, int32_t type, int64_t tokens, int32_t head_dim, int32_t q_heads,

@@ -168,8 +168,10 @@ template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) Eight {
 // are marked in a mask a lane and read once more in one short loop (with the code for them at
 // every logit, 119 KB of it, a turn took twice as long).  A row's sums are taken by places
 // in the row alone, so copies of a row have equal sums wherever they lie.
-// Bound by memory, then by the exponentials: 512 rows of 131,072 in bf16 (134 MB) 40 us (3.4
-// TB/s); 4 rows of 32,000 8 us, a chain of loading, sorting and joining.
+// A turn's loads are waited for before its arithmetic (conversion, maximum, difference, product,
+// exponential, sum, comparison), and four wavefronts a SIMD do not hide them: 512 rows of 131,072 in
+// bf16 (134 MB) 39 us (3.4 TB/s), where reading alone takes 20 to 27; 4 rows of 32,000 8.3 us, a
+// chain of loading, sorting and joining.
 template <typename T> __global__ __launch_bounds__(kThreads) void k_beam_rows(BeamArgs a) {
     __shared__ One lds[kWaves][128];
     __shared__ float tops[kWaves];
@@ -277,7 +279,7 @@ __device__ __forceinline__ uint64_t ordered(double x) {
 }
 __device__ __forceinline__ double number(uint64_t u) { return __longlong_as_double(int64_t(u >> 63 ? u & ~(uint64_t(1) << 63) : ~u)); }
 
-// A workgroup a request (64 of 8 beams 6.1 us, one of 4 beams in 16 splits 4.2 us): beams' sums over
+// A workgroup a request (64 of 8 beams 6.4 us, one of 4 beams in 16 splits 4.1 us): beams' sums over
 // their splits, then, by one wavefront, the best of what they left.
 __global__ __launch_bounds__(kThreads) void k_beam_join(BeamArgs a) {
     __shared__ Two queue[128];

@@ -114,7 +114,7 @@ __device__ __forceinline__ Place place_of(const Cache &c, const Work &w, int i) 
 
 constexpr int kHeld = 16;                   // weights a thread: rows of up to 4,096 tokens are read once
 
-// 1,024 rows of up to 4,096 weights 22 us, 8 rows of 1,500 9.5 us: four rounds of counting
+// 1,024 rows of up to 4,096 weights 20 us, 8 rows of 1,500 11 us: four rounds of counting
 // and a walk, each a few barriers.
 // The want-th largest weight by its bits, eight at a time from the top; then one pass over
 // the tokens in order, equal ones by the lower place.
@@ -214,8 +214,9 @@ __global__ __launch_bounds__(kThreads) void k_evict_select(EvictArgs a, Work w) 
 
 // kTurn tokens move at a time, whole pages; the mask of kStretch is read at a time.  Shorter
 // turns wait more often for their look-ups, longer ones leave the GPU fewer workgroups: 64,
-// 128, 256 tokens take 304, 276, 327 us for 1,024 rows of 2,048 kept of up to 4,096 tokens of
-// 128, and 39, 21, 14 us for 8 rows of 1,000 of 1,500 tokens of 64.
+// 128, 256 tokens take 280, 284, 330 us for 1,024 rows of 2,048 kept of up to 4,096 tokens of
+// 128, and 40, 23, 16 us for 8 rows of 1,000 of 1,500 tokens of 64.  One size for all launches,
+// though the longer one would be better for so few rows.
 constexpr int kTurn = 128, kMoveThreads = 4 * kTurn, kMoveWaves = kMoveThreads / 64, kStretch = 2048;
 
 // Where the tokens of a turn come from.

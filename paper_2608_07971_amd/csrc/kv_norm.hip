@@ -152,8 +152,8 @@ struct Walk {
 // kLanes lanes a token and head (dim / (2 vectors) of them at work), kPer heads of a
 // token, whose angles are worked out once.  Read past the caches: neither input nor output is
 // wanted again here.
-// Bound by memory: 16,383 tokens of 32 + 8 heads of 128 in bf16 (336 MB) 67 us (5.0 TB/s); 256
-// of them 7.6 us, a chain of loads, sums and angles.
+// Bound by memory: 16,383 tokens of 32 + 8 heads of 128 in bf16 (336 MB) 69 us (4.9 TB/s); 256
+// of them 8.1 us, a chain of loads, sums and angles.
 template <typename T, int kBytes, int kLanes, int kPer> __global__ __launch_bounds__(kThreads) void k_norm(NormArgs a) {
     constexpr int kVec = kBytes / int(sizeof(T)), kTeams = kThreads / kLanes;
     int block = blockIdx.x;
@@ -187,11 +187,11 @@ template <typename T, int kBytes, int kLanes, int kPer> __global__ __launch_boun
     }
 }
 
-// The gradient of the former 114 us (503 MB, 4.4 TB/s): 152 registers leave three wavefronts a
-// SIMD; with four the sums are spilled (178 us), and one head at a time takes 143.
+// The gradient of the former 120 us (503 MB, 4.2 TB/s): 152 registers leave three wavefronts a
+// SIMD; with four the sums are spilled (178 us), and one head at a time takes 135.
 // The same teams, each going through many tokens with the sums of its elements' weight
 // gradient in registers; a workgroup's sums go to its row of `partial`, added up by
-// k_norm_weights in an order that depends on nothing but the sizes.
+// k_norm_weights: an order that sizes, types, strides and alignment decide (by the vectors and teams).
 template <typename T, int kBytes, int kLanes, int kPer> __global__ __launch_bounds__(kThreads) void k_norm_back(NormArgs a) {
     constexpr int kVec = kBytes / int(sizeof(T)), kTeams = kThreads / kLanes, kOwn = 2 * kVec;
     __shared__ float lds[4][kMostDim];
@@ -376,7 +376,7 @@ constexpr int64_t kMostBlocks = ((int64_t(1) << 32) - kThreads) / kThreads;    /
 constexpr int kPerHeads = 4, kBackHeads = 2;
 // Workgroups of a gradient, of queries and keys together: those that the GPU holds at once, or
 // twice as many, whose ends lie less far apart, where each still has four turns.  So many / the
-// others: 655,320 heads of 128 in bf16 114 / 135 us; 131,168 of 64 in fp16 21 / 25.
+// others: 655,320 heads of 128 in bf16 120 / 143 us; 131,168 of 64 in fp16 20 / 24.
 constexpr int kBackBlocks = 768;
 
 View view_of(const esp_kv_view &v) { return {v.data, v.token_stride, v.head_stride}; }

@@ -222,8 +222,8 @@ __global__ __launch_bounds__(kThreads) void k_fork_take(Cache c, int n, const in
 
 // ---------------------------------------------------------------------------
 // Reorder: a workgroup a sequence; every row is put together aside before any is written.
-// Three launches: 256 beams of up to 157 pages of 64 KB, some 110 of them copied, 5.5 + 2 + 8.8
-// us; 4 beams 3.2 + 1.6 + 4.2 us.
+// Three launches: 256 beams of up to 157 pages of 64 KB, some 110 of them copied, 5.7 + 2.4 + 9
+// us; 4 beams 3.5 + 1.7 + 4.5 us.
 // ---------------------------------------------------------------------------
 
 constexpr int kInvalid = 1, kWrong = 2, kCopies = 4;

@@ -159,7 +159,7 @@ __device__ __forceinline__ float weight(float product, float scale, float lse) {
 // one kind after another.
 // Bound by the wavefronts' vector instructions (a sixteenth of a tile: difference, product,
 // exponential, sum): 3 sequences of up to 12,000 tokens, up to 2,048 of them new, 32 query
-// heads of 128, 279 GFLOP, 364 us (767 TFLOP/s).  Queries through registers instead of direct
+// heads of 128, 279 GFLOP, 366 us (762 TFLOP/s; up to 535 in the first passes after the GPU was idle).  Queries through registers instead of direct
 // into LDS: 457; one group of wavefronts, or four: 509, 489; heads one after another in the
 // launch instead of next to each other, so that long shares come last: 449.
 template <typename T, int Dim, int Page> __global__ __launch_bounds__(kThreads * kGroups, 4) void k_weigh(WeighArgs a) {

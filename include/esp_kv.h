@@ -213,7 +213,7 @@ esp_status esp_kv_attend(const esp_kv_cache *cache, int32_t layer, int32_t type,
  * tokens or are left out, stay as they were.  A query whose lse is -inf adds nothing.  Sums are float32.
  * max_new chooses the kernel: where rows have few tokens, a loose one has cost up to
  * twice the time.  With rows that have none among the others, each row's own count
- * does, beside it, for one launch more.
+ * does, beside it, for one launch more, or for up to four rounds of 16 rows of a head.
  */
 esp_status esp_kv_weigh(const esp_kv_cache *cache, int32_t layer, int32_t type, int32_t rows, int64_t tokens,
                         const int32_t *offsets, const int32_t *seqs, int32_t q_heads, esp_kv_view q, const float *lse,

@@ -544,8 +544,11 @@ extern "C" esp_status esp_kv_weigh(const esp_kv_cache *cache, int32_t layer, int
     // what the caller allows a row, and the most that it has if no row is without any: where these are of
     // different kinds, each row goes to the lesser kind if it is of that, else to the greater.  One row of
     // 512 tokens among 511 empty ones, group 4, on 4,096: 52 us, 494 in the rounds of the lesser alone.
-    const int64_t even = tokens < rows ? 1 : tokens - rows + 1, longest = even < max_new ? even : max_new;
-    const Kind most = kind_of(int64_t(max_new) * group), least = kind_of(longest * group);
+    const int64_t allowed = tokens < max_new ? tokens : max_new, even = tokens < rows ? 1 : tokens - rows + 1;
+    const Kind least = kind_of((even < allowed ? even : allowed) * group);
+    // four rounds of sixteens are no second launch's worth: 16 single tokens with a loose bound 22 / 25 us (64
+    // sequences of 32 rows among empty ones 168 / 114)
+    const Kind most = least == kSixteens && allowed * group <= 4 * 16 ? least : kind_of(allowed * group);
     if (shares_of(a, least, true) < 0) return ESP_ERR_SHAPE;
     if (least != most) {
         a.most = kMostOf[least];

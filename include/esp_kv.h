@@ -210,7 +210,8 @@ esp_status esp_kv_attend(const esp_kv_cache *cache, int32_t layer, int32_t type,
  * softmax weights.  Rows name distinct sequences, whose own new tokens begin at 0.
  * mass: float32 [layers][sequences][kv_heads][table_width * page_tokens],
  * contiguous; places from a sequence's length on, and sequences of rows that have no
- * tokens or are left out, stay as they were.  A query whose lse is -inf adds nothing.  Sums are float32.
+ * tokens or are left out, stay as they were.  A query whose lse is -inf adds
+ * nothing, whatever it holds.  Sums are float32.
  * max_new chooses the kernel: where rows have few tokens, a loose one has cost up to
  * twice the time.  With rows that have none among the others, each row's own count
  * does, beside it, for one launch more, or for up to four rounds of 16 rows of a head.
